@@ -94,6 +94,7 @@ def lib() -> ctypes.CDLL:
         L.moe_forward_hostio.argtypes = [cfgp, vp, vp, fp, fp, wp, wp, vp, vp, sz, vp]
         L.moe_device_status.argtypes = [vp, vp, i32p]
         L.moe_permute_noalloc.argtypes = [cfgp, vp, vp, vp, vp, vp, vp]
+        attn._bind(L)
         _lib = L
     return _lib
 
@@ -226,3 +227,8 @@ def moe_permute_noalloc(cfg, topk_ids, counts, offsets, sorted_pair, pair_pos, s
     """moe_permute with the library's static scratch instead of a workspace."""
     _check(lib().moe_permute_noalloc(ctypes.byref(cfg), _ptr(topk_ids), _ptr(counts), _ptr(offsets),
                                      _ptr(sorted_pair), _ptr(pair_pos), _stream(stream)), "moe_permute_noalloc")
+
+
+from . import attn  # noqa: E402
+from .attn import (AttnBatch, AttnCache, AttnConfig, AttnRows, attn_append, attn_batch, attn_cache, attn_cached,  # noqa: E402,F401
+                   attn_check_config, attn_config, attn_prompt, attn_rope, attn_rope_table, attn_workspace_size)

@@ -7,11 +7,22 @@
 #include <cstdint>
 #include <cstring>
 
+#include "api_status.h"
 #include "common.cuh"
 #include "ffn_sched.h"
 #include "kernels.h"
 
 using namespace gbmoe;
+
+namespace {
+thread_local int g_last_cuda_error = 0;  // gbmoe_last_cuda_error
+}
+
+int gbmoe::cuda_status(cudaError_t e) {
+    if (e == cudaSuccess) return GBMOE_OK;
+    g_last_cuda_error = (int)e;
+    return GBMOE_ECUDA;
+}
 
 namespace {
 
@@ -257,14 +268,6 @@ Layout layout(const gbmoe_config* c) {
 template <typename T>
 T* at(void* ws, size_t off) {
     return reinterpret_cast<T*>(static_cast<char*>(ws) + off);
-}
-
-thread_local int g_last_cuda_error = 0;  // gbmoe_last_cuda_error
-
-int cuda_status(cudaError_t e) {
-    if (e == cudaSuccess) return GBMOE_OK;
-    g_last_cuda_error = (int)e;
-    return GBMOE_ECUDA;
 }
 
 int check_ws(const gbmoe_config* c, void* ws, size_t bytes) {

@@ -1,0 +1,343 @@
+// Attention on CUDA cores: fp32 activations, and head sizes that the
+// tensor-core kernels do not take. Also the join of a split key axis.
+//
+// One pass over the keys with the running maximum and sum of the softmax: a
+// block holds 32 tokens of one head (packed queries) or 16 rows, token and head
+// of the group (cache), walks its keys in tiles of 32 through shared memory and
+// keeps the weighted sum of values in registers. Bound by the
+// fp32 pipes for prompts, by the latency of its loads for single tokens.
+#include <climits>
+
+#include "attn_plan.cuh"
+
+namespace gbmoe {
+namespace {
+
+constexpr int kThreads = 128;
+constexpr int kKeys = 32;
+
+// Eight elements of key or value row `key` of sequence s, widened; a key whose
+// page is outside the pool gives false.
+template <typename TA, bool kE4m3, bool kPaged>
+struct Source {
+    const AttnProblem& p;
+    const void* pool;
+    const uint8_t* scales;
+    Rows rows;
+    int h, b;
+    int64_t k0;
+
+    __device__ __forceinline__ bool load(int key, int d, float (&v)[8]) const {
+        if (!kPaged) {
+            Vec8<TA>::load(static_cast<const TA*>(rows.p) + (k0 + key) * rows.ts + h * rows.hs + d, v);
+            return true;
+        }
+        const int pg = key / p.page, id = p.page_table[(int64_t)b * p.max_pages + pg];
+        if (id < 0 || id >= p.n_pages) return false;
+        const int64_t head = (int64_t)id * p.Hkv + h;
+        const int64_t at = (head * p.page + (key - pg * p.page)) * p.D + d;
+        if constexpr (kE4m3) {
+            const uint2 c = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(pool) + at);
+            const float sc = e8m0_to_f32(scales[head]);
+            const float2 a = e4m3x2_to_f32x2(c.x & 0xffffu), e = e4m3x2_to_f32x2(c.x >> 16);
+            const float2 f = e4m3x2_to_f32x2(c.y & 0xffffu), g = e4m3x2_to_f32x2(c.y >> 16);
+            v[0] = a.x * sc, v[1] = a.y * sc, v[2] = e.x * sc, v[3] = e.y * sc;
+            v[4] = f.x * sc, v[5] = f.y * sc, v[6] = g.x * sc, v[7] = g.y * sc;
+        } else {
+            Vec8<TA>::load(static_cast<const TA*>(pool) + at, v);
+        }
+        return true;
+    }
+};
+
+template <int DP>
+constexpr int kLd = DP + 4;  // row length in shared memory
+template <int DP, int N>
+constexpr size_t kSmem = ((size_t)(2 * kKeys + 16 * N) * kLd<DP> + 16 * N * (kKeys + 1) + kKeys) * 4;
+
+// DP: head size rounded up to 64, 128 or 256. N: rows of a thread, 2 (packed) or
+// 1. Thread (ty, tx) = (tid / 8, tid % 8) holds rows N ty .., of the scores the
+// keys tx + 8 j, of the result the columns 4 tx + 32 j ..; a row's eight threads
+// lie in one warp.
+template <typename TA, bool kE4m3, int DP, int N>
+__global__ void __launch_bounds__(kThreads) attn_simt_kernel(const AttnProblem p) {
+    pdl_enter();
+    constexpr int kRows = 16 * N;
+    constexpr bool kPaged = N == 1;
+    extern __shared__ float4 smem4[];
+    float* sq = reinterpret_cast<float*>(smem4);
+    float* sk = sq + kRows * kLd<DP>;
+    float* sv = sk + kKeys * kLd<DP>;
+    float* sp = sv + kKeys * kLd<DP>;
+    int* ok = reinterpret_cast<int*>(sp + kRows * (kKeys + 1));
+    __shared__ int64_t plan[plan_words(kThreads)];
+    const int G = p.Hq / p.Hkv, heads = kPaged ? p.Hkv : p.Hq;
+    const int head0 = (blockIdx.x % heads) * p.R;  // query head of row 0
+    const int h = head0 / G;                       // kv head
+    const Item it = find_item<kRows>(p, blockIdx.x / heads, plan);
+    if (it.b < 0) return;
+    const int row0 = it.tile * kRows, R = p.R;
+    const int n_rows = (int)min64(kRows, (int64_t)it.s.nq * R - row0);
+
+    const int tid = threadIdx.x, ty = tid >> 3, tx = tid & 7;
+    for (int i = tid; i < kRows * (DP / 8); i += kThreads) {
+        const int r = i / (DP / 8), d = 8 * (i % (DP / 8));
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (r < n_rows && d < p.D)
+            Vec8<TA>::load(static_cast<const TA*>(p.q.p) + (it.s.q0 + (row0 + r) / R) * p.q.ts + (head0 + (row0 + r) % R) * p.q.hs + d, v);
+        Vec8<float>::store(sq + r * kLd<DP> + d, v);
+    }
+    int lo[N], hi[N];
+#pragma unroll
+    for (int r = 0; r < N; ++r) {
+        lo[r] = 0, hi[r] = -1;
+        if (N * ty + r < n_rows) seen_keys(p, it.s, (row0 + N * ty + r) / R, lo[r], hi[r]);
+    }
+    // keys that some row of the tile sees
+    int k_lo, k_hi, last_lo, last_hi;
+    seen_keys(p, it.s, row0 / R, k_lo, k_hi);
+    seen_keys(p, it.s, (row0 + n_rows - 1) / R, last_lo, last_hi);
+    if (k_hi < 0) k_lo = 0;
+    k_lo = max(it.k_lo, k_lo), k_hi = min(it.k_hi, last_hi + 1);
+
+    constexpr int NC = DP / 32;  // float4 columns of a thread
+    float4 o[N][NC];
+    float m[N], l[N];
+#pragma unroll
+    for (int r = 0; r < N; ++r) {
+        m[r] = neg_inf(), l[r] = 0.0f;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) o[r][c] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    const Source<TA, kE4m3, kPaged> src_k{p, p.k_pool, p.k_scale, p.k, h, it.b, it.s.k0};
+    const Source<TA, kE4m3, kPaged> src_v{p, p.v_pool, p.v_scale, p.v, h, it.b, it.s.k0};
+    for (int k0 = k_lo; k0 < k_hi; k0 += kKeys) {
+        __syncthreads();
+        for (int i = tid; i < kKeys * (DP / 8); i += kThreads) {
+            const int r = i / (DP / 8), d = 8 * (i % (DP / 8));
+            float a[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, b[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            bool good = k0 + r < k_hi;
+            if (good && d < p.D) good = src_k.load(k0 + r, d, a) && src_v.load(k0 + r, d, b);
+            Vec8<float>::store(sk + r * kLd<DP> + d, a);
+            Vec8<float>::store(sv + r * kLd<DP> + d, b);
+            if (d == 0) ok[r] = good;
+        }
+        __syncthreads();
+        float s[N][4] = {};
+        for (int d = 0; d < p.D; d += 4) {
+            float4 a[N], b[4];
+#pragma unroll
+            for (int r = 0; r < N; ++r) a[r] = *reinterpret_cast<const float4*>(sq + (N * ty + r) * kLd<DP> + d);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) b[j] = *reinterpret_cast<const float4*>(sk + (tx + 8 * j) * kLd<DP> + d);
+#pragma unroll
+            for (int r = 0; r < N; ++r)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    s[r][j] = fmaf(a[r].x, b[j].x, fmaf(a[r].y, b[j].y, fmaf(a[r].z, b[j].z, fmaf(a[r].w, b[j].w, s[r][j]))));
+        }
+        bool all = true;  // this thread's rows see every key of the tile
+#pragma unroll
+        for (int r = 0; r < N; ++r) {
+            float mx = neg_inf();
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int key = k0 + tx + 8 * j;
+                const bool see = key >= lo[r] && key <= hi[r] && ok[tx + 8 * j];
+                all &= see;
+                s[r][j] = see ? s[r][j] * p.scale_log2 : neg_inf();
+                mx = fmaxf(mx, s[r][j]);
+            }
+#pragma unroll
+            for (int d = 1; d < 8; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+            const float m_new = fmaxf(m[r], mx);
+            const float base = m_new == neg_inf() ? 0.0f : m_new;
+            const float f = exp2f(m[r] - base);
+            m[r] = m_new;
+            float sum = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                s[r][j] = exp2f(s[r][j] - base);
+                sum += s[r][j];
+                sp[(N * ty + r) * (kKeys + 1) + tx + 8 * j] = s[r][j];
+            }
+            l[r] = l[r] * f + sum;
+#pragma unroll
+            for (int c = 0; c < NC; ++c) o[r][c].x *= f, o[r][c].y *= f, o[r][c].z *= f, o[r][c].w *= f;
+        }
+        all = __all_sync(0xffffffffu, all);
+        __syncwarp();
+        // weights times values; a value that a row does not see is left out, not multiplied by 0 (it may be NaN)
+        for (int j = 0; j < kKeys; ++j) {
+            float w[N];
+            bool see[N];
+#pragma unroll
+            for (int r = 0; r < N; ++r) {
+                w[r] = sp[(N * ty + r) * (kKeys + 1) + j];
+                see[r] = all || (k0 + j >= lo[r] && k0 + j <= hi[r]);
+            }
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                const float4 v = *reinterpret_cast<const float4*>(sv + j * kLd<DP> + 4 * tx + 32 * c);
+#pragma unroll
+                for (int r = 0; r < N; ++r)
+                    if (see[r]) {
+                        o[r][c].x = fmaf(w[r], v.x, o[r][c].x), o[r][c].y = fmaf(w[r], v.y, o[r][c].y);
+                        o[r][c].z = fmaf(w[r], v.z, o[r][c].z), o[r][c].w = fmaf(w[r], v.w, o[r][c].w);
+                    }
+            }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < N; ++r) {
+#pragma unroll
+        for (int d = 1; d < 8; d <<= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], d);
+        const int rr = N * ty + r;
+        if (rr >= n_rows) continue;
+        const int64_t t = it.s.q0 + (row0 + rr) / R;
+        const int hq = head0 + (row0 + rr) % R;
+        if (it.chunks > 1) {
+            const int64_t at = (it.slot * p.Hkv + h) * kSplitRows + rr;
+            if (tx == 0) reinterpret_cast<float4*>(p.part_s)[at] = make_float4(m[r], l[r], m[r], 0.0f);
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+                if (4 * tx + 32 * c < p.D) *reinterpret_cast<float4*>(p.part_o + at * p.D + 4 * tx + 32 * c) = o[r][c];
+            continue;
+        }
+        const bool empty = hi[r] < lo[r];
+        const float inv = empty ? 0.0f : 1.0f / l[r];
+        if (p.lse && tx == 0) p.lse[t * p.Hq + hq] = empty ? neg_inf() : (m[r] + log2f(l[r])) * kLn2;
+        TA* out = const_cast<TA*>(static_cast<const TA*>(p.out.p)) + t * p.out.ts + hq * p.out.hs;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int d = 4 * tx + 32 * c;
+            if (d >= p.D) continue;
+            const float v[4] = {o[r][c].x * inv, o[r][c].y * inv, o[r][c].z * inv, o[r][c].w * inv};
+            if constexpr (sizeof(TA) == 4)
+                *reinterpret_cast<float4*>(out + d) = make_float4(v[0], v[1], v[2], v[3]);
+            else
+                *reinterpret_cast<uint2*>(out + d) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+        }
+    }
+}
+
+template <typename TA, bool kE4m3, int DP, int N>
+cudaError_t simt_as(const AttnProblem& p, cudaStream_t stream) {
+    constexpr auto kernel = attn_simt_kernel<TA, kE4m3, DP, N>;
+    static DeviceOnce once;
+    if (cudaError_t e = once.run([] {
+            return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem<DP, N>);
+        });
+        e != cudaSuccess)
+        return e;
+    const int64_t items = attn_items(p, 16 * N), heads = p.paged ? p.Hkv : p.Hq;
+    if (items * heads > INT32_MAX) return cudaErrorInvalidConfiguration;
+    return launch_k(kernel, dim3((unsigned)(items * heads)), dim3(kThreads), kSmem<DP, N>, stream, p);
+}
+
+template <typename TA, bool kE4m3, int N>
+cudaError_t simt_width(const AttnProblem& p, cudaStream_t stream) {
+    if (p.D <= 64) return simt_as<TA, kE4m3, 64, N>(p, stream);
+    if (p.D <= 128) return simt_as<TA, kE4m3, 128, N>(p, stream);
+    return simt_as<TA, kE4m3, 256, N>(p, stream);
+}
+
+template <typename TA>
+cudaError_t simt_source(const AttnProblem& p, cudaStream_t stream) {
+    if (!p.paged) return simt_width<TA, false, 2>(p, stream);
+    return p.e4m3 ? simt_width<TA, true, 1>(p, stream) : simt_width<TA, false, 1>(p, stream);
+}
+
+// ------------------------------------------------------------------- join
+//
+// Block (x, y, z): row z of kv head y in the x-th row tile that was split. Its
+// chunks' sums, each relative to 2^(its own third statistic), are brought to
+// the largest of those and added in chunk order, the softmax sums likewise
+// relative to the first: out = sum / l. Threads: 4 columns each, the chunks
+// dealt out over the rest.
+constexpr int kJoinThreads = 128;
+
+template <typename TA>
+__global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const AttnProblem p) {
+    pdl_enter();
+    __shared__ int64_t plan[plan_words(kJoinThreads)];
+    __shared__ float4 acc[kJoinThreads];
+    __shared__ float red[3][kJoinThreads / 32];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const Item it = find_item<kSplitRows, true>(p, blockIdx.x, plan);
+    if (it.b < 0) return;
+    const int G = p.Hq / p.Hkv, h = blockIdx.y, row = it.tile * kSplitRows + blockIdx.z;
+    if (row >= it.s.nq * (int64_t)G) return;
+    const int64_t at0 = (it.slot * p.Hkv + h) * kSplitRows + blockIdx.z, step = (int64_t)p.Hkv * kSplitRows;
+    const float4* st = reinterpret_cast<const float4*>(p.part_s);
+    // maxima of the two statistics
+    float m = neg_inf(), mo = neg_inf();
+    for (int c = tid; c < it.chunks; c += kJoinThreads) {
+        const float4 s = st[at0 + c * step];
+        m = fmaxf(m, s.x), mo = fmaxf(mo, s.z);
+    }
+#pragma unroll
+    for (int d = 16; d; d >>= 1) {
+        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+        mo = fmaxf(mo, __shfl_xor_sync(0xffffffffu, mo, d));
+    }
+    if (lane == 0) red[0][warp] = m, red[1][warp] = mo;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kJoinThreads / 32; ++w) m = fmaxf(m, red[0][w]), mo = fmaxf(mo, red[1][w]);
+    const float base = m == neg_inf() ? 0.0f : m, base_o = mo == neg_inf() ? 0.0f : mo;
+    float l = 0.0f;
+    for (int c = tid; c < it.chunks; c += kJoinThreads) {
+        const float4 s = st[at0 + c * step];
+        l += s.y * exp2f(s.x - base);
+    }
+#pragma unroll
+    for (int d = 16; d; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
+    if (lane == 0) red[2][warp] = l;
+    __syncthreads();
+    l = red[2][0] + red[2][1] + red[2][2] + red[2][3];
+
+    const int cols = p.D / 4, groups = kJoinThreads / cols, g = tid / cols, d = 4 * (tid % cols);
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (g < groups)
+        for (int c = g; c < it.chunks; c += groups) {
+            const float f = exp2f(st[at0 + c * step].z - base_o);
+            if (f == 0.0f) continue;  // a chunk that this row does not see (its sums are 0)
+            const float4 v = *reinterpret_cast<const float4*>(p.part_o + (at0 + c * step) * p.D + d);
+            o.x = fmaf(v.x, f, o.x), o.y = fmaf(v.y, f, o.y), o.z = fmaf(v.z, f, o.z), o.w = fmaf(v.w, f, o.w);
+        }
+    acc[tid] = o;
+    __syncthreads();
+    if (tid >= cols) return;
+    for (int w = 1; w < groups; ++w) {
+        const float4 v = acc[tid + w * cols];
+        o.x += v.x, o.y += v.y, o.z += v.z, o.w += v.w;
+    }
+    int lo, hi;
+    seen_keys(p, it.s, row / G, lo, hi);
+    const bool empty = hi < lo;
+    const int64_t t = it.s.q0 + row / G;
+    const int hq = h * G + row % G;
+    if (p.lse && tid == 0) p.lse[t * p.Hq + hq] = empty ? neg_inf() : (base + log2f(l)) * kLn2;
+    const float inv = empty ? 0.0f : exp2f(base_o - base) / l;
+    TA* out = const_cast<TA*>(static_cast<const TA*>(p.out.p)) + t * p.out.ts + hq * p.out.hs + d;
+    if constexpr (sizeof(TA) == 4)
+        *reinterpret_cast<float4*>(out) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+    else
+        *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
+}
+
+}  // namespace
+
+cudaError_t launch_attn_simt(const AttnProblem& p, cudaStream_t stream) {
+    return p.act_dtype == GBMOE_F32 ? simt_source<float>(p, stream) : simt_source<__nv_bfloat16>(p, stream);
+}
+
+cudaError_t launch_attn_join(const AttnProblem& p, cudaStream_t stream) {
+    const int64_t rows = (int64_t)p.T * (p.Hq / p.Hkv);
+    const dim3 grid((unsigned)min64(p.target, rows / kSplitRows + p.B), p.Hkv, (unsigned)min64(kSplitRows, rows));
+    return p.act_dtype == GBMOE_F32 ? launch_k(attn_join_kernel<float>, grid, dim3(kJoinThreads), 0, stream, p)
+                                    : launch_k(attn_join_kernel<__nv_bfloat16>, grid, dim3(kJoinThreads), 0, stream, p);
+}
+
+}  // namespace gbmoe
