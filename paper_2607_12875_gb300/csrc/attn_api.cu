@@ -219,7 +219,8 @@ int attn_prompt(const gbattn_config* cfg, int32_t Tq, int32_t Tk, int32_t B, con
     p.Tk = Tk; p.cu_q = cu_q; p.cu_k = cu_k; p.R = 1;
     if (Tk > 0) p.k = rows_of(k, Tk, cfg->heads_kv), p.v = rows_of(v, Tk, cfg->heads_kv);
     p.target = 1; p.min_chunk = INT_MAX;  // one chunk: a prompt has rows enough
-    return cuda_status(launch_attn_simt(p, static_cast<cudaStream_t>(stream)));
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return cuda_status(attn_prompt_tc_supported(p) ? launch_attn_prompt_tc(p, st) : launch_attn_simt(p, st));
 }
 
 int attn_cached(const gbattn_config* cfg, int32_t T, const gbattn_batch* batch, const gbattn_rows* q,
