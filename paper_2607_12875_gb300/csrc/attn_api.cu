@@ -240,7 +240,7 @@ int attn_cached(const gbattn_config* cfg, int32_t T, const gbattn_batch* batch, 
     p.target = split_target(cfg->heads_kv);
     p.min_chunk = 256;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (int s = cuda_status(launch_attn_simt(p, st))) return s;
+    if (int s = cuda_status(attn_split_supported(p) ? launch_attn_split(p, st) : launch_attn_simt(p, st))) return s;
     // no sequence can have a second chunk: nothing to join
     if ((int64_t)p.max_pages * p.page <= p.min_chunk) return GBMOE_OK;
     return cuda_status(launch_attn_join(p, st));

@@ -204,7 +204,7 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(const AttnProblem p
                 if (4 * tx + 32 * c < p.D) *reinterpret_cast<float4*>(p.part_o + at * p.D + 4 * tx + 32 * c) = o[r][c];
             continue;
         }
-        const bool empty = hi[r] < lo[r];
+        const bool empty = hi[r] < lo[r] || (kPaged && m[r] == neg_inf() && l[r] == 0.0f);  // (or none of its keys has a page)
         const float inv = empty ? 0.0f : 1.0f / l[r];
         if (p.lse && tx == 0) p.lse[t * p.Hq + hq] = empty ? neg_inf() : (m[r] + log2f(l[r])) * kLn2;
         TA* out = const_cast<TA*>(static_cast<const TA*>(p.out.p)) + t * p.out.ts + hq * p.out.hs;
@@ -315,7 +315,7 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const AttnProbl
     }
     int lo, hi;
     seen_keys(p, it.s, row / G, lo, hi);
-    const bool empty = hi < lo;
+    const bool empty = hi < lo || (m == neg_inf() && l == 0.0f);
     const int64_t t = it.s.q0 + row / G;
     const int hq = h * G + row % G;
     if (p.lse && tid == 0) p.lse[t * p.Hq + hq] = empty ? neg_inf() : (base + log2f(l)) * kLn2;

@@ -425,22 +425,23 @@ def test_cached_values_of_very_different_scales(kind):
 def test_cached_masks_pages_outside_the_pool_and_later_tokens(act, kind, D):
     """Tokens without a page are masked; a NaN value that only the last query sees reaches that one alone."""
     rng = np.random.default_rng(8)
-    page, n, lens = 16, [3, 1], [200, 90]
+    page, n, lens = 16, [3, 1, 1], [200, 90, 40]
     c = Cache(rng, act, kind, 2, D, page, lens, poison=True)
     c.table[0, 4], c.table[1, 1] = -1, c.k.shape[0]
+    c.table[2] = -1  # no page at all: as if there were no keys
     pg = int(c.table[0, 199 // page])
     if kind == "act":
         c.v[pg, :, 199 % page] = float("nan")
     else:
         c.v[pg, :, 199 % page] = 0xff
-    q = normal(rng, (4, 4, D), act)
+    q = normal(rng, (5, 4, D), act)
     cfg = gb.attn_config(4, 2, D, act=act, cache=kind, page=page)
-    ws = torch.zeros(gb.attn_workspace_size(cfg, 4, 2), dtype=torch.uint8, device="cuda")
+    ws = torch.zeros(gb.attn_workspace_size(cfg, 5, 3), dtype=torch.uint8, device="cuda")
     out = torch.zeros_like(q)
     keep = (prefix(n), i32(lens), i32(c.table))
     gb.attn_cached(cfg, gb.attn_batch(*keep), q, c.bundle, out, ws)
     got = wide(out)
-    assert np.isnan(got[2]).all()
+    assert np.isnan(got[2]).all() and (got[4] == 0).all()
     if kind == "act":
         c.v[pg, :, 199 % page] = 0.0
     else:
