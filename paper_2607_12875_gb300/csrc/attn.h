@@ -58,31 +58,34 @@ struct AttnProblem {
     const int32_t *kv_len, *page_table;
     const void *k_pool, *v_pool;
     const uint8_t *k_scale, *v_scale;
-    // chunks of a long key axis (cached attention): items aimed at per kv head, the
-    // smallest chunk, and their partial results: [slots, Hkv, rows, D] sums and
-    // [slots, Hkv, rows, 4] statistics
-    int target, min_chunk;
+    int page_log2;
+    // cached attention: CTAs (shares of the work), the least blocks of a share, rows of
+    // a tile, and the partial results [2 * shares, rows, D] sums and [2 * shares, rows, 4]
+    // statistics of tiles cut by the shares' ends
+    int shares, min_blocks, tile_rows;
     float *part_o, *part_s;
     int32_t* err;
 };
 
-constexpr int kSplitRows = 16;      // (token, head of the group) rows of a work item of the split kernels
-constexpr int kMaxSplitItems = 2432; // items aimed at over all kv heads: 16 waves of one CTA on 152 SMs
+constexpr int kBlockKeys = 64;   // keys of a block of work
+constexpr int kMaxTileRows = 16;
+constexpr int kMaxShares = 608;  // four CTAs on each of 152 SMs
 
-// work items aimed at per kv head, and the partial slots that can then be needed
-inline int split_target(int Hkv) { return kMaxSplitItems / Hkv > 1 ? kMaxSplitItems / Hkv : 1; }
-inline int64_t split_slots(int Hkv) { return 2 * (int64_t)split_target(Hkv) + 2; }
-
-// most items (row tiles of `rows` rows times chunks) of a problem
-inline int64_t attn_items(const AttnProblem& p, int rows) {
-    return (int64_t)p.T * p.R / rows + p.B + (p.paged ? p.target : 0);
+// CTAs of cached attention for `rows` rows of a tile and `per_sm` CTAs on an SM: no
+// more than there can be shares of min_blocks
+inline int shares_of(const AttnProblem& p, int rows, int per_sm, int sms) {
+    const int64_t tiles = (int64_t)p.T * p.R / rows + p.B;
+    const int64_t blocks = tiles * p.Hkv * (((int64_t)p.max_pages * p.page + kBlockKeys - 1) / kBlockKeys + 1);
+    const int64_t most = (blocks + p.min_blocks - 1) / p.min_blocks;
+    const int64_t cap = (int64_t)per_sm * sms < kMaxShares ? (int64_t)per_sm * sms : kMaxShares;
+    return (int)(most < cap ? most : cap);
 }
 
 cudaError_t launch_attn_simt(const AttnProblem& p, cudaStream_t stream);
 // cached attention on the tensor cores: bf16, D 64, 96 or 128
 bool attn_split_supported(const AttnProblem& p);
 cudaError_t launch_attn_split(const AttnProblem& p, cudaStream_t stream);
-// joins the chunks' partial results of the two kernels above
+// joins the partial results of the tiles that the two kernels above cut
 cudaError_t launch_attn_join(const AttnProblem& p, cudaStream_t stream);
 // packed attention on the tensor cores: bf16, D up to 128
 bool attn_prompt_tc_supported(const AttnProblem& p);

@@ -14,6 +14,7 @@ namespace {
 constexpr size_t kAlign = 256;
 constexpr int kMaxHeads = 4096;
 constexpr int kMaxRows = 1 << 30;
+constexpr int kMinShareBlocks = 2;  // of 64 keys: a CTA's start costs about as much
 
 size_t align_up(size_t v) { return (v + kAlign - 1) & ~(kAlign - 1); }
 size_t act_bytes(int act) { return act == GBMOE_F32 ? 4 : 2; }
@@ -79,7 +80,7 @@ Layout layout(const gbattn_config* c) {
     Layout L{};
     size_t o = 0;
     auto take = [&](size_t bytes) { size_t at = o; o = align_up(o + bytes); return at; };
-    const size_t rows = (size_t)split_slots(c->heads_kv) * c->heads_kv * kSplitRows;
+    const size_t rows = (size_t)2 * kMaxShares * kMaxTileRows;
     L.err = take(4);
     L.part_s = take(rows * 16);
     L.part_o = take(rows * c->head_dim * 4);
@@ -218,7 +219,6 @@ int attn_prompt(const gbattn_config* cfg, int32_t Tq, int32_t Tk, int32_t B, con
     AttnProblem p = problem(cfg, Tq, B, q, out, lse, ws);
     p.Tk = Tk; p.cu_q = cu_q; p.cu_k = cu_k; p.R = 1;
     if (Tk > 0) p.k = rows_of(k, Tk, cfg->heads_kv), p.v = rows_of(v, Tk, cfg->heads_kv);
-    p.target = 1; p.min_chunk = INT_MAX;  // one chunk: a prompt has rows enough
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     return cuda_status(attn_prompt_tc_supported(p) ? launch_attn_prompt_tc(p, st) : launch_attn_simt(p, st));
 }
@@ -237,13 +237,10 @@ int attn_cached(const gbattn_config* cfg, int32_t T, const gbattn_batch* batch, 
     p.page = cfg->page; p.max_pages = batch->max_pages; p.n_pages = cache->n_pages;
     p.cu_q = batch->cu_q; p.kv_len = batch->kv_len; p.page_table = batch->page_table;
     p.k_pool = cache->k; p.v_pool = cache->v; p.k_scale = cache->k_scale; p.v_scale = cache->v_scale;
-    p.target = split_target(cfg->heads_kv);
-    p.min_chunk = 256;
+    for (p.page_log2 = 0; 1 << p.page_log2 < p.page;) ++p.page_log2;
+    p.min_blocks = kMinShareBlocks;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (int s = cuda_status(attn_split_supported(p) ? launch_attn_split(p, st) : launch_attn_simt(p, st))) return s;
-    // no sequence can have a second chunk: nothing to join
-    if ((int64_t)p.max_pages * p.page <= p.min_chunk) return GBMOE_OK;
-    return cuda_status(launch_attn_join(p, st));
+    return cuda_status(attn_split_supported(p) ? launch_attn_split(p, st) : launch_attn_simt(p, st));
 }
 
 }  // extern "C"

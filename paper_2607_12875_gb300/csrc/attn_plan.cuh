@@ -1,6 +1,6 @@
 // What the attention kernels share: a sequence's lengths, which keys a row
-// sees, and the list of work items that every CTA derives for itself from the
-// lengths on the device (no host read, no planning launch).
+// sees, and the CTA's part of the work, which every CTA derives for itself from
+// the lengths on the device (no host read, no planning launch).
 #pragma once
 
 #include "attn.h"
@@ -47,127 +47,155 @@ __device__ __forceinline__ void seen_keys(const AttnProblem& p, const Seq& s, in
     if (hi < lo) hi = -1, lo = 0;
 }
 
-// rows of queries (token i, head g of R: row i * R + g) in tiles of kRows
-template <int kRows>
-__device__ __forceinline__ int row_tiles(const AttnProblem& p, const Seq& s) {
-    return (int)(((int64_t)s.nq * p.R + kRows - 1) / kRows);
+// tiles of `rows` rows of queries (token i, head g of R: row i * R + g)
+__device__ __forceinline__ int64_t row_tiles(const AttnProblem& p, const Seq& s, int rows) {
+    return ((int64_t)s.nq * p.R + rows - 1) / rows;
 }
 
-// One work item: a row tile of a sequence and a chunk of its keys.
-struct Item {
-    int b;           // -1: none
-    Seq s;
-    int tile;
-    int k_lo, k_hi;  // keys of the chunk (k_hi exclusive)
-    int chunks;      // chunks of this sequence
-    int64_t slot;    // its partial results' slot (chunks > 1)
+// blocks of kBlockKeys keys of a sequence's tiles (at least one, so that rows
+// without keys are written too)
+__device__ __forceinline__ int key_blocks(const Seq& s) {
+    return max(1, (s.len - min(s.start, s.len) + kBlockKeys - 1) / kBlockKeys);
+}
+
+__device__ __forceinline__ int64_t warp_scan(int64_t v) {  // inclusive
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int64_t a = __shfl_up_sync(0xffffffffu, v, d);
+        if (lane >= d) v += a;
+    }
+    return v;
+}
+
+// Where unit `index` of the list lies whose sequence b holds units(b) units: the
+// sequence (-1: past the end) and the unit's place in it. `index` comes from the
+// list's total, whose loads and sums a batch of at most blockDim sequences
+// shares with the search. For the whole block; sm holds plan_words words.
+struct Place {
+    int b;
+    int64_t at;
+};
+template <typename Units, typename Index>
+__device__ __forceinline__ Place find_place(int B, Units units, Index index_of, int64_t* sm) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = blockDim.x, warps = n >> 5;
+    int64_t* found = sm + warps;
+    if (tid == 0) found[0] = -1;
+    int64_t index = -1, before = 0;
+    if (B > n) {  // the total first
+        int64_t v = 0;
+        for (int b = tid; b < B; b += n) v += units(b);
+        v = warp_scan(v);
+        if (lane == 31) sm[warp] = v;
+        __syncthreads();
+        int64_t total = 0;
+        for (int w = 0; w < warps; ++w) total += sm[w];
+        index = index_of(total);
+        __syncthreads();
+    }
+    for (int base = 0; base < B; base += n) {
+        const int b = base + tid;
+        const int64_t v = b < B ? units(b) : 0;
+        const int64_t pre = warp_scan(v);
+        if (lane == 31) sm[warp] = pre;
+        __syncthreads();
+        int64_t here = before, sum = 0;
+        for (int w = 0; w < warps; ++w) {
+            if (w < warp) here += sm[w];
+            sum += sm[w];
+        }
+        if (B <= n) index = index_of(sum);
+        const int64_t first = here + pre - v;
+        if (index >= first && index < first + v) {
+            found[0] = b;
+            found[1] = index - first;
+        }
+        before += sum;
+        __syncthreads();
+        if (index < before) break;  // uniform
+    }
+    return Place{(int)found[0], found[1]};
+}
+constexpr int plan_words(int threads) { return threads / 32 + 2; }
+
+// Row tile `index` of packed queries (sequences in order, their tiles in order).
+__device__ __forceinline__ Place find_tile(const AttnProblem& p, int64_t index, int rows, int64_t* sm) {
+    return find_place(p.B, [&](int b) { return row_tiles(p, load_seq(p, b), rows); }, [&](int64_t) { return index; }, sm);
+}
+
+// Cached attention: the blocks of keys of all row tiles and kv heads, in the
+// order sequence, head, tile, block, are dealt out in equal shares, one per CTA.
+// A share is a run of segments: blocks blk0 .. blk1 - 1 of one tile and head. A
+// tile that lies whole in a share is finished there; the first and the last
+// segment of a share may be parts of tiles, whose results go to the share's
+// partial slots 2 i and 2 i + 1 for the join.
+struct Shares {
+    int64_t total, each;  // blocks, blocks of a share
+
+    __device__ __forceinline__ void set(const AttnProblem& p, int64_t blocks) {
+        total = blocks;
+        each = max64(p.min_blocks, (blocks + p.shares - 1) / p.shares);
+    }
 };
 
-__device__ __forceinline__ int64_t block_sum(int64_t v, int64_t* sm) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n = blockDim.x >> 5;
-#pragma unroll
-    for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
-    __syncthreads();
-    if (lane == 0) sm[warp] = v;
-    __syncthreads();
-    int64_t t = 0;
-    for (int w = 0; w < n; ++w) t += sm[w];
-    return t;
-}
+struct Segment {
+    int b, head, tile, blk0, blk1, nb;
+    Seq s;
+    int64_t slot;  // -1: whole
+};
 
-// keys per chunk: the items aimed at over all row tiles' keys, in multiples of 128
-__device__ __forceinline__ int chunk_keys(const AttnProblem& p, int64_t work) {
-    int64_t c = (work + p.target - 1) / p.target;
-    c = max64(c, p.min_chunk);
-    return (int)min64((c + 127) & ~(int64_t)127, 0x7fffff80);
-}
+template <int kRows>
+struct Walk {
+    Shares sh;
+    int64_t u, u0, u1;
+    int64_t share;
+    int tiles;
+    Segment g;
 
-// Item `index` of the list (sequences in order; a sequence's tiles; a tile's
-// chunks), found by the whole block: sm holds 2 * warps + 8 words of 64 bits.
-// The number of partial slots before a sequence counts only sequences with
-// several chunks; their slots are at most 2 * target. kSplit: the list of row
-// tiles of such sequences instead (slot: their first chunk's).
-template <int kRows, bool kSplit = false>
-__device__ Item find_item(const AttnProblem& p, int64_t index, int64_t* sm) {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = blockDim.x;
-    int64_t work = 0;
-    for (int b = tid; b < p.B; b += n) {
-        const Seq s = load_seq(p, b);
-        work += (int64_t)row_tiles<kRows>(p, s) * (s.len - min(s.start, s.len));
+    // whether share `index` holds anything (then g is its first segment)
+    __device__ __forceinline__ bool begin(const AttnProblem& p, int64_t index, int64_t* sm) {
+        share = index;
+        const Place at = find_place(
+            p.B, [&](int b) { const Seq s = load_seq(p, b); return row_tiles(p, s, kRows) * key_blocks(s) * p.Hkv; },
+            [&](int64_t total) { sh.set(p, total); return index * sh.each; }, sm);
+        if (at.b < 0) return false;
+        u = u0 = index * sh.each;
+        u1 = min64(u0 + sh.each, sh.total);
+        enter(p, at.b);
+        const int64_t per = (int64_t)tiles * g.nb;
+        g.head = (int)(at.at / per);
+        const int64_t rest = at.at - g.head * per;
+        g.tile = (int)(rest / g.nb);
+        g.blk0 = (int)(rest - (int64_t)g.tile * g.nb);
+        cut();
+        return true;
     }
-    const int C = chunk_keys(p, block_sum(work, sm));
-    int64_t* found = sm + 2 * (n >> 5);  // sequence, items before it, slots before it
-    __syncthreads();
-    if (tid == 0) found[0] = -1;
-    int64_t items0 = 0, slots0 = 0;
-    for (int base = 0; base < p.B; base += n) {
-        const int b = base + tid;
-        int64_t it = 0, sl = 0;
-        if (b < p.B) {
-            const Seq s = load_seq(p, b);
-            const int64_t tiles = row_tiles<kRows>(p, s), eff = s.len - min(s.start, s.len);
-            const int64_t chunks = max64(1, (eff + C - 1) / C);
-            sl = chunks > 1 ? tiles * chunks : 0;
-            it = !kSplit ? tiles * chunks : chunks > 1 ? tiles : 0;
+    __device__ __forceinline__ bool next(const AttnProblem& p) {
+        u += g.blk1 - g.blk0;
+        if (u >= u1) return false;
+        g.blk0 = 0;
+        if (++g.tile == tiles) {
+            g.tile = 0;
+            if (++g.head == p.Hkv) {
+                g.head = 0;
+                int b = g.b;
+                do enter(p, ++b);
+                while (tiles == 0);  // (u < u1 <= total: there is one)
+            }
         }
-        int64_t pi = it, ps = sl;  // inclusive prefix sums in the warp
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int64_t a = __shfl_up_sync(0xffffffffu, pi, d), c = __shfl_up_sync(0xffffffffu, ps, d);
-            if (lane >= d) pi += a, ps += c;
-        }
-        __syncthreads();
-        if (lane == 31) sm[2 * warp] = pi, sm[2 * warp + 1] = ps;
-        __syncthreads();
-        int64_t ti = 0, tsl = 0, wi = items0, wsl = slots0;
-        for (int w = 0; w < (n >> 5); ++w) {
-            if (w < warp) wi += sm[2 * w], wsl += sm[2 * w + 1];
-            ti += sm[2 * w], tsl += sm[2 * w + 1];
-        }
-        const int64_t before = wi + pi - it;
-        if (it > 0 && index >= before && index < before + it) {
-            found[0] = b;
-            found[1] = before;
-            found[2] = wsl + ps - sl;
-        }
-        items0 += ti, slots0 += tsl;
-        __syncthreads();
-        if (index < items0) break;  // uniform
+        cut();
+        return true;
     }
-    __syncthreads();
-    Item r;
-    r.b = (int)found[0];
-    if (r.b < 0) return r;
-    r.s = load_seq(p, r.b);
-    const int64_t eff = r.s.len - min(r.s.start, r.s.len);
-    r.chunks = (int)max64(1, (eff + C - 1) / C);
-    const int64_t local = index - found[1];
-    if (kSplit) {
-        r.tile = (int)local;
-        r.slot = found[2] + local * r.chunks;
-        return r;
+    __device__ __forceinline__ void enter(const AttnProblem& p, int b) {
+        g.b = b;
+        g.s = load_seq(p, b);
+        tiles = (int)row_tiles(p, g.s, kRows);
+        g.nb = key_blocks(g.s);
     }
-    r.tile = (int)(local / r.chunks);
-    const int chunk = (int)(local - (int64_t)r.tile * r.chunks);
-    r.k_lo = (int)min64((int64_t)r.s.start + (int64_t)chunk * C, r.s.len);
-    r.k_hi = (int)min64((int64_t)r.k_lo + C, r.s.len);
-    r.slot = found[2] + local;
-    return r;
-}
-
-// sequence of packed row t (rows outside every sequence: -1): the last b with cu_q[b] <= t
-__device__ __forceinline__ int seq_of_row(const int32_t* cu, int B, int t) {
-    int lo = 0, hi = B;  // cu[lo] <= t < cu[hi] when it lies in one
-    if (t < cu[0] || t >= cu[B]) return -1;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (cu[mid] <= t) lo = mid;
-        else hi = mid;
+    __device__ __forceinline__ void cut() {
+        g.blk1 = (int)min64(g.nb, g.blk0 + (u1 - u));
+        g.slot = g.blk0 == 0 && g.blk1 == g.nb ? -1 : 2 * share + (u != u0);
     }
-    return lo;
-}
-
-// what find_item needs in shared memory for a block of n threads
-constexpr int plan_words(int n) { return 2 * (n / 32) + 8; }
+};
 
 }  // namespace gbmoe

@@ -190,13 +190,12 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int groups = pp.pair_heads ? p.Hq / 2 : p.Hq;
-    const int64_t index = blockIdx.x / groups;
-    const Item it = pp.pair_heads ? find_item<kTile>(p, index, plan) : find_item<2 * kTile>(p, index, plan);
-    if (it.b < 0) return;
-    const Seq& s = it.s;
-    // the last tiles, which see the most keys, first
     const int rows_per = pp.pair_heads ? kTile : 2 * kTile;
-    const int tile = (s.nq + rows_per - 1) / rows_per - 1 - it.tile;
+    const Place at = find_tile(p, blockIdx.x / groups, rows_per, plan);
+    if (at.b < 0) return;
+    const Seq s = load_seq(p, at.b);
+    // the last tiles, which see the most keys, first
+    const int tile = (s.nq + rows_per - 1) / rows_per - 1 - (int)at.at;
     const int head0 = pp.pair_heads ? 2 * (blockIdx.x % groups) : blockIdx.x % groups;
     const int head_kv = head0 / (p.Hq / p.Hkv);
     // query tile t: rows row0(t) .. of the sequence, n_rows(t) of them, and the key tiles 0 .. n_tiles(t) - 1 from k_first on
@@ -505,9 +504,9 @@ cudaError_t prompt_as(const AttnProblem& p, cudaStream_t stream) {
     if (!rows_map(&q, p.q, p.T, p.Hq, p.D) || !rows_map(&k, p.k, p.Tk, p.Hkv, p.D) || !rows_map(&v, p.v, p.Tk, p.Hkv, p.D))
         return cudaErrorInvalidValue;
     Params pp{p, (p.Hq / p.Hkv) % 2 == 0, tc_wait_limit_ns()};
-    const int64_t items = attn_items(p, pp.pair_heads ? kTile : 2 * kTile), groups = pp.pair_heads ? p.Hq / 2 : p.Hq;
-    if (items * groups > INT32_MAX) return cudaErrorInvalidConfiguration;
-    return launch_k(kernel, dim3((unsigned)(items * groups)), dim3(kThreads), Smem<DK>::BYTES, stream, q, k, v, pp);
+    const int64_t grid = (p.T / (pp.pair_heads ? kTile : 2 * kTile) + p.B) * (int64_t)(pp.pair_heads ? p.Hq / 2 : p.Hq);
+    if (grid > INT32_MAX) return cudaErrorInvalidConfiguration;
+    return launch_k(kernel, dim3((unsigned)grid), dim3(kThreads), Smem<DK>::BYTES, stream, q, k, v, pp);
 }
 
 }  // namespace

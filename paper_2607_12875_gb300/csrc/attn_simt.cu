@@ -60,8 +60,7 @@ constexpr size_t kSmem = ((size_t)(2 * kKeys + 16 * N) * kLd<DP> + 16 * N * (kKe
 // keys tx + 8 j, of the result the columns 4 tx + 32 j ..; a row's eight threads
 // lie in one warp.
 template <typename TA, bool kE4m3, int DP, int N>
-__global__ void __launch_bounds__(kThreads) attn_simt_kernel(const AttnProblem p) {
-    pdl_enter();
+__device__ __forceinline__ void attend(const AttnProblem& p, const Segment& it) {
     constexpr int kRows = 16 * N;
     constexpr bool kPaged = N == 1;
     extern __shared__ float4 smem4[];
@@ -70,14 +69,14 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(const AttnProblem p
     float* sv = sk + kKeys * kLd<DP>;
     float* sp = sv + kKeys * kLd<DP>;
     int* ok = reinterpret_cast<int*>(sp + kRows * (kKeys + 1));
-    __shared__ int64_t plan[plan_words(kThreads)];
-    const int G = p.Hq / p.Hkv, heads = kPaged ? p.Hkv : p.Hq;
-    const int head0 = (blockIdx.x % heads) * p.R;  // query head of row 0
-    const int h = head0 / G;                       // kv head
-    const Item it = find_item<kRows>(p, blockIdx.x / heads, plan);
-    if (it.b < 0) return;
-    const int row0 = it.tile * kRows, R = p.R;
+    const int G = p.Hq / p.Hkv, R = p.R;
+    const int head0 = it.head * R;  // query head of row 0
+    const int h = head0 / G;        // kv head
+    const int row0 = it.tile * kRows;
     const int n_rows = (int)min64(kRows, (int64_t)it.s.nq * R - row0);
+    // keys of the segment
+    const int c_lo = (int)min64((int64_t)it.s.start + (int64_t)it.blk0 * kBlockKeys, it.s.len);
+    const int c_hi = (int)min64((int64_t)it.s.start + (int64_t)it.blk1 * kBlockKeys, it.s.len);
 
     const int tid = threadIdx.x, ty = tid >> 3, tx = tid & 7;
     for (int i = tid; i < kRows * (DP / 8); i += kThreads) {
@@ -98,7 +97,7 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(const AttnProblem p
     seen_keys(p, it.s, row0 / R, k_lo, k_hi);
     seen_keys(p, it.s, (row0 + n_rows - 1) / R, last_lo, last_hi);
     if (k_hi < 0) k_lo = 0;
-    k_lo = max(it.k_lo, k_lo), k_hi = min(it.k_hi, last_hi + 1);
+    k_lo = max(c_lo, k_lo), k_hi = min(c_hi, last_hi + 1);
 
     constexpr int NC = DP / 32;  // float4 columns of a thread
     float4 o[N][NC];
@@ -196,8 +195,8 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(const AttnProblem p
         if (rr >= n_rows) continue;
         const int64_t t = it.s.q0 + (row0 + rr) / R;
         const int hq = head0 + (row0 + rr) % R;
-        if (it.chunks > 1) {
-            const int64_t at = (it.slot * p.Hkv + h) * kSplitRows + rr;
+        if (it.slot >= 0) {
+            const int64_t at = it.slot * kRows + rr;
             if (tx == 0) reinterpret_cast<float4*>(p.part_s)[at] = make_float4(m[r], l[r], m[r], 0.0f);
 #pragma unroll
             for (int c = 0; c < NC; ++c)
@@ -222,6 +221,28 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(const AttnProblem p
 }
 
 template <typename TA, bool kE4m3, int DP, int N>
+__global__ void __launch_bounds__(kThreads) attn_simt_kernel(const AttnProblem p) {
+    pdl_enter();
+    __shared__ int64_t plan[plan_words(kThreads)];
+    if constexpr (N == 1) {
+        Walk<16> w;
+        if (!w.begin(p, blockIdx.x, plan)) return;
+        do {
+            attend<TA, kE4m3, DP, N>(p, w.g);
+            __syncthreads();
+        } while (w.next(p));
+    } else {
+        Segment g{};
+        g.head = blockIdx.x % p.Hq;
+        const Place at = find_tile(p, blockIdx.x / p.Hq, 16 * N, plan);
+        if (at.b < 0) return;
+        g.b = at.b, g.s = load_seq(p, at.b), g.tile = (int)at.at;
+        g.blk1 = key_blocks(g.s), g.slot = -1;
+        attend<TA, kE4m3, DP, N>(p, g);
+    }
+}
+
+template <typename TA, bool kE4m3, int DP, int N>
 cudaError_t simt_as(const AttnProblem& p, cudaStream_t stream) {
     constexpr auto kernel = attn_simt_kernel<TA, kE4m3, DP, N>;
     static DeviceOnce once;
@@ -230,9 +251,17 @@ cudaError_t simt_as(const AttnProblem& p, cudaStream_t stream) {
         });
         e != cudaSuccess)
         return e;
-    const int64_t items = attn_items(p, 16 * N), heads = p.paged ? p.Hkv : p.Hq;
-    if (items * heads > INT32_MAX) return cudaErrorInvalidConfiguration;
-    return launch_k(kernel, dim3((unsigned)(items * heads)), dim3(kThreads), kSmem<DP, N>, stream, p);
+    if constexpr (N == 1) {
+        AttnProblem a = p;
+        a.tile_rows = 16;
+        a.shares = shares_of(p, 16, DP == 256 ? 2 : 4, sm_count());
+        if (cudaError_t e = launch_k(kernel, dim3(a.shares), dim3(kThreads), kSmem<DP, N>, stream, a); e != cudaSuccess) return e;
+        return a.shares > 1 ? launch_attn_join(a, stream) : cudaSuccess;
+    } else {
+        const int64_t grid = ((int64_t)p.T / (16 * N) + p.B) * p.Hq;
+        if (grid > INT32_MAX) return cudaErrorInvalidConfiguration;
+        return launch_k(kernel, dim3((unsigned)grid), dim3(kThreads), kSmem<DP, N>, stream, p);
+    }
 }
 
 template <typename TA, bool kE4m3, int N>
@@ -250,81 +279,99 @@ cudaError_t simt_source(const AttnProblem& p, cudaStream_t stream) {
 
 // ------------------------------------------------------------------- join
 //
-// Block (x, y, z): row z of kv head y in the x-th row tile that was split. Its
-// chunks' sums, each relative to 2^(its own third statistic), are brought to
-// the largest of those and added in chunk order, the softmax sums likewise
-// relative to the first: out = sum / l. Threads: 4 columns each, the chunks
-// dealt out over the rest.
+// Block (x, y): where share x ends inside a tile that begins in it, rows 4 y ..
+// of that tile, one per warp. The parts' sums, each relative to 2^(its own
+// third statistic), are brought to the largest of those and added in order, the
+// softmax sums likewise relative to the first statistic: out = sum / l.
 constexpr int kJoinThreads = 128;
 
 template <typename TA>
 __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const AttnProblem p) {
     pdl_enter();
     __shared__ int64_t plan[plan_words(kJoinThreads)];
-    __shared__ float4 acc[kJoinThreads];
-    __shared__ float red[3][kJoinThreads / 32];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const Item it = find_item<kSplitRows, true>(p, blockIdx.x, plan);
-    if (it.b < 0) return;
-    const int G = p.Hq / p.Hkv, h = blockIdx.y, row = it.tile * kSplitRows + blockIdx.z;
-    if (row >= it.s.nq * (int64_t)G) return;
-    const int64_t at0 = (it.slot * p.Hkv + h) * kSplitRows + blockIdx.z, step = (int64_t)p.Hkv * kSplitRows;
+    const int lane = threadIdx.x & 31, rows = p.tile_rows;
+    Shares sh;
+    const Place at = find_place(
+        p.B, [&](int b) { const Seq s = load_seq(p, b); return row_tiles(p, s, rows) * key_blocks(s) * p.Hkv; },
+        [&](int64_t total) { sh.set(p, total); return (blockIdx.x + 1) * sh.each; }, plan);
+    if (at.b < 0) return;
+    const Seq s = load_seq(p, at.b);
+    const int nb = key_blocks(s), tiles = (int)row_tiles(p, s, rows);
+    const int64_t ht = at.at / nb;
+    const int blk = (int)(at.at - ht * nb);
+    if (blk == 0 || blk > sh.each) return;  // the tile begins here, or before this share
+    const int h = (int)(ht / tiles), tile = (int)(ht - (int64_t)h * tiles);
+    const int r = blockIdx.y * (kJoinThreads / 32) + (threadIdx.x >> 5), G = p.R;
+    const int64_t row = (int64_t)tile * rows + r;
+    if (r >= rows || row >= (int64_t)s.nq * G) return;
+    // parts: the end of this share, then the beginnings of the next ones
+    const int64_t i0 = blockIdx.x;
+    const int n = (int)((nb - blk + sh.each - 1) / sh.each) + 1;
+    const bool whole_first = blk == sh.each;  // the tile is all of this share
+    auto slot = [&](int c) { return (c > 0 || whole_first ? 2 * (i0 + c) : 2 * i0 + 1) * rows + r; };
     const float4* st = reinterpret_cast<const float4*>(p.part_s);
-    // maxima of the two statistics
     float m = neg_inf(), mo = neg_inf();
-    for (int c = tid; c < it.chunks; c += kJoinThreads) {
-        const float4 s = st[at0 + c * step];
-        m = fmaxf(m, s.x), mo = fmaxf(mo, s.z);
+    for (int c = lane; c < n; c += 32) {
+        const float4 v = st[slot(c)];
+        m = fmaxf(m, v.x), mo = fmaxf(mo, v.z);
     }
 #pragma unroll
     for (int d = 16; d; d >>= 1) {
         m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
         mo = fmaxf(mo, __shfl_xor_sync(0xffffffffu, mo, d));
     }
-    if (lane == 0) red[0][warp] = m, red[1][warp] = mo;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kJoinThreads / 32; ++w) m = fmaxf(m, red[0][w]), mo = fmaxf(mo, red[1][w]);
     const float base = m == neg_inf() ? 0.0f : m, base_o = mo == neg_inf() ? 0.0f : mo;
-    float l = 0.0f;
-    for (int c = tid; c < it.chunks; c += kJoinThreads) {
-        const float4 s = st[at0 + c * step];
-        l += s.y * exp2f(s.x - base);
+    float l = 0.0f, o[2][4] = {};
+    const int d = 4 * lane;
+    for (int c0 = 0; c0 < n; c0 += 32) {
+        float f = 0.0f;
+        if (c0 + lane < n) {
+            const float4 v = st[slot(c0 + lane)];
+            l += v.y * exp2f(v.x - base);
+            f = exp2f(v.z - base_o);
+        }
+        const int k = min(32, n - c0);
+        for (int c = 0; c < k; c += 4) {  // four parts' loads in flight
+            float4 v[4][2];
+            float w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                w[i] = __shfl_sync(0xffffffffu, f, (c + i) & 31);
+                const float* src = p.part_o + slot(c0 + min(c + i, k - 1)) * p.D + d;
+#pragma unroll
+                for (int z = 0; z < 2; ++z)
+                    v[i][z] = d + 128 * z < p.D ? __ldcg(reinterpret_cast<const float4*>(src + 128 * z)) : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (c + i >= k || w[i] == 0.0f) continue;  // (a part that this row does not see: its sums are 0)
+#pragma unroll
+                for (int z = 0; z < 2; ++z) {
+                    o[z][0] = fmaf(v[i][z].x, w[i], o[z][0]), o[z][1] = fmaf(v[i][z].y, w[i], o[z][1]);
+                    o[z][2] = fmaf(v[i][z].z, w[i], o[z][2]), o[z][3] = fmaf(v[i][z].w, w[i], o[z][3]);
+                }
+            }
+        }
     }
 #pragma unroll
-    for (int d = 16; d; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
-    if (lane == 0) red[2][warp] = l;
-    __syncthreads();
-    l = red[2][0] + red[2][1] + red[2][2] + red[2][3];
-
-    const int cols = p.D / 4, groups = kJoinThreads / cols, g = tid / cols, d = 4 * (tid % cols);
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (g < groups)
-        for (int c = g; c < it.chunks; c += groups) {
-            const float f = exp2f(st[at0 + c * step].z - base_o);
-            if (f == 0.0f) continue;  // a chunk that this row does not see (its sums are 0)
-            const float4 v = *reinterpret_cast<const float4*>(p.part_o + (at0 + c * step) * p.D + d);
-            o.x = fmaf(v.x, f, o.x), o.y = fmaf(v.y, f, o.y), o.z = fmaf(v.z, f, o.z), o.w = fmaf(v.w, f, o.w);
-        }
-    acc[tid] = o;
-    __syncthreads();
-    if (tid >= cols) return;
-    for (int w = 1; w < groups; ++w) {
-        const float4 v = acc[tid + w * cols];
-        o.x += v.x, o.y += v.y, o.z += v.z, o.w += v.w;
-    }
+    for (int e = 16; e; e >>= 1) l += __shfl_xor_sync(0xffffffffu, l, e);
     int lo, hi;
-    seen_keys(p, it.s, row / G, lo, hi);
+    seen_keys(p, s, (int)(row / G), lo, hi);
     const bool empty = hi < lo || (m == neg_inf() && l == 0.0f);
-    const int64_t t = it.s.q0 + row / G;
-    const int hq = h * G + row % G;
-    if (p.lse && tid == 0) p.lse[t * p.Hq + hq] = empty ? neg_inf() : (base + log2f(l)) * kLn2;
+    const int64_t t = s.q0 + row / G;
+    const int hq = h * G + (int)(row % G);
+    if (p.lse && lane == 0) p.lse[t * p.Hq + hq] = empty ? neg_inf() : (base + log2f(l)) * kLn2;
     const float inv = empty ? 0.0f : exp2f(base_o - base) / l;
     TA* out = const_cast<TA*>(static_cast<const TA*>(p.out.p)) + t * p.out.ts + hq * p.out.hs + d;
-    if constexpr (sizeof(TA) == 4)
-        *reinterpret_cast<float4*>(out) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-    else
-        *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
+#pragma unroll
+    for (int z = 0; z < 2; ++z) {
+        if (d + 128 * z >= p.D) break;
+        if constexpr (sizeof(TA) == 4)
+            *reinterpret_cast<float4*>(out + 128 * z) = make_float4(o[z][0] * inv, o[z][1] * inv, o[z][2] * inv, o[z][3] * inv);
+        else
+            *reinterpret_cast<uint2*>(out + 128 * z) =
+                make_uint2(pack_bf16x2(o[z][0] * inv, o[z][1] * inv), pack_bf16x2(o[z][2] * inv, o[z][3] * inv));
+    }
 }
 
 }  // namespace
@@ -334,8 +381,7 @@ cudaError_t launch_attn_simt(const AttnProblem& p, cudaStream_t stream) {
 }
 
 cudaError_t launch_attn_join(const AttnProblem& p, cudaStream_t stream) {
-    const int64_t rows = (int64_t)p.T * (p.Hq / p.Hkv);
-    const dim3 grid((unsigned)min64(p.target, rows / kSplitRows + p.B), p.Hkv, (unsigned)min64(kSplitRows, rows));
+    const dim3 grid(p.shares - 1, (p.tile_rows + kJoinThreads / 32 - 1) / (kJoinThreads / 32));
     return p.act_dtype == GBMOE_F32 ? launch_k(attn_join_kernel<float>, grid, dim3(kJoinThreads), 0, stream, p)
                                     : launch_k(attn_join_kernel<__nv_bfloat16>, grid, dim3(kJoinThreads), 0, stream, p);
 }
