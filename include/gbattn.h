@@ -14,6 +14,7 @@
  *    return a negative status; nothing is written then. Lengths, offsets and
  *    page ids live on the device and are not checked there as errors: offsets
  *    are clamped to the batch, and pages outside the pool are left out.
+ *  - Tables are 16-byte aligned, int32 and fp32 arrays 4-byte aligned.
  *  - q, k, v, out are [tokens, heads, head_dim] with strides (gbattn_rows):
  *    slices of one projection's rows are fine. The head_dim elements are
  *    contiguous; base and strides are multiples of 16 bytes.

@@ -36,7 +36,7 @@ struct AppendProblem {
     RopeParams r;
     int T, B, D, Hq, Hkv;  // Hq 0: no queries
     int act_dtype, e4m3;
-    int page, max_pages, n_pages;
+    int page, page_log2, max_pages, n_pages;
     const int32_t *cu_q, *kv_len, *page_table, *positions;
     Rows q, k, v, q_out, k_out;  // k_out.p may be null
     void *k_pool, *v_pool;

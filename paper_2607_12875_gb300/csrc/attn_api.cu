@@ -14,8 +14,13 @@ namespace {
 constexpr size_t kAlign = 256;
 constexpr int kMaxHeads = 4096;
 constexpr int kMaxRows = 1 << 30;
-constexpr int kMinShareBlocks = 2;  // of 64 keys: a CTA's start costs about as much
+constexpr int kMinShareBlocks = 4;
 
+int log2_of(int v) {
+    int b = 0;
+    while (1 << b < v) ++b;
+    return b;
+}
 size_t align_up(size_t v) { return (v + kAlign - 1) & ~(kAlign - 1); }
 size_t act_bytes(int act) { return act == GBMOE_F32 ? 4 : 2; }
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
@@ -165,7 +170,7 @@ int attn_rope(const gbattn_config* cfg, int32_t T, const gbattn_rows* q, const g
     const bool has_q = q && q->data, has_k = k && k->data;
     if (!has_q && !has_k) return GBMOE_EINVAL;
     if (T == 0) return GBMOE_OK;
-    if (cfg->rotary_dim > 0 && (!positions || !table || !aligned(positions, 4) || !aligned(table, 8))) return GBMOE_EINVAL;
+    if (cfg->rotary_dim > 0 && (!positions || !table || !aligned(positions, 4) || !aligned(table, 16))) return GBMOE_EINVAL;
     if (has_q && (!rows_ok(cfg, q, T, cfg->heads_q, false) || !rows_ok(cfg, q_out, T, cfg->heads_q, true))) return GBMOE_EINVAL;
     if (has_k && (!rows_ok(cfg, k, T, cfg->heads_kv, false) || !rows_ok(cfg, k_out, T, cfg->heads_kv, true)))
         return GBMOE_EINVAL;
@@ -184,7 +189,7 @@ int attn_append(const gbattn_config* cfg, int32_t T, const gbattn_batch* batch, 
     if (int s = check_batch(batch, T)) return s;
     if (T == 0 || batch->B == 0) return GBMOE_OK;
     if (int s = check_cache(cfg, cache)) return s;
-    if (cfg->rotary_dim > 0 && (!table || !aligned(table, 8))) return GBMOE_EINVAL;
+    if (cfg->rotary_dim > 0 && (!table || !aligned(table, 16))) return GBMOE_EINVAL;
     if (positions && !aligned(positions, 4)) return GBMOE_EINVAL;
     if (!rows_ok(cfg, k, T, cfg->heads_kv, false) || !rows_ok(cfg, v, T, cfg->heads_kv, false)) return GBMOE_EINVAL;
     const bool has_q = q_out && q_out->data, has_k = k_out && k_out->data;
@@ -195,6 +200,7 @@ int attn_append(const gbattn_config* cfg, int32_t T, const gbattn_batch* batch, 
     p.T = T; p.B = batch->B; p.D = cfg->head_dim; p.Hkv = cfg->heads_kv;
     p.act_dtype = cfg->act_dtype; p.e4m3 = cfg->cache_dtype == GBATTN_CACHE_E4M3;
     p.page = cfg->page; p.max_pages = batch->max_pages; p.n_pages = cache->n_pages;
+    p.page_log2 = log2_of(p.page);
     p.cu_q = batch->cu_q; p.kv_len = batch->kv_len; p.page_table = batch->page_table; p.positions = positions;
     p.k = rows_of(k, T, cfg->heads_kv);
     p.v = rows_of(v, T, cfg->heads_kv);
@@ -237,7 +243,7 @@ int attn_cached(const gbattn_config* cfg, int32_t T, const gbattn_batch* batch, 
     p.page = cfg->page; p.max_pages = batch->max_pages; p.n_pages = cache->n_pages;
     p.cu_q = batch->cu_q; p.kv_len = batch->kv_len; p.page_table = batch->page_table;
     p.k_pool = cache->k; p.v_pool = cache->v; p.k_scale = cache->k_scale; p.v_scale = cache->v_scale;
-    for (p.page_log2 = 0; 1 << p.page_log2 < p.page;) ++p.page_log2;
+    p.page_log2 = log2_of(p.page);
     p.min_blocks = kMinShareBlocks;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     return cuda_status(attn_split_supported(p) ? launch_attn_split(p, st) : launch_attn_simt(p, st));

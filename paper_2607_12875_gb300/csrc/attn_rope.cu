@@ -5,11 +5,11 @@
 // in turns as a binary fraction of 2^64, so the 64-bit product with the
 // position, wrapped, is the fraction of a turn to 2^-64 * position, whatever
 // the position; its top 32 bits go to sincospif (an error of 2^-25 half turns,
-// below fp32's own on the rotated values). One block computes the angles of its
-// tokens once, in shared memory, for all the heads that it turns.
+// below fp32's own on the rotated values). A thread keeps the angles of its eight
+// pairs of a token in registers and takes them through several heads, so
+// neither kernel has shared memory or a barrier between its loads and its stores.
 //
-// Both kernels are bound by HBM: each element is read once and written once
-// (the append's second walk over its few KB hits the L1 cache).
+// Both kernels are bound by HBM: each element is read once and written once.
 #include <climits>
 
 #include "attn_plan.cuh"
@@ -19,91 +19,138 @@ namespace {
 
 constexpr int kRopeThreads = 256;
 
-// (cos, sin) of pair i at position pos
-__device__ __forceinline__ float2 turn(const RopeParams& r, int64_t pos, int i) {
-    const uint64_t f = (uint64_t)pos * r.table[i];
+// (cos, sin) at position pos of the pair that turns by `entry` per position
+__device__ __forceinline__ float2 turn(const RopeParams& r, int64_t pos, uint64_t entry) {
+    const uint64_t f = (uint64_t)pos * entry;
     float s, c;
     sincospif((float)(int32_t)(f >> 32) * 4.656612873077393e-10f, &s, &c);  // 2^-31: half turns
     return make_float2(c * r.mag, s * r.mag * r.sin_sign);
 }
 
-// A unit of a head: for u < R / 16 the eight pairs 8u .. 8u+7, else eight
-// elements that do not turn. Returns the offset of its second half (-1: none).
-__device__ __forceinline__ int unit_offsets(const RopeParams& r, int u, int& first) {
-    const int nr = r.R >> 4;
-    if (u >= nr) {
-        first = r.R + 8 * (u - nr);
-        return -1;
+// A head's units of 16 elements: R / 16 of eight pairs that turn, then the
+// elements that do not (the last unit may be 8).
+struct Unit {
+    int first, second;  // offsets of its two halves (second -1: none)
+    int index;          // its number; below R / 16: it turns
+};
+__host__ __device__ __forceinline__ int head_units(int R, int D) { return (R >> 4) + ((D - R + 15) >> 4); }
+__device__ __forceinline__ Unit unit_of(const RopeParams& r, int D, int u) {
+    if (u < r.R >> 4) {
+        const int first = r.half ? 8 * u : 16 * u;
+        return Unit{first, r.half ? first + (r.R >> 1) : first + 8, u};
     }
-    first = r.half ? 8 * u : 16 * u;
-    return r.half ? first + (r.R >> 1) : first + 8;
+    const int first = 16 * u;
+    return Unit{first, first + 8 < D ? first + 8 : -1, u};
 }
-__device__ __forceinline__ int head_units(const RopeParams& r, int D) { return (r.R >> 4) + ((D - r.R) >> 3); }
-
-// x (first half), y (second half) turned by the eight angles at cs
-__device__ __forceinline__ void turn8(const RopeParams& r, const float2* cs, float (&x)[8], float (&y)[8]) {
-    if (r.half) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float2 t = cs[j];
-            const float a = x[j], b = y[j];
-            x[j] = a * t.x - b * t.y;
-            y[j] = a * t.y + b * t.x;
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float2 t = cs[j], w = cs[j + 4];
-            float a = x[2 * j], b = x[2 * j + 1];
-            x[2 * j] = a * t.x - b * t.y;
-            x[2 * j + 1] = a * t.y + b * t.x;
-            a = y[2 * j], b = y[2 * j + 1];
-            y[2 * j] = a * w.x - b * w.y;
-            y[2 * j + 1] = a * w.y + b * w.x;
-        }
-    }
+// log2 of the threads that a head's units are dealt to
+__host__ __device__ __forceinline__ int unit_bits(int units) {
+    int b = 0;
+    while (1 << b < units) ++b;
+    return b;
 }
 
-// unit u of a head: src turned to dst
+// The angles of a unit's eight pairs.
+struct Angles {
+    float2 cs[8];
+    __device__ __forceinline__ void set(const RopeParams& r, const Unit& u, int64_t pos) {
+        if (u.index >= r.R >> 4) return;
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+            const ulonglong2 f = *reinterpret_cast<const ulonglong2*>(r.table + 8 * u.index + j);
+            cs[j] = turn(r, pos, f.x);
+            cs[j + 1] = turn(r, pos, f.y);
+        }
+    }
+};
+
+// A unit of one row as loaded (several rows' loads in flight), and widened.
 template <typename TA>
-__device__ __forceinline__ void turn_unit(const RopeParams& r, const float2* cs, int u, const TA* src, TA* dst) {
-    int f;
-    const int s = unit_offsets(r, u, f);
-    float x[8];
-    Vec8<TA>::load(src + f, x);
-    if (s >= 0) {
-        float y[8];
-        Vec8<TA>::load(src + s, y);
-        turn8(r, cs + 8 * u, x, y);
-        Vec8<TA>::store(dst + s, y);
+struct Held {
+    Raw8<TA> a, b;
+    __device__ __forceinline__ void load(const Unit& u, const TA* src) {
+        a.load(src + u.first);
+        if (u.second >= 0) b.load(src + u.second);
     }
-    Vec8<TA>::store(dst + f, x);
-}
+};
+struct Values {
+    float x[8], y[8];
+    template <typename TA>
+    __device__ __forceinline__ void from(const Held<TA>& h, const Unit& u) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = h.a.at(j), y[j] = u.second >= 0 ? h.b.at(j) : 0.0f;
+    }
+    __device__ __forceinline__ void turn(const RopeParams& r, const Unit& u, const Angles& t) {
+        if (u.index >= r.R >> 4) return;
+        if (r.half) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float c = t.cs[j].x, s = t.cs[j].y, a = x[j], b = y[j];
+                x[j] = a * c - b * s;
+                y[j] = a * s + b * c;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float c = t.cs[j].x, s = t.cs[j].y, a = x[2 * j], b = x[2 * j + 1];
+                x[2 * j] = a * c - b * s;
+                x[2 * j + 1] = a * s + b * c;
+                c = t.cs[j + 4].x, s = t.cs[j + 4].y, a = y[2 * j], b = y[2 * j + 1];
+                y[2 * j] = a * c - b * s;
+                y[2 * j + 1] = a * s + b * c;
+            }
+        }
+    }
+    template <typename TA>
+    __device__ __forceinline__ void store(const Unit& u, TA* dst) const {
+        Vec8<TA>::store(dst + u.first, x);
+        if (u.second >= 0) Vec8<TA>::store(dst + u.second, y);
+    }
+};
 
 template <typename TA>
 __device__ __forceinline__ TA* row(const Rows& r, int64_t t, int h) {
     return const_cast<TA*>(static_cast<const TA*>(r.p)) + t * r.ts + h * r.hs;
 }
 
-// Block (x, y): tokens x * tokens .., heads y * heads .. of q and k together.
+// Heads of a thread whose loads are in flight together, on their own and with a
+// key and a value row (8192 tokens, 32 + 8 heads of 128, us: rotation 36 with 4 heads,
+// 33 with 2; append 50 with 4, 55 with 1).
 template <typename TA>
-__global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeProblem p, int tokens, int heads) {
+constexpr int kTurnBatch = sizeof(TA) == 2 ? 2 : 1;
+template <typename TA>
+constexpr int kQueryBatch = sizeof(TA) == 2 ? 4 : 2;
+
+// Block x, y: a thread takes one unit of one token through every `heads`-th head
+// of q and k together, starting at its own. bits: log2 of the threads of a head.
+template <typename TA>
+__global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constant__ RopeProblem p, int bits, int heads) {
     pdl_enter();
-    extern __shared__ float2 cs[];
-    const int t0 = blockIdx.x * tokens, nt = min(tokens, p.T - t0);
-    const int h0 = blockIdx.y * heads, nh = min(heads, p.Hq + p.Hk - h0);
-    const int pairs = p.r.R >> 1;
-    for (int i = threadIdx.x; i < nt * pairs; i += kRopeThreads)
-        cs[i] = turn(p.r, p.positions[t0 + i / pairs], i % pairs);
-    __syncthreads();
-    const int nu = head_units(p.r, p.D), per = nh * nu;
-    for (int i = threadIdx.x; i < nt * per; i += kRopeThreads) {
-        const int t = i / per, w = i - t * per, h = h0 + w / nu, u = w % nu;
-        const bool is_q = h < p.Hq;
-        const Rows& src = is_q ? p.q : p.k;
-        const Rows& dst = is_q ? p.q_out : p.k_out;
-        const int hh = is_q ? h : h - p.Hq;
-        turn_unit<TA>(p.r, cs + t * pairs, u, row<TA>(src, t0 + t, hh), row<TA>(dst, t0 + t, hh));
+    constexpr int B = kTurnBatch<TA>;
+    const int64_t i = (int64_t)blockIdx.x * kRopeThreads + threadIdx.x;
+    const int u = (int)i & ((1 << bits) - 1);
+    const int64_t rest = i >> bits;
+    const int t = (int)(rest / heads), h0 = (int)(rest - (int64_t)t * heads), H = p.Hq + p.Hk;
+    if (t >= p.T || u >= head_units(p.r.R, p.D)) return;
+    const Unit unit = unit_of(p.r, p.D, u);
+    const int64_t pos = p.r.R > 0 ? p.positions[t] : 0;
+    Angles angles;
+    for (int h = h0; h < H; h += B * heads) {
+        Held<TA> held[B];
+#pragma unroll
+        for (int k = 0; k < B; ++k) {
+            const int hh = h + k * heads;
+            if (hh < H) held[k].load(unit, hh < p.Hq ? row<TA>(p.q, t, hh) : row<TA>(p.k, t, hh - p.Hq));
+        }
+        if (h == h0) angles.set(p.r, unit, pos);  // computed while the first loads are in flight
+#pragma unroll
+        for (int k = 0; k < B; ++k) {
+            const int hh = h + k * heads;
+            if (hh >= H) break;
+            Values v;
+            v.from(held[k], unit);
+            v.turn(p.r, unit, angles);
+            v.store(unit, hh < p.Hq ? row<TA>(p.q_out, t, hh) : row<TA>(p.k_out, t, hh - p.Hq));
+        }
     }
 }
 
@@ -131,24 +178,23 @@ __device__ __forceinline__ uint2 e4m3x8(const float (&v)[8], float s) {
                       e4m3x2(v[4] * s, v[5] * s) | e4m3x2(v[6] * s, v[7] * s) << 16);
 }
 
-__device__ __forceinline__ float max_finite(float m, const float (&v)[8]) {
+// maximum of |v| and m, infinities and NaN left out where `careful` (else NaN alone)
+__device__ __forceinline__ float max_abs(float m, const Values& v, bool careful) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        const float a = fabsf(v[j]);
-        m = a <= 3.402823466e38f ? fmaxf(m, a) : m;  // (false for NaN)
+        const float a = fabsf(v.x[j]), b = fabsf(v.y[j]);
+        if (!careful) {
+            m = fmaxf(m, fmaxf(a, b));
+        } else {
+            m = a <= 3.402823466e38f ? fmaxf(m, a) : m;  // (false for NaN)
+            m = b <= 3.402823466e38f ? fmaxf(m, b) : m;
+        }
     }
     return m;
 }
 
-__device__ __forceinline__ float block_max(float m, float* sm) {
-#pragma unroll
-    for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) sm[threadIdx.x >> 5] = m;
-    __syncthreads();
-    for (int w = 0; w < (int)(blockDim.x >> 5); ++w) m = fmaxf(m, sm[w]);
-    return m;
-}
+template <bool kWarpTeam>
+constexpr int kAppendThreads = kWarpTeam ? 256 : 512;  // at most
 
 // A segment: the new tokens of one sequence that fall into one of its pages.
 struct Segment {
@@ -157,226 +203,248 @@ struct Segment {
     int page, off;  // pool page (-1: not stored) and slot of the first one
 };
 
-// Segment `index` (sequences in order, a sequence's pages in order), found by
-// the whole block; sm holds warps + 4 words. n = 0: none.
-__device__ Segment find_segment(const AppendProblem& p, int64_t index, int64_t* sm) {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nthr = blockDim.x;
-    int64_t* found = sm + (nthr >> 5);
-    if (tid == 0) found[0] = -1;
+// Segment `index` (sequences in order, a sequence's pages in order). n = 0: none.
+__device__ __forceinline__ Segment find_segment(const AppendProblem& p, int64_t index, int64_t* sm) {
     auto bounds = [&](int b, int& q0, int& n, int64_t& pos0) {
         q0 = min(max(p.cu_q[b], 0), p.T);
         n = min(max(p.cu_q[b + 1], q0), p.T) - q0;
         pos0 = (int64_t)p.kv_len[b] - n;
     };
-    auto page_of = [&](int64_t pos) { return pos >= 0 ? pos / p.page : -1 - (-1 - pos) / p.page; };
-    int64_t before = 0;
-    for (int base = 0; base < p.B; base += nthr) {
-        const int b = base + tid;
-        int64_t segs = 0;
-        if (b < p.B) {
+    const int bits = p.page_log2;  // (shifts: pages before position 0 are negative)
+    Segment s{};
+    const Place at = find_place(
+        p.B,
+        [&](int b) {
             int q0, n;
             int64_t pos0;
             bounds(b, q0, n, pos0);
-            if (n > 0) segs = page_of(pos0 + n - 1) - page_of(pos0) + 1;
-        }
-        int64_t pre = segs;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int64_t a = __shfl_up_sync(0xffffffffu, pre, d);
-            if (lane >= d) pre += a;
-        }
-        __syncthreads();
-        if (lane == 31) sm[warp] = pre;
-        __syncthreads();
-        int64_t w0 = before;
-        for (int w = 0; w < (nthr >> 5); ++w) {
-            if (w < warp) w0 += sm[w];
-            before += sm[w];
-        }
-        if (segs > 0 && index >= w0 + pre - segs && index < w0 + pre) {
-            found[0] = b;
-            found[1] = w0 + pre - segs;
-        }
-        __syncthreads();
-        if (index < before) break;  // uniform
-    }
-    __syncthreads();
-    Segment s{};
-    const int b = (int)found[0];
-    if (b < 0) return s;
+            return n > 0 ? ((pos0 + n - 1) >> bits) - (pos0 >> bits) + 1 : 0;
+        },
+        [&](int64_t) { return index; }, sm);
+    if (at.b < 0) return s;
     int q0, n;
     int64_t pos0;
-    bounds(b, q0, n, pos0);
-    const int64_t pg = page_of(pos0) + (index - found[1]);
-    const int64_t from = max64(pos0, pg * p.page), to = min64(pos0 + n, (pg + 1) * p.page);
+    bounds(at.b, q0, n, pos0);
+    const int64_t pg = (pos0 >> bits) + at.at;
+    const int64_t from = max64(pos0, pg << bits), to = min64(pos0 + n, (pg + 1) << bits);
     s.t0 = q0 + (int)(from - pos0);
     s.n = (int)(to - from);
     s.pos = from;
-    s.off = (int)(from - pg * p.page);
+    s.off = (int)(from - (pg << bits));
     s.page = -1;
     if (pg >= 0 && pg < p.max_pages) {
-        const int id = p.page_table[(int64_t)b * p.max_pages + pg];
+        const int id = p.page_table[(int64_t)at.b * p.max_pages + pg];
         if (id >= 0 && id < p.n_pages) s.page = id;
     }
     return s;
 }
 
-// The segment's rows of one head of k (kTurn) or v to the cache in e4m3.
-template <typename TA, bool kTurn>
-__device__ void append_e4m3(const AppendProblem& p, const RopeParams& r, const Segment& s, const float2* cs, const Rows& src,
-                            int h, uint8_t* pool, uint8_t* scale, const Rows* out, float* sm) {
-    const int nu = head_units(r, p.D), pairs = r.R >> 1, nthr = blockDim.x;
-    const int64_t head = (int64_t)s.page * p.Hkv + h;
-    uint8_t* codes = pool + head * p.page * p.D;
-    float amax = 0.0f;
-    for (int i = threadIdx.x; i < s.n * nu; i += nthr) {
-        const int t = i / nu, u = i - t * nu;
-        const TA* x = row<TA>(src, s.t0 + t, h);
-        int f;
-        const int f2 = unit_offsets(r, u, f);
-        float a[8];
-        Vec8<TA>::load(x + f, a);
-        if (kTurn && f2 >= 0) {
-            float b[8];
-            Vec8<TA>::load(x + f2, b);
-            turn8(r, cs + t * pairs + 8 * u, a, b);
-            amax = max_finite(amax, b);
+// The threads that share a task: a warp, or the whole block.
+template <bool kWarpTeam>
+struct Team {
+    int rank, size;
+    float2* sm;  // block: one word per warp and value
+    __device__ __forceinline__ Team(float2* s)
+        : rank(kWarpTeam ? threadIdx.x & 31 : threadIdx.x), size(kWarpTeam ? 32 : blockDim.x), sm(s) {}
+    // maxima of the team's a and b, to every thread
+    __device__ __forceinline__ void max(float& a, float& b) const {
+#pragma unroll
+        for (int d = 16; d; d >>= 1) {
+            a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, d));
+            b = fmaxf(b, __shfl_xor_sync(0xffffffffu, b, d));
         }
-        amax = max_finite(amax, a);
+        if (kWarpTeam) return;
+        __syncthreads();
+        if ((threadIdx.x & 31) == 0) sm[threadIdx.x >> 5] = make_float2(a, b);
+        __syncthreads();
+        for (int w = 0; w < (int)(blockDim.x >> 5); ++w) a = fmaxf(a, sm[w].x), b = fmaxf(b, sm[w].y);
     }
-    const int need = scale_exponent(block_max(amax, sm));
-    int e = need;
-    if (s.off > 0) {
-        const int old = (int)scale[head] - 127;  // (every thread reads it before the barrier below)
-        e = max(old, need);
-        if (e > old) {  // the earlier tokens' codes to the new scale
-            const float g = old - e >= -126 ? pow2(old - e) : 0.0f;
-            for (int i = threadIdx.x; i < s.off * p.D / 8; i += nthr) {
-                uint2 c = reinterpret_cast<uint2*>(codes)[i];
-                const float2 v0 = e4m3x2_to_f32x2(c.x & 0xffffu), v1 = e4m3x2_to_f32x2(c.x >> 16);
-                const float2 v2 = e4m3x2_to_f32x2(c.y & 0xffffu), v3 = e4m3x2_to_f32x2(c.y >> 16);
-                const float v[8] = {v0.x, v0.y, v1.x, v1.y, v2.x, v2.y, v3.x, v3.y};
-                reinterpret_cast<uint2*>(codes)[i] = e4m3x8(v, g);
+};
+
+// The scale of one page and head that covers amax too, the page's earlier codes
+// brought to it; returns the factor of the new values.
+template <bool kWarpTeam>
+__device__ __forceinline__ float rescale(const AppendProblem& p, const Segment& s, uint8_t* codes, uint8_t* scale, int old,
+                                         float amax, const Team<kWarpTeam>& team) {
+    const int e = ::max(old, scale_exponent(amax));
+    if (s.off > 0 && e > old) {
+        const float f = old - e >= -126 ? pow2(old - e) : 0.0f;
+        for (int i = team.rank; i < s.off * p.D / 8; i += team.size) {
+            const uint2 c = reinterpret_cast<uint2*>(codes)[i];
+            const float2 v0 = e4m3x2_to_f32x2(c.x & 0xffffu), v1 = e4m3x2_to_f32x2(c.x >> 16);
+            const float2 v2 = e4m3x2_to_f32x2(c.y & 0xffffu), v3 = e4m3x2_to_f32x2(c.y >> 16);
+            const float w[8] = {v0.x, v0.y, v1.x, v1.y, v2.x, v2.y, v3.x, v3.y};
+            reinterpret_cast<uint2*>(codes)[i] = e4m3x8(w, f);
+        }
+    }
+    if (team.rank == 0) *scale = (uint8_t)(e + 127);
+    return pow2(-e);  // (e >= -127: at most 2^127)
+}
+
+// A segment's keys and values of kv head h to the cache, its keys to k_out and the
+// query heads of the group to q_out. A thread has one unit of every step-th
+// token. e4m3: up to kHeld tokens of a thread stay in registers between the
+// search for the maximum and the rounding; longer segments are read twice.
+template <typename TA, bool kE4m3, bool kWarpTeam>
+__device__ __forceinline__ void append_head(const AppendProblem& p, const Segment& s, int h, const Team<kWarpTeam>& team) {
+    constexpr int kHeld = 1, B = kQueryBatch<TA>;
+    const int units = head_units(p.r.R, p.D), bits = unit_bits(units);
+    const int u = team.rank & ((1 << bits) - 1), step = team.size >> bits, first = team.rank >> bits;
+    const int n = u < units ? s.n : 0;  // (threads without a unit have no rows)
+    const Unit unit = unit_of(p.r, p.D, u);
+    const int G = p.Hq / p.Hkv;
+    const bool stored = s.page >= 0;
+    const int64_t head = (int64_t)s.page * p.Hkv + h, slot0 = (head * p.page + s.off) * p.D;
+    int old_k = -127, old_v = -127;
+    if (kE4m3 && stored && s.off > 0) old_k = (int)p.k_scale[head] - 127, old_v = (int)p.v_scale[head] - 127;
+    Values kv[kHeld];
+    Held<TA> vh[kHeld];
+    const bool once = s.n <= kHeld * step;
+    float top_k = 0.0f, top_v = 0.0f;
+    auto load = [&](int t0, bool rest) {  // rest: queries and k_out too
+        Held<TA> kh[kHeld];
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k) {
+            if (t0 + k * step >= n) break;
+            kh[k].load(unit, row<TA>(p.k, s.t0 + t0 + k * step, h));
+            vh[k].load(unit, row<TA>(p.v, s.t0 + t0 + k * step, h));
+        }
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k) {
+            const int t = t0 + k * step, tok = s.t0 + t;
+            if (t >= n) break;
+            Angles angles;
+            bool ready = false;
+            if (rest)
+                for (int g0 = 0; g0 < G; g0 += B) {
+                    Held<TA> q[B];
+#pragma unroll
+                    for (int g = 0; g < B; ++g)
+                        if (g0 + g < G) q[g].load(unit, row<TA>(p.q, tok, h * G + g0 + g));
+                    if (!ready) angles.set(p.r, unit, p.positions ? (int64_t)p.positions[tok] : s.pos + t);
+                    ready = true;
+#pragma unroll
+                    for (int g = 0; g < B; ++g) {
+                        if (g0 + g >= G) break;
+                        Values w;
+                        w.from(q[g], unit);
+                        w.turn(p.r, unit, angles);
+                        w.store(unit, row<TA>(p.q_out, tok, h * G + g0 + g));
+                    }
+                }
+            if (!ready) angles.set(p.r, unit, p.positions ? (int64_t)p.positions[tok] : s.pos + t);
+            kv[k].from(kh[k], unit);
+            kv[k].turn(p.r, unit, angles);
+            if (rest && p.k_out.p) kv[k].store(unit, row<TA>(p.k_out, tok, h));
+        }
+    };
+    auto maxima = [&](int t0, bool careful) {
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k) {
+            if (t0 + k * step >= n) break;
+            Values w;
+            w.from(vh[k], unit);
+            top_k = max_abs(top_k, kv[k], careful);
+            top_v = max_abs(top_v, w, careful);
+        }
+    };
+    auto write = [&](int t0, float inv_k, float inv_v) {
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k) {
+            const int t = t0 + k * step;
+            if (t >= n) break;
+            Values w;
+            w.from(vh[k], unit);
+            if constexpr (kE4m3) {
+                uint8_t* dk = static_cast<uint8_t*>(p.k_pool) + slot0 + t * p.D;
+                uint8_t* dv = static_cast<uint8_t*>(p.v_pool) + slot0 + t * p.D;
+                *reinterpret_cast<uint2*>(dk + unit.first) = e4m3x8(kv[k].x, inv_k);
+                *reinterpret_cast<uint2*>(dv + unit.first) = e4m3x8(w.x, inv_v);
+                if (unit.second < 0) continue;
+                *reinterpret_cast<uint2*>(dk + unit.second) = e4m3x8(kv[k].y, inv_k);
+                *reinterpret_cast<uint2*>(dv + unit.second) = e4m3x8(w.y, inv_v);
+            } else {
+                kv[k].store(unit, static_cast<TA*>(p.k_pool) + slot0 + t * p.D);
+                w.store(unit, static_cast<TA*>(p.v_pool) + slot0 + t * p.D);
             }
         }
-        __syncthreads();
+    };
+    for (int t0 = first; t0 < n; t0 += kHeld * step) {
+        load(t0, true);
+        if (kE4m3) maxima(t0, false);
+        else if (stored) write(t0, 1.0f, 1.0f);
     }
-    if (threadIdx.x == 0) scale[head] = (uint8_t)(e + 127);
-    // 2^-e in two factors: 2^127 at e = -127 is a float, 2^-e never overflows
-    const float inv = pow2(-e);
-    for (int i = threadIdx.x; i < s.n * nu; i += nthr) {
-        const int t = i / nu, u = i - t * nu;
-        const TA* x = row<TA>(src, s.t0 + t, h);
-        uint8_t* dst = codes + (int64_t)(s.off + t) * p.D;
-        int f;
-        const int f2 = unit_offsets(r, u, f);
-        float a[8];
-        Vec8<TA>::load(x + f, a);
-        if (kTurn && f2 >= 0) {
-            float b[8];
-            Vec8<TA>::load(x + f2, b);
-            turn8(r, cs + t * pairs + 8 * u, a, b);
-            *reinterpret_cast<uint2*>(dst + f2) = e4m3x8(b, inv);
-            if (out) Vec8<TA>::store(row<TA>(*out, s.t0 + t, h) + f2, b);
+    if constexpr (kE4m3) {
+        if (!stored) return;  // (uniform)
+        team.max(top_k, top_v);
+        if (top_k > 3.402823466e38f || top_v > 3.402823466e38f) {  // an infinity: once more without
+            top_k = top_v = 0.0f;
+            for (int t0 = first; t0 < n; t0 += kHeld * step) {
+                if (!once) load(t0, false);
+                maxima(t0, true);
+            }
+            team.max(top_k, top_v);
         }
-        *reinterpret_cast<uint2*>(dst + f) = e4m3x8(a, inv);
-        if (out) Vec8<TA>::store(row<TA>(*out, s.t0 + t, h) + f, a);
-    }
-}
-
-// The same to a cache of the activations' type, and for rows that are only
-// turned (pool null): one walk.
-template <typename TA>
-__device__ void append_plain(const AppendProblem& p, const RopeParams& r, const Segment& s, const float2* cs, const Rows& src,
-                             int h, TA* pool, const Rows* out) {
-    const int nu = head_units(r, p.D), pairs = r.R >> 1;
-    TA* dst0 = pool ? pool + (((int64_t)s.page * p.Hkv + h) * p.page + s.off) * p.D : nullptr;
-    for (int i = threadIdx.x; i < s.n * nu; i += blockDim.x) {
-        const int t = i / nu, u = i - t * nu;
-        const TA* x = row<TA>(src, s.t0 + t, h);
-        int f;
-        const int f2 = unit_offsets(r, u, f);
-        float a[8], b[8];
-        Vec8<TA>::load(x + f, a);
-        if (f2 >= 0) {
-            Vec8<TA>::load(x + f2, b);
-            turn8(r, cs + t * pairs + 8 * u, a, b);
-        }
-        TA* o = out ? row<TA>(*out, s.t0 + t, h) : nullptr;
-        TA* dst = dst0 ? dst0 + (int64_t)t * p.D : nullptr;
-        if (dst) Vec8<TA>::store(dst + f, a);
-        if (o) Vec8<TA>::store(o + f, a);
-        if (f2 >= 0) {
-            if (dst) Vec8<TA>::store(dst + f2, b);
-            if (o) Vec8<TA>::store(o + f2, b);
+        // (the maxima's exchange has come after every thread's read of the old scales)
+        uint8_t* page = static_cast<uint8_t*>(p.k_pool) + head * p.page * p.D;
+        const float inv_k = rescale(p, s, page, p.k_scale + head, old_k, top_k, team);
+        page = static_cast<uint8_t*>(p.v_pool) + head * p.page * p.D;
+        const float inv_v = rescale(p, s, page, p.v_scale + head, old_v, top_v, team);
+        for (int t0 = first; t0 < n; t0 += kHeld * step) {
+            if (!once) load(t0, false);
+            write(t0, inv_k, inv_v);
         }
     }
 }
 
-// Block x: segment x / Hkv, kv head x % Hkv: its keys and values, and the query heads
-// of its group. One block owns a page and head, so its scale needs no atomics.
-template <typename TA>
-__global__ void __launch_bounds__(kRopeThreads) append_kernel(const AppendProblem p) {
+// Block x: segment x / Hkv, kv head x % Hkv by the whole block; or (kWarpTeam, few
+// tokens per sequence) segment x, its kv heads dealt to the warps. One team owns
+// a page and head, so its scale needs no atomics.
+template <typename TA, bool kE4m3, bool kWarpTeam>
+__global__ void __launch_bounds__(kAppendThreads<kWarpTeam>, 1) append_kernel(const __grid_constant__ AppendProblem p) {
     pdl_enter();
-    extern __shared__ float2 cs[];
-    __shared__ int64_t plan[kRopeThreads / 32 + 4];
-    __shared__ float red[kRopeThreads / 32];
-    const Segment s = find_segment(p, blockIdx.x / p.Hkv, plan);
+    constexpr int kThreads = kAppendThreads<kWarpTeam>;
+    __shared__ int64_t plan[plan_words(kThreads)];
+    __shared__ float2 red[kThreads / 32];
+    const Segment s = find_segment(p, kWarpTeam ? blockIdx.x : blockIdx.x / p.Hkv, plan);
     if (s.n == 0) return;
-    const int h = blockIdx.x % p.Hkv, pairs = p.r.R >> 1;
-    for (int i = threadIdx.x; i < s.n * pairs; i += blockDim.x) {
-        const int t = i / pairs;
-        cs[i] = turn(p.r, p.positions ? (int64_t)p.positions[s.t0 + t] : s.pos + t, i - t * pairs);
-    }
-    __syncthreads();
-    RopeParams still = p.r;  // values do not turn
-    still.R = 0;
-    const Rows* k_out = p.k_out.p ? &p.k_out : nullptr;
-    if (s.page < 0) {
-        if (k_out) append_plain<TA>(p, p.r, s, cs, p.k, h, nullptr, k_out);
-    } else if (p.e4m3) {
-        append_e4m3<TA, true>(p, p.r, s, cs, p.k, h, static_cast<uint8_t*>(p.k_pool), p.k_scale, k_out, red);
-        append_e4m3<TA, false>(p, still, s, cs, p.v, h, static_cast<uint8_t*>(p.v_pool), p.v_scale, nullptr, red);
+    const Team<kWarpTeam> team(red);
+    if constexpr (kWarpTeam) {
+        for (int h = threadIdx.x >> 5; h < p.Hkv; h += blockDim.x / 32) append_head<TA, kE4m3, true>(p, s, h, team);
     } else {
-        append_plain<TA>(p, p.r, s, cs, p.k, h, static_cast<TA*>(p.k_pool), k_out);
-        append_plain<TA>(p, still, s, cs, p.v, h, static_cast<TA*>(p.v_pool), nullptr);
-    }
-    if (p.Hq) {
-        const int G = p.Hq / p.Hkv;
-        for (int g = 0; g < G; ++g) append_plain<TA>(p, p.r, s, cs, p.q, h * G + g, nullptr, &p.q_out);
+        append_head<TA, kE4m3, false>(p, s, blockIdx.x % p.Hkv, team);
     }
 }
 
 template <typename TA>
 cudaError_t rope_as(const RopeProblem& p, cudaStream_t stream) {
-    const int H = p.Hq + p.Hk, nu = p.r.R / 16 + (p.D - p.r.R) / 8;
-    // about 1024 units of work per block, fewer where that would leave SMs idle
-    int tokens = 1024 / (H * nu) > 1 ? 1024 / (H * nu) : 1;
-    while (tokens > 1 && (p.T + tokens - 1) / tokens < 2 * sm_count()) tokens /= 2;
+    const int H = p.Hq + p.Hk, bits = unit_bits(head_units(p.r.R, p.D));
+    // Threads of a token over its heads: a thread's angles cost about as much as four
+    // units of work, so it takes as many heads as leave 1024 threads for each SM.
     int heads = H;
-    while (heads > 1 && (int64_t)((p.T + tokens - 1) / tokens) * ((H + heads - 1) / heads) < 2 * sm_count() &&
-           heads * nu * tokens > kRopeThreads)
-        heads = (heads + 1) / 2;
-    const size_t smem = (size_t)tokens * (p.r.R / 2) * sizeof(float2);
-    return launch_k(rope_kernel<TA>, dim3((p.T + tokens - 1) / tokens, (H + heads - 1) / heads), dim3(kRopeThreads), smem,
-                    stream, p, tokens, heads);
+    while (heads > 1 && ((int64_t)p.T * ((heads + 1) / 2) << bits) >= (int64_t)1024 * sm_count()) heads = (heads + 1) / 2;
+    const int64_t grid = (((int64_t)p.T * heads << bits) + kRopeThreads - 1) / kRopeThreads;
+    if (grid > INT32_MAX) return cudaErrorInvalidConfiguration;
+    return launch_k(rope_kernel<TA>, dim3((unsigned)grid), dim3(kRopeThreads), 0, stream, p, bits, heads);
+}
+
+template <typename TA, bool kE4m3, bool kWarpTeam>
+cudaError_t append_as(const AppendProblem& p, cudaStream_t stream) {
+    const int64_t segs = min64(p.T, (int64_t)p.T / p.page + 2 * (int64_t)p.B);
+    const int64_t grid = kWarpTeam ? segs : segs * p.Hkv;
+    if (grid > INT32_MAX) return cudaErrorInvalidConfiguration;
+    // a thread for each unit of a page's tokens, or a warp for each head
+    int threads = kWarpTeam ? 32 * p.Hkv : p.page << unit_bits(head_units(p.r.R, p.D));
+    threads = threads < 64 ? 64 : threads < kAppendThreads<kWarpTeam> ? threads : kAppendThreads<kWarpTeam>;
+    return launch_k(append_kernel<TA, kE4m3, kWarpTeam>, dim3((unsigned)grid), dim3((unsigned)threads), 0, stream, p);
 }
 
 template <typename TA>
-cudaError_t append_as(const AppendProblem& p, cudaStream_t stream) {
-    const int most = p.page < p.T ? p.page : p.T;  // tokens of a segment
-    const size_t smem = (size_t)most * (p.r.R / 2) * sizeof(float2);
-    static DeviceOnce once;
-    if (cudaError_t e = once.run([] {
-            return cudaFuncSetAttribute(append_kernel<TA>, cudaFuncAttributeMaxDynamicSharedMemorySize, 128 * 128 * 8);
-        });
-        e != cudaSuccess)
-        return e;
-    const int64_t segs = min64(p.T, (int64_t)p.T / p.page + 2 * (int64_t)p.B);
-    // few tokens per sequence: half the threads would have nothing to do
-    const int threads = p.T <= 4 * (int64_t)p.B ? 128 : kRopeThreads;
-    if (segs * p.Hkv > INT32_MAX) return cudaErrorInvalidConfiguration;
-    return launch_k(append_kernel<TA>, dim3((unsigned)(segs * p.Hkv)), dim3(threads), smem, stream, p);
+cudaError_t append_type(const AppendProblem& p, cudaStream_t stream) {
+    // few tokens per sequence: a head is a warp's work
+    const bool few = p.T <= 4 * (int64_t)p.B;
+    if (p.e4m3) return few ? append_as<TA, true, true>(p, stream) : append_as<TA, true, false>(p, stream);
+    return few ? append_as<TA, false, true>(p, stream) : append_as<TA, false, false>(p, stream);
 }
 
 }  // namespace
@@ -386,7 +454,7 @@ cudaError_t launch_rope(const RopeProblem& p, cudaStream_t stream) {
 }
 
 cudaError_t launch_append(const AppendProblem& p, cudaStream_t stream) {
-    return p.act_dtype == GBMOE_F32 ? append_as<float>(p, stream) : append_as<__nv_bfloat16>(p, stream);
+    return p.act_dtype == GBMOE_F32 ? append_type<float>(p, stream) : append_type<__nv_bfloat16>(p, stream);
 }
 
 }  // namespace gbmoe

@@ -279,98 +279,130 @@ cudaError_t simt_source(const AttnProblem& p, cudaStream_t stream) {
 
 // ------------------------------------------------------------------- join
 //
-// Block (x, y): where share x ends inside a tile that begins in it, rows 4 y ..
-// of that tile, one per warp. The parts' sums, each relative to 2^(its own
-// third statistic), are brought to the largest of those and added in order, the
-// softmax sums likewise relative to the first statistic: out = sum / l.
-constexpr int kJoinThreads = 128;
+// Block x: where share x ends inside a tile that begins in it, that tile. The
+// parts' sums, each relative to 2^(its own third statistic), are brought to the
+// largest of those and added, the softmax sums likewise relative to the first
+// statistic: out = sum / l. A row has as many of the eight warps as there are to
+// spare, each adding every so many parts; the order is fixed by the lengths.
+// The search for the tile reads only what the kernel before this launch's
+// predecessor has written, so it runs before the wait for that one.
+constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32;
 
 template <typename TA>
-__global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const AttnProblem p) {
-    pdl_enter();
+__global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const __grid_constant__ AttnProblem p) {
     __shared__ int64_t plan[plan_words(kJoinThreads)];
-    const int lane = threadIdx.x & 31, rows = p.tile_rows;
+    __shared__ float4 acc[kJoinWarps][64];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rows = p.tile_rows;
     Shares sh;
     const Place at = find_place(
         p.B, [&](int b) { const Seq s = load_seq(p, b); return row_tiles(p, s, rows) * key_blocks(s) * p.Hkv; },
         [&](int64_t total) { sh.set(p, total); return (blockIdx.x + 1) * sh.each; }, plan);
-    if (at.b < 0) return;
-    const Seq s = load_seq(p, at.b);
-    const int nb = key_blocks(s), tiles = (int)row_tiles(p, s, rows);
-    const int64_t ht = at.at / nb;
-    const int blk = (int)(at.at - ht * nb);
-    if (blk == 0 || blk > sh.each) return;  // the tile begins here, or before this share
-    const int h = (int)(ht / tiles), tile = (int)(ht - (int64_t)h * tiles);
-    const int r = blockIdx.y * (kJoinThreads / 32) + (threadIdx.x >> 5), G = p.R;
-    const int64_t row = (int64_t)tile * rows + r;
-    if (r >= rows || row >= (int64_t)s.nq * G) return;
+    Seq s{};
+    int nb = 1, blk = 0, h = 0, tile = 0;
+    if (at.b >= 0) {
+        s = load_seq(p, at.b);
+        nb = key_blocks(s);
+        const int tiles = (int)row_tiles(p, s, rows);
+        const int64_t ht = at.at / nb;
+        blk = (int)(at.at - ht * nb);
+        h = (int)(ht / tiles), tile = (int)(ht - (int64_t)h * tiles);
+    }
+    pdl_enter();
+    if (blk == 0 || blk > sh.each) return;  // no tile, or it begins here, or before this share
+    const int G = p.R;
+    const int n_rows = (int)min64(rows, (int64_t)s.nq * G - (int64_t)tile * rows);
+    const int per = n_rows <= 1 ? 8 : n_rows <= 2 ? 4 : n_rows <= 4 ? 2 : 1;  // warps of a row
     // parts: the end of this share, then the beginnings of the next ones
     const int64_t i0 = blockIdx.x;
     const int n = (int)((nb - blk + sh.each - 1) / sh.each) + 1;
-    const bool whole_first = blk == sh.each;  // the tile is all of this share
-    auto slot = [&](int c) { return (c > 0 || whole_first ? 2 * (i0 + c) : 2 * i0 + 1) * rows + r; };
+    const int64_t first = blk == sh.each ? 2 * i0 : 2 * i0 + 1;  // (the tile may be all of this share)
     const float4* st = reinterpret_cast<const float4*>(p.part_s);
-    float m = neg_inf(), mo = neg_inf();
-    for (int c = lane; c < n; c += 32) {
-        const float4 v = st[slot(c)];
-        m = fmaxf(m, v.x), mo = fmaxf(mo, v.z);
-    }
-#pragma unroll
-    for (int d = 16; d; d >>= 1) {
-        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-        mo = fmaxf(mo, __shfl_xor_sync(0xffffffffu, mo, d));
-    }
-    const float base = m == neg_inf() ? 0.0f : m, base_o = mo == neg_inf() ? 0.0f : mo;
-    float l = 0.0f, o[2][4] = {};
-    const int d = 4 * lane;
-    for (int c0 = 0; c0 < n; c0 += 32) {
-        float f = 0.0f;
-        if (c0 + lane < n) {
-            const float4 v = st[slot(c0 + lane)];
-            l += v.y * exp2f(v.x - base);
-            f = exp2f(v.z - base_o);
-        }
-        const int k = min(32, n - c0);
-        for (int c = 0; c < k; c += 4) {  // four parts' loads in flight
-            float4 v[4][2];
-            float w[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                w[i] = __shfl_sync(0xffffffffu, f, (c + i) & 31);
-                const float* src = p.part_o + slot(c0 + min(c + i, k - 1)) * p.D + d;
-#pragma unroll
-                for (int z = 0; z < 2; ++z)
-                    v[i][z] = d + 128 * z < p.D ? __ldcg(reinterpret_cast<const float4*>(src + 128 * z)) : make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int r0 = 0; r0 < n_rows; r0 += kJoinWarps / per) {
+        const int r = r0 + warp / per, mine = warp % per;
+        const bool have = r < n_rows;
+        float m = neg_inf(), mo = neg_inf(), l = 0.0f;
+        float o[2][4] = {};
+        float base = 0.0f, base_o = 0.0f;
+        const int d = 4 * lane;
+        if (have) {
+            auto slot = [&](int c) { return (c > 0 ? 2 * (i0 + c) : first) * rows + r; };
+            for (int c = lane; c < n; c += 32) {
+                const float4 v = __ldcg(st + slot(c));
+                m = fmaxf(m, v.x), mo = fmaxf(mo, v.z);
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (c + i >= k || w[i] == 0.0f) continue;  // (a part that this row does not see: its sums are 0)
+            for (int e = 16; e; e >>= 1) {
+                m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, e));
+                mo = fmaxf(mo, __shfl_xor_sync(0xffffffffu, mo, e));
+            }
+            base = m == neg_inf() ? 0.0f : m, base_o = mo == neg_inf() ? 0.0f : mo;
+            for (int c0 = 0; c0 < n; c0 += 32) {
+                float f = 0.0f;
+                if (c0 + lane < n) {
+                    const float4 v = __ldcg(st + slot(c0 + lane));
+                    l += v.y * exp2f(v.x - base);
+                    f = exp2f(v.z - base_o);
+                }
+                const int k = min(32, n - c0);
+                for (int c = mine; c < k; c += 8 * per) {  // eight parts' loads in flight
+                    float4 v[8][2];
+                    float w[8];
 #pragma unroll
-                for (int z = 0; z < 2; ++z) {
-                    o[z][0] = fmaf(v[i][z].x, w[i], o[z][0]), o[z][1] = fmaf(v[i][z].y, w[i], o[z][1]);
-                    o[z][2] = fmaf(v[i][z].z, w[i], o[z][2]), o[z][3] = fmaf(v[i][z].w, w[i], o[z][3]);
+                    for (int i = 0; i < 8; ++i) {
+                        const int cc = c + i * per;
+                        w[i] = __shfl_sync(0xffffffffu, f, min(cc, k - 1));
+                        const float* src = p.part_o + slot(c0 + min(cc, k - 1)) * p.D + d;
+#pragma unroll
+                        for (int z = 0; z < 2; ++z)
+                            v[i][z] = cc < k && d + 128 * z < p.D ? __ldcg(reinterpret_cast<const float4*>(src + 128 * z))
+                                                                  : make_float4(0.f, 0.f, 0.f, 0.f);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        if (c + i * per >= k || w[i] == 0.0f) continue;  // (a part that this row does not see: its sums are 0)
+#pragma unroll
+                        for (int z = 0; z < 2; ++z) {
+                            o[z][0] = fmaf(v[i][z].x, w[i], o[z][0]), o[z][1] = fmaf(v[i][z].y, w[i], o[z][1]);
+                            o[z][2] = fmaf(v[i][z].z, w[i], o[z][2]), o[z][3] = fmaf(v[i][z].w, w[i], o[z][3]);
+                        }
+                    }
                 }
             }
+#pragma unroll
+            for (int e = 16; e; e >>= 1) l += __shfl_xor_sync(0xffffffffu, l, e);
         }
-    }
+        if (per > 1) {
+            __syncthreads();
 #pragma unroll
-    for (int e = 16; e; e >>= 1) l += __shfl_xor_sync(0xffffffffu, l, e);
-    int lo, hi;
-    seen_keys(p, s, (int)(row / G), lo, hi);
-    const bool empty = hi < lo || (m == neg_inf() && l == 0.0f);
-    const int64_t t = s.q0 + row / G;
-    const int hq = h * G + (int)(row % G);
-    if (p.lse && lane == 0) p.lse[t * p.Hq + hq] = empty ? neg_inf() : (base + log2f(l)) * kLn2;
-    const float inv = empty ? 0.0f : exp2f(base_o - base) / l;
-    TA* out = const_cast<TA*>(static_cast<const TA*>(p.out.p)) + t * p.out.ts + hq * p.out.hs + d;
+            for (int z = 0; z < 2; ++z) acc[warp][lane + 32 * z] = make_float4(o[z][0], o[z][1], o[z][2], o[z][3]);
+            __syncthreads();
+            if (mine == 0)
+                for (int w = 1; w < per; ++w)
 #pragma unroll
-    for (int z = 0; z < 2; ++z) {
-        if (d + 128 * z >= p.D) break;
-        if constexpr (sizeof(TA) == 4)
-            *reinterpret_cast<float4*>(out + 128 * z) = make_float4(o[z][0] * inv, o[z][1] * inv, o[z][2] * inv, o[z][3] * inv);
-        else
-            *reinterpret_cast<uint2*>(out + 128 * z) =
-                make_uint2(pack_bf16x2(o[z][0] * inv, o[z][1] * inv), pack_bf16x2(o[z][2] * inv, o[z][3] * inv));
+                    for (int z = 0; z < 2; ++z) {
+                        const float4 v = acc[warp + w][lane + 32 * z];
+                        o[z][0] += v.x, o[z][1] += v.y, o[z][2] += v.z, o[z][3] += v.w;
+                    }
+        }
+        if (!have || mine != 0) continue;
+        const int64_t row = (int64_t)tile * rows + r;
+        int lo, hi;
+        seen_keys(p, s, (int)(row / G), lo, hi);
+        const bool empty = hi < lo || (m == neg_inf() && l == 0.0f);
+        const int64_t t = s.q0 + row / G;
+        const int hq = h * G + (int)(row % G);
+        if (p.lse && lane == 0) p.lse[t * p.Hq + hq] = empty ? neg_inf() : (base + log2f(l)) * kLn2;
+        const float inv = empty ? 0.0f : exp2f(base_o - base) / l;
+        TA* out = const_cast<TA*>(static_cast<const TA*>(p.out.p)) + t * p.out.ts + hq * p.out.hs + d;
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+            if (d + 128 * z >= p.D) break;
+            if constexpr (sizeof(TA) == 4)
+                *reinterpret_cast<float4*>(out + 128 * z) = make_float4(o[z][0] * inv, o[z][1] * inv, o[z][2] * inv, o[z][3] * inv);
+            else
+                *reinterpret_cast<uint2*>(out + 128 * z) =
+                    make_uint2(pack_bf16x2(o[z][0] * inv, o[z][1] * inv), pack_bf16x2(o[z][2] * inv, o[z][3] * inv));
+        }
     }
 }
 
@@ -381,7 +413,7 @@ cudaError_t launch_attn_simt(const AttnProblem& p, cudaStream_t stream) {
 }
 
 cudaError_t launch_attn_join(const AttnProblem& p, cudaStream_t stream) {
-    const dim3 grid(p.shares - 1, (p.tile_rows + kJoinThreads / 32 - 1) / (kJoinThreads / 32));
+    const dim3 grid(p.shares - 1);
     return p.act_dtype == GBMOE_F32 ? launch_k(attn_join_kernel<float>, grid, dim3(kJoinThreads), 0, stream, p)
                                     : launch_k(attn_join_kernel<__nv_bfloat16>, grid, dim3(kJoinThreads), 0, stream, p);
 }

@@ -43,7 +43,7 @@ def prefix(v):
 @pytest.mark.parametrize("act", ["f32", "bf16"])
 @pytest.mark.parametrize("layout", ["half", "interleaved"])
 @pytest.mark.parametrize("T,Hq,Hkv,D,R", [(1, 4, 1, 64, 64), (37, 6, 2, 128, 32), (130, 3, 3, 80, 48), (5, 1, 1, 256, 256),
-                                          (700, 8, 2, 64, 0)])
+                                          (700, 8, 2, 64, 0), (3000, 1, 1, 16, 16)])
 def test_rope(act, layout, T, Hq, Hkv, D, R):
     rng = np.random.default_rng(T + D)
     q, k = normal(rng, (T, Hq, D), act), strided(normal(rng, (T, Hkv, D), act))
@@ -65,6 +65,8 @@ def test_rope(act, layout, T, Hq, Hkv, D, R):
     q2 = q.clone()
     gb.attn_rope(cfg, q2, None, i32(pos), table, q2, None)
     assert torch.equal(q2, qo)
+    gb.attn_rope(cfg, None, k, i32(pos), table, None, k)
+    assert torch.equal(k, ko)
     plain = gb.attn_config(Hq, Hkv, D, act=act, rotary_dim=R, rotary_layout=layout)
     gb.attn_rope(plain, q, None, i32(pos), table, qo, None)
     gb.attn_rope(plain, qo, None, i32(pos), table, qo, None, inverse=True)
