@@ -13,7 +13,10 @@
 // maximum m is raised, and O in TMEM rescaled, only when a row's maximum has
 // grown by more than 2^8 since the last time: P then stays below 2^8 and the
 // final division by the same row's sum makes up for it.
-// Warps 0-3 and 4-7: softmax of tile 0 and 1; warp 8: TMA; warp 9: MMA.
+// Warps 0-3 and 4-7: softmax of tile 0 and 1 and their results; warp 8: TMA; warp
+// 9: MMA; warp 10: scheduler. A CTA goes on with the work of CTAs that have not
+// started (cluster launch control), so the loads, the first products and the search
+// for the next work run while the softmax warps still write the last results.
 // TMEM columns: S_0, S_1 (128 each), O_0, O_1 (128 each).
 //
 // A masked score gives P = 0, but 0 times a NaN value is a NaN: a row whose
@@ -32,15 +35,16 @@ namespace {
 using namespace tc;
 
 constexpr int kTile = 128;             // query rows of a tile, keys of a tile
-constexpr int kThreads = 320;
+constexpr int kThreads = 384;
 constexpr int kHalf = kTile * 128;     // bytes of 128 rows x 64 bf16
 constexpr float kGrow = 8.0f;          // log2 of how far a row's maximum may run ahead of m
 
 template <int DK>
 struct Smem {
     static constexpr int TILE = DK / 64 * kHalf;          // one Q, K or V tile
-    static constexpr int STAGES = DK == 128 ? 5 : 8;      // K and V tiles in flight, in turn
-    static constexpr int BYTES = 1024 + (2 + STAGES) * TILE + 256;
+    static constexpr int STAGES = DK == 128 ? 4 : 8;      // K and V tiles in flight, in turn
+    static constexpr int OUT = 8 * 2 * 2048;              // output rows on their way: two buffers of each softmax warp
+    static constexpr int BYTES = 1024 + (2 + STAGES) * TILE + OUT + 512;
 };
 
 struct Params {
@@ -54,6 +58,14 @@ __device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, i
         "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
         ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
         : "memory");
+}
+
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, const void* src, int x, int y, int z) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(
+                     reinterpret_cast<uint64_t>(map)),
+                 "r"(x), "r"(y), "r"(z), "r"(smem_u32(src))
+                 : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
 
 // S = A B^T: both K-major
@@ -122,6 +134,18 @@ __device__ __forceinline__ float ex2(float x) {
     return y;
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float y;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+    return y;
+}
+
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {  // two fp32 sums
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
 __device__ __forceinline__ bool finite(float x) { return fabsf(x) <= 3.402823466e38f; }
 
 // The row of token t, head h once more, by a whole warp and without the values
@@ -163,55 +187,88 @@ __device__ __noinline__ void repair_row(const AttnProblem& p, int64_t k0, int64_
         *reinterpret_cast<uint2*>(out + d) = make_uint2(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv));
 }
 
+// One work item as the scheduler warp hands it out.
+struct Work {
+    Seq s;
+    int rows0[2], rows[2];  // query tile t: first row of the sequence, rows (<= 0: none)
+    int n[2];               // its key tiles, from k_first on
+    int k_first, head0, head_kv;
+    int end;                // 1: no more work
+};
+
+// Row tile `index` of the list, by a whole warp (every lane gets it); b = -1: past the end.
+__device__ __forceinline__ Place warp_find_tile(const AttnProblem& p, int64_t index, int rows) {
+    const int lane = threadIdx.x & 31;
+    int64_t before = 0;
+    for (int base = 0; base < p.B; base += 32) {
+        const int64_t v = base + lane < p.B ? row_tiles(p, load_seq(p, base + lane), rows) : 0;
+        const int64_t pre = warp_scan(v) + before;
+        const uint32_t hit = __ballot_sync(0xffffffffu, index < pre);
+        if (hit) {
+            const int l = __ffs(hit) - 1;
+            return Place{base + l, index - __shfl_sync(0xffffffffu, pre - v, l)};
+        }
+        before = __shfl_sync(0xffffffffu, pre, 31);
+    }
+    return Place{-1, 0};
+}
+
+// Asks for a CTA of this grid that has not started (its index comes as 16 bytes at dst, counted on bar).
+__device__ __forceinline__ void try_cancel(void* dst, uint64_t* bar) {
+    mbar_expect_tx(bar, 16);
+    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(smem_u32(dst)),
+                 "r"(smem_u32(bar))
+                 : "memory");
+}
+// the answer: whether there was one, and its blockIdx.x
+__device__ __forceinline__ bool cancelled(const void* src, uint32_t& x) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .b128 h;\n\t.reg .pred q;\n\t.reg .b32 y, z, w;\n\t"
+        "ld.shared.b128 h, [%2];\n\t"
+        "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 q, h;\n\t"
+        "selp.u32 %0, 1, 0, q;\n\t"
+        "mov.b32 %1, 0;\n\t"
+        "@q clusterlaunchcontrol.query_cancel.get_first_ctaid.v4.b32.b128 {%1, y, z, w}, h;\n\t}"
+        : "=r"(ok), "=r"(x)
+        : "r"(smem_u32(src))
+        : "memory");
+    return ok != 0;
+}
+
 template <int DK>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
-                   const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ Params pp) {
+                   const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_o,
+                   const __grid_constant__ Params pp) {
     pdl_enter();
     using L = Smem<DK>;
     constexpr int STAGES = L::STAGES;
     constexpr int TILE = L::TILE;
     const AttnProblem& p = pp.a;
-    __shared__ int64_t plan[plan_words(kThreads)];
+    __shared__ Work work_slots[2];
+    __shared__ __align__(16) uint4 answer;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    uint8_t* sQ = smem;               // two query tiles; at the end the output rows
+    uint8_t* sQ = smem;  // two query tiles
     uint8_t* sKV = smem + 2 * TILE;
-    uint64_t* bars = reinterpret_cast<uint64_t*>(sKV + STAGES * TILE);
+    uint8_t* sO = sKV + STAGES * TILE;
+    uint64_t* bars = reinterpret_cast<uint64_t*>(sO + L::OUT);
     uint64_t* full = bars;            // a K or V tile landed
     uint64_t* empty = full + STAGES;  // the MMAs that read it finished
     uint64_t* q_full = empty + STAGES;
-    uint64_t* s_full = q_full + 2;    // S of a query tile is complete (and so is every MMA before it)
-    uint64_t* p_full = s_full + 2;    // its P is written, O rescaled
+    uint64_t* q_empty = q_full + 2;   // the last product with a query tile finished
+    uint64_t* s_full = q_empty + 2;   // S of a query tile is complete (and so is every MMA before it)
+    uint64_t* p_full = s_full + 2;    // its P is written, O rescaled, and the V and next K tile are there
     uint64_t* o_full = p_full + 2;    // its O is complete
-    uint64_t* drain = o_full + 2;
+    uint64_t* w_full = o_full + 2;    // a work item is in its slot
+    uint64_t* w_empty = w_full + 2;   // every role has read it
+    uint64_t* ans = w_empty + 2;      // the answer to try_cancel
+    uint64_t* drain = ans + 1;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int groups = pp.pair_heads ? p.Hq / 2 : p.Hq;
-    const int rows_per = pp.pair_heads ? kTile : 2 * kTile;
-    const Place at = find_tile(p, blockIdx.x / groups, rows_per, plan);
-    if (at.b < 0) return;
-    const Seq s = load_seq(p, at.b);
-    // the last tiles, which see the most keys, first
-    const int tile = (s.nq + rows_per - 1) / rows_per - 1 - (int)at.at;
-    const int head0 = pp.pair_heads ? 2 * (blockIdx.x % groups) : blockIdx.x % groups;
-    const int head_kv = head0 / (p.Hq / p.Hkv);
-    // query tile t: rows row0(t) .. of the sequence, n_rows(t) of them, and the key tiles 0 .. n_tiles(t) - 1 from k_first on
-    auto row0 = [&](int t) { return tile * rows_per + (pp.pair_heads ? 0 : t * kTile); };
-    auto n_rows = [&](int t) { return min(kTile, s.nq - row0(t)); };
-    int lo0, hi0;
-    seen_keys(p, s, row0(0), lo0, hi0);
-    const int k_first = hi0 < 0 ? 0 : lo0 & ~(kTile - 1);
-    auto n_tiles = [&](int t) {
-        if (n_rows(t) <= 0) return 0;
-        int lo, hi;
-        seen_keys(p, s, row0(t) + n_rows(t) - 1, lo, hi);  // its last row sees the furthest
-        return hi < k_first ? 0 : (hi - k_first) / kTile + 1;
-    };
-    const int n0 = n_tiles(0), n1 = n_tiles(1), n_max = max(n0, n1);
-
     if (threadIdx.x == 0) {
         for (int i = 0; i < STAGES; ++i) {
             mbar_init(&full[i], 1);
@@ -219,10 +276,14 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         }
         for (int t = 0; t < 2; ++t) {
             mbar_init(&q_full[t], 1);
+            mbar_init(&q_empty[t], 1);
             mbar_init(&s_full[t], 1);
-            mbar_init(&p_full[t], 4);  // one arrival per softmax warp
+            mbar_init(&p_full[t], 5);    // one arrival per softmax warp, one of the tile watcher
             mbar_init(&o_full[t], 1);
+            mbar_init(&w_full[t], 1);
+            mbar_init(&w_empty[t], 11);  // softmax warps, TMA, MMA, tile watcher
         }
+        mbar_init(ans, 1);
         mbar_init(drain, 1);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -235,194 +296,128 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_wait(bar, parity, abort_flag, p.err, pp.wait_limit_ns); };
+    auto wait_warp = [&](uint64_t* bar, uint32_t parity) { return warp_wait(bar, parity, abort_flag, p.err, pp.wait_limit_ns); };
 
-    if (warp == 8 && lane == 0 && n_max > 0) {
-        // ------------------------------------------------------ TMA producer
-        uint32_t inflight = 0, par = 0;
-        for (int t = 0; t < 2; ++t) {
-            if ((t ? n1 : n0) == 0) continue;
-            mbar_expect_tx(&q_full[t], TILE);
-            for (int c = 0; c < DK / 64; ++c)
-                tma_load_3d(sQ + t * TILE + c * kHalf, &tm_q, 64 * c, head0 + (pp.pair_heads ? t : 0), s.q0 + row0(t), &q_full[t]);
-        }
-        int stage = 0;
-        uint32_t phase = 0;
-        for (int i = 0; i < 2 * n_max; ++i) {  // K_0, V_0, K_1, V_1, ...
-            if (!mbar_wait(&empty[stage], phase ^ 1, abort_flag, p.err, pp.wait_limit_ns)) break;
-            const CUtensorMap* map = i & 1 ? &tm_v : &tm_k;
-            mbar_expect_tx(&full[stage], TILE);
-            for (int c = 0; c < DK / 64; ++c)
-                tma_load_3d(sKV + stage * TILE + c * kHalf, map, 64 * c, head_kv, (int)(s.k0 + k_first + (i >> 1) * kTile), &full[stage]);
-            inflight |= 1u << stage;
-            par = (par & ~(1u << stage)) | (phase << stage);
-            if (++stage == STAGES) { stage = 0; phase ^= 1; }
-        }
-        // every copy has landed before the CTA leaves
-        const uint64_t t0 = global_ns();
-        for (int t = 0; t < 2; ++t)
-            if ((t ? n1 : n0) > 0) drain_wait(&q_full[t], 0, t0);
-        for (int i = 0; i < STAGES; ++i)
-            if ((inflight >> i) & 1u) drain_wait(&full[i], (par >> i) & 1u, t0);
-    } else if (warp == 9 && n_max > 0) {
-        // ------------------------- MMA issuer (the whole warp, one lane issues)
-        const int ksteps = (p.D + 15) / 16;
-        constexpr uint32_t kIdS = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kTile >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
-        const uint32_t id_o = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(ksteps * 2) << 17) |
-                              ((uint32_t)(kTile >> 4) << 24);
-        const uint64_t dq = sw128_desc(smem_u32(sQ)), dk = sw128_desc(smem_u32(sKV)), dv = v_desc(smem_u32(sKV));
-        bool ok = true, issued = false;
-        auto slot_of = [](int i) { return i % STAGES; };
-        auto wait_tile = [&](int i) {  // tile i of the K_0, V_0, K_1, .. sequence
-            ok = ok && warp_wait(&full[slot_of(i)], (uint32_t)(i / STAGES) & 1u, abort_flag, p.err, pp.wait_limit_ns);
-            return ok;
-        };
-        auto scores = [&](int t, int i) {  // S_t = Q_t K^T with the K tile i
-            if (elect_one()) {
-                const uint64_t a = dq + (uint64_t)(t * TILE >> 4), b = dk + (uint64_t)(slot_of(i) * TILE >> 4);
-                for (int c = 0; c < ksteps; ++c) {
-                    const uint64_t off = (uint64_t)((c >> 2) * kHalf + (c & 3) * 32) >> 4;
-                    mma_ss(tmem + t * kTile, a + off, b + off, kIdS, c != 0);
-                }
-                mma_commit(&s_full[t]);
-            }
-            __syncwarp();
-            issued = true;
-        };
-        for (int t = 0; t < 2 && ok; ++t)
-            if ((t ? n1 : n0) > 0) ok = warp_wait(&q_full[t], 0, abort_flag, p.err, pp.wait_limit_ns);
-        if (ok && wait_tile(0)) {
-            tc_fence_after();
-            for (int t = 0; t < 2; ++t)
-                if ((t ? n1 : n0) > 0) scores(t, 0);
-            if (elect_one()) mma_commit(&empty[slot_of(0)]);
-            __syncwarp();
-        }
-        for (int j = 0; j < n_max && ok; ++j) {
-            if (!wait_tile(2 * j + 1)) break;
-            if (j + 1 < n_max && !wait_tile(2 * j + 2)) break;
-            for (int t = 0; t < 2 && ok; ++t) {
-                const int n = t ? n1 : n0;
-                if (j >= n) continue;
-                ok = warp_wait(&p_full[t], (uint32_t)j & 1u, abort_flag, p.err, pp.wait_limit_ns);
-                if (!ok) break;
-                tc_fence_after();
-                if (elect_one()) {
-                    const uint64_t b = dv + (uint64_t)(slot_of(2 * j + 1) * TILE >> 4);
-                    const uint32_t d = tmem + 2 * kTile + t * kTile, a = tmem + t * kTile;
-#pragma unroll
-                    for (int c = 0; c < kTile / 16; ++c)  // 16 keys: 8 columns of P, 2 KB of V
-                        mma_ts(d, a + 8 * c, b + (uint64_t)(c * 2048 >> 4), id_o, (j | c) != 0);
-                    if (j == n - 1) mma_commit(&o_full[t]);
-                }
-                __syncwarp();
-                if (j + 1 < n) scores(t, 2 * j + 2);
-            }
-            if (!ok) break;
-            if (elect_one()) {
-                mma_commit(&empty[slot_of(2 * j + 1)]);
-                if (j + 1 < n_max) mma_commit(&empty[slot_of(2 * j + 2)]);
-            }
-            __syncwarp();
-        }
-        if (issued) {  // no MMA is in flight when TMEM is released
-            if (elect_one()) mma_commit(drain);
-            __syncwarp();
-            drain_wait(drain, 0);
-        }
-    } else if (warp < 8) {
+    // Registers: 384 threads start with 168 each; the softmax rows take 216, the others keep 72.
+    if (warp < 8) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         // ------------------------------------------------- softmax, one row each
         const int t = warp >> 2, r = (warp & 3) * 32 + lane;
-        const int n = t ? n1 : n0, rows = n_rows(t);
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t tS = tmem + lanes + t * kTile, tO = tmem + lanes + 2 * kTile + t * kTile;
-        int lo = 0, hi = -1;
-        if (r < rows) seen_keys(p, s, row0(t) + r, lo, hi);
         const float scale = p.scale_log2;
-        float m = neg_inf(), l = 0.0f;
+        uint32_t sn = 0, items = 0;  // key tiles and items of this query tile so far
         bool ok = true;
-        for (int j = 0; j < n; ++j) {
-            if (!warp_wait(&s_full[t], (uint32_t)j & 1u, abort_flag, p.err, pp.wait_limit_ns)) { ok = false; break; }
-            tc_fence_after();
-            uint32_t u[4][32];
+        for (int k = 0; ok; ++k) {
+            if (!wait_warp(&w_full[k & 1], (uint32_t)(k >> 1) & 1u)) break;
+            const Work& slot = work_slots[k & 1];
+            const Seq s = slot.s;
+            const int n = slot.n[t], rows = slot.rows[t], row = slot.rows0[t] + r, k_first = slot.k_first, end = slot.end;
+            const int head = slot.head0 + (pp.pair_heads ? t : 0);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&w_empty[k & 1]);
+            if (end) break;
+            int lo = 0, hi = -1;
+            if (r < rows) seen_keys(p, s, row, lo, hi);
+            float m = neg_inf(), l = 0.0f;
+            for (int j = 0; j < n; ++j) {
+                ok = wait_warp(&s_full[t], sn++ & 1u);
+                if (!ok) break;
+                tc_fence_after();
+                uint32_t u[4][32];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_ld32_async(tS + 32 * c, u[c]);
-            ld_wait();
+                for (int c = 0; c < 4; ++c) tmem_ld32_async(tS + 32 * c, u[c]);
+                ld_wait();
 #pragma unroll
-            for (int c = 0; c < 4; ++c) pin32(u[c]);
-            const int first = lo - (k_first + j * kTile), last = hi - (k_first + j * kTile);  // columns first .. last are seen
-            if (__any_sync(0xffffffffu, first > 0 || last < kTile - 1)) {
+                for (int c = 0; c < 4; ++c) pin32(u[c]);
+                const int first = lo - (k_first + j * kTile), last = hi - (k_first + j * kTile);  // columns first .. last are seen
+                if (__any_sync(0xffffffffu, first > 0 || last < kTile - 1)) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c)
+                    for (int c = 0; c < 4; ++c) {
+                        // the columns of this chunk that the row sees, as bits
+                        const int f = first - 32 * c, e = last - 32 * c;
+                        const uint32_t seen = (f <= 0 ? ~0u : f > 31 ? 0u : ~0u << f) & (e >= 31 ? ~0u : e < 0 ? 0u : (2u << e) - 1u);
+                        if (!__any_sync(0xffffffffu, seen != ~0u)) continue;
 #pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (32 * c + i < first || 32 * c + i > last) u[c][i] = 0xff800000u;
-            }
-            float mx[4];
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                mx[c] = __uint_as_float(u[c][0]);
-#pragma unroll
-                for (int i = 1; i < 32; ++i) mx[c] = fmaxf(mx[c], __uint_as_float(u[c][i]));
-            }
-            const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
-            if (__any_sync(0xffffffffu, top > m + kGrow || (j == 0 && top > m))) {
-                const float m_new = fmaxf(m, top);
-                const float f = m_new == neg_inf() ? 1.0f : ex2(m - m_new);  // (m = -inf: 0)
-                l *= f;
-                m = m_new;
-                if (j > 0) {  // (this tile's S is complete, so its last O += P V is too)
-#pragma unroll 1
-                    for (int c = 0; c < p.D; c += 32) {
-                        uint32_t o[32];
-                        tmem_ld32_async(tO + c, o);
-                        ld_wait();
-                        pin32(o);
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                        tmem_st32(tO + c, o);
+                        for (int i = 0; i < 32; ++i) u[c][i] = seen & (1u << i) ? u[c][i] : 0xff800000u;
                     }
                 }
-            }
-            const float base = m == neg_inf() ? 0.0f : -m;
-            const uint64_t sc2 = pack2(scale, scale), nb2 = pack2(base, base);
-            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                float mx[4];
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                uint32_t w[32];
+                for (int c = 0; c < 4; ++c) {
+                    mx[c] = fmaxf(__uint_as_float(u[c][0]), __uint_as_float(u[c][1]));
 #pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    const int e = 64 * half + 2 * i;
-                    const float2 x = unpack2(fma2(pack2(__uint_as_float(u[e >> 5][e & 31]), __uint_as_float(u[e >> 5][(e & 31) + 1])), sc2, nb2));
-                    const float a = ex2(x.x), b = ex2(x.y);
-                    sum[2 * (i & 1)] += a;
-                    sum[2 * (i & 1) + 1] += b;
-                    w[i] = pack_bf16x2(a, b);
+                    for (int i = 2; i < 32; i += 2) mx[c] = max3(mx[c], __uint_as_float(u[c][i]), __uint_as_float(u[c][i + 1]));
                 }
-                tmem_st32(tS + 32 * half, w);
+                const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
+                if (__any_sync(0xffffffffu, top > m + kGrow || (j == 0 && top > m))) {
+                    const float m_new = fmaxf(m, top);
+                    const float f = m_new == neg_inf() ? 1.0f : ex2(m - m_new);  // (m = -inf: 0)
+                    l *= f;
+                    m = m_new;
+                    if (j > 0) {  // (this tile's S is complete, so its last O += P V is too)
+#pragma unroll 1
+                        for (int c = 0; c < p.D; c += 32) {
+                            uint32_t o[32];
+                            tmem_ld32_async(tO + c, o);
+                            ld_wait();
+                            pin32(o);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                            tmem_st32(tO + c, o);
+                        }
+                    }
+                }
+                const float base = m == neg_inf() ? 0.0f : -m;
+                const uint64_t sc2 = pack2(scale, scale), nb2 = pack2(base, base);
+                uint64_t sum[2] = {pack2(0.0f, 0.0f), pack2(0.0f, 0.0f)};
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    uint32_t w[32];
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        const int e = 64 * half + 2 * i;
+                        const float2 x = unpack2(fma2(pack2(__uint_as_float(u[e >> 5][e & 31]), __uint_as_float(u[e >> 5][(e & 31) + 1])), sc2, nb2));
+                        const float a = ex2(x.x), b = ex2(x.y);
+                        sum[i & 1] = add2(sum[i & 1], pack2(a, b));
+                        w[i] = pack_bf16x2(a, b);
+                    }
+                    tmem_st32(tS + 32 * half, w);
+                }
+                const float2 s01 = unpack2(add2(sum[0], sum[1]));
+                l += s01.x + s01.y;
+                st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&p_full[t]);
             }
-            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-            st_wait();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&p_full[t]);
-        }
-        // ------------------------------------------------------------ result
-        if (ok && n > 0) ok = warp_wait(&o_full[t], 0, abort_flag, p.err, pp.wait_limit_ns);
-        tc_fence_after();
-        if (ok && rows > 0) {
+            // -------------------------------------------------------- result
+            if (ok && n > 0) ok = wait_warp(&o_full[t], items++ & 1u);
+            if (!ok) break;
+            tc_fence_after();
+            if (rows <= (warp & 3) * 32) continue;  // no row of this warp
             const bool empty = hi < lo;
             const float inv = empty ? 0.0f : 1.0f / l;
-            const int64_t tok = s.q0 + row0(t) + r;
-            const int head = head0 + (pp.pair_heads ? t : 0);
-            uint8_t* buf = sQ + t * TILE + (warp & 3) * 32 * (2 * DK);  // this warp's 32 rows of 2 DK bytes
-            bool good = true;
+            const int64_t tok = s.q0 + row;
+            __nv_bfloat16* out = const_cast<__nv_bfloat16*>(static_cast<const __nv_bfloat16*>(p.out.p)) + tok * p.out.ts + head * p.out.hs;
+            float check = 0.0f;  // NaN once a value is not finite
+            // all 32 rows of this warp belong to the tile: a TMA store of each 32 columns;
+            // else plain stores of the valid rows (the others are another sequence's)
+            const bool via_tma = (warp & 3) * 32 + 32 <= rows;
+            uint8_t* stage_buf = sO + warp * 4096;
 #pragma unroll 1
-            for (int c = 0; c < DK; c += 32) {
+            for (int c = 0; c < p.D; c += 32) {
                 uint32_t o[32];
                 if (n > 0) {
                     tmem_ld32_async(tO + c, o);
                     ld_wait();
                     pin32(o);
+                }
+                uint8_t* buf = stage_buf + ((c >> 5) & 1) * 2048;
+                if (via_tma) {
+                    if (lane == 0) bulk_wait_read<1>();  // the store that last read buf is done reading
+                    __syncwarp();
                 }
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
@@ -431,37 +426,255 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                     for (int i = 0; i < 4; ++i) {
                         const float a = empty ? 0.0f : __uint_as_float(o[8 * q + 2 * i]) * inv;
                         const float b = empty ? 0.0f : __uint_as_float(o[8 * q + 2 * i + 1]) * inv;
-                        if (c + 8 * q < p.D) good = good && finite(a) && finite(b);
+                        if (c + 8 * q < p.D) check = fmaf(a, 0.0f, fmaf(b, 0.0f, check));
                         w[i] = pack_bf16x2(a, b);
                     }
-                    // 16-byte chunk c/8 + q of row `lane`, spread over the banks
-                    const int chunk = (c / 8 + q) ^ (lane & 7);
-                    *reinterpret_cast<uint4*>(buf + lane * (2 * DK) + chunk * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+                    const uint4 v = make_uint4(w[0], w[1], w[2], w[3]);
+                    // (64-byte rows, 64-byte swizzle; columns past D are not written)
+                    if (via_tma) *reinterpret_cast<uint4*>(buf + lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4)) = v;
+                    else if (r < rows && c + 8 * q < p.D) *reinterpret_cast<uint4*>(out + c + 8 * q) = v;
                 }
-            }
-            __syncwarp();
-            // whole rows to memory: 2 DK / 16 lanes per row
-            constexpr int kChunks = DK / 8;
-            __nv_bfloat16* out = const_cast<__nv_bfloat16*>(static_cast<const __nv_bfloat16*>(p.out.p)) + head * p.out.hs;
-            const int64_t tok0 = tok - lane;
-            const int left = min(32, rows - (warp & 3) * 32);
-#pragma unroll 1
-            for (int i = lane; i < 32 * kChunks; i += 32) {
-                const int rr = i / kChunks, ch = i % kChunks;
-                if (rr < left && 8 * ch < p.D)
-                    *reinterpret_cast<uint4*>(out + (tok0 + rr) * p.out.ts + 8 * ch) =
-                        *reinterpret_cast<const uint4*>(buf + rr * (2 * DK) + ((ch ^ (rr & 7)) * 16));
+                if (via_tma) {
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) tma_store_3d(&tm_o, buf, c, head, (int)tok);
+                }
             }
             if (r < rows && p.lse) p.lse[tok * p.Hq + head] = empty ? neg_inf() : (m + log2f(l)) * kLn2;
             // rows that may hold a masked key's NaN
-            uint32_t again = __ballot_sync(0xffffffffu, r < rows && !empty && !good && finite(m) && finite(l) && l > 0.0f);
+            uint32_t again = __ballot_sync(0xffffffffu, r < rows && !empty && check != check && finite(m) && finite(l) && l > 0.0f);
             while (again) {
                 const int src = __ffs(again) - 1;
                 again &= again - 1;
                 const int rlo = __shfl_sync(0xffffffffu, lo, src), rhi = __shfl_sync(0xffffffffu, hi, src);
                 const float rm = __shfl_sync(0xffffffffu, m, src), rl = __shfl_sync(0xffffffffu, l, src);
-                __syncwarp();  // (the row's first version is stored before the second)
-                repair_row(p, s.k0, tok0 + src, head, rlo, rhi, rm, rl);
+                if (lane == 0) bulk_wait_all();  // the row's first version is stored before the second
+                __syncwarp();
+                repair_row(p, s.k0, tok - lane + src, head, rlo, rhi, rm, rl);
+            }
+        }
+        if (lane == 0) bulk_wait_all();  // stores complete before the CTA leaves
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        if (warp == 10) {
+            // --------------------------------------------------------- scheduler
+            const int groups = pp.pair_heads ? p.Hq / 2 : p.Hq;
+            const int rows_per = pp.pair_heads ? kTile : 2 * kTile;
+            uint32_t block = blockIdx.x;
+            bool more = true, asked = false;
+            uint32_t turn = 0;
+            int k = 0;
+            for (; more; ++turn) {
+                if (lane == 0) try_cancel(&answer, ans);
+                asked = true;
+                const Place at = warp_find_tile(p, block / groups, rows_per);
+                if (at.b >= 0) {
+                    if (!wait_warp(&w_empty[k & 1], ((uint32_t)(k >> 1) & 1u) ^ 1u)) break;
+                    Work w;
+                    w.s = load_seq(p, at.b);
+                    // the last tiles, which see the most keys, first
+                    const int tile = (w.s.nq + rows_per - 1) / rows_per - 1 - (int)at.at;
+                    w.head0 = (int)(block % groups) * (pp.pair_heads ? 2 : 1);
+                    w.head_kv = w.head0 / (p.Hq / p.Hkv);
+                    w.end = 0;
+                    int lo, hi;
+                    seen_keys(p, w.s, tile * rows_per, lo, hi);
+                    w.k_first = hi < 0 ? 0 : lo & ~(kTile - 1);
+    #pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        w.rows0[t] = tile * rows_per + (pp.pair_heads ? 0 : t * kTile);
+                        w.rows[t] = min(kTile, w.s.nq - w.rows0[t]);
+                        w.n[t] = 0;
+                        if (w.rows[t] > 0) {
+                            seen_keys(p, w.s, w.rows0[t] + w.rows[t] - 1, lo, hi);  // its last row sees the furthest
+                            if (hi >= w.k_first) w.n[t] = (hi - w.k_first) / kTile + 1;
+                        }
+                    }
+                    if (lane == 0) {
+                        work_slots[k & 1] = w;
+                        mbar_arrive(&w_full[k & 1]);
+                    }
+                    __syncwarp();
+                    ++k;
+                }
+                if (!wait_warp(ans, turn & 1u)) break;
+                asked = false;
+                more = cancelled(&answer, block);
+                __syncwarp();
+                // the answer is read before the next one is asked for (another proxy writes it)
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            }
+            if (!more && wait_warp(&w_empty[k & 1], ((uint32_t)(k >> 1) & 1u) ^ 1u) && lane == 0) {
+                work_slots[k & 1].end = 1;
+                mbar_arrive(&w_full[k & 1]);
+            }
+            if (asked && lane == 0) drain_wait(ans, turn & 1u);  // (a wait gave up: the answer lands before the CTA leaves)
+        } else if (warp == 8 && lane == 0) {
+            // ------------------------------------------------------ TMA producer
+            uint32_t inflight = 0, par = 0, qn[2] = {0, 0};
+            int stage = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            for (int k = 0; ok; ++k) {
+                if (!wait(&w_full[k & 1], (uint32_t)(k >> 1) & 1u)) break;
+                const Work w = work_slots[k & 1];
+                mbar_arrive(&w_empty[k & 1]);
+                if (w.end) break;
+                const int n_max = max(w.n[0], w.n[1]);
+                for (int t = 0; t < 2 && ok; ++t) {
+                    if (w.n[t] == 0) continue;
+                    ok = wait(&q_empty[t], (qn[t] & 1u) ^ 1u);
+                    if (!ok) break;
+                    mbar_expect_tx(&q_full[t], TILE);
+                    for (int c = 0; c < DK / 64; ++c)
+                        tma_load_3d(sQ + t * TILE + c * kHalf, &tm_q, 64 * c, w.head0 + (pp.pair_heads ? t : 0), w.s.q0 + w.rows0[t], &q_full[t]);
+                    ++qn[t];
+                }
+                for (int i = 0; i < 2 * n_max && ok; ++i) {  // K_0, V_0, K_1, V_1, ...
+                    ok = wait(&empty[stage], phase ^ 1);
+                    if (!ok) break;
+                    const CUtensorMap* map = i & 1 ? &tm_v : &tm_k;
+                    mbar_expect_tx(&full[stage], TILE);
+                    for (int c = 0; c < DK / 64; ++c)
+                        tma_load_3d(sKV + stage * TILE + c * kHalf, map, 64 * c, w.head_kv, (int)(w.s.k0 + w.k_first + (i >> 1) * kTile), &full[stage]);
+                    inflight |= 1u << stage;
+                    par = (par & ~(1u << stage)) | (phase << stage);
+                    if (++stage == STAGES) { stage = 0; phase ^= 1; }
+                }
+            }
+            // every copy has landed before the CTA leaves
+            const uint64_t t0 = global_ns();
+            for (int t = 0; t < 2; ++t)
+                if (qn[t] > 0) drain_wait(&q_full[t], (qn[t] - 1) & 1u, t0);
+            for (int i = 0; i < STAGES; ++i)
+                if ((inflight >> i) & 1u) drain_wait(&full[i], (par >> i) & 1u, t0);
+        } else if (warp == 9) {
+            // ------------------------- MMA issuer (the whole warp, one lane issues)
+            // Every value that an MMA takes comes from constants, kernel parameters and
+            // warp-wide reductions, so that it stays in uniform registers.
+            const int ksteps = (p.D + 15) / 16;
+            constexpr uint32_t kIdS = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kTile >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
+            const uint32_t id_o = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(ksteps * 2) << 17) |
+                                  ((uint32_t)(kTile >> 4) << 24);
+            const uint64_t dq = sw128_desc(smem_u32(sQ)), dk = sw128_desc(smem_u32(sKV)), dv = v_desc(smem_u32(sKV));
+            const uint32_t tm = __reduce_max_sync(0xffffffffu, tmem);
+            bool issued = false;
+            uint32_t qn0 = 0, qn1 = 0, pn0 = 0, pn1 = 0;  // phases of q_full and p_full
+            int stage = 0;  // ring slot of the next tile and its phase
+            uint32_t phase = 0;
+            auto advance = [&](int& st, uint32_t& ph) {
+                if (++st == STAGES) st = 0, ph ^= 1;
+            };
+            // S_t = Q_t K^T with the K tile in slot st; last: the item's last use of Q_t
+            auto scores = [&](int t, int st, bool last) {
+                if (elect_one()) {
+                    const uint64_t a = dq + (uint64_t)(t * TILE >> 4), b = dk + (uint64_t)((uint32_t)(st * TILE) >> 4);
+#pragma unroll
+                    for (int c = 0; c < DK / 16; ++c) {
+                        if (c >= ksteps) break;
+                        const uint64_t off = (uint64_t)((c >> 2) * kHalf + (c & 3) * 32) >> 4;
+                        mma_ss(tm + t * kTile, a + off, b + off, kIdS, c != 0);
+                    }
+                    mma_commit(&s_full[t]);
+                    if (last) mma_commit(&q_empty[t]);
+                }
+                __syncwarp();
+                issued = true;
+            };
+            // O_t += P_t V with the V tile in slot st
+            auto values = [&](int t, int st, bool first, bool last) {
+                if (elect_one()) {
+                    const uint64_t b = dv + (uint64_t)((uint32_t)(st * TILE) >> 4);
+#pragma unroll
+                    for (int c = 0; c < kTile / 16; ++c)  // 16 keys: 8 columns of P, 2 KB of V
+                        mma_ts(tm + 2 * kTile + t * kTile, tm + t * kTile + 8 * c, b + (uint64_t)(c * 2048 >> 4), id_o, c != 0 || !first);
+                    if (last) mma_commit(&o_full[t]);
+                }
+                __syncwarp();
+            };
+            auto release = [&](int st) {
+                if (elect_one()) mma_commit(&empty[st]);
+                __syncwarp();
+            };
+            for (int k = 0;; ++k) {
+                if (!wait_warp(&w_full[k & 1], (uint32_t)(k >> 1) & 1u)) break;
+                const int n0 = __reduce_max_sync(0xffffffffu, work_slots[k & 1].n[0]);
+                const int n1 = __reduce_max_sync(0xffffffffu, work_slots[k & 1].n[1]);
+                const int end = __reduce_max_sync(0xffffffffu, work_slots[k & 1].end);
+                if (lane == 0) mbar_arrive(&w_empty[k & 1]);
+                if (end) break;
+                const int n_max = max(n0, n1);
+                if (n_max == 0) continue;
+                if (n0 > 0 && !wait_warp(&q_full[0], qn0++ & 1u)) break;
+                if (n1 > 0 && !wait_warp(&q_full[1], qn1++ & 1u)) break;
+                if (!wait_warp(&full[stage], phase)) break;
+                tc_fence_after();
+                if (n0 > 0) scores(0, stage, n0 == 1);
+                if (n1 > 0) scores(1, stage, n1 == 1);
+                release(stage);
+                advance(stage, phase);
+                bool ok = true;
+                for (int j = 0; j < n_max; ++j) {
+                    // V_j in slot sv, K_j+1 in slot sk: there when p_full is complete
+                    const int sv = stage;
+                    advance(stage, phase);
+                    const int sk = stage;
+                    if (j + 1 < n_max) advance(stage, phase);
+                    if (j < n0) {
+                        ok = wait_warp(&p_full[0], pn0++ & 1u);
+                        if (!ok) break;
+                        tc_fence_after();
+                        values(0, sv, j == 0, j == n0 - 1);
+                        if (j + 1 < n0) scores(0, sk, j + 2 == n0);
+                    }
+                    if (j < n1) {
+                        ok = wait_warp(&p_full[1], pn1++ & 1u);
+                        if (!ok) break;
+                        tc_fence_after();
+                        values(1, sv, j == 0, j == n1 - 1);
+                        if (j + 1 < n1) scores(1, sk, j + 2 == n1);
+                    }
+                    release(sv);
+                    if (j + 1 < n_max) release(sk);
+                }
+                if (!ok) break;
+            }
+            if (issued) {  // no MMA is in flight when TMEM is released
+                if (elect_one()) mma_commit(drain);
+                __syncwarp();
+                drain_wait(drain, 0);
+            }
+        } else if (warp == 11 && lane == 0) {
+            // ------------------------------------------------------- tile watcher
+            // Waits for the tiles in the MMA warp's stead, whose issue queue is shallow: each
+            // barrier that it waits for itself delays the MMAs behind it.
+            int stage = 0;
+            uint32_t phase = 0, pn[2] = {0, 0};
+            auto next = [&] {
+                if (++stage == STAGES) stage = 0, phase ^= 1;
+            };
+            bool ok = true;
+            for (int k = 0; ok; ++k) {
+                if (!wait(&w_full[k & 1], (uint32_t)(k >> 1) & 1u)) break;
+                const int n0 = work_slots[k & 1].n[0], n1 = work_slots[k & 1].n[1], end = work_slots[k & 1].end;
+                mbar_arrive(&w_empty[k & 1]);
+                if (end) break;
+                const int n_max = max(n0, n1);
+                if (n_max > 0) next();  // (the first K tile: the MMA warp's)
+                for (int j = 0; j < n_max && ok; ++j) {
+                    ok = wait(&full[stage], phase);
+                    next();
+                    if (j + 1 < n_max) {
+                        ok = ok && wait(&full[stage], phase);
+                        next();
+                    }
+                    for (int t = 0; t < 2 && ok; ++t) {
+                        if (j >= (t ? n1 : n0)) continue;
+                        if (pn[t] > 0) ok = wait(&p_full[t], (pn[t] - 1) & 1u);  // one arrival in a phase
+                        ++pn[t];
+                        if (ok) mbar_arrive(&p_full[t]);
+                    }
+                }
             }
         }
     }
@@ -471,16 +684,18 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
 }
 
 // [T, heads, D] bf16 rows as a 3-D tensor in boxes of 64 x 1 x 128 (128-byte
-// swizzled); elements past D and rows past T read as 0
-bool rows_map(CUtensorMap* map, const Rows& r, int64_t T, int heads, int D) {
+// swizzled; elements past D and rows past T read as 0), or, for the output, of
+// 32 x 1 x 32 (64-byte swizzled)
+bool rows_map(CUtensorMap* map, const Rows& r, int64_t T, int heads, int D, bool out = false) {
     EncodeTiled fn = encode_fn();
     if (!fn) return false;
     const cuuint64_t least = (cuuint64_t)(2 * D);
     cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)heads, (cuuint64_t)T};
     cuuint64_t strides[2] = {heads > 1 ? (cuuint64_t)(2 * r.hs) : least, T > 1 ? (cuuint64_t)(2 * r.ts) : least};
-    cuuint32_t box[3] = {64, 1, kTile}, estr[3] = {1, 1, 1};
+    cuuint32_t box[3] = {out ? 32u : 64u, 1, out ? 32u : (cuuint32_t)kTile}, estr[3] = {1, 1, 1};
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(r.p), dims, strides, box, estr,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, out ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -500,13 +715,13 @@ cudaError_t prompt_as(const AttnProblem& p, cudaStream_t stream) {
         });
         e != cudaSuccess)
         return e;
-    CUtensorMap q, k, v;
-    if (!rows_map(&q, p.q, p.T, p.Hq, p.D) || !rows_map(&k, p.k, p.Tk, p.Hkv, p.D) || !rows_map(&v, p.v, p.Tk, p.Hkv, p.D))
+    CUtensorMap q, k, v, o;
+    if (!rows_map(&q, p.q, p.T, p.Hq, p.D) || !rows_map(&o, p.out, p.T, p.Hq, p.D, true) || !rows_map(&k, p.k, p.Tk, p.Hkv, p.D) || !rows_map(&v, p.v, p.Tk, p.Hkv, p.D))
         return cudaErrorInvalidValue;
     Params pp{p, (p.Hq / p.Hkv) % 2 == 0, tc_wait_limit_ns()};
     const int64_t grid = (p.T / (pp.pair_heads ? kTile : 2 * kTile) + p.B) * (int64_t)(pp.pair_heads ? p.Hq / 2 : p.Hq);
     if (grid > INT32_MAX) return cudaErrorInvalidConfiguration;
-    return launch_k(kernel, dim3((unsigned)grid), dim3(kThreads), Smem<DK>::BYTES, stream, q, k, v, pp);
+    return launch_k(kernel, dim3((unsigned)grid), dim3(kThreads), Smem<DK>::BYTES, stream, q, k, v, o, pp);
 }
 
 }  // namespace
@@ -514,7 +729,7 @@ cudaError_t prompt_as(const AttnProblem& p, cudaStream_t stream) {
 // (a negative scale would make a row's smallest product its largest score)
 bool attn_prompt_tc_supported(const AttnProblem& p) {
     return p.act_dtype == GBMOE_BF16 && p.D <= 128 && !p.paged && p.Tk > 0 && p.scale_log2 > 0.0f &&
-           tma_strides(p.q, p.T, p.Hq) && tma_strides(p.k, p.Tk, p.Hkv) && tma_strides(p.v, p.Tk, p.Hkv);
+           tma_strides(p.q, p.T, p.Hq) && tma_strides(p.out, p.T, p.Hq) && tma_strides(p.k, p.Tk, p.Hkv) && tma_strides(p.v, p.Tk, p.Hkv);
 }
 
 cudaError_t launch_attn_prompt_tc(const AttnProblem& p, cudaStream_t stream) {
