@@ -61,11 +61,22 @@ struct AttnProblem {
     int page_log2;
     // cached attention: CTAs (shares of the work), the least blocks of a share, rows of
     // a tile, and the partial results [2 * shares, rows, D] sums and [2 * shares, rows, 4]
-    // statistics of tiles cut by the shares' ends
+    // statistics of tiles cut by the shares' ends, with a record of the tile that each
+    // share's end cuts for the join
     int shares, min_blocks, tile_rows;
     float *part_o, *part_s;
+    struct CutTile* cuts;
     int32_t* err;
 };
+
+// The tile that begins in a share and goes on in the next ones.
+struct CutTile {
+    int parts;           // shares that it lies in; 0: the share cuts none
+    int first;           // slot of its first part (the next ones: 2 (share + 1), 2 (share + 2), ..)
+    int head, tile;      // kv head, row tile
+    int q0, nq, len, pad;  // its sequence
+};
+static_assert(sizeof(CutTile) == 32, "two 16-byte loads");
 
 constexpr int kBlockKeys = 64;   // keys of a block of work
 constexpr int kMaxTileRows = 16;

@@ -186,6 +186,19 @@ struct Walk {
         cut();
         return true;
     }
+    // For one thread, at a segment's end (or, idle, where the share holds nothing): what the join is to know
+    __device__ __forceinline__ void note(const AttnProblem& p) const {
+        if (u + g.blk1 - g.blk0 < u1) return;  // not the share's last segment
+        CutTile c{};
+        if (g.blk0 == 0 && g.blk1 < g.nb) {
+            c.parts = (int)((g.nb - g.blk1 + sh.each - 1) / sh.each) + 1;
+            c.first = (int)g.slot;
+            c.head = g.head, c.tile = g.tile;
+            c.q0 = g.s.q0, c.nq = g.s.nq, c.len = g.s.len;
+        }
+        p.cuts[share] = c;
+    }
+    __device__ __forceinline__ static void note_idle(const AttnProblem& p, int64_t share) { p.cuts[share] = CutTile{}; }
     __device__ __forceinline__ void enter(const AttnProblem& p, int b) {
         g.b = b;
         g.s = load_seq(p, b);

@@ -16,8 +16,35 @@ namespace {
 constexpr int kThreads = 128;
 constexpr int kKeys = 32;
 
-// Eight elements of key or value row `key` of sequence s, widened; a key whose
-// page is outside the pool gives false.
+// Eight elements of a key or value row as loaded (several loads in flight), and
+// their scale; good: false where the key's page is outside the pool.
+template <typename TA, bool kE4m3>
+struct Piece {
+    uint4 v[kE4m3 ? 1 : sizeof(TA) / 2];
+    float sc;
+    bool good;
+    __device__ __forceinline__ void widen(float (&x)[8]) const {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = 0.0f;
+        if (!good) return;
+        if constexpr (kE4m3) {
+            const float2 a = e4m3x2_to_f32x2(v[0].x & 0xffffu), b = e4m3x2_to_f32x2(v[0].x >> 16);
+            const float2 c = e4m3x2_to_f32x2(v[0].y & 0xffffu), d = e4m3x2_to_f32x2(v[0].y >> 16);
+            x[0] = a.x * sc, x[1] = a.y * sc, x[2] = b.x * sc, x[3] = b.y * sc;
+            x[4] = c.x * sc, x[5] = c.y * sc, x[6] = d.x * sc, x[7] = d.y * sc;
+        } else if constexpr (sizeof(TA) == 4) {
+            const uint32_t w[8] = {v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(w[i]);
+        } else {
+            const uint32_t w[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = i & 1 ? bf16hi(w[i >> 1]) : bf16lo(w[i >> 1]);
+        }
+    }
+};
+
+// Key or value rows of sequence b: packed rows, or the pool's.
 template <typename TA, bool kE4m3, bool kPaged>
 struct Source {
     const AttnProblem& p;
@@ -27,26 +54,28 @@ struct Source {
     int h, b;
     int64_t k0;
 
-    __device__ __forceinline__ bool load(int key, int d, float (&v)[8]) const {
+    __device__ __forceinline__ void load(int key, int d, Piece<TA, kE4m3>& x) const {
+        x.good = true;
+        x.sc = 1.0f;
+        const void* src;
         if (!kPaged) {
-            Vec8<TA>::load(static_cast<const TA*>(rows.p) + (k0 + key) * rows.ts + h * rows.hs + d, v);
-            return true;
-        }
-        const int pg = key / p.page, id = p.page_table[(int64_t)b * p.max_pages + pg];
-        if (id < 0 || id >= p.n_pages) return false;
-        const int64_t head = (int64_t)id * p.Hkv + h;
-        const int64_t at = (head * p.page + (key - pg * p.page)) * p.D + d;
-        if constexpr (kE4m3) {
-            const uint2 c = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(pool) + at);
-            const float sc = e8m0_to_f32(scales[head]);
-            const float2 a = e4m3x2_to_f32x2(c.x & 0xffffu), e = e4m3x2_to_f32x2(c.x >> 16);
-            const float2 f = e4m3x2_to_f32x2(c.y & 0xffffu), g = e4m3x2_to_f32x2(c.y >> 16);
-            v[0] = a.x * sc, v[1] = a.y * sc, v[2] = e.x * sc, v[3] = e.y * sc;
-            v[4] = f.x * sc, v[5] = f.y * sc, v[6] = g.x * sc, v[7] = g.y * sc;
+            src = static_cast<const TA*>(rows.p) + (k0 + key) * rows.ts + h * rows.hs + d;
         } else {
-            Vec8<TA>::load(static_cast<const TA*>(pool) + at, v);
+            const int id = p.page_table[(int64_t)b * p.max_pages + (key >> p.page_log2)];
+            x.good = id >= 0 && id < p.n_pages;
+            if (!x.good) return;
+            const int64_t head = (int64_t)id * p.Hkv + h;
+            const int64_t at = (head * p.page + (key & (p.page - 1))) * p.D + d;
+            if constexpr (kE4m3) x.sc = e8m0_to_f32(scales[head]);
+            src = static_cast<const char*>(pool) + at * (kE4m3 ? 1 : (int)sizeof(TA));
         }
-        return true;
+        if constexpr (kE4m3) {
+            const uint2 c = *static_cast<const uint2*>(src);
+            x.v[0].x = c.x, x.v[0].y = c.y;
+        } else {
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(TA) / 2; ++i) x.v[i] = static_cast<const uint4*>(src)[i];
+        }
     }
 };
 
@@ -110,18 +139,37 @@ __device__ __forceinline__ void attend(const AttnProblem& p, const Segment& it) 
     }
     const Source<TA, kE4m3, kPaged> src_k{p, p.k_pool, p.k_scale, p.k, h, it.b, it.s.k0};
     const Source<TA, kE4m3, kPaged> src_v{p, p.v_pool, p.v_scale, p.v, h, it.b, it.s.k0};
+    // A thread's pieces of a tile: rows (tid + 128 i) / (DP / 8). Up to head sizes of 128
+    // the next tile's are in flight while this one is computed (beyond, the registers are short).
+    constexpr int PIECES = kKeys * (DP / 8) / kThreads;
+    constexpr bool kAhead = DP <= 128;
+    Piece<TA, kE4m3> pk[PIECES], pv[PIECES];
+    auto load = [&](int k0) {
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const int x = tid + kThreads * i, r = x / (DP / 8), d = 8 * (x % (DP / 8));
+            pk[i].good = pv[i].good = false;
+            if (k0 + r >= k_hi || d >= p.D) continue;
+            src_k.load(k0 + r, d, pk[i]);
+            src_v.load(k0 + r, d, pv[i]);
+        }
+    };
+    if (kAhead && k_lo < k_hi) load(k_lo);
     for (int k0 = k_lo; k0 < k_hi; k0 += kKeys) {
         __syncthreads();
-        for (int i = tid; i < kKeys * (DP / 8); i += kThreads) {
-            const int r = i / (DP / 8), d = 8 * (i % (DP / 8));
-            float a[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, b[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            bool good = k0 + r < k_hi;
-            if (good && d < p.D) good = src_k.load(k0 + r, d, a) && src_v.load(k0 + r, d, b);
+        if (!kAhead) load(k0);
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const int x = tid + kThreads * i, r = x / (DP / 8), d = 8 * (x % (DP / 8));
+            float a[8];
+            pk[i].widen(a);
             Vec8<float>::store(sk + r * kLd<DP> + d, a);
-            Vec8<float>::store(sv + r * kLd<DP> + d, b);
-            if (d == 0) ok[r] = good;
+            pv[i].widen(a);
+            Vec8<float>::store(sv + r * kLd<DP> + d, a);
+            if (d == 0) ok[r] = pk[i].good;
         }
         __syncthreads();
+        if (kAhead && k0 + kKeys < k_hi) load(k0 + kKeys);
         float s[N][4] = {};
         for (int d = 0; d < p.D; d += 4) {
             float4 a[N], b[4];
@@ -226,9 +274,13 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(const AttnProblem p
     __shared__ int64_t plan[plan_words(kThreads)];
     if constexpr (N == 1) {
         Walk<16> w;
-        if (!w.begin(p, blockIdx.x, plan)) return;
+        if (!w.begin(p, blockIdx.x, plan)) {
+            if (threadIdx.x == 0) w.note_idle(p, blockIdx.x);
+            return;
+        }
         do {
             attend<TA, kE4m3, DP, N>(p, w.g);
+            if (threadIdx.x == 0) w.note(p);
             __syncthreads();
         } while (w.next(p));
     } else {
@@ -279,131 +331,111 @@ cudaError_t simt_source(const AttnProblem& p, cudaStream_t stream) {
 
 // ------------------------------------------------------------------- join
 //
-// Block x: where share x ends inside a tile that begins in it, that tile. The
-// parts' sums, each relative to 2^(its own third statistic), are brought to the
-// largest of those and added, the softmax sums likewise relative to the first
-// statistic: out = sum / l. A row has as many of the eight warps as there are to
-// spare, each adding every so many parts; the order is fixed by the lengths.
-// The search for the tile reads only what the kernel before this launch's
-// predecessor has written, so it runs before the wait for that one.
-constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32;
+// Block (x, y): rows 4 y .. of the tile that share x's end cuts. The parts' sums,
+// each relative to 2^(its own third statistic), are brought to the largest of
+// those and added, the softmax sums likewise relative to the first statistic:
+// out = sum / l. Two warps of a row take every other part; the order is fixed by
+// the lengths.
+constexpr int kJoinThreads = 256, kJoinRows = 4;
+
+// kWide: D over 128, two columns groups of a lane
+template <typename TA, bool kWide>
+__global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const __grid_constant__ AttnProblem p) {
+    pdl_enter();
+    constexpr int Z = kWide ? 2 : 1;
+    __shared__ float4 acc[kJoinRows][32 * Z];
+    const int lane = threadIdx.x & 31, half = (threadIdx.x >> 5) & 1, in = threadIdx.x >> 6;
+    const int4* rec = reinterpret_cast<const int4*>(p.cuts + blockIdx.x);
+    const int4 c0 = __ldcg(rec), c1 = __ldcg(rec + 1);
+    const int n = c0.x, first = c0.y, head = c0.z, tile = c0.w, q0 = c1.x;
+    if (n == 0) return;
+    Seq s{};
+    s.q0 = q0, s.nq = c1.y, s.len = c1.z;
+    const int G = p.R, rows = p.tile_rows, r = blockIdx.y * kJoinRows + in;
+    const int64_t row = (int64_t)tile * rows + r;
+    const bool have = r < rows && row < (int64_t)s.nq * G;
+    const int d = 4 * lane;
+    float m = neg_inf(), mo = neg_inf(), l = 0.0f, base = 0.0f, base_o = 0.0f;
+    float o[Z][4] = {};
+    if (have) {
+        const float4* st = reinterpret_cast<const float4*>(p.part_s);
+        auto slot = [&](int c) { return (c > 0 ? 2 * ((int64_t)blockIdx.x + c) : first) * rows + r; };
+        float4 mine = make_float4(neg_inf(), 0.0f, neg_inf(), 0.0f);  // of part `lane`
+        if (lane < n) mine = __ldcg(st + slot(lane));
+        m = mine.x, mo = mine.z;
+        for (int c = lane + 32; c < n; c += 32) {
+            const float4 v = __ldcg(st + slot(c));
+            m = fmaxf(m, v.x), mo = fmaxf(mo, v.z);
+        }
+#pragma unroll
+        for (int e = 16; e; e >>= 1) {
+            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, e));
+            mo = fmaxf(mo, __shfl_xor_sync(0xffffffffu, mo, e));
+        }
+        base = m == neg_inf() ? 0.0f : m, base_o = mo == neg_inf() ? 0.0f : mo;
+        for (int g0 = 0; g0 < n; g0 += 32) {
+            if (g0 > 0) {
+                mine = make_float4(neg_inf(), 0.0f, neg_inf(), 0.0f);
+                if (g0 + lane < n) mine = __ldcg(st + slot(g0 + lane));
+            }
+            l += mine.y * exp2f(mine.x - base);
+            const float f = exp2f(mine.z - base_o);
+            const int k = min(32, n - g0);
+            for (int c = half; c < k; c += 16) {  // eight parts' loads in flight
+                float4 v[8][Z];
+                float w[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int cc = c + 2 * i;
+                    w[i] = __shfl_sync(0xffffffffu, f, min(cc, k - 1));
+                    const float* src = p.part_o + slot(g0 + min(cc, k - 1)) * p.D + d;
+#pragma unroll
+                    for (int z = 0; z < Z; ++z)
+                        v[i][z] = cc < k && d + 128 * z < p.D ? __ldcg(reinterpret_cast<const float4*>(src + 128 * z))
+                                                              : make_float4(0.f, 0.f, 0.f, 0.f);
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    if (c + 2 * i >= k || w[i] == 0.0f) continue;  // (a part that this row does not see: its sums are 0)
+#pragma unroll
+                    for (int z = 0; z < Z; ++z) {
+                        o[z][0] = fmaf(v[i][z].x, w[i], o[z][0]), o[z][1] = fmaf(v[i][z].y, w[i], o[z][1]);
+                        o[z][2] = fmaf(v[i][z].z, w[i], o[z][2]), o[z][3] = fmaf(v[i][z].w, w[i], o[z][3]);
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int e = 16; e; e >>= 1) l += __shfl_xor_sync(0xffffffffu, l, e);
+    }
+    if (half == 1)
+#pragma unroll
+        for (int z = 0; z < Z; ++z) acc[in][lane + 32 * z] = make_float4(o[z][0], o[z][1], o[z][2], o[z][3]);
+    __syncthreads();
+    if (!have || half == 1) return;
+    int lo, hi;
+    seen_keys(p, s, (int)(row / G), lo, hi);
+    const bool empty = hi < lo || (m == neg_inf() && l == 0.0f);
+    const int64_t t = s.q0 + row / G;
+    const int hq = head * G + (int)(row % G);
+    if (p.lse && lane == 0) p.lse[t * p.Hq + hq] = empty ? neg_inf() : (base + log2f(l)) * kLn2;
+    const float inv = empty ? 0.0f : exp2f(base_o - base) / l;
+    TA* out = const_cast<TA*>(static_cast<const TA*>(p.out.p)) + t * p.out.ts + hq * p.out.hs + d;
+#pragma unroll
+    for (int z = 0; z < Z; ++z) {
+        if (d + 128 * z >= p.D) break;
+        const float4 v = acc[in][lane + 32 * z];
+        const float y[4] = {(o[z][0] + v.x) * inv, (o[z][1] + v.y) * inv, (o[z][2] + v.z) * inv, (o[z][3] + v.w) * inv};
+        if constexpr (sizeof(TA) == 4) *reinterpret_cast<float4*>(out + 128 * z) = make_float4(y[0], y[1], y[2], y[3]);
+        else *reinterpret_cast<uint2*>(out + 128 * z) = make_uint2(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]));
+    }
+}
 
 template <typename TA>
-__global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const __grid_constant__ AttnProblem p) {
-    __shared__ int64_t plan[plan_words(kJoinThreads)];
-    __shared__ float4 acc[kJoinWarps][64];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rows = p.tile_rows;
-    Shares sh;
-    const Place at = find_place(
-        p.B, [&](int b) { const Seq s = load_seq(p, b); return row_tiles(p, s, rows) * key_blocks(s) * p.Hkv; },
-        [&](int64_t total) { sh.set(p, total); return (blockIdx.x + 1) * sh.each; }, plan);
-    Seq s{};
-    int nb = 1, blk = 0, h = 0, tile = 0;
-    if (at.b >= 0) {
-        s = load_seq(p, at.b);
-        nb = key_blocks(s);
-        const int tiles = (int)row_tiles(p, s, rows);
-        const int64_t ht = at.at / nb;
-        blk = (int)(at.at - ht * nb);
-        h = (int)(ht / tiles), tile = (int)(ht - (int64_t)h * tiles);
-    }
-    pdl_enter();
-    if (blk == 0 || blk > sh.each) return;  // no tile, or it begins here, or before this share
-    const int G = p.R;
-    const int n_rows = (int)min64(rows, (int64_t)s.nq * G - (int64_t)tile * rows);
-    const int per = n_rows <= 1 ? 8 : n_rows <= 2 ? 4 : n_rows <= 4 ? 2 : 1;  // warps of a row
-    // parts: the end of this share, then the beginnings of the next ones
-    const int64_t i0 = blockIdx.x;
-    const int n = (int)((nb - blk + sh.each - 1) / sh.each) + 1;
-    const int64_t first = blk == sh.each ? 2 * i0 : 2 * i0 + 1;  // (the tile may be all of this share)
-    const float4* st = reinterpret_cast<const float4*>(p.part_s);
-    for (int r0 = 0; r0 < n_rows; r0 += kJoinWarps / per) {
-        const int r = r0 + warp / per, mine = warp % per;
-        const bool have = r < n_rows;
-        float m = neg_inf(), mo = neg_inf(), l = 0.0f;
-        float o[2][4] = {};
-        float base = 0.0f, base_o = 0.0f;
-        const int d = 4 * lane;
-        if (have) {
-            auto slot = [&](int c) { return (c > 0 ? 2 * (i0 + c) : first) * rows + r; };
-            for (int c = lane; c < n; c += 32) {
-                const float4 v = __ldcg(st + slot(c));
-                m = fmaxf(m, v.x), mo = fmaxf(mo, v.z);
-            }
-#pragma unroll
-            for (int e = 16; e; e >>= 1) {
-                m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, e));
-                mo = fmaxf(mo, __shfl_xor_sync(0xffffffffu, mo, e));
-            }
-            base = m == neg_inf() ? 0.0f : m, base_o = mo == neg_inf() ? 0.0f : mo;
-            for (int c0 = 0; c0 < n; c0 += 32) {
-                float f = 0.0f;
-                if (c0 + lane < n) {
-                    const float4 v = __ldcg(st + slot(c0 + lane));
-                    l += v.y * exp2f(v.x - base);
-                    f = exp2f(v.z - base_o);
-                }
-                const int k = min(32, n - c0);
-                for (int c = mine; c < k; c += 8 * per) {  // eight parts' loads in flight
-                    float4 v[8][2];
-                    float w[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int cc = c + i * per;
-                        w[i] = __shfl_sync(0xffffffffu, f, min(cc, k - 1));
-                        const float* src = p.part_o + slot(c0 + min(cc, k - 1)) * p.D + d;
-#pragma unroll
-                        for (int z = 0; z < 2; ++z)
-                            v[i][z] = cc < k && d + 128 * z < p.D ? __ldcg(reinterpret_cast<const float4*>(src + 128 * z))
-                                                                  : make_float4(0.f, 0.f, 0.f, 0.f);
-                    }
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        if (c + i * per >= k || w[i] == 0.0f) continue;  // (a part that this row does not see: its sums are 0)
-#pragma unroll
-                        for (int z = 0; z < 2; ++z) {
-                            o[z][0] = fmaf(v[i][z].x, w[i], o[z][0]), o[z][1] = fmaf(v[i][z].y, w[i], o[z][1]);
-                            o[z][2] = fmaf(v[i][z].z, w[i], o[z][2]), o[z][3] = fmaf(v[i][z].w, w[i], o[z][3]);
-                        }
-                    }
-                }
-            }
-#pragma unroll
-            for (int e = 16; e; e >>= 1) l += __shfl_xor_sync(0xffffffffu, l, e);
-        }
-        if (per > 1) {
-            __syncthreads();
-#pragma unroll
-            for (int z = 0; z < 2; ++z) acc[warp][lane + 32 * z] = make_float4(o[z][0], o[z][1], o[z][2], o[z][3]);
-            __syncthreads();
-            if (mine == 0)
-                for (int w = 1; w < per; ++w)
-#pragma unroll
-                    for (int z = 0; z < 2; ++z) {
-                        const float4 v = acc[warp + w][lane + 32 * z];
-                        o[z][0] += v.x, o[z][1] += v.y, o[z][2] += v.z, o[z][3] += v.w;
-                    }
-        }
-        if (!have || mine != 0) continue;
-        const int64_t row = (int64_t)tile * rows + r;
-        int lo, hi;
-        seen_keys(p, s, (int)(row / G), lo, hi);
-        const bool empty = hi < lo || (m == neg_inf() && l == 0.0f);
-        const int64_t t = s.q0 + row / G;
-        const int hq = h * G + (int)(row % G);
-        if (p.lse && lane == 0) p.lse[t * p.Hq + hq] = empty ? neg_inf() : (base + log2f(l)) * kLn2;
-        const float inv = empty ? 0.0f : exp2f(base_o - base) / l;
-        TA* out = const_cast<TA*>(static_cast<const TA*>(p.out.p)) + t * p.out.ts + hq * p.out.hs + d;
-#pragma unroll
-        for (int z = 0; z < 2; ++z) {
-            if (d + 128 * z >= p.D) break;
-            if constexpr (sizeof(TA) == 4)
-                *reinterpret_cast<float4*>(out + 128 * z) = make_float4(o[z][0] * inv, o[z][1] * inv, o[z][2] * inv, o[z][3] * inv);
-            else
-                *reinterpret_cast<uint2*>(out + 128 * z) =
-                    make_uint2(pack_bf16x2(o[z][0] * inv, o[z][1] * inv), pack_bf16x2(o[z][2] * inv, o[z][3] * inv));
-        }
-    }
+cudaError_t join_as(const AttnProblem& p, cudaStream_t stream) {
+    const dim3 grid(p.shares - 1, (p.tile_rows + kJoinRows - 1) / kJoinRows);
+    return p.D > 128 ? launch_k(attn_join_kernel<TA, true>, grid, dim3(kJoinThreads), 0, stream, p)
+                     : launch_k(attn_join_kernel<TA, false>, grid, dim3(kJoinThreads), 0, stream, p);
 }
 
 }  // namespace
@@ -413,9 +445,7 @@ cudaError_t launch_attn_simt(const AttnProblem& p, cudaStream_t stream) {
 }
 
 cudaError_t launch_attn_join(const AttnProblem& p, cudaStream_t stream) {
-    const dim3 grid(p.shares - 1);
-    return p.act_dtype == GBMOE_F32 ? launch_k(attn_join_kernel<float>, grid, dim3(kJoinThreads), 0, stream, p)
-                                    : launch_k(attn_join_kernel<__nv_bfloat16>, grid, dim3(kJoinThreads), 0, stream, p);
+    return p.act_dtype == GBMOE_F32 ? join_as<float>(p, stream) : join_as<__nv_bfloat16>(p, stream);
 }
 
 }  // namespace gbmoe

@@ -162,7 +162,10 @@ attn_split_kernel(const __grid_constant__ AttnProblem p, uint64_t wait_limit_ns)
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     Walk<kRows> walk;
-    if (!walk.begin(p, blockIdx.x, plan)) return;  // (every thread synchronised in there)
+    if (!walk.begin(p, blockIdx.x, plan)) {  // (every thread synchronised in there)
+        if (tid == 0) walk.note_idle(p, blockIdx.x);
+        return;
+    }
     int slot = 0;         // of the next stage to be read; fetches run ahead of it
     uint32_t parity = 0;  // of its barrier
 
@@ -532,11 +535,14 @@ attn_split_kernel(const __grid_constant__ AttnProblem p, uint64_t wait_limit_ns)
                 }
             }
         }
+        if (tid == 0) walk.note(p);
         // the next segment's copies follow these reads and writes of the ring
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncthreads();
     } while (walk.next(p));
-    // (a warp whose wait gave up has copies in flight: they land before the CTA leaves)
+    // (a warp whose wait gave up has copies in flight: they land before the CTA leaves;
+    // the join leaves this share's tile alone)
+    if (*abort_flag && tid == 0) walk.note_idle(p, blockIdx.x);
     if (*abort_flag && lane == 0) {
         const uint64_t t0 = global_ns();
         for (int i = 0; i < STAGES; ++i) {
