@@ -168,6 +168,7 @@ attn_split_kernel(const __grid_constant__ AttnProblem p, uint64_t wait_limit_ns)
     }
     int slot = 0;         // of the next stage to be read; fetches run ahead of it
     uint32_t parity = 0;  // of its barrier
+    int pending = 0;      // copies in flight when a wait gave up
 
     do {
         const Segment& it = walk.g;
@@ -288,7 +289,10 @@ attn_split_kernel(const __grid_constant__ AttnProblem p, uint64_t wait_limit_ns)
             }
             const int id = __shfl_sync(kFull, pg[0], i & 31);
             const uint32_t scales = kE4m3 ? __shfl_sync(kFull, sc[0], i & 31) : 0;
-            if (!warp_wait(&full[slot], parity, abort_flag, p.err, wait_limit_ns)) break;
+            if (!warp_wait(&full[slot], parity, abort_flag, p.err, wait_limit_ns)) {
+                pending = ahead - i;
+                break;
+            }
             uint8_t* sk = ring + slot * 2 * S::TILE;
             uint8_t* sv = sk + S::TILE;
             if (++slot == STAGES) slot = 0, parity ^= 1;
@@ -543,9 +547,9 @@ attn_split_kernel(const __grid_constant__ AttnProblem p, uint64_t wait_limit_ns)
     // (a warp whose wait gave up has copies in flight: they land before the CTA leaves;
     // the join leaves this share's tile alone)
     if (*abort_flag && tid == 0) walk.note_idle(p, blockIdx.x);
-    if (*abort_flag && lane == 0) {
+    if (lane == 0) {
         const uint64_t t0 = global_ns();
-        for (int i = 0; i < STAGES; ++i) {
+        for (int i = 0; i < pending; ++i) {
             drain_wait(&full[slot], parity, t0);
             if (++slot == STAGES) slot = 0, parity ^= 1;
         }

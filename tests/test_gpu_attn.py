@@ -521,3 +521,22 @@ def test_prompt_then_decode_on_another_stream():
     assert np.abs(wide(out)[:n] - want[:n]).max() <= 0.03 * vmax
     assert np.abs(wide(out)[n:] - want[n:]).max() <= 0.08 * vmax
     assert np.abs(wide(again)[:n] - want[:n]).max() <= 0.15 * vmax
+
+
+def test_waits_that_run_out_are_reported_and_leave_the_next_call_clean(monkeypatch):
+    """With a limit of 0 ns on the pipeline waits attn_prompt gives up, the error word says so, and a call with the
+    normal limit is right again."""
+    rng = np.random.default_rng(9)
+    n, Hq, Hkv, D = 700, 4, 2, 128
+    q, k, v = (normal(rng, (n, h, D), "bf16") for h in (Hq, Hkv, Hkv))
+    cfg = gb.attn_config(Hq, Hkv, D)
+    ws = torch.zeros(gb.attn_workspace_size(cfg, n, 1), dtype=torch.uint8, device="cuda")
+    cu, out = prefix([n]), torch.zeros_like(q)
+    monkeypatch.setenv("GBMOE_TC_WAIT_LIMIT_NS", "0")
+    gb.attn_prompt(cfg, q, k, v, cu, cu, out, ws)
+    assert gb.moe_device_status(ws) == gb.EDEVICE_TIMEOUT
+    monkeypatch.delenv("GBMOE_TC_WAIT_LIMIT_NS")
+    gb.attn_prompt(cfg, q, k, v, cu, cu, out, ws)
+    assert gb.moe_device_status(ws) == gb.OK
+    want, _ = packed_reference(wide(q), wide(k), wide(v), [n], [n], cfg.scale, True, 0)
+    assert (np.abs(wide(out) - want) <= attention_tolerance("bf16", want, np.abs(wide(v)).max())).all()
