@@ -196,22 +196,29 @@ struct Work {
     int end;                // 1: no more work
 };
 
-// Row tile `index` of the list, by a whole warp (every lane gets it); b = -1: past the end.
-__device__ __forceinline__ Place warp_find_tile(const AttnProblem& p, int64_t index, int rows) {
-    const int lane = threadIdx.x & 31;
-    int64_t before = 0;
-    for (int base = 0; base < p.B; base += 32) {
-        const int64_t v = base + lane < p.B ? row_tiles(p, load_seq(p, base + lane), rows) : 0;
-        const int64_t pre = warp_scan(v) + before;
-        const uint32_t hit = __ballot_sync(0xffffffffu, index < pre);
-        if (hit) {
-            const int l = __ffs(hit) - 1;
-            return Place{base + l, index - __shfl_sync(0xffffffffu, pre - v, l)};
+// Finds row tiles of the list, by a whole warp (every lane gets the answer). The
+// indices that a CTA is given mostly rise, so a search goes on where the last one ended.
+struct TileFinder {
+    int base = 0;        // first of the 32 sequences looked at last
+    int64_t before = 0;  // tiles before them
+
+    // b = -1: past the end
+    __device__ __forceinline__ Place find(const AttnProblem& p, int64_t index, int rows) {
+        const int lane = threadIdx.x & 31;
+        if (index < before) base = 0, before = 0;
+        for (; base < p.B; base += 32) {
+            const int64_t v = base + lane < p.B ? row_tiles(p, load_seq(p, base + lane), rows) : 0;
+            const int64_t pre = warp_scan(v) + before;
+            const uint32_t hit = __ballot_sync(0xffffffffu, index < pre);
+            if (hit) {
+                const int l = __ffs(hit) - 1;
+                return Place{base + l, index - __shfl_sync(0xffffffffu, pre - v, l)};
+            }
+            before = __shfl_sync(0xffffffffu, pre, 31);
         }
-        before = __shfl_sync(0xffffffffu, pre, 31);
+        return Place{-1, 0};
     }
-    return Place{-1, 0};
-}
+};
 
 // Asks for a CTA of this grid that has not started (its index comes as 16 bytes at dst, counted on bar).
 __device__ __forceinline__ void try_cancel(void* dst, uint64_t* bar) {
@@ -318,7 +325,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             __syncwarp();
             if (lane == 0) mbar_arrive(&w_empty[k & 1]);
             if (end) break;
-            int lo = 0, hi = -1;
+            int lo = 0, hi = INT_MAX;  // (rows past the tile's end are never stored: no mask for them)
             if (r < rows) seen_keys(p, s, row, lo, hi);
             float m = neg_inf(), l = 0.0f;
             for (int j = 0; j < n; ++j) {
@@ -461,13 +468,14 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             const int groups = pp.pair_heads ? p.Hq / 2 : p.Hq;
             const int rows_per = pp.pair_heads ? kTile : 2 * kTile;
             uint32_t block = blockIdx.x;
+            TileFinder tiles;
             bool more = true, asked = false;
             uint32_t turn = 0;
             int k = 0;
             for (; more; ++turn) {
                 if (lane == 0) try_cancel(&answer, ans);
                 asked = true;
-                const Place at = warp_find_tile(p, block / groups, rows_per);
+                const Place at = tiles.find(p, block / groups, rows_per);
                 if (at.b >= 0) {
                     if (!wait_warp(&w_empty[k & 1], ((uint32_t)(k >> 1) & 1u) ^ 1u)) break;
                     Work w;
@@ -480,7 +488,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                     int lo, hi;
                     seen_keys(p, w.s, tile * rows_per, lo, hi);
                     w.k_first = hi < 0 ? 0 : lo & ~(kTile - 1);
-    #pragma unroll
+#pragma unroll
                     for (int t = 0; t < 2; ++t) {
                         w.rows0[t] = tile * rows_per + (pp.pair_heads ? 0 : t * kTile);
                         w.rows[t] = min(kTile, w.s.nq - w.rows0[t]);

@@ -318,6 +318,22 @@ def test_prompt(act, Hq, Hkv, D, nq, nk, causal, window):
 
 
 @pytest.mark.parametrize("act", ["f32", "bf16"])
+def test_prompt_of_many_sequences(act):
+    """More sequences than a warp or a block looks at in one go, runs of empty ones, and a long one behind them."""
+    rng = np.random.default_rng(7)
+    nq = [int(v) for v in rng.integers(0, 9, 700)] + [0] * 70 + [260] + [0] * 30 + [1, 2]
+    Hq, Hkv, D = 4, 2, 64
+    q, k, v = normal(rng, (sum(nq), Hq, D), act), normal(rng, (sum(nq), Hkv, D), act), normal(rng, (sum(nq), Hkv, D), act)
+    cfg = gb.attn_config(Hq, Hkv, D, act=act)
+    ws = torch.zeros(gb.attn_workspace_size(cfg, sum(nq), len(nq)), dtype=torch.uint8, device="cuda")
+    out, lse = torch.zeros_like(q), torch.full((sum(nq), Hq), float("nan"), device="cuda")
+    gb.attn_prompt(cfg, q, k, v, prefix(nq), prefix(nq), out, ws, lse=lse)
+    want, want_lse = packed_reference(wide(q), wide(k), wide(v), nq, nq, cfg.scale, True, 0)
+    check_attention(out, lse, want, want_lse, act, np.abs(wide(v)).max())
+    assert gb.moe_device_status(ws) == gb.OK
+
+
+@pytest.mark.parametrize("act", ["f32", "bf16"])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf")])
 def test_prompt_ignores_what_no_query_sees(act, bad):
     """Keys and values of the sequence behind, and of later tokens of the same sequence, hold NaN or infinities."""
@@ -391,6 +407,26 @@ def test_cached(act, kind, Hq, Hkv, D, page, n, lens, causal, window):
     keep = (prefix(n), i32(lens), c.dev_table)
     gb.attn_cached(cfg, gb.attn_batch(*keep), strided(q), c.bundle, out, ws, lse=lse)
     want, want_lse = cached_reference(wide(q), c, n, lens, cfg.scale, causal, window)
+    vmax = max([np.abs(c.rows("v", b, m)[0]).max() for b, m in enumerate(lens) if m > 0])
+    check_attention(out, lse, want, want_lse, act, vmax)
+    assert gb.moe_device_status(ws) == gb.OK
+
+
+@pytest.mark.parametrize("act,kind,D", [("bf16", "e4m3", 64), ("bf16", "act", 128), ("f32", "act", 64)])
+def test_cached_of_many_sequences(act, kind, D):
+    """More sequences than a block looks at in one go, some without tokens or keys, one with most of the keys."""
+    rng = np.random.default_rng(11)
+    lens = [int(v) for v in rng.integers(0, 70, 600)] + [3000] + [int(v) for v in rng.integers(0, 70, 50)]
+    n = [int(v) for v in rng.integers(0, 3, len(lens))]
+    Hq, Hkv, page = 4, 2, 16
+    c = Cache(rng, act, kind, Hkv, D, page, lens)
+    q = normal(rng, (sum(n), Hq, D), act)
+    cfg = gb.attn_config(Hq, Hkv, D, act=act, cache=kind, page=page)
+    ws = torch.zeros(gb.attn_workspace_size(cfg, sum(n), len(n)), dtype=torch.uint8, device="cuda")
+    out, lse = torch.zeros_like(q), torch.full((sum(n), Hq), float("nan"), device="cuda")
+    keep = (prefix(n), i32(lens), c.dev_table)
+    gb.attn_cached(cfg, gb.attn_batch(*keep), q, c.bundle, out, ws, lse=lse)
+    want, want_lse = cached_reference(wide(q), c, n, lens, cfg.scale, True, 0)
     vmax = max([np.abs(c.rows("v", b, m)[0]).max() for b, m in enumerate(lens) if m > 0])
     check_attention(out, lse, want, want_lse, act, vmax)
     assert gb.moe_device_status(ws) == gb.OK
