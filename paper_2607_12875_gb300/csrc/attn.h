@@ -59,11 +59,11 @@ struct AttnProblem {
     const void *k_pool, *v_pool;
     const uint8_t *k_scale, *v_scale;
     int page_log2;
-    // cached attention: CTAs (shares of the work), the least blocks of a share, rows of
-    // a tile, and the partial results [2 * shares, rows, D] sums and [2 * shares, rows, 4]
+    // cached attention: CTAs (shares of the work), the least blocks of a share, blocks that
+    // a tile's set-up is counted as, rows of a tile, and the partial results [2 * shares, rows, D] sums and [2 * shares, rows, 4]
     // statistics of tiles cut by the shares' ends, with a record of the tile that each
     // share's end cuts for the join
-    int shares, min_blocks, tile_rows;
+    int shares, min_blocks, tile_cost, tile_rows;
     float *part_o, *part_s;
     struct CutTile* cuts;
     int32_t* err;
@@ -72,9 +72,10 @@ struct AttnProblem {
 // The tile that begins in a share and goes on in the next ones.
 struct CutTile {
     int parts;           // shares that it lies in; 0: the share cuts none
+    int rows;            // its rows
     int first;           // slot of its first part (the next ones: 2 (share + 1), 2 (share + 2), ..)
     int head, tile;      // kv head, row tile
-    int q0, nq, len, pad;  // its sequence
+    int q0, nq, len;     // its sequence
 };
 static_assert(sizeof(CutTile) == 32, "two 16-byte loads");
 
@@ -82,14 +83,15 @@ constexpr int kBlockKeys = 64;   // keys of a block of work
 constexpr int kMaxTileRows = 16;
 constexpr int kMaxShares = 608;  // four CTAs on each of 152 SMs
 
-// CTAs of cached attention for `rows` rows of a tile and `per_sm` CTAs on an SM: no
-// more than there can be shares of min_blocks
-inline int shares_of(const AttnProblem& p, int rows, int per_sm, int sms) {
+// Deals out the work of cached attention in tiles of `rows` rows to `per_sm` CTAs on an
+// SM, or as many as there can be shares of min_blocks (more than tile_cost).
+inline void set_shares(AttnProblem& p, int rows, int per_sm, int sms, int min_blocks, int tile_cost) {
+    p.tile_rows = rows, p.min_blocks = min_blocks, p.tile_cost = tile_cost;
     const int64_t tiles = (int64_t)p.T * p.R / rows + p.B;
-    const int64_t blocks = tiles * p.Hkv * (((int64_t)p.max_pages * p.page + kBlockKeys - 1) / kBlockKeys + 1);
+    const int64_t blocks = tiles * p.Hkv * (((int64_t)p.max_pages * p.page + kBlockKeys - 1) / kBlockKeys + 1 + p.tile_cost);
     const int64_t most = (blocks + p.min_blocks - 1) / p.min_blocks;
     const int64_t cap = (int64_t)per_sm * sms < kMaxShares ? (int64_t)per_sm * sms : kMaxShares;
-    return (int)(most < cap ? most : cap);
+    p.shares = (int)(most < cap ? most : cap);
 }
 
 cudaError_t launch_attn_simt(const AttnProblem& p, cudaStream_t stream);

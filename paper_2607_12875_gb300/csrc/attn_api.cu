@@ -14,9 +14,6 @@ namespace {
 constexpr size_t kAlign = 256;
 constexpr int kMaxHeads = 4096;
 constexpr int kMaxRows = 1 << 30;
-// Least blocks of 64 keys of a share: one sequence of 4000 e4m3 keys, 8 kv heads, us: 15.9
-// (1), 13.9 (2), 12.3 (3), 15.2 (4); many keys make larger shares anyway.
-constexpr int kMinShareBlocks = 3;
 
 int log2_of(int v) {
     int b = 0;
@@ -248,7 +245,6 @@ int attn_cached(const gbattn_config* cfg, int32_t T, const gbattn_batch* batch, 
     p.cu_q = batch->cu_q; p.kv_len = batch->kv_len; p.page_table = batch->page_table;
     p.k_pool = cache->k; p.v_pool = cache->v; p.k_scale = cache->k_scale; p.v_scale = cache->v_scale;
     p.page_log2 = log2_of(p.page);
-    p.min_blocks = kMinShareBlocks;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     return cuda_status(attn_split_supported(p) ? launch_attn_split(p, st) : launch_attn_simt(p, st));
 }

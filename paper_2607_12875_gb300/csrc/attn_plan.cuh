@@ -123,18 +123,25 @@ __device__ __forceinline__ Place find_tile(const AttnProblem& p, int64_t index, 
     return find_place(p.B, [&](int b) { return row_tiles(p, load_seq(p, b), rows); }, [&](int64_t) { return index; }, sm);
 }
 
+// a / b for a >= 0, b > 0: 64-bit division takes over a hundred instructions
+__device__ __forceinline__ int64_t div64(int64_t a, int64_t b) {
+    return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
 // Cached attention: the blocks of keys of all row tiles and kv heads, in the
 // order sequence, head, tile, block, are dealt out in equal shares, one per CTA.
+// A tile begins with tile_cost empty blocks, about what its set-up and results
+// cost, so that a share of many short tiles is not more work than the others.
 // A share is a run of segments: blocks blk0 .. blk1 - 1 of one tile and head. A
 // tile that lies whole in a share is finished there; the first and the last
 // segment of a share may be parts of tiles, whose results go to the share's
 // partial slots 2 i and 2 i + 1 for the join.
 struct Shares {
-    int64_t total, each;  // blocks, blocks of a share
+    int64_t total, each;  // blocks, blocks of a share (more than tile_cost: its first segment is never empty)
 
     __device__ __forceinline__ void set(const AttnProblem& p, int64_t blocks) {
         total = blocks;
-        each = max64(p.min_blocks, (blocks + p.shares - 1) / p.shares);
+        each = max64(p.min_blocks, div64(blocks + p.shares - 1, p.shares));
     }
 };
 
@@ -147,33 +154,35 @@ struct Segment {
 template <int kRows>
 struct Walk {
     Shares sh;
-    int64_t u, u0, u1;
+    int64_t u, u0, u1;  // where the segment begins; the share's begin and end
     int64_t share;
-    int tiles;
+    int tiles, x0, x1;  // tiles of a head; the segment's place in its tile, the empty blocks counted
     Segment g;
 
     // whether share `index` holds anything (then g is its first segment)
     __device__ __forceinline__ bool begin(const AttnProblem& p, int64_t index, int64_t* sm) {
         share = index;
         const Place at = find_place(
-            p.B, [&](int b) { const Seq s = load_seq(p, b); return row_tiles(p, s, kRows) * key_blocks(s) * p.Hkv; },
+            p.B,
+            [&](int b) { const Seq s = load_seq(p, b); return row_tiles(p, s, kRows) * (key_blocks(s) + p.tile_cost) * p.Hkv; },
             [&](int64_t total) { sh.set(p, total); return index * sh.each; }, sm);
         if (at.b < 0) return false;
         u = u0 = index * sh.each;
         u1 = min64(u0 + sh.each, sh.total);
         enter(p, at.b);
-        const int64_t per = (int64_t)tiles * g.nb;
-        g.head = (int)(at.at / per);
+        const int nx = g.nb + p.tile_cost;
+        const int64_t per = (int64_t)tiles * nx;
+        g.head = (int)div64(at.at, per);
         const int64_t rest = at.at - g.head * per;
-        g.tile = (int)(rest / g.nb);
-        g.blk0 = (int)(rest - (int64_t)g.tile * g.nb);
-        cut();
+        g.tile = (int)div64(rest, nx);
+        x0 = (int)(rest - (int64_t)g.tile * nx);
+        cut(p);
         return true;
     }
     __device__ __forceinline__ bool next(const AttnProblem& p) {
-        u += g.blk1 - g.blk0;
-        if (u >= u1) return false;
-        g.blk0 = 0;
+        if (last(p)) return false;
+        u += x1 - x0;
+        x0 = 0;
         if (++g.tile == tiles) {
             g.tile = 0;
             if (++g.head == p.Hkv) {
@@ -183,16 +192,19 @@ struct Walk {
                 while (tiles == 0);  // (u < u1 <= total: there is one)
             }
         }
-        cut();
+        cut(p);
         return true;
     }
+    // whether nothing but empty blocks of the next tile follows in the share
+    __device__ __forceinline__ bool last(const AttnProblem& p) const { return u + (x1 - x0) + p.tile_cost >= u1; }
     // For one thread, at a segment's end (or, idle, where the share holds nothing): what the join is to know
     __device__ __forceinline__ void note(const AttnProblem& p) const {
-        if (u + g.blk1 - g.blk0 < u1) return;  // not the share's last segment
+        if (!last(p)) return;
         CutTile c{};
         if (g.blk0 == 0 && g.blk1 < g.nb) {
-            c.parts = (int)((g.nb - g.blk1 + sh.each - 1) / sh.each) + 1;
+            c.parts = (int)div64(g.nb - g.blk1 + sh.each - 1, sh.each) + 1;
             c.first = (int)g.slot;
+            c.rows = (int)min64(kRows, (int64_t)g.s.nq * p.R - (int64_t)g.tile * kRows);
             c.head = g.head, c.tile = g.tile;
             c.q0 = g.s.q0, c.nq = g.s.nq, c.len = g.s.len;
         }
@@ -205,8 +217,9 @@ struct Walk {
         tiles = (int)row_tiles(p, g.s, kRows);
         g.nb = key_blocks(g.s);
     }
-    __device__ __forceinline__ void cut() {
-        g.blk1 = (int)min64(g.nb, g.blk0 + (u1 - u));
+    __device__ __forceinline__ void cut(const AttnProblem& p) {
+        x1 = (int)min64(g.nb + p.tile_cost, x0 + (u1 - u));
+        g.blk0 = max(0, x0 - p.tile_cost), g.blk1 = x1 - p.tile_cost;
         g.slot = g.blk0 == 0 && g.blk1 == g.nb ? -1 : 2 * share + (u != u0);
     }
 };

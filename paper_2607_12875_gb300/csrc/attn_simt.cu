@@ -18,6 +18,9 @@ namespace {
 
 constexpr int kThreads = 128;
 constexpr int kKeys = 32;
+// Cached: shares of one block of 64 keys (11 sequences of up to 518 keys, 4 kv heads of 64, e4m3:
+// 18 us, with 2: 24), which take so long that a tile's set-up counts for nothing.
+constexpr int kMinBlocks = 1, kTileCost = 0;
 
 // Eight elements of a key or value row as loaded (several loads in flight), and
 // their scale; good: false where the key's page is outside the pool.
@@ -309,8 +312,7 @@ cudaError_t simt_as(const AttnProblem& p, cudaStream_t stream) {
         return e;
     if constexpr (N == 1) {
         AttnProblem a = p;
-        a.tile_rows = 16;
-        a.shares = shares_of(p, 16, DP == 256 ? 2 : 4, sm_count());
+        set_shares(a, 16, DP == 256 ? 2 : 4, sm_count(), kMinBlocks, kTileCost);
         if (cudaError_t e = launch_k(kernel, dim3(a.shares), dim3(kThreads), kSmem<DP, N>, stream, a); e != cudaSuccess) return e;
         return a.shares > 1 ? launch_attn_join(a, stream) : cudaSuccess;
     } else {
@@ -335,109 +337,162 @@ cudaError_t simt_source(const AttnProblem& p, cudaStream_t stream) {
 
 // ------------------------------------------------------------------- join
 //
-// Block (x, y): rows 4 y .. of the tile that share x's end cuts. The parts' sums,
-// each relative to 2^(its own third statistic), are brought to the largest of
-// those and added, the softmax sums likewise relative to the first statistic:
-// out = sum / l. Two warps of a row take every other part; the order is fixed by
-// the lengths.
-constexpr int kJoinThreads = 256, kJoinRows = 4;
+// Rows of tiles that were cut. The parts' sums, each relative to 2^(its own third
+// statistic), are brought to the largest of those and added, the softmax sums
+// likewise relative to the first statistic: out = sum / l. Every block counts the
+// rows of all cut tiles for itself and takes its share of them, 1 to 8 at a time
+// and then with 8 to 1 warps for a row, which take every so many of its parts: the
+// order is fixed by the lengths. (A block for each share, most of them with
+// nothing to join, cost 2 ns a block.)
+constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32, kJoinChunks = 3;
+static_assert(kMaxShares <= kJoinThreads * kJoinChunks && kJoinWarps * kJoinChunks <= 32, "shares that a block counts");
 
 // kWide: D over 128, two columns groups of a lane
 template <typename TA, bool kWide>
 __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const __grid_constant__ AttnProblem p) {
     pdl_enter();
     constexpr int Z = kWide ? 2 : 1;
-    __shared__ float4 acc[kJoinRows][32 * Z];
-    const int lane = threadIdx.x & 31, half = (threadIdx.x >> 5) & 1, in = threadIdx.x >> 6;
-    const int4* rec = reinterpret_cast<const int4*>(p.cuts + blockIdx.x);
-    const int4 c0 = __ldcg(rec), c1 = __ldcg(rec + 1);
-    const int n = c0.x, first = c0.y, head = c0.z, tile = c0.w, q0 = c1.x;
-    if (n == 0) return;
-    Seq s{};
-    s.q0 = q0, s.nq = c1.y, s.len = c1.z;
-    const int G = p.R, rows = p.tile_rows, r = blockIdx.y * kJoinRows + in;
-    const int64_t row = (int64_t)tile * rows + r;
-    const bool have = r < rows && row < (int64_t)s.nq * G;
-    const int d = 4 * lane;
-    float m = neg_inf(), mo = neg_inf(), l = 0.0f, base = 0.0f, base_o = 0.0f;
-    float o[Z][4] = {};
-    if (have) {
-        const float4* st = reinterpret_cast<const float4*>(p.part_s);
-        auto slot = [&](int c) { return (c > 0 ? 2 * ((int64_t)blockIdx.x + c) : first) * rows + r; };
-        float4 mine = make_float4(neg_inf(), 0.0f, neg_inf(), 0.0f);  // of part `lane`
-        if (lane < n) mine = __ldcg(st + slot(lane));
-        m = mine.x, mo = mine.z;
-        for (int c = lane + 32; c < n; c += 32) {
-            const float4 v = __ldcg(st + slot(c));
-            m = fmaxf(m, v.x), mo = fmaxf(mo, v.z);
-        }
+    __shared__ float4 acc[kJoinWarps][32 * Z];
+    __shared__ int pre[kJoinThreads * kJoinChunks], sums[kJoinWarps * kJoinChunks];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    // rows of the cut tiles: running sums over 32 shares, sums of those
+    int2 rec[kJoinChunks];
 #pragma unroll
-        for (int e = 16; e; e >>= 1) {
-            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, e));
-            mo = fmaxf(mo, __shfl_xor_sync(0xffffffffu, mo, e));
+    for (int c = 0; c < kJoinChunks; ++c) {
+        const int i = c * kJoinThreads + threadIdx.x;
+        rec[c] = i < p.shares - 1 ? __ldcg(reinterpret_cast<const int2*>(p.cuts + i)) : make_int2(0, 0);
+    }
+#pragma unroll
+    for (int c = 0; c < kJoinChunks; ++c) {
+        int v = rec[c].x > 0 ? rec[c].y : 0;
+#pragma unroll
+        for (int e = 1; e < 32; e <<= 1) {
+            const int u = __shfl_up_sync(0xffffffffu, v, e);
+            if (lane >= e) v += u;
         }
-        base = m == neg_inf() ? 0.0f : m, base_o = mo == neg_inf() ? 0.0f : mo;
-        for (int g0 = 0; g0 < n; g0 += 32) {
-            if (g0 > 0) {
-                mine = make_float4(neg_inf(), 0.0f, neg_inf(), 0.0f);
-                if (g0 + lane < n) mine = __ldcg(st + slot(g0 + lane));
+        pre[c * kJoinThreads + threadIdx.x] = v;
+        if (lane == 31) sums[c * kJoinWarps + warp] = v;
+    }
+    __syncthreads();
+    int upto = lane < kJoinWarps * kJoinChunks ? sums[lane] : 0;
+    const int own = upto;
+#pragma unroll
+    for (int e = 1; e < 32; e <<= 1) {
+        const int u = __shfl_up_sync(0xffffffffu, upto, e);
+        if (lane >= e) upto += u;
+    }
+    const int total = __shfl_sync(0xffffffffu, upto, 31), grid = gridDim.x;
+    const int at_once = total > 4 * grid ? 8 : total > 2 * grid ? 4 : total > grid ? 2 : 1;  // rows
+    const int W = kJoinWarps / at_once, in = warp / W, part = warp % W;                     // warps of a row
+    for (int q0 = blockIdx.x * at_once; q0 < total; q0 += grid * at_once) {
+        const int q = q0 + in;
+        const bool have = q < total;
+        int d = 4 * lane, n = 0;
+        float m = neg_inf(), mo = neg_inf(), l = 0.0f, base = 0.0f, base_o = 0.0f;
+        float o[Z][4] = {};
+        int4 c0 = make_int4(0, 0, 0, 0), c1 = c0;
+        int r = 0;
+        if (have) {
+            const int chunk = __ffs(__ballot_sync(0xffffffffu, q < upto)) - 1;
+            r = q - __shfl_sync(0xffffffffu, upto - own, chunk);
+            const int run = pre[32 * chunk + lane];
+            const int at = __ffs(__ballot_sync(0xffffffffu, r < run)) - 1;
+            const int before = __shfl_sync(0xffffffffu, run, max(at - 1, 0));
+            if (at > 0) r -= before;
+            const int share = 32 * chunk + at;
+            const int4* rec4 = reinterpret_cast<const int4*>(p.cuts + share);
+            c0 = __ldcg(rec4), c1 = __ldcg(rec4 + 1);
+            n = c0.x;
+            const int rows = p.tile_rows, first = c0.z;
+            const float4* st = reinterpret_cast<const float4*>(p.part_s);
+            auto slot = [&](int c) { return (c > 0 ? 2 * ((int64_t)share + c) : first) * rows + r; };
+            float4 mine = make_float4(neg_inf(), 0.0f, neg_inf(), 0.0f);  // of part `lane`
+            if (lane < n) mine = __ldcg(st + slot(lane));
+            m = mine.x, mo = mine.z;
+            for (int c = lane + 32; c < n; c += 32) {
+                const float4 v = __ldcg(st + slot(c));
+                m = fmaxf(m, v.x), mo = fmaxf(mo, v.z);
             }
-            l += mine.y * exp2f(mine.x - base);
-            const float f = exp2f(mine.z - base_o);
-            const int k = min(32, n - g0);
-            for (int c = half; c < k; c += 16) {  // eight parts' loads in flight
-                float4 v[8][Z];
-                float w[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int cc = c + 2 * i;
-                    w[i] = __shfl_sync(0xffffffffu, f, min(cc, k - 1));
-                    const float* src = p.part_o + slot(g0 + min(cc, k - 1)) * p.D + d;
-#pragma unroll
-                    for (int z = 0; z < Z; ++z)
-                        v[i][z] = cc < k && d + 128 * z < p.D ? __ldcg(reinterpret_cast<const float4*>(src + 128 * z))
-                                                              : make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int e = 16; e; e >>= 1) {
+                m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, e));
+                mo = fmaxf(mo, __shfl_xor_sync(0xffffffffu, mo, e));
+            }
+            base = m == neg_inf() ? 0.0f : m, base_o = mo == neg_inf() ? 0.0f : mo;
+            for (int g0 = 0; g0 < n; g0 += 32) {
+                if (g0 > 0) {
+                    mine = make_float4(neg_inf(), 0.0f, neg_inf(), 0.0f);
+                    if (g0 + lane < n) mine = __ldcg(st + slot(g0 + lane));
                 }
+                l += mine.y * exp2f(mine.x - base);
+                const float f = exp2f(mine.z - base_o);
+                const int k = min(32, n - g0);
+                for (int c = part; c < k; c += 8 * W) {  // eight parts' loads in flight
+                    float4 v[8][Z];
+                    float w[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    if (c + 2 * i >= k || w[i] == 0.0f) continue;  // (a part that this row does not see: its sums are 0)
+                    for (int i = 0; i < 8; ++i) {
+                        const int cc = c + W * i;
+                        w[i] = __shfl_sync(0xffffffffu, f, min(cc, k - 1));
+                        const float* src = p.part_o + slot(g0 + min(cc, k - 1)) * p.D + d;
 #pragma unroll
-                    for (int z = 0; z < Z; ++z) {
-                        o[z][0] = fmaf(v[i][z].x, w[i], o[z][0]), o[z][1] = fmaf(v[i][z].y, w[i], o[z][1]);
-                        o[z][2] = fmaf(v[i][z].z, w[i], o[z][2]), o[z][3] = fmaf(v[i][z].w, w[i], o[z][3]);
+                        for (int z = 0; z < Z; ++z)
+                            v[i][z] = cc < k && d + 128 * z < p.D ? __ldcg(reinterpret_cast<const float4*>(src + 128 * z))
+                                                                  : make_float4(0.f, 0.f, 0.f, 0.f);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        if (c + W * i >= k || w[i] == 0.0f) continue;  // (a part that this row does not see: its sums are 0)
+#pragma unroll
+                        for (int z = 0; z < Z; ++z) {
+                            o[z][0] = fmaf(v[i][z].x, w[i], o[z][0]), o[z][1] = fmaf(v[i][z].y, w[i], o[z][1]);
+                            o[z][2] = fmaf(v[i][z].z, w[i], o[z][2]), o[z][3] = fmaf(v[i][z].w, w[i], o[z][3]);
+                        }
                     }
                 }
             }
+#pragma unroll
+            for (int e = 16; e; e >>= 1) l += __shfl_xor_sync(0xffffffffu, l, e);
         }
+        if (W > 1) {  // (uniform)
+            if (q0 != blockIdx.x * at_once) __syncthreads();  // the rows before are done with acc
 #pragma unroll
-        for (int e = 16; e; e >>= 1) l += __shfl_xor_sync(0xffffffffu, l, e);
-    }
-    if (half == 1)
+            for (int z = 0; z < Z; ++z) acc[warp][lane + 32 * z] = make_float4(o[z][0], o[z][1], o[z][2], o[z][3]);
+            __syncthreads();
+        }
+        if (!have || part > 0) continue;
+        const int G = p.R, row = c1.x * p.tile_rows + r;
+        Seq s{};
+        s.q0 = c1.y, s.nq = c1.z, s.len = c1.w;
+        int lo, hi;
+        seen_keys(p, s, row / G, lo, hi);
+        const bool empty = hi < lo || (m == neg_inf() && l == 0.0f);
+        const int64_t t = s.q0 + row / G;
+        const int hq = c0.w * G + row % G;
+        if (p.lse && lane == 0) p.lse[t * p.Hq + hq] = empty ? neg_inf() : (base + log2f(l)) * kLn2;
+        const float inv = empty ? 0.0f : exp2f(base_o - base) / l;
+        TA* out = const_cast<TA*>(static_cast<const TA*>(p.out.p)) + t * p.out.ts + hq * p.out.hs + d;
 #pragma unroll
-        for (int z = 0; z < Z; ++z) acc[in][lane + 32 * z] = make_float4(o[z][0], o[z][1], o[z][2], o[z][3]);
-    __syncthreads();
-    if (!have || half == 1) return;
-    int lo, hi;
-    seen_keys(p, s, (int)(row / G), lo, hi);
-    const bool empty = hi < lo || (m == neg_inf() && l == 0.0f);
-    const int64_t t = s.q0 + row / G;
-    const int hq = head * G + (int)(row % G);
-    if (p.lse && lane == 0) p.lse[t * p.Hq + hq] = empty ? neg_inf() : (base + log2f(l)) * kLn2;
-    const float inv = empty ? 0.0f : exp2f(base_o - base) / l;
-    TA* out = const_cast<TA*>(static_cast<const TA*>(p.out.p)) + t * p.out.ts + hq * p.out.hs + d;
+        for (int z = 0; z < Z; ++z) {
+            if (d + 128 * z >= p.D) break;
+            float y[4] = {o[z][0], o[z][1], o[z][2], o[z][3]};
+            for (int w = 1; w < W; ++w) {
+                const float4 v = acc[warp + w][lane + 32 * z];
+                y[0] += v.x, y[1] += v.y, y[2] += v.z, y[3] += v.w;
+            }
 #pragma unroll
-    for (int z = 0; z < Z; ++z) {
-        if (d + 128 * z >= p.D) break;
-        const float4 v = acc[in][lane + 32 * z];
-        const float y[4] = {(o[z][0] + v.x) * inv, (o[z][1] + v.y) * inv, (o[z][2] + v.z) * inv, (o[z][3] + v.w) * inv};
-        if constexpr (sizeof(TA) == 4) *reinterpret_cast<float4*>(out + 128 * z) = make_float4(y[0], y[1], y[2], y[3]);
-        else *reinterpret_cast<uint2*>(out + 128 * z) = make_uint2(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]));
+            for (int i = 0; i < 4; ++i) y[i] *= inv;
+            if constexpr (sizeof(TA) == 4) *reinterpret_cast<float4*>(out + 128 * z) = make_float4(y[0], y[1], y[2], y[3]);
+            else *reinterpret_cast<uint2*>(out + 128 * z) = make_uint2(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]));
+        }
     }
 }
 
 template <typename TA>
 cudaError_t join_as(const AttnProblem& p, cudaStream_t stream) {
-    const dim3 grid(p.shares - 1, (p.tile_rows + kJoinRows - 1) / kJoinRows);
+    // as many blocks as there may be rows, up to two on each SM (one or four: up to 2 us slower at 20)
+    const int64_t rows = min64((int64_t)p.T * p.Hq, (int64_t)(p.shares - 1) * p.tile_rows);
+    const dim3 grid((unsigned)min64(rows, 2 * sm_count()));
     return p.D > 128 ? launch_k(attn_join_kernel<TA, true>, grid, dim3(kJoinThreads), 0, stream, p)
                      : launch_k(attn_join_kernel<TA, false>, grid, dim3(kJoinThreads), 0, stream, p);
 }

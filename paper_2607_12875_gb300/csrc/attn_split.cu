@@ -40,6 +40,11 @@ using namespace tc;
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kKeys = kBlockKeys / kWarps;  // keys of a stage of one warp
 constexpr unsigned kFull = 0xffffffffu;
+// Least blocks of 64 keys of a share, and how many a tile's set-up counts for. Us at (3, 2)
+// and (2, 1): one sequence of 4000 e4m3 keys, 8 kv heads 12.3 and 11.6; two of 19000, 1 kv head 16.9
+// and 20.1; 19 of up to 322 with 5 tokens, 4 kv heads 17.3 and 19.7. With (3, 0), where a share holds
+// up to three tiles of one block in turn, the last takes 25 and three sequences of one key 12.6 instead of 7.0.
+constexpr int kMinBlocks = 3, kTileCost = 2;
 static_assert(kKeys == 16, "one MMA of keys, and never more than a page");
 
 // kRows: 8 or 16
@@ -564,8 +569,7 @@ cudaError_t split_as(AttnProblem p, cudaStream_t stream) {
     if (cudaError_t e = once.run([] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM); });
         e != cudaSuccess)
         return e;
-    p.tile_rows = kRows;
-    p.shares = shares_of(p, kRows, S::PER_SM, sm_count());
+    set_shares(p, kRows, S::PER_SM, sm_count(), kMinBlocks, kTileCost);
     if (cudaError_t e = launch_k(kernel, dim3(p.shares), dim3(kThreads), S::SMEM, stream, p, tc_wait_limit_ns()); e != cudaSuccess)
         return e;
     return p.shares > 1 ? launch_attn_join(p, stream) : cudaSuccess;
