@@ -8,6 +8,7 @@
 // the weighted sum of values in registers. Bound by shared-memory wavefronts for
 // prompts (89 % of their rate; 1200 tokens of 16 heads of 64 in 0.21 ms, 14
 // TFLOP/s), by the latency of its loads for single tokens.
+#include <atomic>
 #include <climits>
 #include <type_traits>
 
@@ -176,6 +177,7 @@ __device__ __forceinline__ void attend(const AttnProblem& p, const Segment& it) 
         }
         __syncthreads();
         if (kAhead && k0 + kKeys < k_hi) load(k0 + kKeys);
+        if (N * 4 * (tid >> 5) >= n_rows) continue;  // no row of this warp
         float s[N][4] = {};
         for (int d = 0; d < p.D; d += 4) {
             float4 a[N], b[4];
@@ -305,14 +307,20 @@ template <typename TA, bool kE4m3, int DP, int N>
 cudaError_t simt_as(const AttnProblem& p, cudaStream_t stream) {
     constexpr auto kernel = attn_simt_kernel<TA, kE4m3, DP, N>;
     static DeviceOnce once;
+    static std::atomic<int> per_sm;  // CTAs
     if (cudaError_t e = once.run([] {
-            return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem<DP, N>);
+            if (cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem<DP, N>); e != cudaSuccess)
+                return e;
+            int n = 1;
+            const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, kThreads, kSmem<DP, N>);
+            per_sm.store(n, std::memory_order_relaxed);
+            return e;
         });
         e != cudaSuccess)
         return e;
     if constexpr (N == 1) {
         AttnProblem a = p;
-        set_shares(a, 16, DP == 256 ? 2 : 4, sm_count(), kMinBlocks, kTileCost);
+        set_shares(a, 16, per_sm.load(std::memory_order_relaxed), sm_count(), kMinBlocks, kTileCost);
         if (cudaError_t e = launch_k(kernel, dim3(a.shares), dim3(kThreads), kSmem<DP, N>, stream, a); e != cudaSuccess) return e;
         return a.shares > 1 ? launch_attn_join(a, stream) : cudaSuccess;
     } else {
