@@ -1,8 +1,9 @@
 // Attention over packed prompts on the tensor cores (bf16, D up to 128).
 //
-// One CTA holds two tiles of 128 query rows that read the same keys: the same
-// 128 tokens of two heads of a group where the group has an even number of
-// heads (equal work under a causal mask), else 256 tokens of one head. Per tile
+// One CTA holds two tiles of 128 query rows that read the same keys. A row is a
+// token and one of H heads of a group, H the largest power of two in the group's
+// number of heads (up to 32): 256 / H tokens, so that short prompts and the ends
+// of long ones fill the tiles. Per tile
 // of 128 keys and for each query tile t:
 //   S_t = Q_t K^T      tcgen05.mma, both operands in shared memory, S in TMEM
 //   P_t = exp2(scale S_t - m)   one thread per row: S from TMEM to registers,
@@ -49,7 +50,7 @@ struct Smem {
 
 struct Params {
     AttnProblem a;
-    int pair_heads;  // the two query tiles are two heads (else 256 tokens)
+    int hlog;  // log2 of the heads of a tile
     uint64_t wait_limit_ns;
 };
 
@@ -190,7 +191,7 @@ __device__ __noinline__ void repair_row(const AttnProblem& p, int64_t k0, int64_
 // One work item as the scheduler warp hands it out.
 struct Work {
     Seq s;
-    int rows0[2], rows[2];  // query tile t: first row of the sequence, rows (<= 0: none)
+    int tok0[2], rows[2];   // query tile t: first token of the sequence, rows (<= 0: none)
     int n[2];               // its key tiles, from k_first on
     int k_first, head0, head_kv;
     int end;                // 1: no more work
@@ -320,8 +321,8 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             if (!wait_warp(&w_full[k & 1], (uint32_t)(k >> 1) & 1u)) break;
             const Work& slot = work_slots[k & 1];
             const Seq s = slot.s;
-            const int n = slot.n[t], rows = slot.rows[t], row = slot.rows0[t] + r, k_first = slot.k_first, end = slot.end;
-            const int head = slot.head0 + (pp.pair_heads ? t : 0);
+            const int n = slot.n[t], rows = slot.rows[t], row = slot.tok0[t] + (r >> pp.hlog), k_first = slot.k_first, end = slot.end;
+            const int head0 = slot.head0, head = head0 + (r & ((1 << pp.hlog) - 1));
             __syncwarp();
             if (lane == 0) mbar_arrive(&w_empty[k & 1]);
             if (end) break;
@@ -444,7 +445,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 if (via_tma) {
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
-                    if (lane == 0) tma_store_3d(&tm_o, buf, c, head, (int)tok);
+                    if (lane == 0) tma_store_3d(&tm_o, buf, c, head0, (int)tok);
                 }
             }
             if (r < rows && p.lse) p.lse[tok * p.Hq + head] = empty ? neg_inf() : (m + log2f(l)) * kLn2;
@@ -457,7 +458,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 const float rm = __shfl_sync(0xffffffffu, m, src), rl = __shfl_sync(0xffffffffu, l, src);
                 if (lane == 0) bulk_wait_all();  // the row's first version is stored before the second
                 __syncwarp();
-                repair_row(p, s.k0, tok - lane + src, head, rlo, rhi, rm, rl);
+                repair_row(p, s.k0, __shfl_sync(0xffffffffu, tok, src), __shfl_sync(0xffffffffu, head, src), rlo, rhi, rm, rl);
             }
         }
         if (lane == 0) bulk_wait_all();  // stores complete before the CTA leaves
@@ -465,8 +466,8 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         if (warp == 10) {
             // --------------------------------------------------------- scheduler
-            const int groups = pp.pair_heads ? p.Hq / 2 : p.Hq;
-            const int rows_per = pp.pair_heads ? kTile : 2 * kTile;
+            const int groups = p.Hq >> pp.hlog;
+            const int tile_toks = kTile >> pp.hlog, toks = 2 * tile_toks;
             uint32_t block = blockIdx.x;
             TileFinder tiles;
             bool more = true, asked = false;
@@ -475,26 +476,26 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             for (; more; ++turn) {
                 if (lane == 0) try_cancel(&answer, ans);
                 asked = true;
-                const Place at = tiles.find(p, block / groups, rows_per);
+                const Place at = tiles.find(p, block / groups, toks);
                 if (at.b >= 0) {
                     if (!wait_warp(&w_empty[k & 1], ((uint32_t)(k >> 1) & 1u) ^ 1u)) break;
                     Work w;
                     w.s = load_seq(p, at.b);
                     // the last tiles, which see the most keys, first
-                    const int tile = (w.s.nq + rows_per - 1) / rows_per - 1 - (int)at.at;
-                    w.head0 = (int)(block % groups) * (pp.pair_heads ? 2 : 1);
+                    const int first = ((w.s.nq + toks - 1) / toks - 1 - (int)at.at) * toks;
+                    w.head0 = (int)(block % groups) << pp.hlog;
                     w.head_kv = w.head0 / (p.Hq / p.Hkv);
                     w.end = 0;
                     int lo, hi;
-                    seen_keys(p, w.s, tile * rows_per, lo, hi);
+                    seen_keys(p, w.s, first, lo, hi);
                     w.k_first = hi < 0 ? 0 : lo & ~(kTile - 1);
 #pragma unroll
                     for (int t = 0; t < 2; ++t) {
-                        w.rows0[t] = tile * rows_per + (pp.pair_heads ? 0 : t * kTile);
-                        w.rows[t] = min(kTile, w.s.nq - w.rows0[t]);
+                        w.tok0[t] = first + t * tile_toks;
+                        w.rows[t] = min(tile_toks, w.s.nq - w.tok0[t]) << pp.hlog;
                         w.n[t] = 0;
                         if (w.rows[t] > 0) {
-                            seen_keys(p, w.s, w.rows0[t] + w.rows[t] - 1, lo, hi);  // its last row sees the furthest
+                            seen_keys(p, w.s, w.tok0[t] + (w.rows[t] >> pp.hlog) - 1, lo, hi);  // its last token sees the furthest
                             if (hi >= w.k_first) w.n[t] = (hi - w.k_first) / kTile + 1;
                         }
                     }
@@ -535,7 +536,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                     if (!ok) break;
                     mbar_expect_tx(&q_full[t], TILE);
                     for (int c = 0; c < DK / 64; ++c)
-                        tma_load_3d(sQ + t * TILE + c * kHalf, &tm_q, 64 * c, w.head0 + (pp.pair_heads ? t : 0), w.s.q0 + w.rows0[t], &q_full[t]);
+                        tma_load_3d(sQ + t * TILE + c * kHalf, &tm_q, 64 * c, w.head0, w.s.q0 + w.tok0[t], &q_full[t]);
                     ++qn[t];
                 }
                 for (int i = 0; i < 2 * n_max && ok; ++i) {  // K_0, V_0, K_1, V_1, ...
@@ -691,16 +692,17 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
 
-// [T, heads, D] bf16 rows as a 3-D tensor in boxes of 64 x 1 x 128 (128-byte
-// swizzled; elements past D and rows past T read as 0), or, for the output, of
-// 32 x 1 x 32 (64-byte swizzled)
-bool rows_map(CUtensorMap* map, const Rows& r, int64_t T, int heads, int D, bool out = false) {
+// [T, heads, D] bf16 rows as a 3-D tensor in boxes of 64 columns (128-byte
+// swizzled; elements past D and rows past T read as 0) of 128 rows, each token's
+// 2^hlog heads beside each other, or, for the output, of 32 columns (64-byte
+// swizzled) of 32 rows
+bool rows_map(CUtensorMap* map, const Rows& r, int64_t T, int heads, int D, int hlog, bool out = false) {
     EncodeTiled fn = encode_fn();
     if (!fn) return false;
     const cuuint64_t least = (cuuint64_t)(2 * D);
     cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)heads, (cuuint64_t)T};
     cuuint64_t strides[2] = {heads > 1 ? (cuuint64_t)(2 * r.hs) : least, T > 1 ? (cuuint64_t)(2 * r.ts) : least};
-    cuuint32_t box[3] = {out ? 32u : 64u, 1, out ? 32u : (cuuint32_t)kTile}, estr[3] = {1, 1, 1};
+    cuuint32_t box[3] = {out ? 32u : 64u, 1u << hlog, (out ? 32u : (cuuint32_t)kTile) >> hlog}, estr[3] = {1, 1, 1};
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(r.p), dims, strides, box, estr,
               CU_TENSOR_MAP_INTERLEAVE_NONE, out ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
@@ -724,10 +726,12 @@ cudaError_t prompt_as(const AttnProblem& p, cudaStream_t stream) {
         e != cudaSuccess)
         return e;
     CUtensorMap q, k, v, o;
-    if (!rows_map(&q, p.q, p.T, p.Hq, p.D) || !rows_map(&o, p.out, p.T, p.Hq, p.D, true) || !rows_map(&k, p.k, p.Tk, p.Hkv, p.D) || !rows_map(&v, p.v, p.Tk, p.Hkv, p.D))
+    Params pp{p, 0, tc_wait_limit_ns()};
+    while (pp.hlog < 5 && p.Hq / p.Hkv % (2 << pp.hlog) == 0) ++pp.hlog;
+    if (!rows_map(&q, p.q, p.T, p.Hq, p.D, pp.hlog) || !rows_map(&o, p.out, p.T, p.Hq, p.D, pp.hlog, true) ||
+        !rows_map(&k, p.k, p.Tk, p.Hkv, p.D, 0) || !rows_map(&v, p.v, p.Tk, p.Hkv, p.D, 0))
         return cudaErrorInvalidValue;
-    Params pp{p, (p.Hq / p.Hkv) % 2 == 0, tc_wait_limit_ns()};
-    const int64_t grid = (p.T / (pp.pair_heads ? kTile : 2 * kTile) + p.B) * (int64_t)(pp.pair_heads ? p.Hq / 2 : p.Hq);
+    const int64_t grid = (p.T / (2 * kTile >> pp.hlog) + p.B) * (int64_t)(p.Hq >> pp.hlog);
     if (grid > INT32_MAX) return cudaErrorInvalidConfiguration;
     return launch_k(kernel, dim3((unsigned)grid), dim3(kThreads), Smem<DK>::BYTES, stream, q, k, v, o, pp);
 }
