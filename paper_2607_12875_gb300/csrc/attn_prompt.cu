@@ -14,6 +14,9 @@
 // maximum m is raised, and O in TMEM rescaled, only when a row's maximum has
 // grown by more than 2^8 since the last time: P then stays below 2^8 and the
 // final division by the same row's sum makes up for it.
+// kDeal, where there is too little work for every SM: the two tiles are one tile
+// of 128 rows twice, with every other tile of keys each, and their results are
+// joined at the end.
 // Warps 0-3 and 4-7: softmax of tile 0 and 1 and their results; warp 8: TMA; warp
 // 9: MMA; warp 10: scheduler. A CTA goes on with the work of CTAs that have not
 // started (cluster launch control), so the loads, the first products and the search
@@ -45,6 +48,7 @@ struct Smem {
     static constexpr int TILE = DK / 64 * kHalf;          // one Q, K or V tile
     static constexpr int STAGES = DK == 128 ? 4 : 8;      // K and V tiles in flight, in turn
     static constexpr int OUT = 8 * 2 * 2048;              // output rows on their way: two buffers of each softmax warp
+    static_assert(STAGES * 16 + 256 <= 512, "barriers");
     static constexpr int BYTES = 1024 + (2 + STAGES) * TILE + OUT + 512;
 };
 
@@ -244,7 +248,7 @@ __device__ __forceinline__ bool cancelled(const void* src, uint32_t& x) {
     return ok != 0;
 }
 
-template <int DK>
+template <int DK, bool kDeal>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                    const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_o,
@@ -260,6 +264,8 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint8_t* sQ = smem;  // two query tiles
     uint8_t* sKV = smem + 2 * TILE;
+    // kDeal, which has one query tile: maximum, sum and results' check of the softmax warps' rows
+    float(*stats)[8][32] = reinterpret_cast<float(*)[8][32]>(sQ + TILE);
     uint8_t* sO = sKV + STAGES * TILE;
     uint64_t* bars = reinterpret_cast<uint64_t*>(sO + L::OUT);
     uint64_t* full = bars;            // a K or V tile landed
@@ -273,7 +279,8 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     uint64_t* w_empty = w_full + 2;   // every role has read it
     uint64_t* ans = w_empty + 2;      // the answer to try_cancel
     uint64_t* drain = ans + 1;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
+    uint64_t* pair = drain + 1;       // kDeal: the two warps of the same rows
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(pair + 4);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -293,6 +300,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         }
         mbar_init(ans, 1);
         mbar_init(drain, 1);
+        for (int i = 0; i < 4; ++i) mbar_init(&pair[i], 2);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -314,14 +322,21 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         const int t = warp >> 2, r = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t tS = tmem + lanes + t * kTile, tO = tmem + lanes + 2 * kTile + t * kTile;
+        const uint32_t tO2 = tmem + lanes + 2 * kTile + (t ^ 1) * kTile;
         const float scale = p.scale_log2;
-        uint32_t sn = 0, items = 0;  // key tiles and items of this query tile so far
+        uint32_t sn = 0, items = 0, items2 = 0;  // key tiles and items of this query tile so far; items of the other
+        uint32_t meets = 0;
+        auto meet = [&] {  // with the other warp of the same rows
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&pair[warp & 3]);
+            return wait_warp(&pair[warp & 3], meets++ & 1u);
+        };
         bool ok = true;
         for (int k = 0; ok; ++k) {
             if (!wait_warp(&w_full[k & 1], (uint32_t)(k >> 1) & 1u)) break;
             const Work& slot = work_slots[k & 1];
             const Seq s = slot.s;
-            const int n = slot.n[t], rows = slot.rows[t], row = slot.tok0[t] + (r >> pp.hlog), k_first = slot.k_first, end = slot.end;
+            const int n = slot.n[t], n2 = slot.n[t ^ 1], rows = slot.rows[t], row = slot.tok0[t] + (r >> pp.hlog), k_first = slot.k_first, end = slot.end;
             const int head0 = slot.head0, head = head0 + (r & ((1 << pp.hlog) - 1));
             __syncwarp();
             if (lane == 0) mbar_arrive(&w_empty[k & 1]);
@@ -339,7 +354,8 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 ld_wait();
 #pragma unroll
                 for (int c = 0; c < 4; ++c) pin32(u[c]);
-                const int first = lo - (k_first + j * kTile), last = hi - (k_first + j * kTile);  // columns first .. last are seen
+                const int key0 = k_first + (kDeal ? 2 * j + t : j) * kTile;
+                const int first = lo - key0, last = hi - key0;  // columns first .. last are seen
                 if (__any_sync(0xffffffffu, first > 0 || last < kTile - 1)) {
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
@@ -402,11 +418,23 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             }
             // -------------------------------------------------------- result
             if (ok && n > 0) ok = wait_warp(&o_full[t], items++ & 1u);
+            if (kDeal && ok && n2 > 0) ok = wait_warp(&o_full[t ^ 1], items2++ & 1u);
             if (!ok) break;
             tc_fence_after();
             if (rows <= (warp & 3) * 32) continue;  // no row of this warp
             const bool empty = hi < lo;
-            const float inv = empty ? 0.0f : 1.0f / l;
+            float inv = empty ? 0.0f : 1.0f / l, inv2 = 0.0f;  // (kDeal: factors of this tile's and the other's sums)
+            if constexpr (kDeal) {
+                stats[0][warp][lane] = m, stats[1][warp][lane] = l;
+                ok = meet();
+                if (!ok) break;
+                const float m2 = stats[0][warp ^ 4][lane], l2 = stats[1][warp ^ 4][lane];
+                const float top = fmaxf(m, m2), base = top == neg_inf() ? 0.0f : top;
+                const float f = ex2(m - base), f2 = ex2(m2 - base);
+                l = t == 0 ? fmaf(l, f, l2 * f2) : fmaf(l2, f2, l * f);  // the same in both warps
+                inv = empty ? 0.0f : f / l, inv2 = empty ? 0.0f : f2 / l;
+                m = top;
+            }
             const int64_t tok = s.q0 + row;
             __nv_bfloat16* out = const_cast<__nv_bfloat16*>(static_cast<const __nv_bfloat16*>(p.out.p)) + tok * p.out.ts + head * p.out.hs;
             float check = 0.0f;  // NaN once a value is not finite
@@ -415,14 +443,27 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             const bool via_tma = (warp & 3) * 32 + 32 <= rows;
             uint8_t* stage_buf = sO + warp * 4096;
 #pragma unroll 1
-            for (int c = 0; c < p.D; c += 32) {
+            for (int c = kDeal ? 32 * t : 0; c < p.D; c += kDeal ? 64 : 32) {
                 uint32_t o[32];
-                if (n > 0) {
+                if constexpr (kDeal) {
+                    uint32_t o2[32];
+                    tmem_ld32_async(tO + c, o);
+                    tmem_ld32_async(tO2 + c, o2);
+                    ld_wait();
+                    pin32(o), pin32(o2);
+                    // (a tile without keys for this row has a factor of 0; what it holds may be anything. Loads
+                    // that depend on n made the compiler spill 540 bytes)
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        const float a = inv != 0.0f ? __uint_as_float(o[i]) * inv : 0.0f;
+                        o[i] = __float_as_uint(inv2 != 0.0f ? fmaf(__uint_as_float(o2[i]), inv2, a) : a);
+                    }
+                } else if (n > 0) {
                     tmem_ld32_async(tO + c, o);
                     ld_wait();
                     pin32(o);
                 }
-                uint8_t* buf = stage_buf + ((c >> 5) & 1) * 2048;
+                uint8_t* buf = stage_buf + ((c >> (kDeal ? 6 : 5)) & 1) * 2048;
                 if (via_tma) {
                     if (lane == 0) bulk_wait_read<1>();  // the store that last read buf is done reading
                     __syncwarp();
@@ -432,8 +473,8 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                     uint32_t w[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const float a = empty ? 0.0f : __uint_as_float(o[8 * q + 2 * i]) * inv;
-                        const float b = empty ? 0.0f : __uint_as_float(o[8 * q + 2 * i + 1]) * inv;
+                        const float a = empty ? 0.0f : __uint_as_float(o[8 * q + 2 * i]) * (kDeal ? 1.0f : inv);
+                        const float b = empty ? 0.0f : __uint_as_float(o[8 * q + 2 * i + 1]) * (kDeal ? 1.0f : inv);
                         if (c + 8 * q < p.D) check = fmaf(a, 0.0f, fmaf(b, 0.0f, check));
                         w[i] = pack_bf16x2(a, b);
                     }
@@ -448,9 +489,23 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                     if (lane == 0) tma_store_3d(&tm_o, buf, c, head0, (int)tok);
                 }
             }
-            if (r < rows && p.lse) p.lse[tok * p.Hq + head] = empty ? neg_inf() : (m + log2f(l)) * kLn2;
+            if constexpr (kDeal) {
+                stats[2][warp][lane] = check;
+                tc_fence_before();
+                ok = meet();  // the other warp has read this tile's sums
+                if (!ok) break;
+                check += stats[2][warp ^ 4][lane];
+            }
+            if (r < rows && p.lse && (!kDeal || t == 0)) p.lse[tok * p.Hq + head] = empty ? neg_inf() : (m + log2f(l)) * kLn2;
             // rows that may hold a masked key's NaN
             uint32_t again = __ballot_sync(0xffffffffu, r < rows && !empty && check != check && finite(m) && finite(l) && l > 0.0f);
+            if (kDeal && again) {  // (the same in both warps; one repairs, when both have stored)
+                if (lane == 0) bulk_wait_all();
+                __syncwarp();
+                __threadfence();
+                ok = meet();
+                if (t != 0 || !ok) again = 0;
+            }
             while (again) {
                 const int src = __ffs(again) - 1;
                 again &= again - 1;
@@ -467,7 +522,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         if (warp == 10) {
             // --------------------------------------------------------- scheduler
             const int groups = p.Hq >> pp.hlog;
-            const int tile_toks = kTile >> pp.hlog, toks = 2 * tile_toks;
+            const int tile_toks = kTile >> pp.hlog, toks = kDeal ? tile_toks : 2 * tile_toks;
             uint32_t block = blockIdx.x;
             TileFinder tiles;
             bool more = true, asked = false;
@@ -491,7 +546,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                     w.k_first = hi < 0 ? 0 : lo & ~(kTile - 1);
 #pragma unroll
                     for (int t = 0; t < 2; ++t) {
-                        w.tok0[t] = first + t * tile_toks;
+                        w.tok0[t] = first + (kDeal ? 0 : t * tile_toks);
                         w.rows[t] = min(tile_toks, w.s.nq - w.tok0[t]) << pp.hlog;
                         w.n[t] = 0;
                         if (w.rows[t] > 0) {
@@ -499,6 +554,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                             if (hi >= w.k_first) w.n[t] = (hi - w.k_first) / kTile + 1;
                         }
                     }
+                    if (kDeal) w.n[0] = (w.n[0] + 1) / 2, w.n[1] /= 2;
                     if (lane == 0) {
                         work_slots[k & 1] = w;
                         mbar_arrive(&w_full[k & 1]);
@@ -530,7 +586,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 mbar_arrive(&w_empty[k & 1]);
                 if (w.end) break;
                 const int n_max = max(w.n[0], w.n[1]);
-                for (int t = 0; t < 2 && ok; ++t) {
+                for (int t = 0; t < (kDeal ? 1 : 2) && ok; ++t) {
                     if (w.n[t] == 0) continue;
                     ok = wait(&q_empty[t], (qn[t] & 1u) ^ 1u);
                     if (!ok) break;
@@ -539,13 +595,21 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                         tma_load_3d(sQ + t * TILE + c * kHalf, &tm_q, 64 * c, w.head0, w.s.q0 + w.tok0[t], &q_full[t]);
                     ++qn[t];
                 }
-                for (int i = 0; i < 2 * n_max && ok; ++i) {  // K_0, V_0, K_1, V_1, ...
+                // K_0, V_0, K_1, V_1, ..; kDeal: K_0, K_1, V_0, K_2, V_1, .., K_n-1, V_n-2, V_n-1
+                const int n_all = kDeal ? w.n[0] + w.n[1] : n_max;
+                for (int i = 0; i < 2 * n_all && ok; ++i) {
                     ok = wait(&empty[stage], phase ^ 1);
                     if (!ok) break;
-                    const CUtensorMap* map = i & 1 ? &tm_v : &tm_k;
+                    bool value = i & 1;
+                    int at = i >> 1;
+                    if constexpr (kDeal) {
+                        value = i == 2 * n_all - 1 || (i > 0 && !(i & 1));
+                        at = i == 0 ? 0 : i == 2 * n_all - 1 ? n_all - 1 : value ? at - 1 : at + 1;
+                    }
+                    const CUtensorMap* map = value ? &tm_v : &tm_k;
                     mbar_expect_tx(&full[stage], TILE);
                     for (int c = 0; c < DK / 64; ++c)
-                        tma_load_3d(sKV + stage * TILE + c * kHalf, map, 64 * c, w.head_kv, (int)(w.s.k0 + w.k_first + (i >> 1) * kTile), &full[stage]);
+                        tma_load_3d(sKV + stage * TILE + c * kHalf, map, 64 * c, w.head_kv, (int)(w.s.k0 + w.k_first + at * kTile), &full[stage]);
                     inflight |= 1u << stage;
                     par = (par & ~(1u << stage)) | (phase << stage);
                     if (++stage == STAGES) { stage = 0; phase ^= 1; }
@@ -574,10 +638,10 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             auto advance = [&](int& st, uint32_t& ph) {
                 if (++st == STAGES) st = 0, ph ^= 1;
             };
-            // S_t = Q_t K^T with the K tile in slot st; last: the item's last use of Q_t
+            // S_t = Q_t K^T with the K tile in slot st; last: the item's last use of Q_t (kDeal: of the one Q)
             auto scores = [&](int t, int st, bool last) {
                 if (elect_one()) {
-                    const uint64_t a = dq + (uint64_t)(t * TILE >> 4), b = dk + (uint64_t)((uint32_t)(st * TILE) >> 4);
+                    const uint64_t a = dq + (kDeal ? 0 : (uint64_t)(t * TILE >> 4)), b = dk + (uint64_t)((uint32_t)(st * TILE) >> 4);
 #pragma unroll
                     for (int c = 0; c < DK / 16; ++c) {
                         if (c >= ksteps) break;
@@ -585,7 +649,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                         mma_ss(tm + t * kTile, a + off, b + off, kIdS, c != 0);
                     }
                     mma_commit(&s_full[t]);
-                    if (last) mma_commit(&q_empty[t]);
+                    if (last) mma_commit(&q_empty[kDeal ? 0 : t]);
                 }
                 __syncwarp();
                 issued = true;
@@ -614,6 +678,34 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 if (end) break;
                 const int n_max = max(n0, n1);
                 if (n_max == 0) continue;
+                if constexpr (kDeal) {
+                    const int n = n0 + n1;
+                    bool ok = wait_warp(&q_full[0], qn0++ & 1u);
+                    for (int i = 0; i < min(n, 2) && ok; ++i) {
+                        ok = wait_warp(&full[stage], phase);
+                        if (!ok) break;
+                        tc_fence_after();
+                        scores(i, stage, i + 1 == n);
+                        release(stage);
+                        advance(stage, phase);
+                    }
+                    for (int i = 0; i < n && ok; ++i) {
+                        const int t = i & 1, sv = stage;  // V_i, then K_i+2: there when p_full is complete
+                        advance(stage, phase);
+                        ok = wait_warp(&p_full[t], (t ? pn1++ : pn0++) & 1u);
+                        if (!ok) break;
+                        tc_fence_after();
+                        values(t, sv, i < 2, i + 2 >= n);
+                        release(sv);
+                        if (i + 2 < n) {
+                            scores(t, stage, i + 3 == n);
+                            release(stage);
+                            advance(stage, phase);
+                        }
+                    }
+                    if (!ok) break;
+                    continue;
+                }
                 if (n0 > 0 && !wait_warp(&q_full[0], qn0++ & 1u)) break;
                 if (n1 > 0 && !wait_warp(&q_full[1], qn1++ & 1u)) break;
                 if (!wait_warp(&full[stage], phase)) break;
@@ -669,6 +761,21 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 mbar_arrive(&w_empty[k & 1]);
                 if (end) break;
                 const int n_max = max(n0, n1);
+                if constexpr (kDeal) {
+                    const int n = n0 + n1;
+                    for (int i = 0; i < min(n, 2); ++i) next();  // (the first K tiles: the MMA warp's)
+                    for (int i = 0; i < n && ok; ++i) {
+                        for (int x = 0; x < (i + 2 < n ? 2 : 1) && ok; ++x) {
+                            ok = wait(&full[stage], phase);
+                            next();
+                        }
+                        const int t = i & 1;
+                        if (ok && pn[t] > 0) ok = wait(&p_full[t], (pn[t] - 1) & 1u);
+                        ++pn[t];
+                        if (ok) mbar_arrive(&p_full[t]);
+                    }
+                    continue;
+                }
                 if (n_max > 0) next();  // (the first K tile: the MMA warp's)
                 for (int j = 0; j < n_max && ok; ++j) {
                     ok = wait(&full[stage], phase);
@@ -716,9 +823,12 @@ bool tma_strides(const Rows& r, int64_t T, int heads) {
     return (T <= 1 || (r.ts > 0 && r.ts < most)) && (heads <= 1 || (r.hs > 0 && r.hs < most));
 }
 
-template <int DK>
-cudaError_t prompt_as(const AttnProblem& p, cudaStream_t stream) {
-    constexpr auto kernel = attn_prompt_kernel<DK>;
+// the most items of `rows` rows that the lengths can make
+int64_t items_of(const AttnProblem& p, int rows, int hlog) { return (p.T / (rows >> hlog) + p.B) * (int64_t)(p.Hq >> hlog); }
+
+template <int DK, bool kDeal>
+cudaError_t prompt_as(const AttnProblem& p, int hlog, cudaStream_t stream) {
+    constexpr auto kernel = attn_prompt_kernel<DK, kDeal>;
     static DeviceOnce once;
     if (cudaError_t e = once.run([] {
             return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<DK>::BYTES);
@@ -726,12 +836,11 @@ cudaError_t prompt_as(const AttnProblem& p, cudaStream_t stream) {
         e != cudaSuccess)
         return e;
     CUtensorMap q, k, v, o;
-    Params pp{p, 0, tc_wait_limit_ns()};
-    while (pp.hlog < 5 && p.Hq / p.Hkv % (2 << pp.hlog) == 0) ++pp.hlog;
+    Params pp{p, hlog, tc_wait_limit_ns()};
     if (!rows_map(&q, p.q, p.T, p.Hq, p.D, pp.hlog) || !rows_map(&o, p.out, p.T, p.Hq, p.D, pp.hlog, true) ||
         !rows_map(&k, p.k, p.Tk, p.Hkv, p.D, 0) || !rows_map(&v, p.v, p.Tk, p.Hkv, p.D, 0))
         return cudaErrorInvalidValue;
-    const int64_t grid = (p.T / (2 * kTile >> pp.hlog) + p.B) * (int64_t)(p.Hq >> pp.hlog);
+    const int64_t grid = items_of(p, kDeal ? kTile : 2 * kTile, hlog);
     if (grid > INT32_MAX) return cudaErrorInvalidConfiguration;
     return launch_k(kernel, dim3((unsigned)grid), dim3(kThreads), Smem<DK>::BYTES, stream, q, k, v, o, pp);
 }
@@ -745,7 +854,15 @@ bool attn_prompt_tc_supported(const AttnProblem& p) {
 }
 
 cudaError_t launch_attn_prompt_tc(const AttnProblem& p, cudaStream_t stream) {
-    return p.D <= 64 ? prompt_as<64>(p, stream) : prompt_as<128>(p, stream);
+    int hlog = 0;
+    while (hlog < 5 && p.Hq / p.Hkv % (2 << hlog) == 0) ++hlog;
+    // Too few items for every SM (or, of long prompts, to even out over them). Us without and with: 7596
+    // tokens, 4 heads 91 and 62; two prompts of 7344 in all, 8 heads 77 and 65; 476 tokens, 4 heads 13.4
+    // and 9.8; 16 prompts of 2242 in all, 7 heads, which the second condition leaves out, 10.8 and 12.8.
+    const int64_t items = items_of(p, 2 * kTile, hlog);
+    const bool deal = items <= sm_count() || (items <= 2 * sm_count() && p.T >= (int64_t)2 * kTile * p.B);
+    if (p.D <= 64) return deal ? prompt_as<64, true>(p, hlog, stream) : prompt_as<64, false>(p, hlog, stream);
+    return deal ? prompt_as<128, true>(p, hlog, stream) : prompt_as<128, false>(p, hlog, stream);
 }
 
 }  // namespace gbmoe

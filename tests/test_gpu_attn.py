@@ -317,6 +317,68 @@ def test_prompt(act, Hq, Hkv, D, nq, nk, causal, window):
     assert gb.moe_device_status(ws) == gb.OK
 
 
+MANY_HEADS = [
+    # as above, with so many heads that each CTA takes several tiles of rows
+    (160, 160, 64, [1, 0, 7, 130], None, True, 0),
+    (512, 64, 64, [257, 33], None, True, 0),
+    (192, 64, 128, [150], None, True, 0),           # three heads per kv head
+    (256, 128, 64, [200, 128], None, True, 100),
+    (256, 128, 64, [50, 100], [233, 100], True, 0),
+    (256, 64, 64, [40, 3], [10, 0], True, 0),
+    (256, 64, 64, [100, 60], [300, 20], False, 0),
+    (384, 128, 80, [70, 65], None, True, 0),        # head sizes between
+    (1024, 32, 32, [37], None, True, 0),            # 32 heads per kv head: a token fills a warp's rows
+    (640, 16, 16, [37, 5], None, True, 0),          # 40: tiles of 8 of them
+]
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,nq,nk,causal,window", MANY_HEADS)
+def test_prompt_of_many_heads(Hq, Hkv, D, nq, nk, causal, window):
+    test_prompt("bf16", Hq, Hkv, D, nq, nk, causal, window)
+
+
+@pytest.mark.parametrize("H", [2, 200])
+def test_prompt_with_infinite_and_nan_scores(H):
+    """Where every score of a row is not a number, or one is infinite, the row is not a number; rows before are right."""
+    rng = np.random.default_rng(3)
+    n, D = 300, 64
+    for bad in (float("nan"), float("inf")):
+        q, k, v = (normal(rng, (n, H, D), "bf16") for _ in range(3))
+        q[280] = float("nan")
+        k[290, :, 3] = bad
+        cfg = gb.attn_config(H, H, D)
+        ws = torch.zeros(gb.attn_workspace_size(cfg, n, 1), dtype=torch.uint8, device="cuda")
+        out = torch.zeros_like(q)
+        gb.attn_prompt(cfg, q, k, v, prefix([n]), prefix([n]), out, ws)
+        got = wide(out)
+        assert np.isnan(got[280]).all()
+        right = [i for i in range(290) if i != 280]
+        clean = q.clone()
+        clean[280] = 0.0
+        want, _ = packed_reference(wide(clean)[:290], wide(k)[:290], wide(v)[:290], [290], [290], cfg.scale, True, 0)
+        tol = attention_tolerance("bf16", want, np.abs(wide(v)).max())
+        assert (np.abs(got[right] - want[right]) <= tol[right]).all()
+        if np.isnan(bad):
+            assert np.isnan(got[290:]).all()
+
+
+def test_waits_that_run_out_in_a_call_of_many_tiles(monkeypatch):
+    rng = np.random.default_rng(10)
+    n, H, D = 300, 200, 64
+    q, k, v = (normal(rng, (n, H, D), "bf16") for _ in range(3))
+    cfg = gb.attn_config(H, H, D)
+    ws = torch.zeros(gb.attn_workspace_size(cfg, n, 1), dtype=torch.uint8, device="cuda")
+    cu, out = prefix([n]), torch.zeros_like(q)
+    monkeypatch.setenv("GBMOE_TC_WAIT_LIMIT_NS", "0")
+    gb.attn_prompt(cfg, q, k, v, cu, cu, out, ws)
+    assert gb.moe_device_status(ws) == gb.EDEVICE_TIMEOUT
+    monkeypatch.delenv("GBMOE_TC_WAIT_LIMIT_NS")
+    gb.attn_prompt(cfg, q, k, v, cu, cu, out, ws)
+    assert gb.moe_device_status(ws) == gb.OK
+    want, _ = packed_reference(wide(q), wide(k), wide(v), [n], [n], cfg.scale, True, 0)
+    assert (np.abs(wide(out) - want) <= attention_tolerance("bf16", want, np.abs(wide(v)).max())).all()
+
+
 @pytest.mark.parametrize("act", ["f32", "bf16"])
 def test_prompt_of_many_sequences(act):
     """More sequences than a warp or a block looks at in one go, runs of empty ones, and a long one behind them."""
