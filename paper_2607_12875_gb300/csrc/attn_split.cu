@@ -40,6 +40,7 @@ using namespace tc;
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kKeys = kBlockKeys / kWarps;  // keys of a stage of one warp
 constexpr unsigned kFull = 0xffffffffu;
+constexpr float kGrow = 6.0f;  // log2 of how far a row's maximum may run ahead
 // Least blocks of 64 keys of a share, and how many a tile's set-up counts for. Us at (3, 2)
 // and (2, 1): one sequence of 4000 e4m3 keys, 8 kv heads 12.3 and 11.6; two of 19000, 1 kv head 16.9
 // and 20.1; 19 of up to 322 with 5 tokens, 4 kv heads 17.3 and 19.7. With (3, 0), where a share holds
@@ -342,41 +343,54 @@ attn_split_kernel(const __grid_constant__ AttnProblem p, uint64_t wait_limit_ns)
                 }
 
             // ---- running maximum and sum of rows 2 c + z
-            float f_o[NQ][2];
-            bool moved = false;
+            // The maxima are raised, and the sums rescaled, only when a score has passed its row's by more
+            // than 2^kGrow (a power that fp16 weights have room for): most stages exchange nothing.
+            bool raise = false;
 #pragma unroll
             for (int n = 0; n < NQ; ++n)
 #pragma unroll
                 for (int z = 0; z < 2; ++z) {
-                    float top = fmaxf(s[n][z], s[n][2 + z]);
-                    top = fmaxf(top, __shfl_xor_sync(kFull, top, 4));
-                    top = fmaxf(top, __shfl_xor_sync(kFull, top, 8));
-                    top = fmaxf(top, __shfl_xor_sync(kFull, top, 16));
-                    const float m_new = fmaxf(m[n][z], top), b = m_new == neg_inf() ? 0.0f : m_new;
-                    const float f = ex2(m[n][z] - b);
-                    m[n][z] = m_new;
+                    const float top = fmaxf(s[n][z], s[n][2 + z]);
+                    raise = raise || top > m[n][z] + kGrow || (kE4m3 && top + ve > mo[n][z] + kGrow);
+                }
+            if (__any_sync(kFull, raise)) {
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) {
+                    float f_o[2];
+#pragma unroll
+                    for (int z = 0; z < 2; ++z) {
+                        float top = fmaxf(s[n][z], s[n][2 + z]);
+                        top = fmaxf(top, __shfl_xor_sync(kFull, top, 4));
+                        top = fmaxf(top, __shfl_xor_sync(kFull, top, 8));
+                        top = fmaxf(top, __shfl_xor_sync(kFull, top, 16));
+                        const float m_new = fmaxf(m[n][z], top);
+                        f_o[z] = ex2(m[n][z] - (m_new == neg_inf() ? 0.0f : m_new));
+                        l[n][z] *= f_o[z];
+                        m[n][z] = m_new;
+                        if constexpr (kE4m3) {
+                            const float mo_new = fmaxf(mo[n][z], top + ve);
+                            f_o[z] = ex2(mo[n][z] - (mo_new == neg_inf() ? 0.0f : mo_new));
+                            mo[n][z] = mo_new;
+                        }
+                    }
+#pragma unroll
+                    for (int y = 0; y < KS; ++y) o[n][y][0] *= f_o[0], o[n][y][1] *= f_o[1], o[n][y][2] *= f_o[0], o[n][y][3] *= f_o[1];
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                for (int z = 0; z < 2; ++z) {
+                    const float b = m[n][z] == neg_inf() ? 0.0f : m[n][z];
                     const float p0 = ex2(s[n][z] - b), p1 = ex2(s[n][2 + z] - b);
-                    l[n][z] = l[n][z] * f + (p0 + p1);
+                    l[n][z] += p0 + p1;
                     if constexpr (kE4m3) {
-                        const float mo_new = fmaxf(mo[n][z], top + ve), bo = mo_new == neg_inf() ? 0.0f : mo_new;
-                        f_o[n][z] = ex2(mo[n][z] - bo);
-                        mo[n][z] = mo_new;
-                        const float v = ve - bo;
+                        const float v = ve - (mo[n][z] == neg_inf() ? 0.0f : mo[n][z]);
                         s[n][z] = ex2(s[n][z] + v), s[n][2 + z] = ex2(s[n][2 + z] + v);
                     } else {
-                        f_o[n][z] = f;
-                        mo[n][z] = m_new;
                         s[n][z] = p0, s[n][2 + z] = p1;
                     }
-                    moved = moved || f_o[n][z] != 1.0f;
                 }
-            if (__any_sync(kFull, moved)) {
-#pragma unroll
-                for (int n = 0; n < NQ; ++n)
-#pragma unroll
-                    for (int y = 0; y < KS; ++y)
-                        o[n][y][0] *= f_o[n][0], o[n][y][1] *= f_o[n][1], o[n][y][2] *= f_o[n][0], o[n][y][3] *= f_o[n][1];
-            }
             uint32_t pb[NQ][2];
 #pragma unroll
             for (int n = 0; n < NQ; ++n) {
@@ -494,7 +508,7 @@ attn_split_kernel(const __grid_constant__ AttnProblem p, uint64_t wait_limit_ns)
 #pragma unroll
                 for (int y = 0; y < KS; ++y)
                     *reinterpret_cast<float2*>(row + g * 2 * KS + 2 * y) = make_float2(o[n][y][z], o[n][y][2 + z]);
-                if (g == 0) *reinterpret_cast<float4*>(row + D) = make_float4(m[n][z], l[n][z], mo[n][z], 0.0f);
+                if (g == 0) *reinterpret_cast<float4*>(row + D) = make_float4(m[n][z], l[n][z], kE4m3 ? mo[n][z] : m[n][z], 0.0f);
             }
         __syncthreads();
         constexpr int LANES = kThreads / kRows;  // threads of a row
