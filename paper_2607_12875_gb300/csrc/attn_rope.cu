@@ -193,25 +193,22 @@ __device__ __forceinline__ float max_abs(float m, const Values& v, bool careful)
     return m;
 }
 
-template <bool kWarpTeam>
-constexpr int kAppendThreads = kWarpTeam ? 256 : 512;  // at most
-
-// A segment: the new tokens of one sequence that fall into one of its pages.
-struct Segment {
+// The new tokens of one sequence that fall into one of its pages.
+struct PageTokens {
     int t0, n;      // its tokens
     int64_t pos;    // position of the first one in the sequence
     int page, off;  // pool page (-1: not stored) and slot of the first one
 };
 
-// Segment `index` (sequences in order, a sequence's pages in order). n = 0: none.
-__device__ __forceinline__ Segment find_segment(const AppendProblem& p, int64_t index, int64_t* sm) {
+// PageTokens `index` (sequences in order, a sequence's pages in order). n = 0: none.
+__device__ __forceinline__ PageTokens find_segment(const AppendProblem& p, int64_t index, int64_t* sm) {
     auto bounds = [&](int b, int& q0, int& n, int64_t& pos0) {
         q0 = min(max(p.cu_q[b], 0), p.T);
         n = min(max(p.cu_q[b + 1], q0), p.T) - q0;
         pos0 = (int64_t)p.kv_len[b] - n;
     };
     const int bits = p.page_log2;  // (shifts: pages before position 0 are negative)
-    Segment s{};
+    PageTokens s{};
     const Place at = find_place(
         p.B,
         [&](int b) {
@@ -264,7 +261,7 @@ struct Team {
 // The scale of one page and head that covers amax too, the page's earlier codes
 // brought to it; returns the factor of the new values.
 template <bool kWarpTeam>
-__device__ __forceinline__ float rescale(const AppendProblem& p, const Segment& s, uint8_t* codes, uint8_t* scale, int old,
+__device__ __forceinline__ float rescale(const AppendProblem& p, const PageTokens& s, uint8_t* codes, uint8_t* scale, int old,
                                          float amax, const Team<kWarpTeam>& team) {
     const int e = ::max(old, scale_exponent(amax));
     if (s.off > 0 && e > old) {
@@ -286,7 +283,7 @@ __device__ __forceinline__ float rescale(const AppendProblem& p, const Segment& 
 // token. e4m3: up to kHeld tokens of a thread stay in registers between the
 // search for the maximum and the rounding; longer segments are read twice.
 template <typename TA, bool kE4m3, bool kWarpTeam>
-__device__ __forceinline__ void append_head(const AppendProblem& p, const Segment& s, int h, const Team<kWarpTeam>& team) {
+__device__ __forceinline__ void append_head(const AppendProblem& p, const PageTokens& s, int h, const Team<kWarpTeam>& team) {
     constexpr int kHeld = 1, B = kQueryBatch<TA>;
     const int units = head_units(p.r.R, p.D), bits = unit_bits(units);
     const int u = team.rank & ((1 << bits) - 1), step = team.size >> bits, first = team.rank >> bits;
@@ -400,13 +397,12 @@ __device__ __forceinline__ void append_head(const AppendProblem& p, const Segmen
 // Block x: segment x / Hkv, kv head x % Hkv by the whole block; or (kWarpTeam, few
 // tokens per sequence) segment x, its kv heads dealt to the warps. One team owns
 // a page and head, so its scale needs no atomics.
-template <typename TA, bool kE4m3, bool kWarpTeam>
-__global__ void __launch_bounds__(kAppendThreads<kWarpTeam>, 1) append_kernel(const __grid_constant__ AppendProblem p) {
+template <typename TA, bool kE4m3, bool kWarpTeam, int kThreads>
+__global__ void __launch_bounds__(kThreads, kWarpTeam || kThreads == 512 ? 1 : 2) append_kernel(const __grid_constant__ AppendProblem p) {
     pdl_enter();
-    constexpr int kThreads = kAppendThreads<kWarpTeam>;
     __shared__ int64_t plan[plan_words(kThreads)];
     __shared__ float2 red[kThreads / 32];
-    const Segment s = find_segment(p, kWarpTeam ? blockIdx.x : blockIdx.x / p.Hkv, plan);
+    const PageTokens s = find_segment(p, kWarpTeam ? blockIdx.x : blockIdx.x / p.Hkv, plan);
     if (s.n == 0) return;
     const Team<kWarpTeam> team(red);
     if constexpr (kWarpTeam) {
@@ -428,23 +424,26 @@ cudaError_t rope_as(const RopeProblem& p, cudaStream_t stream) {
     return launch_k(rope_kernel<TA>, dim3((unsigned)grid), dim3(kRopeThreads), 0, stream, p, bits, heads);
 }
 
-template <typename TA, bool kE4m3, bool kWarpTeam>
-cudaError_t append_as(const AppendProblem& p, cudaStream_t stream) {
+template <typename TA, bool kE4m3, bool kWarpTeam, int kThreads>
+cudaError_t append_as(const AppendProblem& p, int threads, cudaStream_t stream) {
     const int64_t segs = min64(p.T, (int64_t)p.T / p.page + 2 * (int64_t)p.B);
     const int64_t grid = kWarpTeam ? segs : segs * p.Hkv;
     if (grid > INT32_MAX) return cudaErrorInvalidConfiguration;
-    // a thread for each unit of a page's tokens, or a warp for each head
-    int threads = kWarpTeam ? 32 * p.Hkv : p.page << unit_bits(head_units(p.r.R, p.D));
-    threads = threads < 64 ? 64 : threads < kAppendThreads<kWarpTeam> ? threads : kAppendThreads<kWarpTeam>;
-    return launch_k(append_kernel<TA, kE4m3, kWarpTeam>, dim3((unsigned)grid), dim3((unsigned)threads), 0, stream, p);
+    threads = threads < 64 ? 64 : threads < kThreads ? threads : kThreads;
+    return launch_k(append_kernel<TA, kE4m3, kWarpTeam, kThreads>, dim3((unsigned)grid), dim3((unsigned)threads), 0, stream, p);
 }
 
-template <typename TA>
+template <typename TA, bool kE4m3>
 cudaError_t append_type(const AppendProblem& p, cudaStream_t stream) {
     // few tokens per sequence: a head is a warp's work
-    const bool few = p.T <= 4 * (int64_t)p.B;
-    if (p.e4m3) return few ? append_as<TA, true, true>(p, stream) : append_as<TA, true, false>(p, stream);
-    return few ? append_as<TA, false, true>(p, stream) : append_as<TA, false, false>(p, stream);
+    if (p.T <= 4 * (int64_t)p.B) return append_as<TA, kE4m3, true, 256>(p, 32 * p.Hkv, stream);
+    // else a thread for each unit of a page's tokens. One block of 512 fills an SM's registers, but
+    // spares e4m3 a second reading of its values: 8192 tokens of 8 kv heads, D 128, pages of 64 in 47 us,
+    // with blocks of 256 58. Other caches take two blocks of 256 on an SM: 1583 tokens, 4 kv heads of 64, pages of 128
+    // 9.4 us (blocks of 512: 14.4).
+    const int threads = p.page << unit_bits(head_units(p.r.R, p.D));
+    return kE4m3 && threads > 256 ? append_as<TA, kE4m3, false, kE4m3 ? 512 : 256>(p, threads, stream)
+                                  : append_as<TA, kE4m3, false, 256>(p, threads, stream);
 }
 
 }  // namespace
@@ -454,7 +453,8 @@ cudaError_t launch_rope(const RopeProblem& p, cudaStream_t stream) {
 }
 
 cudaError_t launch_append(const AppendProblem& p, cudaStream_t stream) {
-    return p.act_dtype == GBMOE_F32 ? append_type<float>(p, stream) : append_type<__nv_bfloat16>(p, stream);
+    if (p.act_dtype == GBMOE_F32) return p.e4m3 ? append_type<float, true>(p, stream) : append_type<float, false>(p, stream);
+    return p.e4m3 ? append_type<__nv_bfloat16, true>(p, stream) : append_type<__nv_bfloat16, false>(p, stream);
 }
 
 }  // namespace gbmoe
