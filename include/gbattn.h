@@ -83,7 +83,7 @@ typedef struct gbattn_cache {
 /* A batch of B sequences over the cache: cu_q [B+1] offsets of their query (or
  * new) tokens, kv_len [B] their keys (the new ones among them, which are the
  * last), page_table [B, max_pages] the pool pages of tokens 0.., page, 2*page..
- * of each sequence. Lengths beyond max_pages * page are cut to it. */
+ * of each sequence. attn_cached cuts lengths beyond max_pages * page to it. */
 typedef struct gbattn_batch {
     int32_t B, max_pages;
     const int32_t *cu_q, *kv_len, *page_table;
@@ -175,6 +175,7 @@ int attn_prompt(const gbattn_config* cfg, int32_t Tq, int32_t Tk, int32_t B, con
  * number works. Long contexts are split over CTAs and joined by a second
  * launch, deterministically. bf16 with D 64, 96 or 128 runs on the tensor
  * cores, else on CUDA cores. A token whose page is outside the pool is masked.
+ * T * G and max_pages * page up to 2^30, else GBMOE_EUNSUPPORTED.
  */
 int attn_cached(const gbattn_config* cfg, int32_t T, const gbattn_batch* batch, const gbattn_rows* q,
                 const gbattn_cache* cache, const gbattn_rows* out, float* lse, void* workspace,

@@ -18,8 +18,8 @@ struct Rows {
 struct RopeParams {
     int R;          // rotary_dim (0: nothing turns)
     int half;       // 1: pairs (i, i + R/2), 0: (2i, 2i + 1)
-    float mag;      // factor of cos and sin, negative angle for the inverse:
-    float sin_sign; // -1 turns back
+    float mag;      // factor of cos and sin
+    float sin_sign; // 1, or -1: turns back
     const uint64_t* table;
 };
 

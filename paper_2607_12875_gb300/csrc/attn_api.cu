@@ -1,6 +1,5 @@
 // C ABI of the attention operators (declared in include/gbattn.h): argument
 // checks on the host and the choice of kernels.
-#include <climits>
 #include <cmath>
 #include <cstdint>
 
@@ -13,7 +12,7 @@ namespace {
 
 constexpr size_t kAlign = 256;
 constexpr int kMaxHeads = 4096;
-constexpr int kMaxRows = 1 << 30;
+constexpr int kMaxRows = 1 << 30;  // tokens, query rows of a sequence (tokens times G), keys: the kernels count them in 32 bits
 
 int log2_of(int v) {
     int b = 0;
@@ -239,6 +238,8 @@ int attn_cached(const gbattn_config* cfg, int32_t T, const gbattn_batch* batch, 
     if (int s = check_cache(cfg, cache)) return s;
     if (!aligned(lse, 4)) return GBMOE_EINVAL;
     if (!rows_ok(cfg, q, T, cfg->heads_q, false) || !rows_ok(cfg, out, T, cfg->heads_q, true)) return GBMOE_EINVAL;
+    if ((int64_t)T * (cfg->heads_q / cfg->heads_kv) > kMaxRows || (int64_t)batch->max_pages * cfg->page > kMaxRows)
+        return GBMOE_EUNSUPPORTED;
     AttnProblem p = problem(cfg, T, batch->B, q, out, lse, ws);
     p.paged = 1; p.e4m3 = cfg->cache_dtype == GBATTN_CACHE_E4M3; p.R = cfg->heads_q / cfg->heads_kv;
     p.page = cfg->page; p.max_pages = batch->max_pages; p.n_pages = cache->n_pages;

@@ -202,3 +202,15 @@ def test_attention_refusals(lib):
     assert cached(batch=changed(batch, B=0)) == gb.OK
     with pytest.raises(ValueError):
         gb.attn_cached(c, batch, Rows(strides=(2048, 256, 2)), cache, out, ws, stream=0)
+
+
+def test_sizes_that_do_not_fit_32_bits_are_refused(lib):
+    c = cfg(heads_q=64, heads_kv=1, page=128)
+    cache, batch = bundles()
+    ws = Ws(gb.attn_workspace_size(c, 4, 2))
+
+    def cached(T, max_pages):
+        q = Rows(T=T, H=64)
+        return status_of(gb.attn_cached, c, changed(batch, max_pages=max_pages), q, cache, q, ws)
+    assert cached((1 << 24) + 1, 3) == gb.EUNSUPPORTED       # rows: tokens times heads of a group
+    assert cached(4, (1 << 23) + 1) == gb.EUNSUPPORTED       # keys of a sequence
