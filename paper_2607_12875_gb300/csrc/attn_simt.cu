@@ -9,7 +9,6 @@
 // prompts (89 % of their rate; 1200 tokens of 16 heads of 64 in 0.21 ms, 14
 // TFLOP/s), by the latency of its loads for single tokens.
 #include <atomic>
-#include <climits>
 #include <type_traits>
 
 #include "attn_plan.cuh"
