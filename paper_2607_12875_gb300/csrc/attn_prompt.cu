@@ -3,7 +3,8 @@
 // One CTA holds two tiles of 128 query rows that read the same keys. A row is a
 // token and one of H heads of a group, H the largest power of two in the group's
 // number of heads (up to 32): 256 / H tokens, so that short prompts and the ends
-// of long ones fill the tiles. Per tile
+// of long ones fill the tiles. Or, for short prompts, the group's heads and empty
+// rows up to the next power of two (kPad). Per tile
 // of 128 keys and for each query tile t:
 //   S_t = Q_t K^T      tcgen05.mma, both operands in shared memory, S in TMEM
 //   P_t = exp2(scale S_t - m)   one thread per row: S from TMEM to registers,
@@ -60,7 +61,7 @@ struct Smem {
 
 struct Params {
     AttnProblem a;
-    int hlog;  // log2 of the heads of a tile
+    int hlog, heads;  // log2 of a token's rows in a tile, and how many of them are heads
     uint64_t wait_limit_ns;
 };
 
@@ -254,7 +255,7 @@ __device__ __forceinline__ bool cancelled(const void* src, uint32_t& x) {
     return ok != 0;
 }
 
-template <int DK, bool kDeal>
+template <int DK, bool kDeal, bool kPad>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                    const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_o,
@@ -343,12 +344,13 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             const Work& slot = work_slots[k & 1];
             const Seq s = slot.s;
             const int n = slot.n[t], n2 = slot.n[t ^ 1], rows = slot.rows[t], row = slot.tok0[t] + (r >> pp.hlog), k_first = slot.k_first, end = slot.end;
-            const int head0 = slot.head0, head = head0 + (r & ((1 << pp.hlog) - 1));
+            const int head0 = slot.head0, place = r & ((1 << pp.hlog) - 1), head = head0 + place;
+            const bool have = r < rows && (!kPad || place < pp.heads);
             __syncwarp();
             if (lane == 0) mbar_arrive(&w_empty[k & 1]);
             if (end) break;
-            int lo = 0, hi = INT_MAX;  // (rows past the tile's end are never stored: no mask for them)
-            if (r < rows) seen_keys(p, s, row, lo, hi);
+            int lo = 0, hi = INT_MAX;  // (rows past the tile's end and empty ones are never stored: no mask for them)
+            if (have) seen_keys(p, s, row, lo, hi);
             float m = neg_inf(), l = 0.0f;
             for (int j = 0; j < n; ++j) {
                 ok = wait_warp(&s_full[t], sn++ & 1u);
@@ -445,8 +447,8 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             __nv_bfloat16* out = const_cast<__nv_bfloat16*>(static_cast<const __nv_bfloat16*>(p.out.p)) + tok * p.out.ts + head * p.out.hs;
             float check = 0.0f;  // NaN once a value is not finite
             // all 32 rows of this warp belong to the tile: a TMA store of each 32 columns;
-            // else plain stores of the valid rows (the others are another sequence's)
-            const bool via_tma = (warp & 3) * 32 + 32 <= rows;
+            // else plain stores of the valid rows (the others are another sequence's or group's)
+            const bool via_tma = !kPad && (warp & 3) * 32 + 32 <= rows;
             uint8_t* stage_buf = sO + warp * 4096;
 #pragma unroll 1
             for (int c = kDeal ? 32 * t : 0; c < p.D; c += kDeal ? 64 : 32) {
@@ -487,7 +489,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                     const uint4 v = make_uint4(w[0], w[1], w[2], w[3]);
                     // (64-byte rows, 64-byte swizzle; columns past D are not written)
                     if (via_tma) *reinterpret_cast<uint4*>(buf + lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4)) = v;
-                    else if (r < rows && c + 8 * q < p.D) *reinterpret_cast<uint4*>(out + c + 8 * q) = v;
+                    else if (have && c + 8 * q < p.D) *reinterpret_cast<uint4*>(out + c + 8 * q) = v;
                 }
                 if (via_tma) {
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -502,9 +504,9 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 if (!ok) break;
                 check += stats[2][warp ^ 4][lane];
             }
-            if (r < rows && p.lse && (!kDeal || t == 0)) p.lse[tok * p.Hq + head] = empty ? neg_inf() : (m + log2f(l)) * kLn2;
+            if (have && p.lse && (!kDeal || t == 0)) p.lse[tok * p.Hq + head] = empty ? neg_inf() : (m + log2f(l)) * kLn2;
             // rows that may hold a masked key's NaN
-            uint32_t again = __ballot_sync(0xffffffffu, r < rows && !empty && check != check && finite(m) && finite(l) && l > 0.0f);
+            uint32_t again = __ballot_sync(0xffffffffu, have && !empty && check != check && finite(m) && finite(l) && l > 0.0f);
             if (kDeal && again) {  // (the same in both warps; one repairs, when both have stored)
                 if (lane == 0) bulk_wait_all();
                 __syncwarp();
@@ -527,7 +529,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         if (warp == 10) {
             // --------------------------------------------------------- scheduler
-            const int groups = p.Hq >> pp.hlog;
+            const int groups = kPad ? p.Hq / pp.heads : p.Hq >> pp.hlog;
             const int tile_toks = kTile >> pp.hlog, toks = kDeal ? tile_toks : 2 * tile_toks;
             uint32_t block = blockIdx.x;
             TileFinder tiles;
@@ -544,7 +546,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                     w.s = load_seq(p, at.b);
                     // the last tiles, which see the most keys, first
                     const int first = ((w.s.nq + toks - 1) / toks - 1 - (int)at.at) * toks;
-                    w.head0 = (int)(block % groups) << pp.hlog;
+                    w.head0 = kPad ? (int)(block % groups) * pp.heads : (int)(block % groups) << pp.hlog;
                     w.head_kv = w.head0 / (p.Hq / p.Hkv);
                     w.end = 0;
                     int lo, hi;
@@ -830,11 +832,11 @@ bool tma_strides(const Rows& r, int64_t T, int heads) {
 }
 
 // the most items of `rows` rows that the lengths can make
-int64_t items_of(const AttnProblem& p, int rows, int hlog) { return (p.T / (rows >> hlog) + p.B) * (int64_t)(p.Hq >> hlog); }
+int64_t items_of(const AttnProblem& p, int rows, int hlog, int heads) { return (p.T / (rows >> hlog) + p.B) * (int64_t)(p.Hq / heads); }
 
-template <int DK, bool kDeal>
-cudaError_t prompt_as(const AttnProblem& p, int hlog, cudaStream_t stream) {
-    constexpr auto kernel = attn_prompt_kernel<DK, kDeal>;
+template <int DK, bool kDeal, bool kPad>
+cudaError_t prompt_as(const AttnProblem& p, int hlog, int heads, cudaStream_t stream) {
+    constexpr auto kernel = attn_prompt_kernel<DK, kDeal, kPad>;
     static DeviceOnce once;
     if (cudaError_t e = once.run([] {
             return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<DK>::BYTES);
@@ -842,11 +844,11 @@ cudaError_t prompt_as(const AttnProblem& p, int hlog, cudaStream_t stream) {
         e != cudaSuccess)
         return e;
     CUtensorMap q, k, v, o;
-    Params pp{p, hlog, tc_wait_limit_ns()};
+    Params pp{p, hlog, heads, tc_wait_limit_ns()};
     if (!rows_map(&q, p.q, p.T, p.Hq, p.D, pp.hlog) || !rows_map(&o, p.out, p.T, p.Hq, p.D, pp.hlog, true) ||
         !rows_map(&k, p.k, p.Tk, p.Hkv, p.D, 0) || !rows_map(&v, p.v, p.Tk, p.Hkv, p.D, 0))
         return cudaErrorInvalidValue;
-    const int64_t grid = items_of(p, kDeal ? kTile : 2 * kTile, hlog);
+    const int64_t grid = items_of(p, kDeal ? kTile : 2 * kTile, hlog, heads);
     if (grid > INT32_MAX) return cudaErrorInvalidConfiguration;
     return launch_k(kernel, dim3((unsigned)grid), dim3(kThreads), Smem<DK>::BYTES, stream, q, k, v, o, pp);
 }
@@ -860,15 +862,24 @@ bool attn_prompt_tc_supported(const AttnProblem& p) {
 }
 
 cudaError_t launch_attn_prompt_tc(const AttnProblem& p, cudaStream_t stream) {
+    const int G = p.Hq / p.Hkv;
     int hlog = 0;
-    while (hlog < 5 && p.Hq / p.Hkv % (2 << hlog) == 0) ++hlog;
+    while (hlog < 5 && G % (2 << hlog) == 0) ++hlog;
+    const int heads = 1 << hlog;
+    // The whole group with empty rows, where there are more items than SMs and a prompt of the mean
+    // length makes fewer so: 16 prompts of 36 tokens in all, 56 and 8 heads 10 us, one head at a time 32.
+    int all = 0;
+    while (1 << all < G) ++all;
+    auto of_mean = [&](int log, int n) { return (((int64_t)p.T << log) / p.B + 2 * kTile) / (2 * kTile) * (G / n); };
+    if (all <= 5 && items_of(p, 2 * kTile, hlog, heads) > sm_count() && of_mean(all, G) < of_mean(hlog, heads))
+        return p.D <= 64 ? prompt_as<64, false, true>(p, all, G, stream) : prompt_as<128, false, true>(p, all, G, stream);
     // Too few items for every SM (or, of long prompts, to even out over them). Us without and with: 7596
     // tokens, 4 heads 91 and 62; two prompts of 7344 in all, 8 heads 77 and 65; 476 tokens, 4 heads 13.4
     // and 9.8; 16 prompts of 2242 in all, 7 heads, which the second condition leaves out, 10.8 and 12.8.
-    const int64_t items = items_of(p, 2 * kTile, hlog);
+    const int64_t items = items_of(p, 2 * kTile, hlog, heads);
     const bool deal = items <= sm_count() || (items <= 2 * sm_count() && p.T >= (int64_t)2 * kTile * p.B);
-    if (p.D <= 64) return deal ? prompt_as<64, true>(p, hlog, stream) : prompt_as<64, false>(p, hlog, stream);
-    return deal ? prompt_as<128, true>(p, hlog, stream) : prompt_as<128, false>(p, hlog, stream);
+    if (p.D <= 64) return deal ? prompt_as<64, true, false>(p, hlog, heads, stream) : prompt_as<64, false, false>(p, hlog, heads, stream);
+    return deal ? prompt_as<128, true, false>(p, hlog, heads, stream) : prompt_as<128, false, false>(p, hlog, heads, stream);
 }
 
 }  // namespace gbmoe

@@ -337,6 +337,16 @@ def test_prompt_of_many_heads(Hq, Hkv, D, nq, nk, causal, window):
     test_prompt("bf16", Hq, Hkv, D, nq, nk, causal, window)
 
 
+@pytest.mark.parametrize("Hq,Hkv,D,nq,nk,causal,window", [
+    (168, 24, 64, [3, 1, 0, 40, 7, 18, 2, 25], None, True, 0),       # 7 heads per kv head: rows of 8
+    (240, 40, 128, [9, 33, 1, 14, 60], None, True, 0),               # 6
+    (150, 50, 80, [37, 5, 12, 70], None, True, 20),                  # 3
+    (320, 16, 64, [3, 5, 11], [203, 5, 11], True, 0),                # 20 of 32 rows
+])
+def test_short_prompts_of_odd_groups(Hq, Hkv, D, nq, nk, causal, window):
+    test_prompt("bf16", Hq, Hkv, D, nq, nk, causal, window)
+
+
 @pytest.mark.parametrize("H", [2, 200])
 def test_prompt_with_infinite_and_nan_scores(H):
     """Where every score of a row is not a number, or one is infinite, the row is not a number; rows before are right."""
