@@ -473,7 +473,13 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 }
                 uint8_t* buf = stage_buf + ((c >> (kDeal ? 6 : 5)) & 1) * 2048;
                 if (via_tma) {
-                    if (lane == 0) bulk_wait_read<1>();  // the store that last read buf is done reading
+                    // The store that last read buf is done reading: within an item the one before the latest. An
+                    // item begins with the same buffer whatever the last one ended with (an odd number of chunks: with this
+                    // one too, and an item without keys comes here at once), so there every store.
+                    if (lane == 0) {
+                        if (c < (kDeal ? 64 : 32)) bulk_wait_read<0>();
+                        else bulk_wait_read<1>();
+                    }
                     __syncwarp();
                 }
 #pragma unroll

@@ -1,0 +1,67 @@
+"""Attention operators at the edges of their buffers and value ranges, each
+element held to what its own sum can be off by."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2607_12875_gb300 as gb
+from test_gpu_attn import i32, normal, prefix
+
+pytestmark = pytest.mark.gpu
+
+
+def attention64(q, k, v, nq, nk, scale, causal=True, window=0):
+    """Packed attention in 64 bits on the GPU: (out, size) with size = sum_j p_j |v_j| of each element."""
+    out, size, a, b = [], [], 0, 0
+    for n, m in zip(nq, nk):
+        qs, ks, vs = q[a:a + n].double(), k[b:b + m].double(), v[b:b + m].double()
+        a, b = a + n, b + m
+        G = q.shape[1] // k.shape[1]
+        ks, vs = ks.repeat_interleave(G, 1), vs.repeat_interleave(G, 1)
+        pos = torch.arange(m - n, m, device=q.device)[:, None]
+        j = torch.arange(m, device=q.device)[None, :]
+        see = torch.ones((n, m), dtype=torch.bool, device=q.device)
+        if causal:
+            see &= j <= pos
+        if window > 0:
+            see &= j > pos - window
+        s = torch.einsum("ihd,jhd->hij", qs, ks) * scale
+        s = s.masked_fill(~see, -np.inf)
+        top = s.amax(2, keepdim=True) if m else s.new_zeros((q.shape[1], n, 1))
+        p = torch.exp(s - top.masked_fill(torch.isneginf(top), 0.0))
+        p = p / p.sum(2, keepdim=True).masked_fill(~see.any(1)[None, :, None], 1.0)
+        out.append(torch.einsum("hij,jhd->ihd", p, vs))
+        size.append(torch.einsum("hij,jhd->ihd", p, vs.abs()))
+    return torch.cat(out), torch.cat(size)
+
+
+def bf16_bound(want, size):
+    """The result's rounding to bf16 and the weights', each at most 2^-8 of itself; fp32 scores and exponentials."""
+    return 1.05 * 2.0 ** -8 * (want.abs() + size) + 2e-5 * size
+
+
+# ------------------------------------------------------------------- prompt
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,nq,nk", [
+    # more items than SMs, items without keys between the others; head sizes whose results leave in an odd number of pieces
+    (400, 400, 96, [128, 128, 256, 130, 128], [128, 0, 100, 0, 256]),
+    (400, 400, 32, [128, 128, 256, 130, 128], [128, 0, 100, 0, 256]),
+    (800, 400, 80, [64, 64, 128, 64], [64, 0, 128, 0]),
+    # so few that a tile's keys are dealt to both halves
+    (20, 20, 64, [512, 512, 512, 512], [512, 0, 600, 0]),
+    (20, 20, 96, [512, 512, 512, 512], [512, 0, 600, 0]),
+    (20, 20, 32, [512, 512, 512, 512], [512, 0, 600, 0]),
+])
+def test_prompt_items_with_and_without_keys_in_turn(Hq, Hkv, D, nq, nk):
+    rng = np.random.default_rng(D)
+    q, k, v = (normal(rng, (sum(n), h, D), "bf16") for n, h in ((nq, Hq), (nk, Hkv), (nk, Hkv)))
+    cfg = gb.attn_config(Hq, Hkv, D)
+    ws = torch.zeros(gb.attn_workspace_size(cfg, sum(nq), len(nq)), dtype=torch.uint8, device="cuda")
+    want, size = attention64(q, k, v, nq, nk, cfg.scale)
+    bound, cu_q, cu_k = bf16_bound(want, size), prefix(nq), prefix(nk)
+    for _ in range(10):
+        out = torch.full_like(q, float("nan"))
+        gb.attn_prompt(cfg, q, k, v, cu_q, cu_k, out, ws)
+        assert ((out.double() - want).abs() <= bound).all()
+    assert gb.moe_device_status(ws) == gb.OK
