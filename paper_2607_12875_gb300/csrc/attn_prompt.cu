@@ -429,7 +429,12 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             if (kDeal && ok && n2 > 0) ok = wait_warp(&o_full[t ^ 1], items2++ & 1u);
             if (!ok) break;
             tc_fence_after();
-            if (rows <= (warp & 3) * 32) continue;  // no row of this warp
+            if (rows <= (warp & 3) * 32) {  // no row of this warp
+                // kDeal: the two warps of these rows meet all the same. Each has waited for both halves' sums then, so neither
+                // barrier can complete a phase of the next item before the other warp has seen this item's.
+                if (kDeal) ok = meet();
+                continue;
+            }
             const bool empty = hi < lo;
             float inv = empty ? 0.0f : 1.0f / l, inv2 = 0.0f;  // (kDeal: factors of this tile's and the other's sums)
             if constexpr (kDeal) {

@@ -65,3 +65,19 @@ def test_prompt_items_with_and_without_keys_in_turn(Hq, Hkv, D, nq, nk):
         gb.attn_prompt(cfg, q, k, v, cu_q, cu_k, out, ws)
         assert ((out.double() - want).abs() <= bound).all()
     assert gb.moe_device_status(ws) == gb.OK
+
+
+def test_prompt_dealt_keys_of_ragged_ends():
+    """Dealt keys, more items than SMs, tiles whose last rows no warp has and whose keys are all in one half."""
+    rng = np.random.default_rng(1)
+    nq, nk, H, D = [272, 260, 290, 272], [100, 260, 20, 272], 20, 64
+    q, k, v = (normal(rng, (sum(n), H, D), "bf16") for n in (nq, nk, nk))
+    cfg = gb.attn_config(H, H, D)
+    ws = torch.zeros(gb.attn_workspace_size(cfg, sum(nq), len(nq)), dtype=torch.uint8, device="cuda")
+    want, size = attention64(q, k, v, nq, nk, cfg.scale)
+    bound, cu_q, cu_k = bf16_bound(want, size), prefix(nq), prefix(nk)
+    for _ in range(20):
+        out = torch.full_like(q, float("nan"))
+        gb.attn_prompt(cfg, q, k, v, cu_q, cu_k, out, ws)
+        assert ((out.double() - want).abs() <= bound).all()
+    assert gb.moe_device_status(ws) == gb.OK
