@@ -282,7 +282,8 @@ __device__ __forceinline__ float rescale(const AppendProblem& p, const PageToken
 // A segment's keys and values of kv head h to the cache, its keys to k_out and the
 // query heads of the group to q_out. A thread has one unit of every step-th
 // token. e4m3: up to kHeld tokens of a thread stay in registers between the
-// search for the maximum and the rounding; longer segments are read twice.
+// search for the maximum and the rounding; longer segments are read twice, and
+// k_out, which may be k, is written at the last reading.
 template <typename TA, bool kE4m3, bool kWarpTeam>
 __device__ __forceinline__ void append_head(const AppendProblem& p, const PageTokens& s, int h, const Team<kWarpTeam>& team) {
     constexpr int kHeld = 1, B = kQueryBatch<TA>;
@@ -297,9 +298,9 @@ __device__ __forceinline__ void append_head(const AppendProblem& p, const PageTo
     if (kE4m3 && stored && s.off > 0) old_k = (int)p.k_scale[head] - 127, old_v = (int)p.v_scale[head] - 127;
     Values kv[kHeld];
     Held<TA> vh[kHeld];
-    const bool once = s.n <= kHeld * step;
+    const bool once = s.n <= kHeld * step || !kE4m3 || !stored;  // k is read once
     float top_k = 0.0f, top_v = 0.0f;
-    auto load = [&](int t0, bool rest) {  // rest: queries and k_out too
+    auto load = [&](int t0, bool queries, bool keys_out) {
         Held<TA> kh[kHeld];
 #pragma unroll
         for (int k = 0; k < kHeld; ++k) {
@@ -313,7 +314,7 @@ __device__ __forceinline__ void append_head(const AppendProblem& p, const PageTo
             if (t >= n) break;
             Angles angles;
             bool ready = false;
-            if (rest)
+            if (queries)
                 for (int g0 = 0; g0 < G; g0 += B) {
                     Held<TA> q[B];
 #pragma unroll
@@ -333,7 +334,7 @@ __device__ __forceinline__ void append_head(const AppendProblem& p, const PageTo
             if (!ready) angles.set(p.r, unit, p.positions ? (int64_t)p.positions[tok] : s.pos + t);
             kv[k].from(kh[k], unit);
             kv[k].turn(p.r, unit, angles);
-            if (rest && p.k_out.p) kv[k].store(unit, row<TA>(p.k_out, tok, h));
+            if (keys_out && p.k_out.p) kv[k].store(unit, row<TA>(p.k_out, tok, h));
         }
     };
     auto maxima = [&](int t0, bool careful) {
@@ -368,7 +369,7 @@ __device__ __forceinline__ void append_head(const AppendProblem& p, const PageTo
         }
     };
     for (int t0 = first; t0 < n; t0 += kHeld * step) {
-        load(t0, true);
+        load(t0, true, once);
         if (kE4m3) maxima(t0, false);
         else if (stored) write(t0, 1.0f, 1.0f);
     }
@@ -378,7 +379,7 @@ __device__ __forceinline__ void append_head(const AppendProblem& p, const PageTo
         if (top_k > 3.402823466e38f || top_v > 3.402823466e38f) {  // an infinity: once more without
             top_k = top_v = 0.0f;
             for (int t0 = first; t0 < n; t0 += kHeld * step) {
-                if (!once) load(t0, false);
+                if (!once) load(t0, false, false);
                 maxima(t0, true);
             }
             team.max(top_k, top_v);
@@ -389,7 +390,7 @@ __device__ __forceinline__ void append_head(const AppendProblem& p, const PageTo
         page = static_cast<uint8_t*>(p.v_pool) + head * p.page * p.D;
         const float inv_v = rescale(p, s, page, p.v_scale + head, old_v, top_v, team);
         for (int t0 = first; t0 < n; t0 += kHeld * step) {
-            if (!once) load(t0, false);
+            if (!once) load(t0, false, true);
             write(t0, inv_k, inv_v);
         }
     }

@@ -4,8 +4,9 @@ import numpy as np
 import pytest
 import torch
 
+import attn_reference as ref
 import paper_2607_12875_gb300 as gb
-from test_gpu_attn import i32, normal, prefix
+from test_gpu_attn import U, Cache, i32, normal, prefix, wide
 
 pytestmark = pytest.mark.gpu
 
@@ -38,6 +39,59 @@ def attention64(q, k, v, nq, nk, scale, causal=True, window=0):
 def bf16_bound(want, size):
     """The result's rounding to bf16 and the weights', each at most 2^-8 of itself; fp32 scores and exponentials."""
     return 1.05 * 2.0 ** -8 * (want.abs() + size) + 2e-5 * size
+
+
+# ------------------------------------------------------------------- append
+
+
+@pytest.mark.parametrize("act", ["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["act", "e4m3"])
+@pytest.mark.parametrize("infinite", [False, True])
+@pytest.mark.parametrize("page,D,R,new,lens", [
+    (128, 128, 128, [300], [300]),                          # more tokens in a page than a block takes at a time
+    (64, 256, 64, [100, 64], [130, 64]),
+    (64, 64, 64, [13, 1, 1, 1], [13, 70, 1, 64]),           # few tokens a sequence on average: a warp's work, several passes
+    (16, 128, 32, [13, 1, 1, 1], [40, 33, 1, 16]),
+    (64, 64, 64, [40, 3], [40, 80]),                        # one pass
+])
+def test_append_in_place(act, kind, infinite, page, D, R, new, lens):
+    """Rotated queries and keys over the ones that came: the cache holds what it holds with outputs of their own."""
+    rng = np.random.default_rng(page + D)
+    Hkv, G, T = 3, 2, sum(new)
+    k, v, q = normal(rng, (T, Hkv, D), act), normal(rng, (T, Hkv, D), act), normal(rng, (T, Hkv * G, D), act)
+    if infinite:  # in the scale's way, so that the maxima are searched again
+        v[1, 0, 3], v[2, 2, D - 1] = float("inf"), float("-inf")
+        if R < D:
+            k[1, 1, D - 1] = float("inf")
+    cfg = gb.attn_config(Hkv * G, Hkv, D, act=act, rotary_dim=R, rotary_scale=1.25, cache=kind, page=page)
+    table = gb.attn_rope_table(R)
+    caches = [Cache(np.random.default_rng(1), act, kind, Hkv, D, page, lens) for _ in range(2)]
+    want = [caches[0].stored(w) for w in "kv"]
+    keep = (prefix(new), i32(lens), caches[0].dev_table)
+    outs = []
+    for c, alias in zip(caches, (False, True)):
+        kk, qq = k.clone(), q.clone()
+        ko, qo = (kk, qq) if alias else (torch.empty_like(k), torch.empty_like(q))
+        gb.attn_append(cfg, gb.attn_batch(*keep), kk, v, table, c.bundle, q=qq, q_out=qo, k_out=ko)
+        outs.append([ko, qo, c.k, c.v] + ([c.ks, c.vs] if kind == "e4m3" else []))
+    bits = {4: torch.int32, 2: torch.int16, 1: torch.uint8}
+    for a, b in zip(*outs):
+        assert torch.equal(a.view(bits[a.element_size()]), b.view(bits[b.element_size()]))
+    pos = np.concatenate([np.arange(m - n, m) for n, m in zip(new, lens)])
+    turned = ref.rotate(wide(k), pos, ref.frequencies(R), "half", 1.25)
+    for which, (vals, exps), x in (("k", want[0], turned), ("v", want[1], wide(v))):
+        ref.append(vals, exps, x, new, lens, caches[1].table, page)
+        got, got_e = caches[1].stored(which)
+        if exps is None:
+            fin = np.isfinite(vals)
+            assert np.array_equal(np.isfinite(got), fin)
+            assert (np.abs(got[fin] - vals[fin]) <= U[act] * np.abs(vals[fin]) + 1e-6 * np.abs(vals[fin]).max()).all()
+            continue
+        assert np.array_equal(got_e, exps)
+        # equal codes, but where fp32's rotation falls on the other side of a rounding boundary: then the next code
+        differ = got != vals
+        assert differ.mean() <= (1e-4 if which == "k" else 0.0)
+        assert (np.abs(got - vals)[differ] <= np.abs(vals[differ]) / 8 + 2.0 ** -9).all()
 
 
 # ------------------------------------------------------------------- prompt
