@@ -336,7 +336,7 @@ attn_split_kernel(const __grid_constant__ AttnProblem p, uint64_t wait_limit_ns)
                 }
             }
             const float kf = kE4m3 ? e8m0_to_f32(scales & 255u) : 1.0f;
-            const float ve = !kE4m3 ? 0.0f : scales >> 8 == 255u ? __uint_as_float(0x7fc00000u) : (float)((int)(scales >> 8) - 127);
+            const float ve = kE4m3 ? (float)((int)(scales >> 8) - 127) : 0.0f;
             const bool all = id >= 0 && key0 >= all_lo && key0 + kKeys - 1 <= all_hi;
 #pragma unroll
             for (int n = 0; n < NQ; ++n)
@@ -396,6 +396,15 @@ attn_split_kernel(const __grid_constant__ AttnProblem p, uint64_t wait_limit_ns)
                         s[n][z] = p0, s[n][2 + z] = p1;
                     }
                 }
+            if (kE4m3 && scales >> 8 == 255u) {  // values that are no numbers, for the rows that see them
+#pragma unroll
+                for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int key = key0 + g + 8 * (e >> 1);
+                        if (key >= lo[n][e & 1] && key <= hi[n][e & 1]) s[n][e] = __uint_as_float(0x7fc00000u);
+                    }
+            }
             uint32_t pb[NQ][2];
 #pragma unroll
             for (int n = 0; n < NQ; ++n) {

@@ -6,7 +6,7 @@ import torch
 
 import attn_reference as ref
 import paper_2607_12875_gb300 as gb
-from test_gpu_attn import U, Cache, i32, normal, prefix, wide
+from test_gpu_attn import U, Cache, attention_tolerance, cached_reference, i32, normal, prefix, wide
 
 pytestmark = pytest.mark.gpu
 
@@ -92,6 +92,35 @@ def test_append_in_place(act, kind, infinite, page, D, R, new, lens):
         differ = got != vals
         assert differ.mean() <= (1e-4 if which == "k" else 0.0)
         assert (np.abs(got - vals)[differ] <= np.abs(vals[differ]) / 8 + 2.0 ** -9).all()
+
+
+# ------------------------------------------------------------------- cached
+
+
+@pytest.mark.parametrize("act", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [64, 96, 128])
+def test_cached_scale_that_is_no_number_at_keys_unseen(act, D):
+    """A page's scale byte of 255 (NaN) matters to the rows that see one of its keys alone."""
+    rng = np.random.default_rng(D)
+    page, n, lens = 16, [1, 3], [320, 194]
+    c = Cache(rng, act, "e4m3", 2, D, page, lens)
+    q = normal(rng, (4, 4, D), act)
+    cfg = gb.attn_config(4, 2, D, act=act, window=100, cache="e4m3", page=page)
+    ws = torch.zeros(gb.attn_workspace_size(cfg, 4, 2), dtype=torch.uint8, device="cuda")
+    keep = (prefix(n), i32(lens), c.dev_table)
+    # keys 192 .. 207: of the first sequence before its token's window (220 ..), in a block of 64 keys that it reaches
+    # into; of the second one the tokens at 192 and 193 see some of them, the token at 191 none
+    ids = [int(c.table[b, 12]) for b in range(2)]
+    keep_scale = c.vs.clone()
+    c.vs[ids] = 255
+    out, lse = torch.zeros_like(q), torch.zeros((4, 4), device="cuda")
+    gb.attn_cached(cfg, gb.attn_batch(*keep), q, c.bundle, out, ws, lse=lse)
+    got = wide(out)
+    assert np.isnan(got[2:]).all() and torch.isfinite(lse).all()
+    c.vs.copy_(keep_scale)
+    want, _ = cached_reference(wide(q), c, n, lens, cfg.scale, True, 100)
+    vmax = max(np.abs(c.rows("v", b, m)[0]).max() for b, m in enumerate(lens))
+    assert (np.abs(got - want)[:2] <= attention_tolerance(act, want, vmax)[:2]).all()
 
 
 # ------------------------------------------------------------------- prompt
