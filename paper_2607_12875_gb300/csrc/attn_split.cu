@@ -46,6 +46,7 @@ constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kKeys = kBlockKeys / kWarps;  // keys of a stage of one warp
 constexpr unsigned kFull = 0xffffffffu;
 constexpr float kGrow = 6.0f;  // log2 of how far a row's maximum may run ahead
+constexpr float kRoom = 9.0f;  // e4m3: log2 of a weight as large as the maximum; kGrow + kRoom is fp16's largest power
 // Least blocks of 64 keys of a share, and how many a tile's set-up counts for. Us at (3, 2)
 // and (2, 1): one sequence of 4000 e4m3 keys, 8 kv heads 12.3 and 11.6; two of 19000, 1 kv head 16.9
 // and 20.1; 19 of up to 322 with 5 tokens, 4 kv heads 17.3 and 19.7. With (3, 0), where a share holds
@@ -349,7 +350,7 @@ attn_split_kernel(const __grid_constant__ AttnProblem p, uint64_t wait_limit_ns)
 
             // ---- running maximum and sum of rows 2 c + z
             // The maxima are raised, and the sums rescaled, only when a score has passed its row's by more
-            // than 2^kGrow (a power that fp16 weights have room for): most stages exchange nothing.
+            // than 2^kGrow (a power that the weights have room for): most stages exchange nothing.
             bool raise = false;
 #pragma unroll
             for (int n = 0; n < NQ; ++n)
@@ -390,7 +391,7 @@ attn_split_kernel(const __grid_constant__ AttnProblem p, uint64_t wait_limit_ns)
                     const float p0 = ex2(s[n][z] - b), p1 = ex2(s[n][2 + z] - b);
                     l[n][z] += p0 + p1;
                     if constexpr (kE4m3) {
-                        const float v = ve - (mo[n][z] == neg_inf() ? 0.0f : mo[n][z]);
+                        const float v = ve + kRoom - (mo[n][z] == neg_inf() ? 0.0f : mo[n][z]);
                         s[n][z] = ex2(s[n][z] + v), s[n][2 + z] = ex2(s[n][2 + z] + v);
                     } else {
                         s[n][z] = p0, s[n][2 + z] = p1;
@@ -541,6 +542,7 @@ attn_split_kernel(const __grid_constant__ AttnProblem p, uint64_t wait_limit_ns)
             for (int w = 0; w < kWarps; ++w) {
                 L += rows[w * kRows * LD + D + 1] * ex2(rows[w * kRows * LD + D] - b);
                 wt[w] = ex2(rows[w * kRows * LD + D + 2] - bo);
+                if (kE4m3) wt[w] *= 1.0f / (1 << (int)kRoom);
             }
             int rlo, rhi;
             seen_keys(p, it.s, (row0 + r) / G, rlo, rhi);

@@ -123,6 +123,31 @@ def test_cached_scale_that_is_no_number_at_keys_unseen(act, D):
     assert (np.abs(got - want)[:2] <= attention_tolerance(act, want, vmax)[:2]).all()
 
 
+def test_cached_many_small_weights_beside_a_large_one():
+    """One key far ahead of all others, its value 0: the result is the sum of the others' small weights. The kernel's
+    weights are fp16 and the largest is 2^9 or more, so each is off by 2^-11 of itself or 2^-34 of the largest; sums and
+    scores by fp32's rounding."""
+    for D, m in [(64, 192), (96, 192), (128, 192), (128, 40000)]:
+        page = 64
+        per = -(-m // page)
+        k, v = (torch.zeros((per, 1, page, D), dtype=torch.uint8, device="cuda") for _ in range(2))
+        ks, vs = (torch.full((per, 1), 127, dtype=torch.uint8, device="cuda") for _ in range(2))
+        v.fill_(0x38)                      # 1.0
+        k[0, 0, 0, 0], v[0, 0, 0] = 0x55, 0   # 13.0
+        q = torch.zeros((1, 1, D), dtype=torch.bfloat16, device="cuda")
+        q[0, 0, 0] = 1.4375
+        cfg = gb.attn_config(1, 1, D, scale=1.0, cache="e4m3", page=page)
+        ws = torch.zeros(gb.attn_workspace_size(cfg, 1, 1), dtype=torch.uint8, device="cuda")
+        out = torch.zeros_like(q)
+        keep = (i32([0, 1]), i32([m]), i32(np.arange(per)[None]))
+        gb.attn_cached(cfg, gb.attn_batch(*keep), q, gb.attn_cache(k, v, ks, vs), out, ws)
+        w = np.exp(-13.0 * 1.4375)
+        want = (m - 1) * w / (1 + (m - 1) * w)
+        assert 2.0 ** -28 < w < 2.0 ** -26  # the test's premise
+        bound = 1.05 * (2.0 ** -8 + 2.0 ** -11 + 2.0 ** -34 / w) * want + 2e-5 * want
+        assert (np.abs(wide(out) - want) <= bound).all(), (D, m, float(out[0, 0, 0]), want)
+
+
 # ------------------------------------------------------------------- prompt
 
 
