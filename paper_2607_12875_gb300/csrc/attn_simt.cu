@@ -449,7 +449,7 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const __grid_co
                     }
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        if (c + W * i >= k || w[i] == 0.0f) continue;  // (a part that this row does not see: its sums are 0)
+                        if (c + W * i >= k) continue;  // (a part that this row does not see: its sums are 0)
 #pragma unroll
                         for (int z = 0; z < Z; ++z) {
                             o[z][0] = fmaf(v[i][z].x, w[i], o[z][0]), o[z][1] = fmaf(v[i][z].y, w[i], o[z][1]);

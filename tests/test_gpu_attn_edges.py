@@ -6,7 +6,7 @@ import torch
 
 import attn_reference as ref
 import paper_2607_12875_gb300 as gb
-from test_gpu_attn import U, Cache, attention_tolerance, cached_reference, i32, normal, prefix, wide
+from test_gpu_attn import DT, U, Cache, attention_tolerance, cached_reference, i32, normal, prefix, wide
 
 pytestmark = pytest.mark.gpu
 
@@ -146,6 +146,33 @@ def test_cached_many_small_weights_beside_a_large_one():
         assert 2.0 ** -28 < w < 2.0 ** -26  # the test's premise
         bound = 1.05 * (2.0 ** -8 + 2.0 ** -11 + 2.0 ** -34 / w) * want + 2e-5 * want
         assert (np.abs(wide(out) - want) <= bound).all(), (D, m, float(out[0, 0, 0]), want)
+
+
+@pytest.mark.parametrize("act", ["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["act", "e4m3"])
+def test_cached_nan_values_of_no_weight(act, kind):
+    """A value that is no number makes its column so for every row that sees it, however small its weight, whether it
+    lies in the part of the keys that has the largest score or in another one."""
+    D, page, m = 64, 64, 4096
+    k, v = (torch.zeros((m // page, 1, page, D), dtype=torch.uint8 if kind == "e4m3" else torch.float32, device="cuda") for _ in range(2))
+    scales = [torch.full((m // page, 1), 127, dtype=torch.uint8, device="cuda") for _ in range(2)] if kind == "e4m3" else [None] * 2
+    one, nan = (0x38, 0x7f) if kind == "e4m3" else (1.0, float("nan"))
+    k[:, 0, :, 0] = one                   # every key's score is q's first element, but
+    k[m // page - 1, 0, 5, 1] = one       # one that is 300 ahead
+    v.fill_(one)
+    v[3, 0, 7, 20] = nan
+    if kind == "act":
+        k, v = k.to(DT[act]), v.to(DT[act])
+    q = torch.zeros((1, 1, D), dtype=DT[act], device="cuda")
+    q[0, 0, 0], q[0, 0, 1] = 1.0, 300.0
+    cfg = gb.attn_config(1, 1, D, act=act, scale=1.0, cache=kind, page=page)
+    ws = torch.zeros(gb.attn_workspace_size(cfg, 1, 1), dtype=torch.uint8, device="cuda")
+    out = torch.zeros_like(q)
+    keep = (i32([0, 1]), i32([m]), i32(np.arange(m // page)[None]))
+    gb.attn_cached(cfg, gb.attn_batch(*keep), q, gb.attn_cache(k, v, *scales), out, ws)
+    want = np.ones(D)
+    want[20] = np.nan
+    assert np.array_equal(wide(out)[0, 0], want, equal_nan=True)
 
 
 # ------------------------------------------------------------------- prompt
