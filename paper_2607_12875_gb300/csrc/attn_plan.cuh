@@ -47,6 +47,15 @@ __device__ __forceinline__ void seen_keys(const AttnProblem& p, const Seq& s, in
     if (hi < lo) hi = -1, lo = 0;
 }
 
+// whether one of sequence b's cached keys lo .. hi has a page in the pool
+__device__ __forceinline__ bool any_page(const AttnProblem& p, int b, int lo, int hi) {
+    if (hi < lo) return false;
+    const int32_t* pages = p.page_table + (int64_t)b * p.max_pages;
+    for (int i = lo >> p.page_log2; i <= hi >> p.page_log2; ++i)
+        if (pages[i] >= 0 && pages[i] < p.n_pages) return true;
+    return false;
+}
+
 // tiles of `rows` rows of queries (token i, head g of R: row i * R + g)
 __device__ __forceinline__ int64_t row_tiles(const AttnProblem& p, const Seq& s, int rows) {
     return ((int64_t)s.nq * p.R + rows - 1) / rows;

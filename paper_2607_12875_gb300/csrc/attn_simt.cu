@@ -251,15 +251,18 @@ __device__ __forceinline__ void attend(const AttnProblem& p, const Segment& it) 
         if (rr >= n_rows) continue;
         const int64_t t = it.s.q0 + (row0 + rr) / R;
         const int hq = head0 + (row0 + rr) % R;
+        // Without a score above -inf: whether the row sees a key at all (if not it gives 0, else 0 / 0)
+        const bool blank = m[r] == neg_inf() && l[r] == 0.0f;
+        const bool sees = !kPaged || !blank || any_page(p, it.b, max(lo[r], c_lo), min(hi[r], c_hi - 1));
         if (it.slot >= 0) {
             const int64_t at = it.slot * kRows + rr;
-            if (tx == 0) reinterpret_cast<float4*>(p.part_s)[at] = make_float4(m[r], l[r], m[r], 0.0f);
+            if (tx == 0) reinterpret_cast<float4*>(p.part_s)[at] = make_float4(m[r], l[r], m[r], sees ? 1.0f : 0.0f);
 #pragma unroll
             for (int c = 0; c < NC; ++c)
                 if (4 * tx + 32 * c < p.D) *reinterpret_cast<float4*>(p.part_o + at * p.D + 4 * tx + 32 * c) = o[r][c];
             continue;
         }
-        const bool empty = hi[r] < lo[r] || (kPaged && m[r] == neg_inf() && l[r] == 0.0f);  // (or none of its keys has a page)
+        const bool empty = hi[r] < lo[r] || !sees;
         const float inv = empty ? 0.0f : 1.0f / l[r];
         if (p.lse && tx == 0) p.lse[t * p.Hq + hq] = empty ? neg_inf() : (m[r] + log2f(l[r])) * kLn2;
         TA* out = const_cast<TA*>(static_cast<const TA*>(p.out.p)) + t * p.out.ts + hq * p.out.hs;
@@ -346,7 +349,8 @@ cudaError_t simt_source(const AttnProblem& p, cudaStream_t stream) {
 //
 // Rows of tiles that were cut. The parts' sums, each relative to 2^(its own third
 // statistic), are brought to the largest of those and added, the softmax sums
-// likewise relative to the first statistic: out = sum / l. Every block counts the
+// likewise relative to the first statistic: out = sum / l. (The fourth: 0 where the row sees
+// no key of the part.) Every block counts the
 // rows of all cut tiles for itself and takes its share of them, 1 to 8 at a time
 // and then with 8 to 1 warps for a row, which take every so many of its parts: the
 // order is fixed by the lengths. (A block for each share, most of them with
@@ -399,6 +403,7 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const __grid_co
         float o[Z][4] = {};
         int4 c0 = make_int4(0, 0, 0, 0), c1 = c0;
         int r = 0;
+        bool sees = true;
         if (have) {
             const int chunk = __ffs(__ballot_sync(0xffffffffu, q < upto)) - 1;
             r = q - __shfl_sync(0xffffffffu, upto - own, chunk);
@@ -460,6 +465,11 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const __grid_co
             }
 #pragma unroll
             for (int e = 16; e; e >>= 1) l += __shfl_xor_sync(0xffffffffu, l, e);
+            if (m == neg_inf() && l == 0.0f) {  // no score above -inf: whether a part saw a key
+                sees = false;
+                for (int c = lane; c < n; c += 32) sees = sees || __ldcg(st + slot(c)).w != 0.0f;
+                sees = __any_sync(0xffffffffu, sees);
+            }
         }
         if (W > 1) {  // (uniform)
             if (q0 != blockIdx.x * at_once) __syncthreads();  // the rows before are done with acc
@@ -473,7 +483,7 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const __grid_co
         s.q0 = c1.y, s.nq = c1.z, s.len = c1.w;
         int lo, hi;
         seen_keys(p, s, row / G, lo, hi);
-        const bool empty = hi < lo || (m == neg_inf() && l == 0.0f);
+        const bool empty = hi < lo || !sees;
         const int64_t t = s.q0 + row / G;
         const int hq = c0.w * G + row % G;
         if (p.lse && lane == 0) p.lse[t * p.Hq + hq] = empty ? neg_inf() : (base + log2f(l)) * kLn2;

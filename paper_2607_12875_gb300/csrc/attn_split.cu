@@ -546,13 +546,15 @@ attn_split_kernel(const __grid_constant__ AttnProblem p, uint64_t wait_limit_ns)
             }
             int rlo, rhi;
             seen_keys(p, it.s, (row0 + r) / G, rlo, rhi);
-            const bool empty = rhi < rlo || (M == neg_inf() && L == 0.0f);  // (or none of its keys has a page)
+            // without a score above -inf: whether the row sees a key at all (if not it gives 0, else 0 / 0)
+            const bool sees = !(M == neg_inf() && L == 0.0f) || any_page(p, it.b, max(rlo, base), min(rhi, (int)k_end - 1));
+            const bool empty = rhi < rlo || !sees;
             const int64_t t = it.s.q0 + (row0 + r) / G;
             const int hq = h * G + (row0 + r) % G;
             const int64_t at = it.slot * kRows + r;
             const float inv = empty ? 0.0f : ex2(bo - b) / L;
             if (x == 0) {
-                if (it.slot >= 0) reinterpret_cast<float4*>(p.part_s)[at] = make_float4(M, L, MO, 0.0f);
+                if (it.slot >= 0) reinterpret_cast<float4*>(p.part_s)[at] = make_float4(M, L, MO, sees ? 1.0f : 0.0f);
                 else if (p.lse) p.lse[t * p.Hq + hq] = empty ? neg_inf() : (b + log2f(L)) * kLn2;
             }
             for (int d = 4 * x; d < D; d += 4 * LANES) {

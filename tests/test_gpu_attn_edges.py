@@ -175,6 +175,32 @@ def test_cached_nan_values_of_no_weight(act, kind):
     assert np.array_equal(wide(out)[0, 0], want, equal_nan=True)
 
 
+@pytest.mark.parametrize("act", ["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["act", "e4m3"])
+@pytest.mark.parametrize("m", [40, 3000])
+def test_cached_scores_of_minus_infinity(act, kind, m):
+    """A row that sees keys, all with scores of -inf, is 0 / 0 as the formula has it; a row whose keys have no page is 0."""
+    rng = np.random.default_rng(m)
+    D, page = 64, 16
+    c = Cache(rng, act, kind, 1, D, page, [m, m])
+    if kind == "act":
+        c.k.abs_().clamp_(min=0.5)
+    else:
+        c.k.bitwise_and_(0x7f).clamp_(min=8)
+    c.table[1] = -1
+    c.table[0, 3:] = -1
+    q = normal(rng, (2, 3, D), act)
+    q[0, 1] = float("-inf")
+    cfg = gb.attn_config(3, 1, D, act=act, cache=kind, page=page)
+    ws = torch.zeros(gb.attn_workspace_size(cfg, 2, 2), dtype=torch.uint8, device="cuda")
+    out, lse = torch.zeros_like(q), torch.zeros((2, 3), device="cuda")
+    keep = (i32([0, 1, 2]), i32([m, m]), i32(c.table))
+    gb.attn_cached(cfg, gb.attn_batch(*keep), q, c.bundle, out, ws, lse=lse)
+    got = wide(out)
+    assert np.isnan(got[0, 1]).all() and np.isfinite(got[0, [0, 2]]).all() and (got[1] == 0).all()
+    assert torch.isneginf(lse[0, 1]) and torch.isfinite(lse[0, 0]) and torch.isneginf(lse[1]).all()
+
+
 # ------------------------------------------------------------------- prompt
 
 
