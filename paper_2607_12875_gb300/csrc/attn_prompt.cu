@@ -32,7 +32,9 @@
 //
 // A masked score gives P = 0, but 0 times a NaN value is a NaN: a row whose
 // sums are finite and whose result is not is checked for non-finite values at
-// keys that it does not see and computed again without them (repair_row).
+// keys of its tiles that it does not see, and computed again without them if there
+// are any (repair_rows: by one warp, 0.15 us for each key of a row; a function of its own, of
+// no more registers than leave the softmax its own).
 //
 // Waits are bounded as in the GEMM kernels (tc_ptx.cuh).
 #include <climits>
@@ -160,10 +162,35 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {  // two fp32 
 
 __device__ __forceinline__ bool finite(float x) { return fabsf(x) <= 3.402823466e38f; }
 
+// The first and last of the keys from .. to - 1 of kv head hk, those that every
+// row of the warp sees (seen_lo .. seen_hi) left out, at which a value is not
+// finite (x > y: none). By a whole warp, a key for each lane.
+__device__ __forceinline__ int2 bad_keys(const AttnProblem& p, int64_t k0, int hk, int from, int to, int seen_lo, int seen_hi) {
+    const int lane = threadIdx.x & 31;
+    const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(p.v.p) + k0 * p.v.ts + hk * p.v.hs;
+    int first = INT_MAX, last = -1;
+    for (int j0 = from; j0 < to; j0 += 32) {
+        if (j0 >= seen_lo && j0 < seen_hi - 31) {  // (on to the keys that some row does not see)
+            j0 += (seen_hi - 31 - j0) / 32 * 32;
+            continue;
+        }
+        const int j = j0 + lane;
+        if (j >= to || (j >= seen_lo && j <= seen_hi)) continue;
+        bool bad = false;
+        for (int c = 0; c < p.D; c += 8) {
+            const uint4 u = *reinterpret_cast<const uint4*>(v + j * p.v.ts + c);
+            bad = bad || (__vcmpgeu2(u.x & 0x7fff7fffu, 0x7f807f80u) | __vcmpgeu2(u.y & 0x7fff7fffu, 0x7f807f80u) |
+                          __vcmpgeu2(u.z & 0x7fff7fffu, 0x7f807f80u) | __vcmpgeu2(u.w & 0x7fff7fffu, 0x7f807f80u)) != 0;
+        }
+        if (bad) first = min(first, j), last = j;
+    }
+    return make_int2(__reduce_min_sync(0xffffffffu, first), __reduce_max_sync(0xffffffffu, last));
+}
+
 // The row of token t, head h once more, by a whole warp and without the values
 // it does not see: m and l are its softmax's maximum (base 2) and sum, lo .. hi
 // the keys it sees. Stops when every column is NaN.
-__device__ __noinline__ void repair_row(const AttnProblem& p, int64_t k0, int64_t t, int h, int lo, int hi, float m, float l) {
+__device__ __forceinline__ void repair_row(const AttnProblem& p, int64_t k0, int64_t t, int h, int lo, int hi, float m, float l) {
     const int lane = threadIdx.x & 31, hk = h / (p.Hq / p.Hkv), d = 4 * lane;
     const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(p.q.p) + t * p.q.ts + h * p.q.hs;
     const __nv_bfloat16* k = static_cast<const __nv_bfloat16*>(p.k.p) + hk * p.k.hs;
@@ -182,12 +209,16 @@ __device__ __noinline__ void repair_row(const AttnProblem& p, int64_t k0, int64_
             }
             w = exp2f(fmaf(s, p.scale_log2, -m));
         }
-        for (int i = 0; i < 32 && j0 + i <= hi; ++i) {
-            const float wi = __shfl_sync(0xffffffffu, w, i);
-            if (d < p.D) {
-                const uint2 u = *reinterpret_cast<const uint2*>(v + (k0 + j0 + i) * p.v.ts + d);
-                o[0] = fmaf(wi, bf16lo(u.x), o[0]), o[1] = fmaf(wi, bf16hi(u.x), o[1]);
-                o[2] = fmaf(wi, bf16lo(u.y), o[2]), o[3] = fmaf(wi, bf16hi(u.y), o[3]);
+        for (int i0 = 0; i0 < 32 && j0 + i0 <= hi; i0 += 8) {  // loads in flight
+            uint2 u[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                u[i] = d < p.D && j0 + i0 + i <= hi ? *reinterpret_cast<const uint2*>(v + (k0 + j0 + i0 + i) * p.v.ts + d) : make_uint2(0, 0);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float wi = __shfl_sync(0xffffffffu, w, i0 + i);
+                o[0] = fmaf(wi, bf16lo(u[i].x), o[0]), o[1] = fmaf(wi, bf16hi(u[i].x), o[1]);
+                o[2] = fmaf(wi, bf16lo(u[i].y), o[2]), o[3] = fmaf(wi, bf16hi(u[i].y), o[3]);
             }
         }
         const bool dead = d >= p.D || (isnan(o[0]) && isnan(o[1]) && isnan(o[2]) && isnan(o[3]));
@@ -197,6 +228,29 @@ __device__ __noinline__ void repair_row(const AttnProblem& p, int64_t k0, int64_
     const float inv = 1.0f / l;
     if (d < p.D)
         *reinterpret_cast<uint2*>(out + d) = make_uint2(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv));
+}
+
+// Rows `again` of the warp, which hold values that are not finite (a lane's own: token t, head h and so on):
+// those are computed again that have such a value among the keys of their `tiles` tiles that they do not
+// see. (A row that sees it is not a number, and computing it again takes as long as all its
+// products.) Keys of the tiles: up to the end of the buffer, past which the tiles hold zeros.
+__device__ __noinline__ void repair_rows(const AttnProblem& p, uint32_t again, int64_t k0, int k_first, int tiles, int64_t t, int h,
+                                         int lo, int hi, float m, float l) {
+    const int lane = threadIdx.x & 31;
+    const bool mine = again >> lane & 1u;
+    const int seen_lo = __reduce_max_sync(0xffffffffu, mine ? lo : 0), seen_hi = __reduce_min_sync(0xffffffffu, mine ? hi : INT_MAX);
+    const int hk = __shfl_sync(0xffffffffu, h / (p.Hq / p.Hkv), __ffs(again) - 1);
+    const int2 bad = bad_keys(p, k0, hk, k_first, (int)min64(k_first + (int64_t)tiles * kTile, p.Tk - k0), seen_lo, seen_hi);
+    again = __ballot_sync(0xffffffffu, mine && (bad.x < lo || bad.y > hi));
+    if (again == 0) return;
+    if (lane == 0) bulk_wait_all();  // the rows' first versions are stored before the second
+    __syncwarp();
+    while (again) {
+        const int src = __ffs(again) - 1;
+        again &= again - 1;
+        repair_row(p, k0, __shfl_sync(0xffffffffu, t, src), __shfl_sync(0xffffffffu, h, src), __shfl_sync(0xffffffffu, lo, src),
+                   __shfl_sync(0xffffffffu, hi, src), __shfl_sync(0xffffffffu, m, src), __shfl_sync(0xffffffffu, l, src));
+    }
 }
 
 // One work item as the scheduler warp hands it out.
@@ -525,15 +579,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 ok = meet();
                 if (t != 0 || !ok) again = 0;
             }
-            while (again) {
-                const int src = __ffs(again) - 1;
-                again &= again - 1;
-                const int rlo = __shfl_sync(0xffffffffu, lo, src), rhi = __shfl_sync(0xffffffffu, hi, src);
-                const float rm = __shfl_sync(0xffffffffu, m, src), rl = __shfl_sync(0xffffffffu, l, src);
-                if (lane == 0) bulk_wait_all();  // the row's first version is stored before the second
-                __syncwarp();
-                repair_row(p, s.k0, __shfl_sync(0xffffffffu, tok, src), __shfl_sync(0xffffffffu, head, src), rlo, rhi, rm, rl);
-            }
+            if (again) repair_rows(p, again, s.k0, k_first, kDeal ? n + n2 : n, tok, head, lo, hi, m, l);
         }
         if (lane == 0) bulk_wait_all();  // stores complete before the CTA leaves
     } else {

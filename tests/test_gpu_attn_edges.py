@@ -242,3 +242,67 @@ def test_prompt_dealt_keys_of_ragged_ends():
         gb.attn_prompt(cfg, q, k, v, cu_q, cu_k, out, ws)
         assert ((out.double() - want).abs() <= bound).all()
     assert gb.moe_device_status(ws) == gb.OK
+
+
+def elapsed(call, n=3):
+    a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+    call()
+    best = float("inf")
+    for _ in range(n):
+        torch.cuda.synchronize()
+        a.record()
+        call()
+        b.record()
+        torch.cuda.synchronize()
+        best = min(best, a.elapsed_time(b))
+    return best
+
+
+@pytest.mark.parametrize("H,n", [(16, 3000), (2, 2500)])
+def test_prompt_rows_that_see_a_nan_value_cost_no_more(H, n):
+    """A value that is not a number at the first token: every row sees it and its column is NaN, in about the time of
+    any other call."""
+    rng = np.random.default_rng(n)
+    D = 128
+    q, k, v = (normal(rng, (n, H, D), "bf16") for _ in range(3))
+    cfg = gb.attn_config(H, H, D)
+    ws = torch.zeros(gb.attn_workspace_size(cfg, n, 1), dtype=torch.uint8, device="cuda")
+    cu, out = prefix([n]), torch.empty_like(q)
+    call = lambda: gb.attn_prompt(cfg, q, k, v, cu, cu, out, ws)  # noqa: E731
+    plain = elapsed(call)
+    want, size = attention64(q, k, v, [n], [n], cfg.scale)
+    v[0, 1, 70] = float("nan")
+    took = elapsed(call)
+    hit = torch.zeros_like(want, dtype=torch.bool)
+    hit[:, 1, 70] = True
+    assert torch.equal(torch.isnan(out), hit)
+    assert ((out.double() - want).abs() <= bf16_bound(want, size))[~hit].all()
+    assert gb.moe_device_status(ws) == gb.OK
+    assert took <= 2 * plain + 0.1, (took, plain)
+
+
+@pytest.mark.parametrize("window", [0, 150])
+@pytest.mark.parametrize("Hq,Hkv", [(2, 2), (200, 100), (168, 24)])
+def test_prompt_rows_beside_values_they_do_not_see(Hq, Hkv, window):
+    """Values that are no numbers at a token in the middle, one of them infinite, and in the rows behind the last
+    sequence: rows that see them have them in their columns, all others are right (heads that are no power of two in a
+    group, keys dealt to two halves, tiles of many items)."""
+    rng = np.random.default_rng(window + Hq)
+    D, nq = 64, [140, 260, 33]
+    T = sum(nq)
+    q, k, v = (normal(rng, (T + 40, h, D), "bf16") for h in (Hq, Hkv, Hkv))
+    cfg = gb.attn_config(Hq, Hkv, D, window=window)
+    ws = torch.zeros(gb.attn_workspace_size(cfg, T, 3), dtype=torch.uint8, device="cuda")
+    want, size = attention64(q[:T], k[:T], v[:T], nq, nq, cfg.scale, window=window)
+    v[T:] = float("nan")
+    v[140 + 77, 1, 5] = float("nan")
+    v[140 + 90, 0, 9] = float("inf")
+    out = torch.empty_like(q)
+    gb.attn_prompt(cfg, q, k, v, prefix(nq), prefix(nq), out, ws)
+    hit, G = torch.zeros_like(want, dtype=torch.bool), Hq // Hkv
+    end = lambda at: min(400, at + window if window else 400)  # noqa: E731
+    hit[217:end(217), G:2 * G, 5] = True
+    hit[230:end(230), :G, 9] = True
+    assert torch.equal(~torch.isfinite(out[:T]), hit)
+    assert ((out[:T].double() - want).abs() <= bf16_bound(want, size))[~hit].all()
+    assert gb.moe_device_status(ws) == gb.OK
