@@ -306,3 +306,22 @@ def test_prompt_rows_beside_values_they_do_not_see(Hq, Hkv, window):
     assert torch.equal(~torch.isfinite(out[:T]), hit)
     assert ((out[:T].double() - want).abs() <= bf16_bound(want, size))[~hit].all()
     assert gb.moe_device_status(ws) == gb.OK
+
+
+@pytest.mark.parametrize("H,n", [(16, 3000), (2, 2500)])
+def test_prompt_values_behind_the_end_cost_nothing(H, n):
+    """What lies behind the last sequence in its buffer is never looked at twice, whatever it holds."""
+    rng = np.random.default_rng(n)
+    D = 128
+    q, k, v = (normal(rng, (n + 100, H, D), "bf16") for _ in range(3))
+    cfg = gb.attn_config(H, H, D)
+    ws = torch.zeros(gb.attn_workspace_size(cfg, n, 1), dtype=torch.uint8, device="cuda")
+    cu, out = prefix([n]), torch.empty_like(q)
+    call = lambda: gb.attn_prompt(cfg, q, k, v, cu, cu, out, ws)  # noqa: E731
+    plain = elapsed(call)
+    want = out[:n].clone()
+    v[n:], k[n:] = float("nan"), float("inf")
+    took = elapsed(call)
+    assert torch.equal(out[:n], want)
+    assert gb.moe_device_status(ws) == gb.OK
+    assert took <= 2 * plain + 0.1, (took, plain)
