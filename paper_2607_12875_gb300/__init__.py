@@ -123,14 +123,15 @@ _current = None
 
 def _stream(stream):
     """The caller's stream, or torch's current one on the current device (as an address: looking it up through
-    torch.cuda.current_stream() builds a Stream object, 3 us against 0.2)."""
+    torch.cuda.current_stream() builds a Stream object, 3 us against 0.2; that is the way where torch does not have the
+    short one, which it does not document)."""
     global _current
     if stream is not None:
         return stream
     if _current is None:
         import torch
-        device, raw = torch.cuda.current_device, torch._C._cuda_getCurrentRawStream
-        _current = lambda: raw(device())  # noqa: E731
+        device, raw = torch.cuda.current_device, getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        _current = (lambda: raw(device())) if raw else (lambda: torch.cuda.current_stream().cuda_stream)
     return _current()
 
 

@@ -18,6 +18,9 @@ class NoLibrary:
         return call
 
 
+STREAM = gb._stream
+
+
 @pytest.fixture(autouse=True)
 def no_library(monkeypatch):
     monkeypatch.setattr(gb, "lib", NoLibrary)
@@ -113,3 +116,13 @@ def test_caches_that_do_not_fit_are_refused(bad):
 def test_rows_of_strided_heads_stay_refused():
     with pytest.raises(ValueError):
         attn._rows(rows(3, 2, 128)[:, :, ::2], 3, 2, 64)
+
+
+def test_current_stream_without_the_undocumented_lookup(monkeypatch):
+    class Current:
+        cuda_stream = 1234
+    monkeypatch.setattr(gb, "_current", None)
+    monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream", raising=False)
+    monkeypatch.setattr(torch.cuda, "current_stream", Current)
+    assert STREAM(None) == 1234
+    assert STREAM(77) == 77 and STREAM(0) == 0
