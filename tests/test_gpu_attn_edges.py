@@ -201,6 +201,28 @@ def test_cached_scores_of_minus_infinity(act, kind, m):
     assert torch.isneginf(lse[0, 1]) and torch.isfinite(lse[0, 0]) and torch.isneginf(lse[1]).all()
 
 
+@pytest.mark.parametrize("act,kind,D", [("bf16", "e4m3", 64), ("bf16", "e4m3", 96), ("bf16", "e4m3", 128), ("bf16", "act", 64),
+                                        ("bf16", "act", 128), ("f32", "act", 64), ("f32", "e4m3", 80)])
+@pytest.mark.parametrize("Hq,Hkv,n,lens", [(8, 1, [1, 1], [9000, 70]), (8, 2, [5, 1], [7001, 2500])])
+def test_cached_long_contexts_element_by_element(act, kind, D, Hq, Hkv, n, lens):
+    """The average of thousands of values is small beside the largest of them: each element is held to the sum that
+    it is made of. Weights of 8 (bf16 cache) or 11 bits (e4m3), results of 8, fp32 scores and sums."""
+    rng = np.random.default_rng(D + Hq)
+    c = Cache(rng, act, kind, Hkv, D, 32, lens)
+    q = normal(rng, (sum(n), Hq, D), act, 0.5)
+    cfg = gb.attn_config(Hq, Hkv, D, act=act, cache=kind, page=32)
+    ws = torch.zeros(gb.attn_workspace_size(cfg, sum(n), len(n)), dtype=torch.uint8, device="cuda")
+    out = torch.zeros_like(q)
+    keep = (prefix(n), i32(lens), c.dev_table)
+    gb.attn_cached(cfg, gb.attn_batch(*keep), q, c.bundle, out, ws)
+    k, v = (torch.from_numpy(np.concatenate([c.rows(w, b, m)[0] for b, m in enumerate(lens)])).cuda() for w in "kv")
+    want, size = attention64(q, k, v, n, lens, cfg.scale)
+    weight, result = (2.0 ** -24, 2.0 ** -24) if act == "f32" else (2.0 ** -8 if kind == "act" else 2.0 ** -11, 2.0 ** -8)
+    bound = 1.05 * (result * want.abs() + weight * size) + 2e-5 * size
+    assert ((out.double() - want).abs() <= bound).all()
+    assert gb.moe_device_status(ws) == gb.OK
+
+
 # ------------------------------------------------------------------- prompt
 
 
@@ -325,3 +347,16 @@ def test_prompt_values_behind_the_end_cost_nothing(H, n):
     assert torch.equal(out[:n], want)
     assert gb.moe_device_status(ws) == gb.OK
     assert took <= 2 * plain + 0.1, (took, plain)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,n,window", [(8, 2, 128, [3001, 513], 0), (4, 4, 64, [2600], 700), (6, 2, 96, [1500, 900], 0)])
+def test_prompt_long_rows_element_by_element(Hq, Hkv, D, n, window):
+    rng = np.random.default_rng(D)
+    q, k, v = (normal(rng, (sum(n), h, D), "bf16") for h in (Hq, Hkv, Hkv))
+    cfg = gb.attn_config(Hq, Hkv, D, window=window)
+    ws = torch.zeros(gb.attn_workspace_size(cfg, sum(n), len(n)), dtype=torch.uint8, device="cuda")
+    out, cu = torch.zeros_like(q), prefix(n)
+    gb.attn_prompt(cfg, q, k, v, cu, cu, out, ws)
+    want, size = attention64(q, k, v, n, n, cfg.scale, window=window)
+    assert ((out.double() - want).abs() <= bf16_bound(want, size)).all()
+    assert gb.moe_device_status(ws) == gb.OK
