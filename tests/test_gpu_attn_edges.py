@@ -360,3 +360,43 @@ def test_prompt_long_rows_element_by_element(Hq, Hkv, D, n, window):
     want, size = attention64(q, k, v, n, n, cfg.scale, window=window)
     assert ((out.double() - want).abs() <= bf16_bound(want, size)).all()
     assert gb.moe_device_status(ws) == gb.OK
+
+
+# ------------------------------------------------------------------- strides
+
+
+LAYOUTS = {
+    "heads first": lambda t: t.transpose(0, 1).contiguous().transpose(0, 1),
+    "tokens apart by no multiple of a head": lambda t: torch.cat([t.flatten(1), t.new_zeros((t.shape[0], 24))], 1)[:, :t[0].numel()].view(t.shape),
+    "heads wide apart": lambda t: torch.cat([t, t.new_zeros(t.shape)], 1).view(t.shape[0], 2, t.shape[1], t.shape[2])[:, 0],
+}
+
+
+@pytest.mark.parametrize("layout", sorted(LAYOUTS))
+@pytest.mark.parametrize("act", ["f32", "bf16"])
+def test_layouts(act, layout):
+    """Every operator on rows laid out otherwise gives what it gives on contiguous ones, bit for bit, and leaves its inputs alone."""
+    rng = np.random.default_rng(12)
+    Hq, Hkv, D, n = 6, 2, 64, [130, 77, 1]
+    T, lay = sum(n), LAYOUTS[layout]
+    q, k, v = normal(rng, (T, Hq, D), act), normal(rng, (T, Hkv, D), act), normal(rng, (T, Hkv, D), act)
+    cfg = gb.attn_config(Hq, Hkv, D, act=act, rotary_dim=32, cache="e4m3", page=16)
+    ws = torch.zeros(gb.attn_workspace_size(cfg, T, 3), dtype=torch.uint8, device="cuda")
+    table, pos, cu = gb.attn_rope_table(32), i32(rng.integers(0, 999, T)), prefix(n)
+    results = []
+    for put in (lambda t: t.clone(), lay):
+        a, b, c = put(q), put(k), put(v)
+        outs = [put(torch.zeros_like(t)) for t in (q, k, q, k, q, q)]
+        cache = Cache(np.random.default_rng(5), act, "e4m3", Hkv, D, 16, n)
+        keep = (cu, i32(n), cache.dev_table)
+        batch = gb.attn_batch(*keep)
+        assert all(torch.equal(x, y) for x, y in zip((a, b, c), (q, k, v)))
+        gb.attn_rope(cfg, a, b, pos, table, outs[0], outs[1])
+        gb.attn_append(cfg, batch, b, c, table, cache.bundle, q=a, q_out=outs[2], k_out=outs[3])
+        gb.attn_prompt(cfg, outs[2], outs[3], c, cu, cu, outs[4], ws)
+        gb.attn_cached(cfg, batch, outs[2], cache.bundle, outs[5], ws)
+        assert all(torch.equal(x, y) for x, y in zip((a, b, c), (q, k, v)))
+        results.append([t.clone(memory_format=torch.contiguous_format) for t in outs] + [cache.k, cache.v, cache.ks, cache.vs])
+    for x, y in zip(*results):
+        assert torch.equal(x, y)
+    assert gb.moe_device_status(ws) == gb.OK
