@@ -28,7 +28,11 @@
  * (and -inf as its log sum). Keys and values that no query sees, other
  * sequences' rows and unwritten cache slots may hold anything, NaN included.
  *   out = sum_j softmax_j(scale * q.k_j) v_j; lse = ln sum_j exp(scale * q.k_j)
- * fp32 sums and softmax statistics; out rounded once to act_dtype.
+ * fp32 sums and softmax statistics; out rounded once to act_dtype. Where the
+ * tensor cores do it (see attn_prompt, attn_cached) the softmax weights are
+ * rounded to 16 bits before the second product, their sum is not.
+ * A value that is no number makes its column so for the queries that see it,
+ * whatever its weight; a query that sees keys, all with scores of -inf, is 0 / 0.
  */
 #ifndef GBATTN_H
 #define GBATTN_H
@@ -160,9 +164,11 @@ int attn_append(const gbattn_config* cfg, int32_t T, const gbattn_batch* batch, 
  * Attention over packed sequences: q, out [Tq, heads_q, D], k, v [Tk,
  * heads_kv, D], cu_q and cu_k [B+1] (equal for whole prompts; a sequence with
  * more keys than queries has its queries at the end). lse [Tq, heads_q] fp32
- * or NULL. bf16 with D up to 128 runs on the tensor cores (probabilities
- * rounded to bf16 before the second product), else on CUDA cores. out may not
- * overlap the inputs.
+ * or NULL. bf16 with D up to 128 runs on the tensor cores (weights rounded to
+ * bf16: off by 2^-8 of themselves), else on CUDA cores. out may not overlap
+ * the inputs. (A value that is no number at a key that some queries of a tile
+ * of up to 256 tokens see and others do not: those others take 0.15 us for each
+ * of their keys, one after the other.)
  */
 int attn_prompt(const gbattn_config* cfg, int32_t Tq, int32_t Tk, int32_t B, const gbattn_rows* q,
                 const gbattn_rows* k, const gbattn_rows* v, const int32_t* cu_q, const int32_t* cu_k,
@@ -174,7 +180,11 @@ int attn_prompt(const gbattn_config* cfg, int32_t Tq, int32_t Tk, int32_t B, con
  * NULL. Meant for few query tokens per sequence (decoding, draft tokens); any
  * number works. Long contexts are split over CTAs and joined by a second
  * launch, deterministically. bf16 with D 64, 96 or 128 runs on the tensor
- * cores, else on CUDA cores. A token whose page is outside the pool is masked.
+ * cores, else on CUDA cores. There the weights are rounded to bf16 (bf16 cache:
+ * off by 2^-8 of themselves) or fp16 (e4m3: by 2^-11, or by 2^-34 of the row's
+ * largest), and with an e4m3 cache the queries to fp16 relative to the largest
+ * of their row (exact down to 2^-14 of it). A token whose page is outside the
+ * pool is masked.
  * T * G and max_pages * page up to 2^30, else GBMOE_EUNSUPPORTED.
  */
 int attn_cached(const gbattn_config* cfg, int32_t T, const gbattn_batch* batch, const gbattn_rows* q,

@@ -6,12 +6,14 @@
 // position, wrapped, is the fraction of a turn to 2^-64 * position, whatever
 // the position; its top 32 bits go to sincospif (an error of 2^-25 half turns,
 // below fp32's own on the rotated values). A thread keeps the angles of its eight
-// pairs of a token in registers and takes them through several heads, so
-// neither kernel has shared memory or a barrier between its loads and its stores.
+// pairs of a token in registers and takes them through several heads. The rotation has
+// no shared memory and no barrier; an append looks its page up through shared memory first, and
+// one to e4m3 exchanges the maxima of a page and head through it between its loads and its rounding.
 //
-// Both kernels are bound by HBM: each element is read once and written once (8192 tokens, 32
-// query and 8 kv heads of 128, bf16: rotation 33 us, 5.1 TB/s; append of e4m3 with the queries 47 us,
-// 3.9 TB/s, held back by one block of 512 threads on an SM between its loads and its rounding).
+// Each element is read once and written once, but for e4m3 pages of more new tokens than a block takes
+// at a time, whose keys and values are read twice. 8192 tokens, 32 query and 8 kv heads of 128, bf16: rotation
+// 33 us, 5.1 TB/s, bound by HBM (768 blocks, 1.7 times what is resident); append of e4m3 with the queries 46 us,
+// 4.0 TB/s (pages of 128, read twice: 8 % more), held back by one block of 512 threads on an SM between its loads and its rounding.
 
 #include "attn_plan.cuh"
 

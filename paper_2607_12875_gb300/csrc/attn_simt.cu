@@ -6,8 +6,9 @@
 // against 20 for 333 tokens of 16 heads of 64) or 16 rows, token and head of the
 // group (cache), walks its keys in tiles of 32 through shared memory and keeps
 // the weighted sum of values in registers. Bound by shared-memory wavefronts for
-// prompts (89 % of their rate; 1200 tokens of 16 heads of 64 in 0.21 ms, 14
-// TFLOP/s), by the latency of its loads for single tokens.
+// long prompts (1200 tokens of 16 heads of 64 in 0.2 ms, 15 TFLOP/s: 70 % of their
+// rate, ends of the grid included), by too few warps for short ones (333 tokens: 208 blocks, 8 % of an SM's
+// warps, 21 % of that rate, 19 us), by the latency of its loads for single tokens.
 #include <atomic>
 #include <type_traits>
 

@@ -11,7 +11,7 @@
 // shared memory.
 //
 // Bound by HBM for long keys (32 sequences, 1.07 GB of e4m3 pages of 8 kv heads of
-// 128: 177 us, 6.0 TB/s), by its instructions with tiles of 16 rows (half of that
+// 128: 176 us, 6.1 TB/s), by its instructions with tiles of 16 rows (half of that
 // rate), by latency for few keys: 4000 in 12 us, of which three blocks' loop is
 // 2.5, the search for the share 1.5, page ids and scales 1.3, the queries 0.8, the
 // warps' join 1 and the join kernel 3.
@@ -29,10 +29,16 @@
 // scores in fp32; the power of two of a page of values is added to its scores
 // instead (base 2), with a maximum of its own: the weights that enter the second
 // product are relative to the largest weight times scale, so pages of tiny
-// values keep their accuracy. The queries enter in fp16, each row divided by a
-// power of two that brings its largest value into [1, 2): exact for values down
-// to 2^-14 of it, an error of 2^-25 of it below. The weights are rounded to fp16
-// (e4m3) or bf16; sums and statistics are fp32.
+// values keep their accuracy. They are 2^kRoom at that weight, which uses fp16 up
+// to its largest power: a weight is off by 2^-11 of itself or 2^-34 of the
+// largest, so many keys of little weight beside one of much weight still count.
+// The queries enter in fp16, each row divided by a power of two that brings its
+// largest value into [1, 2): exact for values down to 2^-14 of it, an error of
+// 2^-25 of it below.
+//
+// The weights are rounded to the 16-bit type of the MMA's other operand: fp16
+// (e4m3) does not show beside the result's own rounding to bf16 (1.7e-3 of it on
+// average), bf16 does (2.1e-3). Sums and statistics are fp32.
 
 #include "attn_plan.cuh"
 #include "tc_ptx.cuh"
