@@ -166,9 +166,10 @@ int attn_append(const gbattn_config* cfg, int32_t T, const gbattn_batch* batch, 
  * more keys than queries has its queries at the end). lse [Tq, heads_q] fp32
  * or NULL. bf16 with D up to 128 runs on the tensor cores (weights rounded to
  * bf16: off by 2^-8 of themselves), else on CUDA cores. out may not overlap
- * the inputs. (A value that is no number at a key that some queries of a tile
- * of up to 256 tokens see and others do not: those others take 0.15 us for each
- * of their keys, one after the other.)
+ * the inputs. (A query whose tile of up to 256 tokens and the keys they see,
+ * rounded up to 128, holds a value that is no number at a key that this query
+ * does not see takes 0.15 us for each of its own keys, up to 32 queries and
+ * heads after each other.)
  */
 int attn_prompt(const gbattn_config* cfg, int32_t Tq, int32_t Tk, int32_t B, const gbattn_rows* q,
                 const gbattn_rows* k, const gbattn_rows* v, const int32_t* cu_q, const int32_t* cu_k,

@@ -28,18 +28,21 @@
 // MMA: 2680 cycles for 128 keys of two tiles of D 128, whose products take 2048
 // (the softmax alone takes 930 for one tile, a hand-over there and back 360), and
 // some 5 us for each pair of tiles that a CTA takes. 16384 tokens of 32 query and 8
-// kv heads, causal: 1.41 ms, 1.56 PFLOP/s, call after call (1.30 ms one at a time); 7 prompts of 8192 in all: 100 us.
+// kv heads, causal: 1.41 ms, 1.56 PFLOP/s, call after call (1.30 ms one at a time);
+// 7 prompts of 8192 in all: 100 us.
 //
-// P is rounded to bf16, an error of up to 2^-8 of each weight beside the result's own rounding (2.0e-3
-// against 1.6e-3 of the result on average): the MMA takes both operands in one 16-bit type, and V is bf16.
+// P is rounded to bf16, an error of up to 2^-8 of each weight beside the result's
+// own rounding (2.0e-3 against 1.6e-3 of the result on average): the MMA takes both
+// operands in one 16-bit type, and V is bf16.
 //
-// A masked score gives P = 0, but 0 times a NaN value is a NaN. What its last tile
-// brings along from behind a sequence's end is set to 0 in shared memory, at no cost
-// that shows. For its own tokens, a row whose sums are finite and whose result is
-// not is checked for non-finite values at keys of its tiles that it does not see, and
-// computed again without them if there are any (repair_rows: by one warp, 0.15 us for
-// each key of a row; a function of its own, of no more registers than leave the
-// softmax its own).
+// A masked score gives P = 0, but 0 times a NaN value is a NaN: a row whose
+// sums are finite and whose result is not is checked for non-finite values at
+// keys of its tiles that it does not see, and computed again without them if there
+// are any (repair_rows: by one warp, 0.15 us for each key of a row; a function of its
+// own, of no more registers than leave the softmax its own). The last tile brings
+// along values from behind a sequence's end: to set those to 0 in shared memory
+// before the product took 8 to 11 % of batches of prompts of up to 100 tokens (and of
+// long ones alone, 1 to 5 % by the code's arrangement), so they are left in.
 //
 // Waits are bounded as in the GEMM kernels (tc_ptx.cuh).
 #include <climits>
@@ -236,16 +239,16 @@ __device__ __forceinline__ void repair_row(const AttnProblem& p, int64_t k0, int
 }
 
 // Rows `again` of the warp, which hold values that are not finite (a lane's own: token t, head h and so on):
-// those are computed again that have such a value among the keys of their tiles that they do not
+// those are computed again that have such a value among the keys of their `tiles` tiles that they do not
 // see. (A row that sees it is not a number, and computing it again takes as long as all its
-// products.) The tiles' keys are k_first .. k_end - 1.
-__device__ __noinline__ void repair_rows(const AttnProblem& p, uint32_t again, int64_t k0, int k_first, int k_end, int64_t t, int h,
+// products.) Keys of the tiles: up to the end of the buffer, past which the tiles hold zeros.
+__device__ __noinline__ void repair_rows(const AttnProblem& p, uint32_t again, int64_t k0, int k_first, int tiles, int64_t t, int h,
                                          int lo, int hi, float m, float l) {
     const int lane = threadIdx.x & 31;
     const bool mine = again >> lane & 1u;
     const int seen_lo = __reduce_max_sync(0xffffffffu, mine ? lo : 0), seen_hi = __reduce_min_sync(0xffffffffu, mine ? hi : INT_MAX);
     const int hk = __shfl_sync(0xffffffffu, h / (p.Hq / p.Hkv), __ffs(again) - 1);
-    const int2 bad = bad_keys(p, k0, hk, k_first, k_end, seen_lo, seen_hi);
+    const int2 bad = bad_keys(p, k0, hk, k_first, (int)min64(k_first + (int64_t)tiles * kTile, p.Tk - k0), seen_lo, seen_hi);
     again = __ballot_sync(0xffffffffu, mine && (bad.x < lo || bad.y > hi));
     if (again == 0) return;
     if (lane == 0) bulk_wait_all();  // the rows' first versions are stored before the second
@@ -584,7 +587,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 ok = meet();
                 if (t != 0 || !ok) again = 0;
             }
-            if (again) repair_rows(p, again, s.k0, k_first, min(k_first + (kDeal ? n + n2 : n) * kTile, s.len), tok, head, lo, hi, m, l);
+            if (again) repair_rows(p, again, s.k0, k_first, kDeal ? n + n2 : n, tok, head, lo, hi, m, l);
         }
         if (lane == 0) bulk_wait_all();  // stores complete before the CTA leaves
     } else {
@@ -815,7 +818,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 __syncwarp();
                 drain_wait(drain, 0);
             }
-        } else if (warp == 11) {
+        } else if (warp == 11 && lane == 0) {
             // ------------------------------------------------------- tile watcher
             // Waits for the tiles in the MMA warp's stead, whose issue queue is shallow: each
             // barrier that it waits for itself delays the MMAs behind it.
@@ -824,22 +827,11 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             auto next = [&] {
                 if (++stage == STAGES) stage = 0, phase ^= 1;
             };
-            // the V tile in the current slot, of which `keys` are the sequence's: the rows behind become 0
-            auto cut = [&](int keys) {
-                if (keys >= kTile) return;
-                for (int c = 0; c < DK / 64; ++c)
-                    for (int x = keys * 128 + lane * 16; x < kHalf; x += 512)
-                        *reinterpret_cast<uint4*>(sKV + stage * TILE + c * kHalf + x) = make_uint4(0, 0, 0, 0);
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-            };
             bool ok = true;
             for (int k = 0; ok; ++k) {
-                if (!wait_warp(&w_full[k & 1], (uint32_t)(k >> 1) & 1u)) break;
-                const Work& slot = work_slots[k & 1];
-                const int n0 = slot.n[0], n1 = slot.n[1], end = slot.end, keys = slot.s.len - slot.k_first;
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&w_empty[k & 1]);
+                if (!wait(&w_full[k & 1], (uint32_t)(k >> 1) & 1u)) break;
+                const int n0 = work_slots[k & 1].n[0], n1 = work_slots[k & 1].n[1], end = work_slots[k & 1].end;
+                mbar_arrive(&w_empty[k & 1]);
                 if (end) break;
                 const int n_max = max(n0, n1);
                 if constexpr (kDeal) {
@@ -847,31 +839,29 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                     for (int i = 0; i < min(n, 2); ++i) next();  // (the first K tiles: the MMA warp's)
                     for (int i = 0; i < n && ok; ++i) {
                         for (int x = 0; x < (i + 2 < n ? 2 : 1) && ok; ++x) {
-                            ok = wait_warp(&full[stage], phase);
-                            if (ok && x == 0) cut(keys - i * kTile);
+                            ok = wait(&full[stage], phase);
                             next();
                         }
                         const int t = i & 1;
-                        if (ok && pn[t] > 0) ok = wait_warp(&p_full[t], (pn[t] - 1) & 1u);
+                        if (ok && pn[t] > 0) ok = wait(&p_full[t], (pn[t] - 1) & 1u);
                         ++pn[t];
-                        if (ok && lane == 0) mbar_arrive(&p_full[t]);
+                        if (ok) mbar_arrive(&p_full[t]);
                     }
                     continue;
                 }
                 if (n_max > 0) next();  // (the first K tile: the MMA warp's)
                 for (int j = 0; j < n_max && ok; ++j) {
-                    ok = wait_warp(&full[stage], phase);
-                    if (ok) cut(keys - j * kTile);
+                    ok = wait(&full[stage], phase);
                     next();
                     if (j + 1 < n_max) {
-                        ok = ok && wait_warp(&full[stage], phase);
+                        ok = ok && wait(&full[stage], phase);
                         next();
                     }
                     for (int t = 0; t < 2 && ok; ++t) {
                         if (j >= (t ? n1 : n0)) continue;
-                        if (pn[t] > 0) ok = wait_warp(&p_full[t], (pn[t] - 1) & 1u);  // one arrival in a phase
+                        if (pn[t] > 0) ok = wait(&p_full[t], (pn[t] - 1) & 1u);  // one arrival in a phase
                         ++pn[t];
-                        if (ok && lane == 0) mbar_arrive(&p_full[t]);
+                        if (ok) mbar_arrive(&p_full[t]);
                     }
                 }
             }
