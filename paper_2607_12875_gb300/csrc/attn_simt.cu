@@ -7,8 +7,9 @@
 // group (cache), walks its keys in tiles of 32 through shared memory and keeps
 // the weighted sum of values in registers. Bound by shared-memory wavefronts for
 // long prompts (1200 tokens of 16 heads of 64 in 0.2 ms, 15 TFLOP/s: 70 % of their
-// rate, ends of the grid included), by too few warps for short ones (333 tokens: 208 blocks, 8 % of an SM's
-// warps, 21 % of that rate, 19 us), by the latency of its loads for single tokens.
+// rate, ends of the grid included), by too few warps for short ones (333 tokens:
+// 208 blocks, 8 % of an SM's warps, 21 % of that rate, 19 us), by the latency of its
+// loads for single tokens.
 #include <atomic>
 #include <type_traits>
 
@@ -350,8 +351,8 @@ cudaError_t simt_source(const AttnProblem& p, cudaStream_t stream) {
 //
 // Rows of tiles that were cut. The parts' sums, each relative to 2^(its own third
 // statistic), are brought to the largest of those and added, the softmax sums
-// likewise relative to the first statistic: out = sum / l. (The fourth: 0 where the row sees
-// no key of the part.) Every block counts the
+// likewise relative to the first statistic: out = sum / l. (The fourth: 0 where the
+// row sees no key of the part.) Every block counts the
 // rows of all cut tiles for itself and takes its share of them, 1 to 8 at a time
 // and then with 8 to 1 warps for a row, which take every so many of its parts: the
 // order is fixed by the lengths. (A block for each share, most of them with
