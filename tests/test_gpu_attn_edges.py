@@ -41,6 +41,32 @@ def bf16_bound(want, size):
     return 1.05 * 2.0 ** -8 * (want.abs() + size) + 2e-5 * size
 
 
+# ------------------------------------------------------------------- rotary
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_rope_angles(layout):
+    """cos and sin themselves (a pair of 1 and 0), near the multiples of a quarter turn, where one of them is small and has the
+    angle's error alone: 2^-27 half turns (and 2^-32 turns cut off), beside two units in the last place (sincospif and
+    the pair's 0 * sin)."""
+    T, R = 200000, 32
+    pos = np.random.default_rng(0).integers(-(1 << 20), 1 << 20, T)
+    cfg = gb.attn_config(1, 1, R, act="f32", rotary_dim=R, rotary_layout=layout)
+    x = torch.zeros((T, 1, R), device="cuda")
+    first = np.arange(R // 2) if layout == "half" else 2 * np.arange(R // 2)
+    x[:, 0, first] = 1.0
+    y = torch.empty_like(x)
+    gb.attn_rope(cfg, x, None, i32(pos), gb.attn_rope_table(R), y, None)
+    turn = np.array([10000.0 ** (-2.0 * i / R) for i in range(R // 2)], dtype=np.longdouble) * pos[:, None].astype(np.longdouble)
+    for got, want in ((wide(y)[:, 0, first], np.cos(turn)), (wide(y)[:, 0, first + (R // 2 if layout == "half" else 1)], np.sin(turn))):
+        small = np.abs(want) < 0.1
+        assert small.sum() > 10000
+        err = np.abs(got - want)
+        # (the table's entries: 2^-64 turns; frequencies in 64 bits: 2^-53 of up to 2^20 radians)
+        assert (err <= np.pi * 2.0 ** -27 + 2 * np.pi * 2.0 ** -32 + 2.0 ** -22 * np.abs(want) + 2.0 ** -31)[small].all(), err[small].max()
+        assert (err <= np.pi * 2.0 ** -27 + 2.0 ** -22).all()
+
+
 # ------------------------------------------------------------------- append
 
 
