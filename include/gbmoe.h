@@ -250,6 +250,23 @@ int gbmoe_gate_route(const gbmoe_config* cfg);
 int moe_rmsnorm(const gbmoe_config* cfg, const void* x, const void* gamma, float eps, void* y, void* stream);
 
 /*
+ * The residual's addition and the norm in one pass, what a decoder layer does
+ * before the MoE Gate and before its attention:
+ *   s = x + residual          rounded to act_dtype (residual NULL: s = x)
+ *   y = moe_rmsnorm(s)        bit for bit
+ * sum_out [T, H] takes s (NULL: not wanted; it may be x or residual). y [T, H] may
+ * be NULL where codes and scales are given: the norm before its rounding to
+ * act_dtype as e4m3 codes [T, H] with one fp32 scale per row and 128 columns [T, H
+ * / 128], the smallest power of two 2^e >= 2^-126 with max |y in the block| <= 448
+ * * 2^e; element = e4m3(code) * scale, rounded to the nearest code, ties to even. A
+ * NaN gives the NaN code and an infinity +-448 (both are left out of the maximum).
+ * Every pointer 16-byte aligned (scales: 4); outputs may not overlap anything else.
+ * eps >= 0 and finite. Uses cfg's T, H and act_dtype only. No workspace.
+ */
+int moe_rmsnorm_add(const gbmoe_config* cfg, const void* x, const void* residual, const void* gamma, float eps,
+                    void* sum_out, void* y, uint8_t* codes, float* scales, void* stream);
+
+/*
  * MoE Gate (Fig. 1 and Fig. 3). For every token t:
  *   l[t,e] = x[t,:] . w_router[e,:] (+ logit_bias[e]), fp32, in a fixed order:
  *     32 partial sums, partial p takes the 8-element chunks p, p+32, ... in

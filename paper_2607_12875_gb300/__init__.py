@@ -34,7 +34,7 @@ KERNELS = {**ROUTES, "fm": 16, "joined": 17}  # what ffn_kernel reports
 EXPORTS = ("gbmoe_status_string", "gbmoe_check_config", "gbmoe_workspace_size", "gbmoe_ffn_route",
            "gbmoe_ffn_kernel", "gbmoe_gate_route", "moe_route", "moe_permute",
            "moe_grouped_ffn", "moe_shared_ffn", "moe_combine", "moe_forward", "moe_forward_hostio",
-           "moe_device_status", "moe_permute_noalloc", "gbmoe_last_cuda_error", "moe_rmsnorm")
+           "moe_device_status", "moe_permute_noalloc", "gbmoe_last_cuda_error", "moe_rmsnorm", "moe_rmsnorm_add")
 
 
 class GbmoeError(RuntimeError):
@@ -86,6 +86,7 @@ def lib() -> ctypes.CDLL:
         L.gbmoe_gate_route.argtypes = [cfgp]
         L.moe_route.argtypes = [cfgp, vp, vp, fp, fp, vp, vp, vp, sz, vp]
         L.moe_rmsnorm.argtypes = [cfgp, vp, vp, ctypes.c_float, vp, vp]
+        L.moe_rmsnorm_add.argtypes = [cfgp, vp, vp, vp, ctypes.c_float, vp, vp, vp, vp, vp]
         L.moe_permute.argtypes = [cfgp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.moe_grouped_ffn.argtypes = [cfgp, vp, vp, vp, vp, wp, vp, vp, sz, vp]
         L.moe_shared_ffn.argtypes = [cfgp, vp, wp, vp, vp, sz, vp]
@@ -95,6 +96,7 @@ def lib() -> ctypes.CDLL:
         L.moe_device_status.argtypes = [vp, vp, i32p]
         L.moe_permute_noalloc.argtypes = [cfgp, vp, vp, vp, vp, vp, vp]
         attn._bind(L)
+        latent._bind(L)
         _lib = L
     return _lib
 
@@ -183,6 +185,16 @@ def moe_rmsnorm(cfg, x, gamma, eps, y, stream=None):
            "moe_rmsnorm")
 
 
+def moe_rmsnorm_add(cfg, x, residual, gamma, eps, sum_out, y, codes=None, scales=None, stream=None):
+    """residual and sum_out may be None (the norm of x alone; no sum wanted), y too where codes and scales are given."""
+    n = cfg.T * cfg.H
+    for t, least in ((x, n), (residual, n), (gamma, cfg.H), (sum_out, n), (y, n), (codes, n), (scales, n // 128)):
+        if t is not None and (t.numel() < least or not t.is_contiguous()):
+            raise ValueError(f"{t.numel()} elements, or not contiguous, where the call takes {least}")
+    _check(lib().moe_rmsnorm_add(ctypes.byref(cfg), _ptr(x), _ptr(residual), _ptr(gamma), float(eps), _ptr(sum_out), _ptr(y),
+                                 _ptr(codes), _ptr(scales), _stream(stream)), "moe_rmsnorm_add")
+
+
 def moe_route(cfg, x, w_router, logit_bias, select_bias, topk_ids, topk_w, ws, stream=None):
     _check(lib().moe_route(ctypes.byref(cfg), _ptr(x), _ptr(w_router), _ptr(logit_bias), _ptr(select_bias),
                            _ptr(topk_ids), _ptr(topk_w), _ptr(ws), ws.numel() * ws.element_size(),
@@ -242,3 +254,6 @@ def moe_permute_noalloc(cfg, topk_ids, counts, offsets, sorted_pair, pair_pos, s
 from . import attn  # noqa: E402
 from .attn import (AttnBatch, AttnCache, AttnConfig, AttnRows, attn_append, attn_batch, attn_cache, attn_cached,  # noqa: E402,F401
                    attn_check_config, attn_config, attn_prompt, attn_rope, attn_rope_table, attn_workspace_size)
+from . import latent  # noqa: E402
+from .latent import (LatentCache, LatentConfig, latent_append, latent_cache, latent_cached, latent_check_config,  # noqa: E402,F401
+                     latent_config, latent_prompt, latent_workspace_size)

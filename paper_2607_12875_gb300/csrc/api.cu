@@ -478,6 +478,39 @@ int moe_rmsnorm(const gbmoe_config* cfg, const void* x, const void* gamma, float
                                       static_cast<cudaStream_t>(stream)));
 }
 
+int moe_rmsnorm_add(const gbmoe_config* cfg, const void* x, const void* residual, const void* gamma, float eps, void* sum_out,
+                    void* y, uint8_t* codes, float* scales, void* stream) {
+    int s = check_cfg(cfg);
+    if (s) return s;
+    if (!(eps >= 0.0f) || !std::isfinite(eps)) return GBMOE_EINVAL;
+    if ((codes == nullptr) != (scales == nullptr) || (!y && !codes)) return GBMOE_EINVAL;
+    if (cfg->T == 0) return GBMOE_OK;
+    if (!x || !gamma || !aligned(scales, 4)) return GBMOE_EINVAL;
+    for (const void* p : {x, residual, gamma, static_cast<const void*>(sum_out), static_cast<const void*>(y),
+                          static_cast<const void*>(codes)})
+        if (!aligned(p, 16)) return GBMOE_EINVAL;
+    // outputs apart from everything else (the sum may take the place of one of its terms)
+    const size_t n = (size_t)cfg->T * cfg->H, rows = n * act_bytes(cfg->act_dtype);
+    struct Span {
+        const void* p;
+        size_t bytes;
+    };
+    const Span in[] = {{x, rows}, {residual, rows}, {gamma, (size_t)cfg->H * act_bytes(cfg->act_dtype)}};
+    const Span out[] = {{sum_out, rows}, {y, rows}, {codes, n}, {scales, n / 128 * 4}};
+    auto meet = [](const Span& a, const Span& b) {
+        const char *ap = static_cast<const char*>(a.p), *bp = static_cast<const char*>(b.p);
+        return ap && bp && ap < bp + b.bytes && bp < ap + a.bytes;
+    };
+    for (int i = 0; i < 4; ++i) {
+        for (int j = 0; j < 3; ++j)
+            if (meet(out[i], in[j]) && !(i == 0 && j < 2 && out[i].p == in[j].p)) return GBMOE_EINVAL;
+        for (int j = 0; j < i; ++j)
+            if (meet(out[i], out[j])) return GBMOE_EINVAL;
+    }
+    return cuda_status(launch_rmsnorm_add(x, residual, gamma, eps, cfg->T, cfg->H, cfg->act_dtype, sum_out, y, codes, scales,
+                                          static_cast<cudaStream_t>(stream)));
+}
+
 int moe_route(const gbmoe_config* cfg, const void* x, const void* w_router, const float* logit_bias,
               const float* select_bias, int32_t* topk_ids, float* topk_w, void* ws, size_t ws_bytes,
               void* stream) {

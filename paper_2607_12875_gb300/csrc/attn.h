@@ -85,10 +85,10 @@ constexpr int kMaxShares = 608;  // four CTAs on each of 152 SMs
 
 // Deals out the work of cached attention in tiles of `rows` rows to `per_sm` CTAs on an
 // SM, or as many as there can be shares of min_blocks (more than tile_cost).
-inline void set_shares(AttnProblem& p, int rows, int per_sm, int sms, int min_blocks, int tile_cost) {
+inline void set_shares(AttnProblem& p, int rows, int per_sm, int sms, int min_blocks, int tile_cost, int block_keys = kBlockKeys) {
     p.tile_rows = rows, p.min_blocks = min_blocks, p.tile_cost = tile_cost;
     const int64_t tiles = (int64_t)p.T * p.R / rows + p.B;
-    const int64_t blocks = tiles * p.Hkv * (((int64_t)p.max_pages * p.page + kBlockKeys - 1) / kBlockKeys + 1 + p.tile_cost);
+    const int64_t blocks = tiles * p.Hkv * (((int64_t)p.max_pages * p.page + block_keys - 1) / block_keys + 1 + p.tile_cost);
     const int64_t most = (blocks + p.min_blocks - 1) / p.min_blocks;
     const int64_t cap = (int64_t)per_sm * sms < kMaxShares ? (int64_t)per_sm * sms : kMaxShares;
     p.shares = (int)(most < cap ? most : cap);

@@ -61,10 +61,11 @@ __device__ __forceinline__ int64_t row_tiles(const AttnProblem& p, const Seq& s,
     return ((int64_t)s.nq * p.R + rows - 1) / rows;
 }
 
-// blocks of kBlockKeys keys of a sequence's tiles (at least one, so that rows
+// blocks of kBlock keys of a sequence's tiles (at least one, so that rows
 // without keys are written too)
+template <int kBlock = kBlockKeys>
 __device__ __forceinline__ int key_blocks(const Seq& s) {
-    return max(1, (s.len - min(s.start, s.len) + kBlockKeys - 1) / kBlockKeys);
+    return max(1, (s.len - min(s.start, s.len) + kBlock - 1) / kBlock);
 }
 
 __device__ __forceinline__ int64_t warp_scan(int64_t v) {  // inclusive
@@ -137,7 +138,7 @@ __device__ __forceinline__ int64_t div64(int64_t a, int64_t b) {
     return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
 }
 
-// Cached attention: the blocks of keys of all row tiles and kv heads, in the
+// Cached attention: the blocks of kBlock keys of all row tiles and kv heads, in the
 // order sequence, head, tile, block, are dealt out in equal shares, one per CTA.
 // A tile begins with tile_cost empty blocks, about what its set-up and results
 // cost, so that a share of many short tiles is not more work than the others.
@@ -160,7 +161,7 @@ struct Segment {
     int64_t slot;  // -1: whole
 };
 
-template <int kRows>
+template <int kRows, int kBlock = kBlockKeys>
 struct Walk {
     Shares sh;
     int64_t u, u0, u1;  // where the segment begins; the share's begin and end
@@ -173,7 +174,7 @@ struct Walk {
         share = index;
         const Place at = find_place(
             p.B,
-            [&](int b) { const Seq s = load_seq(p, b); return row_tiles(p, s, kRows) * (key_blocks(s) + p.tile_cost) * p.Hkv; },
+            [&](int b) { const Seq s = load_seq(p, b); return row_tiles(p, s, kRows) * (key_blocks<kBlock>(s) + p.tile_cost) * p.Hkv; },
             [&](int64_t total) { sh.set(p, total); return index * sh.each; }, sm);
         if (at.b < 0) return false;
         u = u0 = index * sh.each;
@@ -224,7 +225,7 @@ struct Walk {
         g.b = b;
         g.s = load_seq(p, b);
         tiles = (int)row_tiles(p, g.s, kRows);
-        g.nb = key_blocks(g.s);
+        g.nb = key_blocks<kBlock>(g.s);
     }
     __device__ __forceinline__ void cut(const AttnProblem& p) {
         x1 = (int)min64(g.nb + p.tile_cost, x0 + (u1 - u));

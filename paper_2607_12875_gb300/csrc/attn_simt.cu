@@ -360,11 +360,11 @@ cudaError_t simt_source(const AttnProblem& p, cudaStream_t stream) {
 constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32, kJoinChunks = 3;
 static_assert(kMaxShares <= kJoinThreads * kJoinChunks && kJoinWarps * kJoinChunks <= 32, "shares that a block counts");
 
-// kWide: D over 128, two columns groups of a lane
-template <typename TA, bool kWide>
+// Z: groups of 128 columns, of which a lane takes four each; kFly: parts whose loads are in flight
+template <typename TA, int Z>
 __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const __grid_constant__ AttnProblem p) {
     pdl_enter();
-    constexpr int Z = kWide ? 2 : 1;
+    constexpr int kFly = Z > 2 ? 4 : 8;
     __shared__ float4 acc[kJoinWarps][32 * Z];
     __shared__ int pre[kJoinThreads * kJoinChunks], sums[kJoinWarps * kJoinChunks];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -441,11 +441,11 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const __grid_co
                 l += mine.y * exp2f(mine.x - base);
                 const float f = exp2f(mine.z - base_o);
                 const int k = min(32, n - g0);
-                for (int c = part; c < k; c += 8 * W) {  // eight parts' loads in flight
-                    float4 v[8][Z];
-                    float w[8];
+                for (int c = part; c < k; c += kFly * W) {
+                    float4 v[kFly][Z];
+                    float w[kFly];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
+                    for (int i = 0; i < kFly; ++i) {
                         const int cc = c + W * i;
                         w[i] = __shfl_sync(0xffffffffu, f, min(cc, k - 1));
                         const float* src = p.part_o + slot(g0 + min(cc, k - 1)) * p.D + d;
@@ -455,7 +455,7 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const __grid_co
                                                                   : make_float4(0.f, 0.f, 0.f, 0.f);
                     }
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
+                    for (int i = 0; i < kFly; ++i) {
                         if (c + W * i >= k) continue;  // (a part that this row does not see: its sums are 0)
 #pragma unroll
                         for (int z = 0; z < Z; ++z) {
@@ -512,8 +512,8 @@ cudaError_t join_as(const AttnProblem& p, cudaStream_t stream) {
     // as many blocks as there may be rows, up to two on each SM (one or four: up to 2 us slower at 20)
     const int64_t rows = min64((int64_t)p.T * p.Hq, (int64_t)(p.shares - 1) * p.tile_rows);
     const dim3 grid((unsigned)min64(rows, 2 * sm_count()));
-    return p.D > 128 ? launch_k(attn_join_kernel<TA, true>, grid, dim3(kJoinThreads), 0, stream, p)
-                     : launch_k(attn_join_kernel<TA, false>, grid, dim3(kJoinThreads), 0, stream, p);
+    auto as = [&](auto kernel) { return launch_k(kernel, grid, dim3(kJoinThreads), 0, stream, p); };
+    return p.D > 256 ? as(attn_join_kernel<TA, 4>) : p.D > 128 ? as(attn_join_kernel<TA, 2>) : as(attn_join_kernel<TA, 1>);
 }
 
 }  // namespace

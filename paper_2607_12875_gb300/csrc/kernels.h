@@ -31,6 +31,8 @@ cudaError_t launch_route(const RouteParams& rp, const void* x, const void* w_rou
                          const float* select_bias, float* logits, int32_t* topk_ids, float* topk_w,
                          const RouteScratch& rs, cudaStream_t stream);
 // RMSNorm of x [T, H] (act dtype) with gamma [H] into y, in the gate's order
+cudaError_t launch_rmsnorm_add(const void* x, const void* residual, const void* gamma, float eps, int T, int H, int act_dtype,
+                               void* sum, void* y, uint8_t* codes, float* scales, cudaStream_t stream);
 cudaError_t launch_rmsnorm(const void* x, const void* gamma, float eps, int T, int H, int act_dtype, void* y,
                            cudaStream_t stream);
 // router logits on the tensor cores (bf16 x and router weight; ffn_tc.cu), as

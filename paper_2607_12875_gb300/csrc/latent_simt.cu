@@ -1,0 +1,306 @@
+// Latent attention on CUDA cores: fp32 activations, and sizes that the tensor-core
+// kernels do not take. Both forms.
+//
+// One pass over the keys with the running maximum and sum of the softmax: a block
+// holds 16 rows, token and head (absorbed), or 32 tokens of one head (expanded), walks
+// its keys in tiles of 32 through two buffers in shared memory (cp.async) and keeps
+// the weighted sums in registers. Absorbed: a tile's rows are keys and values at once.
+#include <type_traits>
+
+#include "attn_plan.cuh"
+#include "latent.h"
+#include "tc_ptx.cuh"
+
+namespace gbmoe {
+namespace {
+
+constexpr int kThreads = 128;
+constexpr int kKeys = 32;
+constexpr int kMinBlocks = 1, kTileCost = 0;  // shares of one block of 64 keys, as attn_simt.cu
+
+// 16 bytes global -> shared, or 16 bytes of zeros
+__device__ __forceinline__ void cp_async_or_zero(void* dst, const void* src, bool good) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(tc::smem_u32(dst)), "l"(src), "r"(good ? 16 : 0) : "memory");
+}
+
+template <typename TA>
+__device__ __forceinline__ float4 load4(const uint8_t* p) {
+    if constexpr (sizeof(TA) == 4) return *reinterpret_cast<const float4*>(p);
+    const uint2 u = *reinterpret_cast<const uint2*>(p);
+    return make_float4(bf16lo(u.x), bf16hi(u.x), bf16lo(u.y), bf16hi(u.y));
+}
+
+// Shared memory: query rows, two buffers of key (and value) rows, weights, marks of
+// keys whose page is in the pool. Rows lie an odd number of 16-byte pieces apart.
+struct Sizes {
+    int q_pitch, k_pitch, total;
+};
+__host__ __device__ __forceinline__ Sizes sizes_of(int key, int value, int eb, int rows) {
+    Sizes s;
+    s.q_pitch = ((key * eb / 16) | 1) * 16;
+    s.k_pitch = (((key + value) * eb / 16) | 1) * 16;
+    s.total = rows * s.q_pitch + 2 * kKeys * s.k_pitch + rows * (kKeys + 1) * 4 + 2 * kKeys * 4;
+    return s;
+}
+
+// N: rows of a thread, 2 (expanded) or 1 (absorbed); NC: its float4 columns. Thread
+// (ty, tx) = (tid / 8, tid % 8) holds rows N ty .., of the scores the keys tx + 8 j,
+// of the result the columns 4 tx + 32 j ..; a row's eight threads lie in one warp.
+template <typename TA, int N, int NC>
+__device__ __forceinline__ void attend(const LatentProblem& lp, const Segment& it) {
+    constexpr int kRows = 16 * N, EB = sizeof(TA);
+    constexpr bool kPaged = N == 1;
+    const AttnProblem& p = lp.a;
+    extern __shared__ float4 smem4[];
+    uint8_t* sq = reinterpret_cast<uint8_t*>(smem4);
+    const Sizes sz = sizes_of(lp.K, kPaged ? 0 : p.D, EB, kRows);
+    uint8_t* skv = sq + kRows * sz.q_pitch;
+    float* sp = reinterpret_cast<float*>(skv + 2 * kKeys * sz.k_pitch);
+    int* marks = reinterpret_cast<int*>(sp + kRows * (kKeys + 1));
+    const int R = p.R, head0 = kPaged ? 0 : it.head, row0 = it.tile * kRows;
+    const int n_rows = (int)min64(kRows, (int64_t)it.s.nq * R - row0);
+    const int c_lo = (int)min64((int64_t)it.blk0 * kBlockKeys, it.s.len);
+    const int c_hi = (int)min64((int64_t)it.blk1 * kBlockKeys, it.s.len);
+
+    const int tid = threadIdx.x, ty = tid >> 3, tx = tid & 7;
+    const int qp = lp.K * EB / 16;  // pieces of a query
+    for (int i = tid; i < kRows * qp; i += kThreads) {
+        const int r = i / qp, c = i % qp;
+        const bool good = r < n_rows;
+        const int rr = row0 + (good ? r : 0);
+        const TA* src = static_cast<const TA*>(p.q.p) + (it.s.q0 + rr / R) * p.q.ts + (head0 + rr % R) * p.q.hs;
+        cp_async_or_zero(sq + r * sz.q_pitch + 16 * c, reinterpret_cast<const uint8_t*>(src) + 16 * c, good);
+    }
+    int lo[N], hi[N];
+#pragma unroll
+    for (int r = 0; r < N; ++r) {
+        lo[r] = 0, hi[r] = -1;
+        if (N * ty + r < n_rows) seen_keys(p, it.s, (row0 + N * ty + r) / R, lo[r], hi[r]);
+    }
+    // keys that some row of the tile sees
+    int k_lo, last_hi;
+    seen_keys(p, it.s, (row0 + n_rows - 1) / R, k_lo, last_hi);
+    k_lo = c_lo;
+    const int k_hi = min(c_hi, last_hi + 1);
+
+    const int own = lp.own * EB / 16, key = lp.K * EB / 16, all_pieces = key + (kPaged ? 0 : p.D * EB / 16);
+    auto load = [&](int k0, int buf) {
+        for (int i = tid; i < kKeys * all_pieces; i += kThreads) {
+            const int r = i / all_pieces, c = i % all_pieces;
+            bool good = k0 + r < k_hi;
+            const uint8_t* src = static_cast<const uint8_t*>(p.q.p);  // (not read where good is false)
+            if constexpr (kPaged) {
+                if (good) {
+                    const int id = p.page_table[(int64_t)it.b * p.max_pages + ((k0 + r) >> p.page_log2)];
+                    good = id >= 0 && id < p.n_pages;
+                    if (good)
+                        src = static_cast<const uint8_t*>(p.k_pool) +
+                              ((int64_t)id * p.page + ((k0 + r) & (p.page - 1))) * lp.K * EB + 16 * c;
+                }
+                if (c == 0) marks[buf * kKeys + r] = good;
+            } else if (good) {
+                const int64_t at = it.s.k0 + k0 + r;
+                const Rows& from = c < own ? p.k : c < key ? lp.k_rope : p.v;
+                const int h = c >= own && c < key ? 0 : it.head;
+                src = reinterpret_cast<const uint8_t*>(static_cast<const TA*>(from.p) + at * from.ts + h * from.hs) +
+                      16 * (c < own ? c : c < key ? c - own : c - key);
+            }
+            cp_async_or_zero(skv + (buf * kKeys + r) * sz.k_pitch + 16 * c, src, good);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+
+    float4 o[N][NC];
+    float m[N], l[N];
+#pragma unroll
+    for (int r = 0; r < N; ++r) {
+        m[r] = neg_inf(), l[r] = 0.0f;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) o[r][c] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    if (k_lo < k_hi) load(k_lo, 0);
+    int buf = 0;
+    for (int k0 = k_lo; k0 < k_hi; k0 += kKeys, buf ^= 1) {
+        if (k0 + kKeys < k_hi) {
+            load(k0 + kKeys, buf ^ 1);
+            asm volatile("cp.async.wait_group 1;" ::: "memory");
+        } else {
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+        }
+        __syncthreads();
+        const uint8_t* tile = skv + buf * kKeys * sz.k_pitch;
+        if (N * 4 * (tid >> 5) < n_rows) {  // (else no row of this warp)
+            float s[N][4] = {};
+            for (int d = 0; d < lp.K; d += 4) {
+                float4 a[N], b[4];
+#pragma unroll
+                for (int r = 0; r < N; ++r) a[r] = load4<TA>(sq + (N * ty + r) * sz.q_pitch + d * EB);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) b[j] = load4<TA>(tile + (tx + 8 * j) * sz.k_pitch + d * EB);
+#pragma unroll
+                for (int r = 0; r < N; ++r)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        s[r][j] = fmaf(a[r].x, b[j].x, fmaf(a[r].y, b[j].y, fmaf(a[r].z, b[j].z, fmaf(a[r].w, b[j].w, s[r][j]))));
+            }
+            bool all = true;  // this thread's rows see every key of the tile
+#pragma unroll
+            for (int r = 0; r < N; ++r) {
+                float mx = neg_inf();
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int k = k0 + tx + 8 * j;
+                    const bool see = k >= lo[r] && k <= hi[r] && k < k_hi && (!kPaged || marks[buf * kKeys + tx + 8 * j]);
+                    all &= see;
+                    s[r][j] = see ? s[r][j] * p.scale_log2 : neg_inf();
+                    mx = fmaxf(mx, s[r][j]);
+                }
+#pragma unroll
+                for (int d = 1; d < 8; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+                const float m_new = fmaxf(m[r], mx);
+                const float base = m_new == neg_inf() ? 0.0f : m_new;
+                const float f = exp2f(m[r] - base);
+                m[r] = m_new;
+                float sum = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    s[r][j] = exp2f(s[r][j] - base);
+                    sum += s[r][j];
+                    sp[(N * ty + r) * (kKeys + 1) + tx + 8 * j] = s[r][j];
+                }
+                l[r] = l[r] * f + sum;
+#pragma unroll
+                for (int c = 0; c < NC; ++c) o[r][c].x *= f, o[r][c].y *= f, o[r][c].z *= f, o[r][c].w *= f;
+            }
+            all = __all_sync(0xffffffffu, all);
+            __syncwarp();
+            const uint8_t* values = tile + (kPaged ? 0 : lp.K * EB);
+            // weights times values; a value that a row does not see is left out, not multiplied by 0 (it may be NaN)
+            auto products = [&](auto masked) {
+#pragma unroll 4
+                for (int j = 0; j < kKeys; ++j) {
+                    float w[N];
+                    bool see[N];
+#pragma unroll
+                    for (int r = 0; r < N; ++r) {
+                        w[r] = sp[(N * ty + r) * (kKeys + 1) + j];
+                        see[r] = k0 + j >= lo[r] && k0 + j <= hi[r];
+                    }
+#pragma unroll
+                    for (int c = 0; c < NC; ++c) {
+                        const int d = 4 * tx + 32 * c;
+                        if (d >= p.D) break;
+                        const float4 v = load4<TA>(values + j * sz.k_pitch + d * EB);
+#pragma unroll
+                        for (int r = 0; r < N; ++r) {
+                            if (decltype(masked)::value && !see[r]) continue;
+                            o[r][c].x = fmaf(w[r], v.x, o[r][c].x), o[r][c].y = fmaf(w[r], v.y, o[r][c].y);
+                            o[r][c].z = fmaf(w[r], v.z, o[r][c].z), o[r][c].w = fmaf(w[r], v.w, o[r][c].w);
+                        }
+                    }
+                }
+            };
+            if (all) products(std::false_type{});
+            else products(std::true_type{});
+        }
+        __syncthreads();
+    }
+    if (k_lo >= k_hi) asm volatile("cp.async.wait_all;" ::: "memory");
+#pragma unroll
+    for (int r = 0; r < N; ++r) {
+#pragma unroll
+        for (int d = 1; d < 8; d <<= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], d);
+        const int rr = N * ty + r;
+        if (rr >= n_rows) continue;
+        const int64_t t = it.s.q0 + (row0 + rr) / R;
+        const int hq = head0 + (row0 + rr) % R;
+        // Without a score above -inf: whether the row sees a key at all (if not it gives 0, else 0 / 0)
+        const bool blank = m[r] == neg_inf() && l[r] == 0.0f;
+        const bool sees = !kPaged || !blank || any_page(p, it.b, max(lo[r], c_lo), min(hi[r], c_hi - 1));
+        if (it.slot >= 0) {
+            const int64_t at = it.slot * kRows + rr;
+            if (tx == 0) reinterpret_cast<float4*>(p.part_s)[at] = make_float4(m[r], l[r], m[r], sees ? 1.0f : 0.0f);
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+                if (4 * tx + 32 * c < p.D) *reinterpret_cast<float4*>(p.part_o + at * p.D + 4 * tx + 32 * c) = o[r][c];
+            continue;
+        }
+        const bool empty = hi[r] < lo[r] || !sees;
+        const float inv = empty ? 0.0f : 1.0f / l[r];
+        if (p.lse && tx == 0) p.lse[t * p.Hq + hq] = empty ? neg_inf() : (m[r] + log2f(l[r])) * kLn2;
+        TA* out = const_cast<TA*>(static_cast<const TA*>(p.out.p)) + t * p.out.ts + hq * p.out.hs;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int d = 4 * tx + 32 * c;
+            if (d >= p.D) continue;
+            const float v[4] = {o[r][c].x * inv, o[r][c].y * inv, o[r][c].z * inv, o[r][c].w * inv};
+            if constexpr (EB == 4)
+                *reinterpret_cast<float4*>(out + d) = make_float4(v[0], v[1], v[2], v[3]);
+            else
+                *reinterpret_cast<uint2*>(out + d) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+        }
+    }
+}
+
+template <typename TA, int N, int NC>
+__global__ void __launch_bounds__(kThreads) latent_simt_kernel(const __grid_constant__ LatentProblem lp) {
+    pdl_enter();
+    const AttnProblem& p = lp.a;
+    __shared__ int64_t plan[plan_words(kThreads)];
+    if constexpr (N == 1) {
+        Walk<16> w;
+        if (!w.begin(p, blockIdx.x, plan)) {
+            if (threadIdx.x == 0) w.note_idle(p, blockIdx.x);
+            return;
+        }
+        do {
+            attend<TA, N, NC>(lp, w.g);
+            if (threadIdx.x == 0) w.note(p);
+            __syncthreads();
+        } while (w.next(p));
+    } else {
+        Segment g{};
+        g.head = blockIdx.x % p.Hq;
+        const Place at = find_tile(p, blockIdx.x / p.Hq, 16 * N, plan);
+        if (at.b < 0) return;
+        g.b = at.b, g.s = load_seq(p, at.b), g.tile = (int)at.at;
+        g.blk1 = key_blocks(g.s), g.slot = -1;
+        attend<TA, N, NC>(lp, g);
+    }
+}
+
+template <typename TA, int N, int NC>
+cudaError_t simt_as(const LatentProblem& p, cudaStream_t stream) {
+    constexpr auto kernel = latent_simt_kernel<TA, N, NC>;
+    static DeviceOnce once;
+    constexpr int kMost = 227 * 1024;
+    if (cudaError_t e = once.run([] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost - 1024); });
+        e != cudaSuccess)
+        return e;
+    const int smem = sizes_of(p.K, N == 1 ? 0 : p.a.D, (int)sizeof(TA), 16 * N).total;
+    if constexpr (N == 1) {
+        LatentProblem a = p;
+        const int fit = kMost / (smem + 2048);
+        set_shares(a.a, 16, fit < 1 ? 1 : fit > 4 ? 4 : fit, sm_count(), kMinBlocks, kTileCost);
+        if (cudaError_t e = launch_k(kernel, dim3(a.a.shares), dim3(kThreads), smem, stream, a); e != cudaSuccess) return e;
+        return a.a.shares > 1 ? launch_attn_join(a.a, stream) : cudaSuccess;
+    } else {
+        const int64_t grid = ((int64_t)p.a.T / (16 * N) + p.a.B) * p.a.Hq;
+        if (grid > INT32_MAX) return cudaErrorInvalidConfiguration;
+        return launch_k(kernel, dim3((unsigned)grid), dim3(kThreads), smem, stream, p);
+    }
+}
+
+template <typename TA>
+cudaError_t simt_type(const LatentProblem& p, cudaStream_t stream) {
+    if (p.a.paged) return p.a.D <= 256 ? simt_as<TA, 1, 8>(p, stream) : simt_as<TA, 1, 16>(p, stream);
+    return p.a.D <= 64 ? simt_as<TA, 2, 2>(p, stream) : simt_as<TA, 2, 4>(p, stream);
+}
+
+}  // namespace
+
+cudaError_t launch_latent_simt(const LatentProblem& p, cudaStream_t stream) {
+    return p.a.act_dtype == GBMOE_F32 ? simt_type<float>(p, stream) : simt_type<__nv_bfloat16>(p, stream);
+}
+
+}  // namespace gbmoe
