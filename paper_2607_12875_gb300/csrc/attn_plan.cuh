@@ -161,8 +161,10 @@ struct Segment {
     int64_t slot;  // -1: whole
 };
 
+// kRows: rows of a tile (0: p.tile_rows).
 template <int kRows, int kBlock = kBlockKeys>
 struct Walk {
+    __device__ __forceinline__ static int tile_rows(const AttnProblem& p) { return kRows > 0 ? kRows : p.tile_rows; }
     Shares sh;
     int64_t u, u0, u1;  // where the segment begins; the share's begin and end
     int64_t share;
@@ -174,7 +176,7 @@ struct Walk {
         share = index;
         const Place at = find_place(
             p.B,
-            [&](int b) { const Seq s = load_seq(p, b); return row_tiles(p, s, kRows) * (key_blocks<kBlock>(s) + p.tile_cost) * p.Hkv; },
+            [&](int b) { const Seq s = load_seq(p, b); return row_tiles(p, s, tile_rows(p)) * (key_blocks<kBlock>(s) + p.tile_cost) * p.Hkv; },
             [&](int64_t total) { sh.set(p, total); return index * sh.each; }, sm);
         if (at.b < 0) return false;
         u = u0 = index * sh.each;
@@ -214,7 +216,7 @@ struct Walk {
         if (g.blk0 == 0 && g.blk1 < g.nb) {
             c.parts = (int)div64(g.nb - g.blk1 + sh.each - 1, sh.each) + 1;
             c.first = (int)g.slot;
-            c.rows = (int)min64(kRows, (int64_t)g.s.nq * p.R - (int64_t)g.tile * kRows);
+            c.rows = (int)min64(tile_rows(p), (int64_t)g.s.nq * p.R - (int64_t)g.tile * tile_rows(p));
             c.head = g.head, c.tile = g.tile;
             c.q0 = g.s.q0, c.nq = g.s.nq, c.len = g.s.len;
         }
@@ -224,7 +226,7 @@ struct Walk {
     __device__ __forceinline__ void enter(const AttnProblem& p, int b) {
         g.b = b;
         g.s = load_seq(p, b);
-        tiles = (int)row_tiles(p, g.s, kRows);
+        tiles = (int)row_tiles(p, g.s, tile_rows(p));
         g.nb = key_blocks<kBlock>(g.s);
     }
     __device__ __forceinline__ void cut(const AttnProblem& p) {

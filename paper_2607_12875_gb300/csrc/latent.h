@@ -36,4 +36,8 @@ cudaError_t launch_latent_append(const LatentAppend& p, cudaStream_t stream);
 // CUDA cores: any covered sizes and types
 cudaError_t launch_latent_simt(const LatentProblem& p, cudaStream_t stream);
 
+// absorbed on the tensor cores: bf16, R a multiple of 128, P up to 64
+bool latent_cached_tc_supported(const LatentProblem& p);
+cudaError_t launch_latent_cached_tc(const LatentProblem& p, cudaStream_t stream);
+
 }  // namespace gbmoe

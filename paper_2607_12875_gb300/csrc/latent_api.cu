@@ -194,7 +194,8 @@ int latent_cached(const gblatent_config* cfg, int32_t T, const gbattn_batch* bat
     a.cu_q = batch->cu_q; a.kv_len = batch->kv_len; a.page_table = batch->page_table; a.k_pool = cache->rows;
     a.q = rows_of(q, T, H); a.out = rows_of(out, T, H);
     p.K = W; p.own = W;
-    return cuda_status(launch_latent_simt(p, static_cast<cudaStream_t>(stream)));
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return cuda_status(latent_cached_tc_supported(p) ? launch_latent_cached_tc(p, st) : launch_latent_simt(p, st));
 }
 
 }  // extern "C"
