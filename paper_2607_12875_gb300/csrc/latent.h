@@ -39,5 +39,8 @@ cudaError_t launch_latent_simt(const LatentProblem& p, cudaStream_t stream);
 // absorbed on the tensor cores: bf16, R a multiple of 128, P up to 64
 bool latent_cached_tc_supported(const LatentProblem& p);
 cudaError_t launch_latent_cached_tc(const LatentProblem& p, cudaStream_t stream);
+// expanded on the tensor cores: bf16, P up to 64
+bool latent_prompt_tc_supported(const LatentProblem& p);
+cudaError_t launch_latent_prompt_tc(const LatentProblem& p, cudaStream_t stream);
 
 }  // namespace gbmoe

@@ -173,7 +173,8 @@ int latent_prompt(const gblatent_config* cfg, int32_t Tq, int32_t Tk, int32_t B,
         a.k = rows_of(k, Tk, H), a.v = rows_of(v, Tk, H);
         if (P > 0) p.k_rope = rows_of(k_rope, Tk, 1);
     }
-    return cuda_status(launch_latent_simt(p, static_cast<cudaStream_t>(stream)));
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return cuda_status(latent_prompt_tc_supported(p) ? launch_latent_prompt_tc(p, st) : launch_latent_simt(p, st));
 }
 
 int latent_cached(const gblatent_config* cfg, int32_t T, const gbattn_batch* batch, const gbattn_rows* q,

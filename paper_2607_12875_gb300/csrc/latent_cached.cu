@@ -12,9 +12,12 @@
 //   P^T = exp2(scale S^T - m)   a thread has one key and half of the columns
 //   O^T += C^T P^T   the same tiles, read MN-major; P^T in shared memory, in the place of
 //                    the rotary keys, which the second product does not need
-// The columns' maxima m are shared by all keys of a tile: they are raised, and O^T
-// rescaled, only when a score passes its column's by 2^8. A thread sums its own key's
-// weights, and the threads' sums are joined at the end of a segment.
+// The columns' maxima m are shared by all keys of a tile. They come from a segment's first
+// tile and are raised, and O^T rescaled, only when a score passes its column's by 2^16:
+// fp32 and bf16 weights lose nothing by that (their exponents reach 2^127), and tiles
+// need no exchange between threads. The thread that finds such a score leaves a note, the
+// MMA warp, which meets all of them anyway, sends the tile back once more.
+// A thread sums its own key's weights, and the threads' sums are joined at the end of a segment.
 // More rows than N: up to kMostSides CTAs beside each other take the same keys with N rows
 // each, at about the same time, so that HBM is read once.
 // Warps 0-3 and 4-7: softmax of the first and second half of the columns, queries and
@@ -43,7 +46,7 @@ constexpr int kKeys = 128;                // keys of a tile
 constexpr int kThreads = 320;
 constexpr int kChunk = kKeys * 128;       // bytes of 128 rows x 64 elements
 constexpr unsigned kFull = 0xffffffffu;
-constexpr float kGrow = 8.0f;             // log2 of how far a column's maximum may run ahead of m
+constexpr float kGrow = 16.0f;            // log2 of how far a column's maximum may run ahead of m
 constexpr float kMost = 3.402823466e38f;  // -kMost: a maximum of nothing
 constexpr int kMinBlocks = 1, kTileCost = 0;
 constexpr int kMostSides = 8;
@@ -168,9 +171,10 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
     uint64_t* half = drain + 1;         // the four warps of half of the columns meet
     uint64_t* both = half + 2;          // all eight
     __shared__ uint32_t tmem_slot, good[TAILS];  // good: pages of the tile that are in the pool
-    __shared__ int abort_word, top[N], raised[2][3], row_hi[N];
+    __shared__ int abort_word, top[N], row_hi[N];
+    __shared__ uint32_t raised, again;  // a score far above its maximum was found in tile .. - 1; that tile is to be done once more
     __shared__ float sums[8][COLS];
-    __shared__ __align__(16) float peak[N], factor[N];  // the columns' maxima m, and what a raise multiplies by
+    __shared__ __align__(16) float low[N], factor[N];  // the columns' -m, and what a raise multiplies by
     __shared__ int64_t plan[plan_words(kThreads)];
     volatile int* abort_flag = &abort_word;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -188,7 +192,7 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
         mbar_init(&half[1], 4);
         mbar_init(both, 8);
         abort_word = 0;
-        for (int i = 0; i < 6; ++i) raised[i / 3][i % 3] = 0;
+        raised = again = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 9) {
@@ -197,7 +201,9 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
     }
     tc_fence_before();
     Walk<0, kKeys> walk;
-    const bool any = walk.begin(p, share, plan);
+    const bool any = __any_sync(kFull, walk.begin(p, share, plan));
+    // (votes: loops whose length the compiler takes for different in each lane keep the MMA's operands out of uniform registers)
+    auto next = [&] { return __any_sync(kFull, walk.next(p)); };
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_slot, tS = tmem, tO = tmem + 128;  // O: pairs_of_tile times N columns
@@ -212,8 +218,8 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
         const uint32_t mS = tS + lanes + c0, mO = tO + lanes + c0;
         const float scale = p.scale_log2;
         uint32_t n_tiles = 0;  // so far
-        int tail = 0, turn = 0, pair = 0;
-        uint32_t tphase = 0;
+        int tail = 0, pair = 0;
+        uint32_t tphase = 0, sn = 0;
         uint32_t meets = 0, meets_both = 0;
         // (mbarriers, not bar.sync: a warp whose wait gave up does not come)
         auto meet = [&](uint64_t* bar, uint32_t& n) {
@@ -245,7 +251,7 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
                 }
                 if (wt < COLS) {
                     top[c0 + wt] = ordered(-kMost);
-                    peak[c0 + wt] = -kMost;
+                    low[c0 + wt] = kMost;
                     int lo, hi = -1;
                     if (c0 + wt < x.rows) seen_keys(p, g.s, (x.row0 + c0 + wt) / p.R, lo, hi);
                     row_hi[c0 + wt] = hi;
@@ -253,27 +259,19 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
                 ok = meet(&half[wg], meets);
                 if (!ok) break;
             }
-            float l[COLS];
+            uint64_t l[COLS / 2];  // sums of the weights of this thread's keys, two columns each
 #pragma unroll
-            for (int c = 0; c < COLS; ++c) l[c] = 0.0f;
-            for (int t = 0; t < x.tiles; ++t) {
+            for (int c = 0; c < COLS / 2; ++c) l[c] = pack2(0.0f, 0.0f);
+            if (x.tiles > 0) ok = wait_warp(s_full, sn++ & 1u);
+            for (int t = 0; t < x.tiles && ok; ++t) {
                 const int key = x.key0 + t * kKeys + r;
-                ok = wait_warp(s_full, n_tiles & 1u) && wait_warp(&tfull[tail], tphase);
+                ok = wait_warp(&tfull[tail], tphase);
                 if (!ok) break;
-                tc_fence_after();
                 const uint32_t pages = *const_cast<volatile uint32_t*>(&good[tail]);
-                uint32_t u[COLS];
-                tmem_load<COLS>(mS, u);
-                float s[COLS];
-#pragma unroll
-                for (int c = 0; c < COLS; ++c) s[c] = __uint_as_float(u[c]) * scale;
                 const bool all = x.key0 + (t + 1) * kKeys - 1 <= x.all_hi && pages == (1u << (kKeys >> p.page_log2)) - 1u;
+                const bool mine = pages >> (r >> p.page_log2) & 1u;
                 bool poison = false;
                 if (!all) {
-                    const bool mine = pages >> (r >> p.page_log2) & 1u;
-#pragma unroll
-                    for (int c = 0; c < COLS; ++c)
-                        if (!mine || key > row_hi[c0 + c]) s[c] = neg_inf();
                     auto at = [&](int i) {  // piece i of this key's latent
                         int slot = pair + (i >> 4);
                         if (slot >= PAIRS) slot -= PAIRS;
@@ -291,74 +289,96 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
                     if (poison || key > x.most_hi)
                         for (int i = wg * (R / 16); i < (wg + 1) * (R / 16); ++i) *at(i) = make_uint4(0, 0, 0, 0);
                 }
-                // maxima
-                bool over = false;
-#pragma unroll
-                for (int c = 0; c < COLS; c += 4) {
-                    const float4 m = *reinterpret_cast<const float4*>(&peak[c0 + c]);
-                    over = over || s[c] > m.x + kGrow || s[c + 1] > m.y + kGrow || s[c + 2] > m.z + kGrow || s[c + 3] > m.w + kGrow;
-                }
-                if (__any_sync(kFull, over)) {
-#pragma unroll
-                    for (int c = 0; c < COLS; ++c) {
-                        const int best = __reduce_max_sync(kFull, ordered(fmaxf(s[c], -kMost)));
-                        if (lane == (c & 31)) atomicMax(&top[c0 + c], best);
-                    }
-                    if (lane == 0) *const_cast<volatile int*>(&raised[wg][turn]) = 1;
-                }
-                const int next = turn == 2 ? 0 : turn + 1;
-                if (wt == 0) *const_cast<volatile int*>(&raised[wg][next]) = 0;  // (read last before the meeting before this one)
-                ok = meet(&half[wg], meets);
-                if (!ok) break;
-                if (*const_cast<volatile int*>(&raised[wg][turn])) {
-                    if (wt < COLS) {
-                        const float m = unordered(top[c0 + wt]);
-                        factor[c0 + wt] = ex2(peak[c0 + wt] - m);  // (nothing yet: 0)
-                        peak[c0 + wt] = m;
-                    }
-                    ok = meet(&half[wg], meets) && (t == 0 || wait_warp(o_full, (n_tiles - 1) & 1u));
-                    if (!ok) break;
-                    tc_fence_after();
-#pragma unroll
-                    for (int c = 0; c < COLS; ++c) l[c] *= factor[c0 + c];
-                    if (t > 0) {
-#pragma unroll 1
-                        for (int i = 0; i < pairs_of_tile; ++i) {
-                            tmem_load<COLS>(mO + i * N, u);
-#pragma unroll
-                            for (int c = 0; c < COLS; ++c) u[c] = __float_as_uint(__uint_as_float(u[c]) * factor[c0 + c]);
-                            tmem_store<COLS>(mO + i * N, u);
-                        }
-                        st_wait();
-                    }
-                }
-                turn = next;
-                // weights
                 uint8_t* dst = tails + tail * kChunk;
+                // One pass over the tile's scores. raise: the maxima are brought up to them first (the first tile, and
+                // where a pass before found one too far above); else, whether one is. count: the weights enter the sums.
+                auto pass = [&](bool raise, bool count) {
+                    tc_fence_after();
+                    uint32_t u[COLS];
+                    tmem_load<COLS>(mS, u);
+                    auto unseen = [&](int c) { return !all && (!mine || key > row_hi[c0 + c]); };
+                    if (raise) {
 #pragma unroll
-                for (int c = 0; c < COLS; c += 8) {
-                    uint32_t w[4];
-                    float m[8];
-                    *reinterpret_cast<float4*>(m) = *reinterpret_cast<const float4*>(&peak[c0 + c]);
-                    *reinterpret_cast<float4*>(m + 4) = *reinterpret_cast<const float4*>(&peak[c0 + c + 4]);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        float e[2];
-#pragma unroll
-                        for (int z = 0; z < 2; ++z) {
-                            const int k = c + 2 * i + z;
-                            e[z] = ex2(s[k] - m[2 * i + z]);
-                            if (poison && key <= row_hi[c0 + k]) e[z] = __uint_as_float(0x7fc00000u);
-                            l[k] += e[z];
+                        for (int c = 0; c < COLS; ++c) {
+                            const int best = __reduce_max_sync(kFull, ordered(unseen(c) ? -kMost : fmaxf(__uint_as_float(u[c]) * scale, -kMost)));
+                            if (lane == (c & 31)) atomicMax(&top[c0 + c], best);
                         }
-                        w[i] = pack_bf16x2(e[0], e[1]);
+                        ok = meet(&half[wg], meets);
+                        if (!ok) return false;
+                        if (wt < COLS) {
+                            const float m = unordered(top[c0 + wt]);
+                            factor[c0 + wt] = ex2(-low[c0 + wt] - m);  // (nothing yet: 0)
+                            low[c0 + wt] = -m;
+                        }
+                        ok = meet(&half[wg], meets) && (t == 0 || wait_warp(o_full, (n_tiles - 1) & 1u));
+                        if (!ok) return false;
+                        if (t > 0) {
+                            tc_fence_after();
+#pragma unroll
+                            for (int c = 0; c < COLS / 2; ++c) {
+                                const float2 f = *reinterpret_cast<const float2*>(&factor[c0 + 2 * c]);
+                                l[c] = fma2(l[c], pack2(f.x, f.y), pack2(0.0f, 0.0f));
+                            }
+#pragma unroll 1
+                            for (int i = 0; i < pairs_of_tile; ++i) {
+                                uint32_t o[COLS];
+                                tmem_load<COLS>(mO + i * N, o);
+#pragma unroll
+                                for (int c = 0; c < COLS; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * factor[c0 + c]);
+                                tmem_store<COLS>(mO + i * N, o);
+                            }
+                            st_wait();
+                        }
                     }
-                    *reinterpret_cast<uint4*>(dst + sw128_off(r, (c0 + c) >> 3)) = make_uint4(w[0], w[1], w[2], w[3]);
+                    const uint64_t sc2 = pack2(scale, scale);
+                    float most = -kMost;
+#pragma unroll
+                    for (int c = 0; c < COLS; c += 4) {
+                        const float4 m = *reinterpret_cast<const float4*>(&low[c0 + c]);
+                        float2 a = unpack2(fma2(pack2(__uint_as_float(u[c]), __uint_as_float(u[c + 1])), sc2, pack2(m.x, m.y)));
+                        float2 b = unpack2(fma2(pack2(__uint_as_float(u[c + 2]), __uint_as_float(u[c + 3])), sc2, pack2(m.z, m.w)));
+                        if (!all) {
+                            a.x = unseen(c) ? neg_inf() : a.x, a.y = unseen(c + 1) ? neg_inf() : a.y;
+                            b.x = unseen(c + 2) ? neg_inf() : b.x, b.y = unseen(c + 3) ? neg_inf() : b.y;
+                        }
+                        most = max3(most, fmaxf(a.x, a.y), fmaxf(b.x, b.y));
+                        u[c] = __float_as_uint(a.x), u[c + 1] = __float_as_uint(a.y);
+                        u[c + 2] = __float_as_uint(b.x), u[c + 3] = __float_as_uint(b.y);
+                    }
+                    const bool over = __any_sync(kFull, most > kGrow) && !raise;
+                    if (over) {
+                        if (lane == 0) *const_cast<volatile uint32_t*>(&raised) = n_tiles + 1;
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < COLS; c += 8) {
+                            uint32_t w[4];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const int k = c + 2 * i;
+                                float e0 = ex2(__uint_as_float(u[k])), e1 = ex2(__uint_as_float(u[k + 1]));
+                                if (poison) {
+                                    if (key <= row_hi[c0 + k]) e0 = __uint_as_float(0x7fc00000u);
+                                    if (key <= row_hi[c0 + k + 1]) e1 = __uint_as_float(0x7fc00000u);
+                                }
+                                if (count) l[k >> 1] = add2(l[k >> 1], pack2(e0, e1));
+                                w[i] = pack_bf16x2(e0, e1);
+                            }
+                            *reinterpret_cast<uint4*>(dst + sw128_off(r, (c0 + c) >> 3)) = make_uint4(w[0], w[1], w[2], w[3]);
+                        }
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    }
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(p_full);
+                    return over;
+                };
+                const bool over = pass(t == 0, true);
+                // the next tile's scores, or the last tile's results, or this tile once more
+                ok = ok && wait_warp(s_full, sn++ & 1u);
+                if (ok && *const_cast<volatile uint32_t*>(&again) == n_tiles + 1) {
+                    pass(true, over);
+                    ok = ok && wait_warp(s_full, sn++ & 1u);
                 }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(p_full);
                 ++n_tiles;
                 pair += pairs_of_tile;
                 while (pair >= PAIRS) pair -= PAIRS;
@@ -368,24 +388,23 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
             // ------------------------------------------------------------ result
             if (x.rows > 0) {
                 // each column's sum of weights over the keys, a transposing sum within the warp first
+                float lc[COLS];
+#pragma unroll
+                for (int c = 0; c < COLS / 2; ++c) lc[2 * c] = unpack2(l[c]).x, lc[2 * c + 1] = unpack2(l[c]).y;
 #pragma unroll
                 for (int d = 16; d >= COLS; d >>= 1)
 #pragma unroll
-                    for (int c = 0; c < COLS; ++c) l[c] += __shfl_xor_sync(kFull, l[c], d);
+                    for (int c = 0; c < COLS; ++c) lc[c] += __shfl_xor_sync(kFull, lc[c], d);
 #pragma unroll
                 for (int d = COLS / 2; d; d >>= 1)
 #pragma unroll
                     for (int c = 0; c < d; ++c) {
                         const bool up = lane & d;
-                        const float give = up ? l[c] : l[c + d], keep = up ? l[c + d] : l[c];
-                        l[c] = keep + __shfl_xor_sync(kFull, give, d);
+                        const float give = up ? lc[c] : lc[c + d], keep = up ? lc[c + d] : lc[c];
+                        lc[c] = keep + __shfl_xor_sync(kFull, give, d);
                     }
-                if (lane < COLS) sums[warp][lane] = l[0];
-                if (x.tiles > 0) {
-                    ok = wait_warp(o_full, (n_tiles - 1) & 1u);
-                    if (!ok) break;
-                    tc_fence_after();
-                }
+                if (lane < COLS) sums[warp][lane] = lc[0];
+                tc_fence_after();
                 ok = meet(&half[wg], meets);
                 if (!ok) break;
                 if (wt < COLS && c0 + wt < x.rows) {
@@ -393,7 +412,7 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
                     float sum = 0.0f;
 #pragma unroll
                     for (int w = 0; w < 4; ++w) sum += sums[4 * wg + w][wt];
-                    const float mx = peak[c] == -kMost ? neg_inf() : peak[c];
+                    const float mx = low[c] == kMost ? neg_inf() : -low[c];
                     // Without a score above -inf: whether the row sees a key at all (if not it gives 0, else 0 / 0)
                     const bool blank = mx == neg_inf() && sum == 0.0f;
                     const bool sees = !blank || any_page(p, g.b, x.key0, min(row_hi[c], (int)min64((int64_t)g.blk1 * kKeys, g.s.len) - 1));
@@ -438,7 +457,7 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
                 if (!ok) break;
             }
             if (side == 0 && tid == 0) walk.note(p);
-        } while (walk.next(p));
+        } while (next());
         if (!ok && side == 0 && tid == 0) walk.note_idle(p, share);
     } else if (warp == 8) {
         // ------------------------------------------------------------ TMA producer
@@ -488,7 +507,7 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
                 if (++tail == TAILS) tail = 0, tphase ^= 1;
                 row = ahead;
             }
-        } while (ok && walk.next(p));
+        } while (ok && next());
         // every copy has landed before the CTA leaves
         if (lane == 0) {
             const uint64_t t0 = global_ns();
@@ -506,7 +525,7 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
         const uint64_t dv = mn_desc(smem_u32(pairs)), dp = mn_desc(smem_u32(tails));
         const int tail_steps = (W - R + 15) / 16;
         int slot = 0, tail = 0;
-        uint32_t phase = 0, tphase = 0, qn = 0, pn = 0;
+        uint32_t phase = 0, tphase = 0, qn = 0, pn = 0, tile = 0;
         bool ok = true, issued = false;
         do {
             const Part x = part_of<N>(p, walk.g, side);
@@ -541,6 +560,16 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
                 __syncwarp();
                 ok = wait_warp(p_full, pn++ & 1u);
                 if (!ok) break;
+                ++tile;
+                if (__any_sync(kFull, *const_cast<volatile uint32_t*>(&raised) == tile)) {
+                    if (lane == 0) {
+                        *const_cast<volatile uint32_t*>(&again) = tile;
+                        mbar_arrive(s_full);
+                    }
+                    __syncwarp();
+                    ok = wait_warp(p_full, pn++ & 1u);
+                    if (!ok) break;
+                }
                 tc_fence_after();
                 int sv = slot0;
                 for (int i = 0; i < pairs_of_tile; ++i) {
@@ -553,6 +582,7 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
                         if (i == pairs_of_tile - 1) {
                             mma_commit(&tempty[tail]);
                             mma_commit(o_full);
+                            if (t == tiles - 1) mma_commit(s_full);
                         }
                     }
                     __syncwarp();
@@ -560,7 +590,7 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
                 }
                 if (++tail == TAILS) tail = 0, tphase ^= 1;
             }
-        } while (ok && walk.next(p));
+        } while (ok && next());
         if (issued) {  // no MMA is in flight when TMEM is released
             if (elect_one()) mma_commit(drain);
             __syncwarp();
