@@ -107,12 +107,13 @@ latent_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
     // kDeal, which has one query tile: maximum, sum and results' check of the softmax warps' rows
     float(*stats)[8][32] = reinterpret_cast<float(*)[8][32]>(sQ + kQTile);
     uint64_t* bars = reinterpret_cast<uint64_t*>(sKV + kSlots * kHalf);
-    uint64_t* full = bars;            // a chunk of K or V landed
-    uint64_t* empty = full + kSlots;  // the MMAs that read it finished
-    uint64_t* q_full = empty + kSlots;
+    // tiles of K and V in the order in which they are loaded, tile i on the barriers i % kSlots (a tile has a slot at least)
+    uint64_t* full = bars;            // it landed
+    uint64_t* done = full + kSlots;   // the MMAs that read it finished
+    uint64_t* q_full = done + kSlots;
     uint64_t* q_empty = q_full + 2;   // the last product with a query tile finished
     uint64_t* s_full = q_empty + 2;   // S of a query tile is complete (and so is every MMA before it)
-    uint64_t* p_full = s_full + 2;    // its P is written, O rescaled, and the V and next K tile are there
+    uint64_t* p_full = s_full + 2;    // its P is written, O rescaled, and the V tile is there
     uint64_t* o_full = p_full + 2;    // its O is complete
     uint64_t* w_full = o_full + 2;    // a work item is in its slot
     uint64_t* w_empty = w_full + 2;   // every role has read it
@@ -126,7 +127,7 @@ latent_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
     if (threadIdx.x == 0) {
         for (int i = 0; i < kSlots; ++i) {
             mbar_init(&full[i], 1);
-            mbar_init(&empty[i], 1);
+            mbar_init(&done[i], 1);
         }
         for (int t = 0; t < 2; ++t) {
             mbar_init(&q_full[t], 1);
@@ -392,20 +393,11 @@ latent_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             if (asked && lane == 0) drain_wait(ans, turn & 1u);  // (a wait gave up: the answer lands before the CTA leaves)
         } else if (warp == 8 && lane == 0) {
             // ------------------------------------------------------ TMA producer
-            uint32_t inflight = 0, par = 0, qn[2] = {0, 0};
-            int slot = 0;
-            uint32_t phase = 0;
+            uint32_t qn[2] = {0, 0};
+            int slot = 0, used = 0;       // next slot, slots that are not free
+            uint32_t seq = 0, oldest = 0;  // tiles begun, and of those the first whose slots are not free
+            uint64_t sizes = 0;           // slots of the latest tiles, four bits each
             bool ok = true;
-            auto open = [&](uint32_t bytes) {  // the next slot, free
-                ok = ok && wait(&empty[slot], phase ^ 1);
-                if (ok) mbar_expect_tx(&full[slot], bytes);
-                return ok;
-            };
-            auto close = [&] {
-                inflight |= 1u << slot;
-                par = (par & ~(1u << slot)) | (phase << slot);
-                if (++slot == kSlots) slot = 0, phase ^= 1;
-            };
             const int v_boxes = (p.D + 63) / 64;
             for (int k = 0; ok; ++k) {
                 if (!wait(&w_full[k & 1], (uint32_t)(k >> 1) & 1u)) break;
@@ -432,16 +424,29 @@ latent_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                         at = i == 0 ? 0 : i == 2 * n_all - 1 ? n_all - 1 : value ? at - 1 : at + 1;
                     }
                     const int key = (int)(w.s.k0 + w.k_first + at * kTile);
-                    for (int c = 0; c < (value ? 2 : k_chunks); ++c) {
-                        if (!open(value ? v_boxes * kHalf / 2 : kHalf)) break;
+                    const int chunks = value ? 2 : k_chunks, bits = 4 * (int)(seq % kSlots);
+                    uint64_t* bar = &full[seq % kSlots];
+                    sizes = (sizes & ~((uint64_t)15 << bits)) | (uint64_t)chunks << bits;
+                    for (int c = 0; c < chunks; ++c) {
+                        while (ok && used == kSlots) {
+                            ok = wait(&done[oldest % kSlots], (oldest / kSlots) & 1u);
+                            used -= (int)(sizes >> 4 * (oldest % kSlots) & 15);
+                            ++oldest;
+                        }
+                        if (!ok) break;
+                        if (c == 0) {
+                            mbar_expect_tx(bar, value ? v_boxes * kHalf : k_chunks * kHalf);
+                            ++seq;
+                        }
                         uint8_t* dst = sKV + slot * kHalf;
                         if (value)
-                            for (int x = 0; x < v_boxes; ++x) tma_load_3d(dst + x * kHalf / 2, &tm_v, 64 * x, w.head0, key + 64 * c, &full[slot]);
+                            for (int x = 0; x < v_boxes; ++x) tma_load_3d(dst + x * kHalf / 2, &tm_v, 64 * x, w.head0, key + 64 * c, bar);
                         else if (c < own_chunks)
-                            tma_load_3d(dst, &tm_k, 64 * c, w.head0, key, &full[slot]);
+                            tma_load_3d(dst, &tm_k, 64 * c, w.head0, key, bar);
                         else
-                            tma_load_3d(dst, &tm_r, 0, 0, key, &full[slot]);
-                        close();
+                            tma_load_3d(dst, &tm_r, 0, 0, key, bar);
+                        ++used;
+                        if (++slot == kSlots) slot = 0;
                     }
                 }
             }
@@ -449,8 +454,7 @@ latent_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             const uint64_t t0 = global_ns();
             for (int t = 0; t < 2; ++t)
                 if (qn[t] > 0) drain_wait(&q_full[t], (qn[t] - 1) & 1u, t0);
-            for (int i = 0; i < kSlots; ++i)
-                if ((inflight >> i) & 1u) drain_wait(&full[i], (par >> i) & 1u, t0);
+            for (uint32_t i = seq > kSlots ? seq - kSlots : 0; i < seq; ++i) drain_wait(&full[i % kSlots], (i / kSlots) & 1u, t0);
         } else if (warp == 9) {
             // ------------------------- MMA issuer (the whole warp, one lane issues)
             // Every value that an MMA takes comes from constants, kernel parameters and
@@ -462,20 +466,31 @@ latent_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             const uint32_t tm = __reduce_max_sync(0xffffffffu, tmem);
             bool issued = false;
             uint32_t qn0 = 0, qn1 = 0, pn0 = 0, pn1 = 0;  // phases of q_full and p_full
-            int slot = 0;  // ring slot of the next tile's first chunk and its phase
-            uint32_t phase = 0;
+            int slot = 0;      // ring slot of the next tile's first chunk
+            uint32_t seq = 0;  // tiles before it
             auto advance = [&](int chunks) {
-                slot += chunks;
-                if (slot >= kSlots) slot -= kSlots, phase ^= 1;
+                slot += chunks, ++seq;
+                if (slot >= kSlots) slot -= kSlots;
             };
             auto place = [&](int at) { return at >= kSlots ? at - kSlots : at; };
-            // S_t = Q_t K^T with the K tile in the slots from st on; last: the item's last use of Q_t (kDeal: of the one Q)
-            auto scores = [&](int t, int st, bool last) {
-                if (elect_one()) {
-                    const uint64_t a = dq + (kDeal ? 0 : (uint64_t)(t * kQTile >> 4));
+            // The issue queue is shallow: what a wait takes after a batch of MMAs the tensor cores stand still. So the next
+            // batch's barrier is looked at before the last MMAs of this one, and mostly it is complete by then.
+            auto peek = [&](uint64_t* bar, uint32_t parity) { return bar && __all_sync(0xffffffffu, mbar_test_wait(bar, parity)); };
+            auto landed = [&](uint32_t tile, bool ready) {
+                const bool ok = ready || wait_warp(&full[tile % kSlots], (tile / kSlots) & 1u);
+                tc_fence_after();
+                return ok;
+            };
+            // S_t = Q_t K^T with K tile `tile` in the slots from st on; last: the item's last use of Q_t (kDeal: of the one
+            // Q); free: the tile's last use. Returns what a peek at `bar` on the way found.
+            auto scores = [&](int t, int st, uint32_t tile, bool last, bool free, uint64_t* bar, uint32_t parity) {
+                const uint64_t a = dq + (kDeal ? 0 : (uint64_t)(t * kQTile >> 4));
+                bool ready = false;
 #pragma unroll
-                    for (int c = 0; c < 3; ++c) {
-                        if (c >= k_chunks) break;
+                for (int c = 0; c < 3; ++c) {
+                    if (c >= k_chunks) break;
+                    if (c == k_chunks - 1) ready = peek(bar, parity);
+                    if (elect_one()) {
                         const int part = c < own_chunks ? own - 64 * c : rope;  // elements of the chunk, or more
                         const uint64_t b = dk + (uint64_t)((uint32_t)(place(st + c) * kHalf) >> 4);
 #pragma unroll
@@ -483,38 +498,40 @@ latent_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                             if (16 * i >= part) break;
                             mma_ss(tm + t * kTile, a + (uint64_t)((c * kHalf + i * 32) >> 4), b + (uint64_t)(i * 32 >> 4), kIdS, c + i != 0);
                         }
+                        if (c == k_chunks - 1) {
+                            mma_commit(&s_full[t]);
+                            if (free) mma_commit(&done[tile % kSlots]);
+                            if (last) mma_commit(&q_empty[kDeal ? 0 : t]);
+                        }
                     }
-                    mma_commit(&s_full[t]);
-                    if (last) mma_commit(&q_empty[kDeal ? 0 : t]);
+                    __syncwarp();
                 }
-                __syncwarp();
                 issued = true;
+                return ready;
             };
-            // O_t += P_t V with the V tile in the slots from st on
-            auto values = [&](int t, int st, bool first, bool last) {
-                if (elect_one()) {
+            // O_t += P_t V with V tile `tile` in the slots from st on; the same
+            auto values = [&](int t, int st, uint32_t tile, bool first, bool last, bool free, uint64_t* bar, uint32_t parity) {
+                bool ready = false;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
+                for (int h = 0; h < 2; ++h) {
+                    if (h == 1) ready = peek(bar, parity);
+                    if (elect_one()) {
                         const uint64_t b = dv + (uint64_t)((uint32_t)(place(st + h) * kHalf) >> 4);
 #pragma unroll
                         for (int c = 0; c < 4; ++c)  // 16 keys: 8 columns of P, 2 KB of V
                             mma_ts(tm + 2 * kTile + t * kTile, tm + t * kTile + 8 * (4 * h + c), b + (uint64_t)(c * 2048 >> 4), id_o,
                                    h + c != 0 || !first);
+                        if (h == 1) {
+                            if (free) mma_commit(&done[tile % kSlots]);
+                            if (last) mma_commit(&o_full[t]);
+                        }
                     }
-                    if (last) mma_commit(&o_full[t]);
+                    __syncwarp();
                 }
-                __syncwarp();
+                return ready;
             };
-            auto release = [&](int st, int chunks) {
-                if (elect_one())
-                    for (int c = 0; c < chunks; ++c) mma_commit(&empty[place(st + c)]);
-                __syncwarp();
-            };
-            auto wait_tile = [&] {  // the next tile's chunks (a K tile)
-                bool ok = true;
-                for (int c = 0; c < k_chunks && ok; ++c) ok = wait_warp(&full[place(slot + c)], slot + c >= kSlots ? phase ^ 1 : phase);
-                return ok;
-            };
+            auto bar_of = [&](bool there, uint32_t tile) { return there ? &full[tile % kSlots] : nullptr; };
+            auto parity_of = [&](uint32_t tile) { return (tile / kSlots) & 1u; };
             for (int k = 0;; ++k) {
                 if (!wait_warp(&w_full[k & 1], (uint32_t)(k >> 1) & 1u)) break;
                 const int n0 = __reduce_max_sync(0xffffffffu, work_slots[k & 1].n[0]);
@@ -526,26 +543,28 @@ latent_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 if (n_max == 0) continue;
                 if constexpr (kDeal) {
                     const int n = n0 + n1;
-                    bool ok = wait_warp(&q_full[0], qn0++ & 1u);
+                    bool ok = wait_warp(&q_full[0], qn0++ & 1u), ready = false;
                     for (int i = 0; i < min(n, 2) && ok; ++i) {
-                        ok = wait_tile();
+                        ok = landed(seq, false);
                         if (!ok) break;
-                        tc_fence_after();
-                        scores(i, slot, i + 1 == n);
-                        release(slot, k_chunks);
+                        scores(i, slot, seq, i + 1 == n, true, nullptr, 0);
                         advance(k_chunks);
                     }
                     for (int i = 0; i < n && ok; ++i) {
-                        const int t = i & 1, sv = slot;  // V_i, then K_i+2: there when p_full is complete
-                        advance(2);
-                        ok = wait_warp(&p_full[t], (t ? pn1++ : pn0++) & 1u);
+                        const int t = i & 1;
+                        ok = ready || wait_warp(&p_full[t], (t ? pn1 : pn0) & 1u);
                         if (!ok) break;
+                        if (t) ++pn1;
+                        else ++pn0;
                         tc_fence_after();
-                        values(t, sv, i < 2, i + 2 >= n);
-                        release(sv, 2);
-                        if (i + 2 < n) {
-                            scores(t, slot, i + 3 == n);
-                            release(slot, k_chunks);
+                        // V_i, then K_i+2
+                        const bool more = i + 2 < n;
+                        ready = values(t, slot, seq, i < 2, !more, true, bar_of(more, seq + 1), parity_of(seq + 1));
+                        advance(2);
+                        if (more) {
+                            ok = landed(seq, ready);
+                            if (!ok) break;
+                            ready = scores(t, slot, seq, i + 3 == n, true, &p_full[t ^ 1], (t ? pn0 : pn1) & 1u);
                             advance(k_chunks);
                         }
                     }
@@ -554,35 +573,45 @@ latent_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 }
                 if (n0 > 0 && !wait_warp(&q_full[0], qn0++ & 1u)) break;
                 if (n1 > 0 && !wait_warp(&q_full[1], qn1++ & 1u)) break;
-                if (!wait_tile()) break;
-                tc_fence_after();
-                if (n0 > 0) scores(0, slot, n0 == 1);
-                if (n1 > 0) scores(1, slot, n1 == 1);
-                release(slot, k_chunks);
+                if (!landed(seq, false)) break;
+                if (n0 > 0) scores(0, slot, seq, n0 == 1, n1 == 0, nullptr, 0);
+                if (n1 > 0) scores(1, slot, seq, n1 == 1, true, nullptr, 0);
                 advance(k_chunks);
-                bool ok = true;
+                bool ok = true, ready = false;  // ready: the next wait's barrier was complete at the peek
                 for (int j = 0; j < n_max; ++j) {
-                    // V_j in slot sv, K_j+1 in slot sk: there when p_full is complete
+                    // V_j from slot sv on, K_j+1 from slot sk on
                     const int sv = slot;
+                    const uint32_t tv = seq;
                     advance(2);
                     const int sk = slot;
+                    const uint32_t tk = seq;
                     if (j + 1 < n_max) advance(k_chunks);
                     if (j < n0) {
-                        ok = wait_warp(&p_full[0], pn0++ & 1u);
+                        ok = ready || wait_warp(&p_full[0], pn0 & 1u);
                         if (!ok) break;
+                        ++pn0;
                         tc_fence_after();
-                        values(0, sv, j == 0, j == n0 - 1);
-                        if (j + 1 < n0) scores(0, sk, j + 2 == n0);
+                        const bool more = j + 1 < n0;
+                        ready = values(0, sv, tv, j == 0, !more, j >= n1, bar_of(more, tk), parity_of(tk));
+                        if (more) {
+                            ok = landed(tk, ready);
+                            if (!ok) break;
+                            ready = scores(0, sk, tk, j + 2 == n0, j + 1 >= n1, j < n1 ? &p_full[1] : nullptr, pn1 & 1u);
+                        }
                     }
                     if (j < n1) {
-                        ok = wait_warp(&p_full[1], pn1++ & 1u);
+                        ok = ready || wait_warp(&p_full[1], pn1 & 1u);
                         if (!ok) break;
+                        ++pn1;
                         tc_fence_after();
-                        values(1, sv, j == 0, j == n1 - 1);
-                        if (j + 1 < n1) scores(1, sk, j + 2 == n1);
+                        const bool more = j + 1 < n1;
+                        ready = values(1, sv, tv, j == 0, !more, true, bar_of(more, tk), parity_of(tk));
+                        if (more) {
+                            ok = landed(tk, ready);
+                            if (!ok) break;
+                            ready = scores(1, sk, tk, j + 2 == n1, true, j + 1 < n0 ? &p_full[0] : nullptr, pn0 & 1u);
+                        }
                     }
-                    release(sv, 2);
-                    if (j + 1 < n_max) release(sk, k_chunks);
                 }
                 if (!ok) break;
             }
@@ -593,50 +622,27 @@ latent_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             }
         } else if (warp == 11 && lane == 0) {
             // ------------------------------------------------------- tile watcher
-            // Waits for the tiles in the MMA warp's stead, whose issue queue is shallow: each
-            // barrier that it waits for itself delays the MMAs behind it.
-            int slot = 0;
-            uint32_t phase = 0, pn[2] = {0, 0};
-            auto next = [&] {
-                if (++slot == kSlots) slot = 0, phase ^= 1;
-            };
-            auto land = [&](int chunks) {
-                bool ok = true;
-                for (int c = 0; c < chunks && ok; ++c) {
-                    ok = wait(&full[slot], phase);
-                    next();
-                }
-                return ok;
-            };
+            // Waits for the V tiles in the MMA warp's stead. (For K as well, and so that the products of V wait for them:
+            // 2059 us for 16384 tokens of 32 heads.)
+            uint32_t seq = 0, pn[2] = {0, 0};
             bool ok = true;
             for (int k = 0; ok; ++k) {
                 if (!wait(&w_full[k & 1], (uint32_t)(k >> 1) & 1u)) break;
                 const int n0 = work_slots[k & 1].n[0], n1 = work_slots[k & 1].n[1], end = work_slots[k & 1].end;
                 mbar_arrive(&w_empty[k & 1]);
                 if (end) break;
-                const int n_max = max(n0, n1);
-                if constexpr (kDeal) {
-                    const int n = n0 + n1;
-                    for (int i = 0; i < min(n, 2) * k_chunks; ++i) next();  // (the first K tiles: the MMA warp's)
-                    for (int i = 0; i < n && ok; ++i) {
-                        ok = land(i + 2 < n ? 2 + k_chunks : 2);
-                        const int t = i & 1;
-                        if (ok && pn[t] > 0) ok = wait(&p_full[t], (pn[t] - 1) & 1u);
-                        ++pn[t];
-                        if (ok) mbar_arrive(&p_full[t]);
-                    }
-                    continue;
-                }
-                for (int c = 0; c < (n_max > 0 ? k_chunks : 0); ++c) next();  // (the first K tile: the MMA warp's)
-                for (int j = 0; j < n_max && ok; ++j) {
-                    ok = land(j + 1 < n_max ? 2 + k_chunks : 2);
+                const int n = kDeal ? n0 + n1 : max(n0, n1);
+                for (int j = 0; j < n && ok; ++j) {
+                    const uint32_t tile = seq + (kDeal && j < n - 1 ? 2 * j + 2 : 2 * j + 1);
+                    ok = wait(&full[tile % kSlots], (tile / kSlots) & 1u);
                     for (int t = 0; t < 2 && ok; ++t) {
-                        if (j >= (t ? n1 : n0)) continue;
+                        if (kDeal ? t != (j & 1) : j >= (t ? n1 : n0)) continue;
                         if (pn[t] > 0) ok = wait(&p_full[t], (pn[t] - 1) & 1u);  // one arrival in a phase
                         ++pn[t];
                         if (ok) mbar_arrive(&p_full[t]);
                     }
                 }
+                seq += 2 * n;
             }
         }
     }
