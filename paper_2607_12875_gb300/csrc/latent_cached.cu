@@ -111,27 +111,28 @@ __device__ __forceinline__ uint64_t mn_desc(uint32_t saddr) {
            (uint64_t)2 << 61;
 }
 
-// floats in an order of integers (NaN is not passed)
-__device__ __forceinline__ int ordered(float x) {
-    const int i = __float_as_int(x);
-    return i >= 0 ? i : i ^ 0x7fffffff;
-}
-__device__ __forceinline__ float unordered(int i) { return __int_as_float(i >= 0 ? i : i ^ 0x7fffffff); }
-
-// The segment as one CTA sees it: its rows and its tiles of keys.
-struct Part {
+// A segment as one CTA sees it: its rows and its tiles of keys. The TMA warp walks the
+// share and hands the segments to the other warps.
+struct Job {
     int row0, rows;       // first row of the sequence's, how many (<= 0: none)
     int key0, tiles;
     int all_hi, most_hi;  // last key that all rows see, that any row sees
+    int q0, pos0;         // the sequence's first token, its position
+    int len, key_end;     // the sequence's keys; end of the segment's
+    int b;
+    int end;              // 1: no more segments
+    int64_t slot;
 };
 template <int N>
-__device__ __forceinline__ Part part_of(const AttnProblem& p, const Segment& g, int side) {
-    Part x;
+__device__ __forceinline__ Job job_of(const AttnProblem& p, const Segment& g, int side) {
+    Job x;
     const int64_t row0 = (int64_t)g.tile * p.tile_rows + side * N;
     x.row0 = (int)row0;
     x.rows = (int)min64(N, (int64_t)g.s.nq * p.R - row0);
     x.key0 = g.blk0 * kKeys;
-    x.tiles = 0;
+    x.tiles = 0, x.all_hi = x.most_hi = -1;
+    x.q0 = g.s.q0, x.pos0 = g.s.len - g.s.nq, x.len = g.s.len, x.b = g.b, x.end = 0, x.slot = g.slot;
+    x.key_end = (int)min64((int64_t)g.blk1 * kKeys, g.s.len);
     if (x.rows <= 0) return x;
     int lo;
     seen_keys(p, g.s, x.row0 / p.R, lo, x.all_hi);
@@ -158,7 +159,8 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
     uint8_t* sq = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint8_t* pairs = sq + L::Q;
     uint8_t* tails = pairs + PAIRS * 2 * kChunk;
-    __shared__ uint64_t bars[2 * (PAIRS + TAILS) + 8];
+    __shared__ uint64_t bars[2 * (PAIRS + TAILS) + 12];
+    __shared__ Job jobs[2];
     uint64_t* full = bars;              // a pair landed
     uint64_t* empty = full + PAIRS;     // the products that read it finished
     uint64_t* tfull = empty + PAIRS;
@@ -170,8 +172,10 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
     uint64_t* drain = o_full + 1;
     uint64_t* half = drain + 1;         // the four warps of half of the columns meet
     uint64_t* both = half + 2;          // all eight
+    uint64_t* j_full = both + 1;        // a job is in its slot
+    uint64_t* j_empty = j_full + 2;     // every role has read it
     __shared__ uint32_t tmem_slot, good[TAILS];  // good: pages of the tile that are in the pool
-    __shared__ int abort_word, top[N], row_hi[N];
+    __shared__ int abort_word, row_hi[N];
     __shared__ uint32_t raised, again;  // a score far above its maximum was found in tile .. - 1; that tile is to be done once more
     __shared__ float sums[8][COLS];
     __shared__ __align__(16) float low[N], factor[N];  // the columns' -m, and what a raise multiplies by
@@ -191,6 +195,7 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
         mbar_init(&half[0], 4);
         mbar_init(&half[1], 4);
         mbar_init(both, 8);
+        for (int i = 0; i < 2; ++i) mbar_init(&j_full[i], 1), mbar_init(&j_empty[i], 9);  // (softmax warps, MMA)
         abort_word = 0;
         raised = again = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -202,8 +207,6 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
     tc_fence_before();
     Walk<0, kKeys> walk;
     const bool any = __any_sync(kFull, walk.begin(p, share, plan));
-    // (votes: loops whose length the compiler takes for different in each lane keep the MMA's operands out of uniform registers)
-    auto next = [&] { return __any_sync(kFull, walk.next(p)); };
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_slot, tS = tmem, tO = tmem + 128;  // O: pairs_of_tile times N columns
@@ -228,33 +231,37 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
             return wait_warp(bar, n++ & 1u);
         };
         bool ok = true;
-        do {
-            const Segment& g = walk.g;
-            const Part x = part_of<N>(p, g, side);
+        for (int j = 0; ok; ++j) {
+            ok = wait_warp(&j_full[j & 1], (uint32_t)(j >> 1) & 1u);
+            if (!ok) break;
+            const Job x = jobs[j & 1];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&j_empty[j & 1]);
+            if (x.end) break;
             if (x.rows > 0) {
                 // queries: rows of N x 64 elements, 128-byte swizzled, zeros where there are none
                 if (x.tiles > 0) {
                     const int pieces = (pairs_of_tile * 2 + 1) * 8;
                     for (int i = tid; i < N * pieces; i += 256) {
                         const int row = i / pieces, c = i - row * pieces;
-                        uint4 v = make_uint4(0, 0, 0, 0);
-                        if (row < x.rows && 8 * c < W) {
-                            const int rr = x.row0 + row, tok = rr / p.R;
-                            v = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q.p) + (g.s.q0 + tok) * p.q.ts +
-                                                                (rr - tok * p.R) * p.q.hs + 8 * c);
-                        }
-                        *reinterpret_cast<uint4*>(sq + (c >> 3) * (N * 128) + sw128_off(row, c & 7)) = v;
+                        const bool there = row < x.rows && 8 * c < W;
+                        const int rr = x.row0 + (there ? row : 0), tok = rr / p.R;
+                        const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(p.q.p) + (int64_t)(x.q0 + tok) * p.q.ts +
+                                                   (rr - tok * p.R) * p.q.hs + (there ? 8 * c : 0);
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(sq + (c >> 3) * (N * 128) + sw128_off(row, c & 7))),
+                                     "l"(src), "r"(there ? 16 : 0)
+                                     : "memory");
                     }
+                    asm volatile("cp.async.wait_all;" ::: "memory");
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
                     if (lane == 0) mbar_arrive(q_full);
                 }
                 if (wt < COLS) {
-                    top[c0 + wt] = ordered(-kMost);
                     low[c0 + wt] = kMost;
-                    int lo, hi = -1;
-                    if (c0 + wt < x.rows) seen_keys(p, g.s, (x.row0 + c0 + wt) / p.R, lo, hi);
-                    row_hi[c0 + wt] = hi;
+                    int hi = -1;
+                    if (c0 + wt < x.rows) hi = p.causal ? min(x.pos0 + (x.row0 + c0 + wt) / p.R, x.len - 1) : x.len - 1;
+                    row_hi[c0 + wt] = hi < 0 ? -1 : hi;
                 }
                 ok = meet(&half[wg], meets);
                 if (!ok) break;
@@ -298,15 +305,30 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
                     tmem_load<COLS>(mS, u);
                     auto unseen = [&](int c) { return !all && (!mine || key > row_hi[c0 + c]); };
                     if (raise) {
+                        // each column's largest score: over the warp's keys by a transposing maximum (lane: column), then
+                        // over the four warps
+                        float best[COLS];
 #pragma unroll
-                        for (int c = 0; c < COLS; ++c) {
-                            const int best = __reduce_max_sync(kFull, ordered(unseen(c) ? -kMost : fmaxf(__uint_as_float(u[c]) * scale, -kMost)));
-                            if (lane == (c & 31)) atomicMax(&top[c0 + c], best);
-                        }
+                        for (int c = 0; c < COLS; ++c) best[c] = unseen(c) ? -kMost : fmaxf(__uint_as_float(u[c]) * scale, -kMost);
+#pragma unroll
+                        for (int d = 16; d >= COLS; d >>= 1)
+#pragma unroll
+                            for (int c = 0; c < COLS; ++c) best[c] = fmaxf(best[c], __shfl_xor_sync(kFull, best[c], d));
+#pragma unroll
+                        for (int d = COLS / 2; d; d >>= 1)
+#pragma unroll
+                            for (int c = 0; c < d; ++c) {
+                                const bool up = lane & d;
+                                const float give = up ? best[c] : best[c + d], keep = up ? best[c + d] : best[c];
+                                best[c] = fmaxf(keep, __shfl_xor_sync(kFull, give, d));
+                            }
+                        if (lane < COLS) sums[warp][lane] = best[0];
                         ok = meet(&half[wg], meets);
                         if (!ok) return false;
                         if (wt < COLS) {
-                            const float m = unordered(top[c0 + wt]);
+                            float m = -low[c0 + wt];
+#pragma unroll
+                            for (int w = 0; w < 4; ++w) m = fmaxf(m, sums[4 * wg + w][wt]);
                             factor[c0 + wt] = ex2(-low[c0 + wt] - m);  // (nothing yet: 0)
                             low[c0 + wt] = -m;
                         }
@@ -415,13 +437,13 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
                     const float mx = low[c] == kMost ? neg_inf() : -low[c];
                     // Without a score above -inf: whether the row sees a key at all (if not it gives 0, else 0 / 0)
                     const bool blank = mx == neg_inf() && sum == 0.0f;
-                    const bool sees = !blank || any_page(p, g.b, x.key0, min(row_hi[c], (int)min64((int64_t)g.blk1 * kKeys, g.s.len) - 1));
+                    const bool sees = !blank || any_page(p, x.b, x.key0, min(row_hi[c], x.key_end - 1));
                     const bool none = row_hi[c] < 0 || !sees;
                     factor[c] = none ? 0.0f : 1.0f / sum;
-                    if (g.slot >= 0)
-                        reinterpret_cast<float4*>(p.part_s)[g.slot * p.tile_rows + side * N + c] = make_float4(mx, sum, mx, sees ? 1.0f : 0.0f);
+                    if (x.slot >= 0)
+                        reinterpret_cast<float4*>(p.part_s)[x.slot * p.tile_rows + side * N + c] = make_float4(mx, sum, mx, sees ? 1.0f : 0.0f);
                     else if (p.lse)
-                        p.lse[(int64_t)g.s.q0 * p.Hq + row] = none ? neg_inf() : (mx + log2f(sum)) * kLn2;
+                        p.lse[(int64_t)x.q0 * p.Hq + row] = none ? neg_inf() : (mx + log2f(sum)) * kLn2;
                 }
                 ok = meet(&half[wg], meets);
                 if (!ok) break;
@@ -434,8 +456,8 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
 #pragma unroll
                         for (int c = 0; c < COLS; ++c) u[c] = 0;
                     }
-                    if (g.slot >= 0) {
-                        float* dst = p.part_o + (g.slot * p.tile_rows + side * N + c0) * R + d;
+                    if (x.slot >= 0) {
+                        float* dst = p.part_o + (x.slot * p.tile_rows + side * N + c0) * R + d;
 #pragma unroll
                         for (int c = 0; c < COLS; ++c)
                             if (c0 + c < x.rows) dst[(int64_t)c * R] = __uint_as_float(u[c]);
@@ -445,7 +467,7 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
                             if (c0 + c >= x.rows) break;
                             const int row = x.row0 + c0 + c, tok = row / p.R;
                             __nv_bfloat16* out = const_cast<__nv_bfloat16*>(static_cast<const __nv_bfloat16*>(p.out.p)) +
-                                                 (g.s.q0 + tok) * p.out.ts + (row - tok * p.R) * p.out.hs + d;
+                                                 (int64_t)(x.q0 + tok) * p.out.ts + (row - tok * p.R) * p.out.hs + d;
                             const float f = factor[c0 + c];
                             *out = __float2bfloat16_rn(f == 0.0f ? 0.0f : __uint_as_float(u[c]) * f);
                         }
@@ -456,9 +478,7 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
                 ok = meet(&half[wg], meets);
                 if (!ok) break;
             }
-            if (side == 0 && tid == 0) walk.note(p);
-        } while (next());
-        if (!ok && side == 0 && tid == 0) walk.note_idle(p, share);
+        }
     } else if (warp == 8) {
         // ------------------------------------------------------------ TMA producer
         uint32_t inflight = 0, par = 0, tinflight = 0, tpar = 0;
@@ -466,10 +486,20 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
         uint32_t phase = 0, tphase = 0;
         const int per_tile = kKeys >> p.page_log2, box = p.page * 128;
         const int nowhere = p.n_pages << p.page_log2;  // rows past the pool: the copy brings zeros
-        bool ok = true;
-        do {
-            const Part x = part_of<N>(p, walk.g, side);
-            const int32_t* ids = p.page_table + (int64_t)walk.g.b * p.max_pages;
+        bool ok = true, more = true;
+        for (int j = 0; ok; ++j) {
+            ok = wait_warp(&j_empty[j & 1], ((uint32_t)(j >> 1) & 1u) ^ 1u);
+            if (!ok) break;
+            Job x = job_of<N>(p, walk.g, side);
+            if (!more) x.end = 1;
+            if (lane == 0) {
+                jobs[j & 1] = x;
+                mbar_arrive(&j_full[j & 1]);
+                if (more && side == 0) walk.note(p);
+            }
+            __syncwarp();
+            if (!more) break;
+            const int32_t* ids = p.page_table + (int64_t)x.b * p.max_pages;
             auto first_row = [&](int t) {  // of this lane's page of tile t
                 const int at = x.key0 + t * kKeys + (lane << p.page_log2);
                 if (lane >= per_tile || t >= x.tiles || at > x.most_hi) return nowhere;
@@ -507,7 +537,8 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
                 if (++tail == TAILS) tail = 0, tphase ^= 1;
                 row = ahead;
             }
-        } while (ok && next());
+            more = walk.next(p);
+        }
         // every copy has landed before the CTA leaves
         if (lane == 0) {
             const uint64_t t0 = global_ns();
@@ -527,29 +558,45 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
         int slot = 0, tail = 0;
         uint32_t phase = 0, tphase = 0, qn = 0, pn = 0, tile = 0;
         bool ok = true, issued = false;
-        do {
-            const Part x = part_of<N>(p, walk.g, side);
-            const int tiles = __reduce_max_sync(kFull, x.tiles);
+        for (int j = 0; ok; ++j) {
+            ok = wait_warp(&j_full[j & 1], (uint32_t)(j >> 1) & 1u);
+            if (!ok) break;
+            // (what the loops run to comes from warp-wide reductions, so that the MMA's operands stay in uniform registers)
+            const int tiles = __reduce_max_sync(kFull, jobs[j & 1].tiles), end = __reduce_max_sync(kFull, jobs[j & 1].end);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&j_empty[j & 1]);
+            if (end) break;
             if (tiles <= 0) continue;
             ok = wait_warp(q_full, qn++ & 1u);
             for (int t = 0; t < tiles && ok; ++t) {
                 const int slot0 = slot;
+                // The issue queue is shallow: what a wait takes after a batch of MMAs the tensor cores stand still. So the
+                // next batch's barrier is looked at before the last MMAs of this one.
+                auto peek = [&](uint64_t* bar, uint32_t parity) { return __all_sync(kFull, mbar_test_wait(bar, parity)); };
+                bool ready = false;
                 for (int i = 0; i < pairs_of_tile; ++i) {
-                    ok = wait_warp(&full[slot], phase);
+                    ok = ready || wait_warp(&full[slot], phase);
                     if (!ok) break;
                     tc_fence_after();
+                    const uint64_t a = dk + (uint64_t)((uint32_t)(slot * 2 * kChunk) >> 4), b = dq + (uint64_t)((uint32_t)(i * 2 * N * 128) >> 4);
+                    if (++slot == PAIRS) slot = 0, phase ^= 1;
                     if (elect_one()) {
-                        const uint64_t a = dk + (uint64_t)((uint32_t)(slot * 2 * kChunk) >> 4), b = dq + (uint64_t)((uint32_t)(i * 2 * N * 128) >> 4);
 #pragma unroll
-                        for (int k = 0; k < 8; ++k)
+                        for (int k = 0; k < 5; ++k)
                             mma_ss(tm, a + (((k >> 2) * kChunk + (k & 3) * 32) >> 4), b + (((k >> 2) * N * 128 + (k & 3) * 32) >> 4), kId, i > 0 || k > 0);
                     }
                     __syncwarp();
+                    ready = i + 1 < pairs_of_tile ? peek(&full[slot], phase) : peek(&tfull[tail], tphase);
+                    if (elect_one()) {
+#pragma unroll
+                        for (int k = 5; k < 8; ++k)
+                            mma_ss(tm, a + (((k >> 2) * kChunk + (k & 3) * 32) >> 4), b + (((k >> 2) * N * 128 + (k & 3) * 32) >> 4), kId, 1);
+                    }
+                    __syncwarp();
                     issued = true;
-                    if (++slot == PAIRS) slot = 0, phase ^= 1;
                 }
                 if (!ok) break;
-                ok = wait_warp(&tfull[tail], tphase);
+                ok = ready || wait_warp(&tfull[tail], tphase);
                 if (!ok) break;
                 tc_fence_after();
                 if (elect_one()) {
@@ -590,7 +637,7 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
                 }
                 if (++tail == TAILS) tail = 0, tphase ^= 1;
             }
-        } while (ok && next());
+        }
         if (issued) {  // no MMA is in flight when TMEM is released
             if (elect_one()) mma_commit(drain);
             __syncwarp();
@@ -599,6 +646,7 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
     }
     tc_fence_before();
     __syncthreads();
+    if (tid == 0 && side == 0 && *abort_flag) Walk<0, kKeys>::note_idle(p, share);  // (the join leaves this share's tile alone)
     if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
 

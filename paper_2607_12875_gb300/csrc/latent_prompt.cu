@@ -19,8 +19,8 @@
 // kDeal, where there is too little work for every SM: the two tiles are one tile
 // of 128 rows twice, with every other tile of keys each, and their results are
 // joined at the end.
-// Warps 0-3 and 4-7: softmax of tile 0 and 1 and their results; warp 8: TMA; warp
-// 9: MMA; warp 10: scheduler. A CTA goes on with the work of CTAs that have not
+// Warps 0-3 and 4-7: softmax of tile 0 and 1 and their results; warp 8: TMA; warps 9
+// and 11: MMA of tile 0 and 1; warp 10: scheduler. A CTA goes on with the work of CTAs that have not
 // started (cluster launch control), so the loads, the first products and the search
 // for the next work run while the softmax warps still write the last results.
 // TMEM columns: S_0, S_1 (128 each), O_0, O_1 (128 each).
@@ -109,17 +109,17 @@ latent_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
     uint64_t* bars = reinterpret_cast<uint64_t*>(sKV + kSlots * kHalf);
     // tiles of K and V in the order in which they are loaded, tile i on the barriers i % kSlots (a tile has a slot at least)
     uint64_t* full = bars;            // it landed
-    uint64_t* done = full + kSlots;   // the MMAs that read it finished
+    uint64_t* done = full + kSlots;   // the MMAs of both query tiles that read it finished
     uint64_t* q_full = done + kSlots;
     uint64_t* q_empty = q_full + 2;   // the last product with a query tile finished
     uint64_t* s_full = q_empty + 2;   // S of a query tile is complete (and so is every MMA before it)
-    uint64_t* p_full = s_full + 2;    // its P is written, O rescaled, and the V tile is there
+    uint64_t* p_full = s_full + 2;    // its P is written and O rescaled
     uint64_t* o_full = p_full + 2;    // its O is complete
     uint64_t* w_full = o_full + 2;    // a work item is in its slot
     uint64_t* w_empty = w_full + 2;   // every role has read it
     uint64_t* ans = w_empty + 2;      // the answer to try_cancel
     uint64_t* drain = ans + 1;
-    uint64_t* pair = drain + 1;       // kDeal: the two warps of the same rows
+    uint64_t* pair = drain + 2;       // kDeal: the two warps of the same rows
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(pair + 4);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
@@ -127,19 +127,20 @@ latent_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
     if (threadIdx.x == 0) {
         for (int i = 0; i < kSlots; ++i) {
             mbar_init(&full[i], 1);
-            mbar_init(&done[i], 1);
+            mbar_init(&done[i], 2);
         }
         for (int t = 0; t < 2; ++t) {
             mbar_init(&q_full[t], 1);
-            mbar_init(&q_empty[t], 1);
+            mbar_init(&q_empty[t], kDeal ? 2 : 1);
             mbar_init(&s_full[t], 1);
-            mbar_init(&p_full[t], 5);    // one arrival per softmax warp, one of the tile watcher
+            mbar_init(&p_full[t], 4);
             mbar_init(&o_full[t], 1);
             mbar_init(&w_full[t], 1);
-            mbar_init(&w_empty[t], 11);  // softmax warps, TMA, MMA, tile watcher
+            mbar_init(&w_empty[t], 11);  // softmax warps, TMA, MMA warps
         }
         mbar_init(ans, 1);
-        mbar_init(drain, 1);
+        mbar_init(&drain[0], 1);
+        mbar_init(&drain[1], 1);
         for (int i = 0; i < 4; ++i) mbar_init(&pair[i], 2);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -455,194 +456,127 @@ latent_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             for (int t = 0; t < 2; ++t)
                 if (qn[t] > 0) drain_wait(&q_full[t], (qn[t] - 1) & 1u, t0);
             for (uint32_t i = seq > kSlots ? seq - kSlots : 0; i < seq; ++i) drain_wait(&full[i % kSlots], (i / kSlots) & 1u, t0);
-        } else if (warp == 9) {
-            // ------------------------- MMA issuer (the whole warp, one lane issues)
-            // Every value that an MMA takes comes from constants, kernel parameters and
-            // warp-wide reductions, so that it stays in uniform registers.
+        } else if (warp == 9 || warp == 11) {
+            // ------------------------- MMA issuers, one for each query tile (a whole warp, one lane issues)
+            // What a warp's wait or commit takes between two of its MMAs its own MMAs stand still (some 100 and 50
+            // cycles); two warps fill each other's gaps. Every value that an MMA takes comes from constants, kernel
+            // parameters and warp-wide reductions, so that it stays in uniform registers.
+            const int t = __reduce_max_sync(0xffffffffu, warp == 11);
             constexpr uint32_t kIdS = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kTile >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
             const uint32_t id_o = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)((p.D + 15) / 16 * 2) << 17) |
                                   ((uint32_t)(kTile >> 4) << 24);
-            const uint64_t dq = sw128_desc(smem_u32(sQ)), dk = sw128_desc(smem_u32(sKV)), dv = half_desc(smem_u32(sKV));
-            const uint32_t tm = __reduce_max_sync(0xffffffffu, tmem);
-            bool issued = false;
-            uint32_t qn0 = 0, qn1 = 0, pn0 = 0, pn1 = 0;  // phases of q_full and p_full
-            int slot = 0;      // ring slot of the next tile's first chunk
-            uint32_t seq = 0;  // tiles before it
-            auto advance = [&](int chunks) {
-                slot += chunks, ++seq;
-                if (slot >= kSlots) slot -= kSlots;
-            };
+            const uint64_t dq = sw128_desc(smem_u32(sQ + (kDeal ? 0 : t * kQTile))), dk = sw128_desc(smem_u32(sKV));
+            const uint64_t dv = half_desc(smem_u32(sKV));
+            const uint32_t tm = __reduce_max_sync(0xffffffffu, tmem), tS = tm + t * kTile, tO = tm + 2 * kTile + t * kTile;
+            bool issued = false, ok = true;
+            uint32_t qn = 0, pn = 0;  // phases of q_full and p_full
+            int slot = 0;             // ring slot of the next tile's first chunk
+            uint32_t seq = 0;         // tiles before it
             auto place = [&](int at) { return at >= kSlots ? at - kSlots : at; };
-            // The issue queue is shallow: what a wait takes after a batch of MMAs the tensor cores stand still. So the next
-            // batch's barrier is looked at before the last MMAs of this one, and mostly it is complete by then.
-            auto peek = [&](uint64_t* bar, uint32_t parity) { return bar && __all_sync(0xffffffffu, mbar_test_wait(bar, parity)); };
-            auto landed = [&](uint32_t tile, bool ready) {
-                const bool ok = ready || wait_warp(&full[tile % kSlots], (tile / kSlots) & 1u);
+            auto landed = [&] {
+                ok = wait_warp(&full[seq % kSlots], (seq / kSlots) & 1u);
                 tc_fence_after();
                 return ok;
             };
-            // S_t = Q_t K^T with K tile `tile` in the slots from st on; last: the item's last use of Q_t (kDeal: of the one
-            // Q); free: the tile's last use. Returns what a peek at `bar` on the way found.
-            auto scores = [&](int t, int st, uint32_t tile, bool last, bool free, uint64_t* bar, uint32_t parity) {
-                const uint64_t a = dq + (kDeal ? 0 : (uint64_t)(t * kQTile >> 4));
-                bool ready = false;
+            auto advance = [&](int chunks) {
+                slot = place(slot + chunks);
+                ++seq;
+            };
+            // A tile that this query tile does not read. (It has landed: so its barriers' next phase has not begun.)
+            auto skip = [&](int chunks) {
+                if (!landed()) return;
+                if (lane == 0) mbar_arrive(&done[seq % kSlots]);
+                __syncwarp();
+                advance(chunks);
+            };
+            // S = Q K^T with the next tile; last: the item's last use of Q
+            auto scores = [&](bool last) {
+                if (!landed()) return;
+                if (elect_one()) {
 #pragma unroll
-                for (int c = 0; c < 3; ++c) {
-                    if (c >= k_chunks) break;
-                    if (c == k_chunks - 1) ready = peek(bar, parity);
-                    if (elect_one()) {
+                    for (int c = 0; c < 3; ++c) {
+                        if (c >= k_chunks) break;
                         const int part = c < own_chunks ? own - 64 * c : rope;  // elements of the chunk, or more
-                        const uint64_t b = dk + (uint64_t)((uint32_t)(place(st + c) * kHalf) >> 4);
+                        const uint64_t b = dk + (uint64_t)((uint32_t)(place(slot + c) * kHalf) >> 4);
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             if (16 * i >= part) break;
-                            mma_ss(tm + t * kTile, a + (uint64_t)((c * kHalf + i * 32) >> 4), b + (uint64_t)(i * 32 >> 4), kIdS, c + i != 0);
-                        }
-                        if (c == k_chunks - 1) {
-                            mma_commit(&s_full[t]);
-                            if (free) mma_commit(&done[tile % kSlots]);
-                            if (last) mma_commit(&q_empty[kDeal ? 0 : t]);
+                            mma_ss(tS, dq + (uint64_t)((c * kHalf + i * 32) >> 4), b + (uint64_t)(i * 32 >> 4), kIdS, c + i != 0);
                         }
                     }
-                    __syncwarp();
+                    mma_commit(&s_full[t]);
+                    mma_commit(&done[seq % kSlots]);
+                    if (last) mma_commit(&q_empty[kDeal ? 0 : t]);
                 }
+                __syncwarp();
                 issued = true;
-                return ready;
+                advance(k_chunks);
             };
-            // O_t += P_t V with V tile `tile` in the slots from st on; the same
-            auto values = [&](int t, int st, uint32_t tile, bool first, bool last, bool free, uint64_t* bar, uint32_t parity) {
-                bool ready = false;
+            // O += P V with the next tile
+            auto values = [&](bool first, bool last) {
+                if (!landed()) return;
+                ok = wait_warp(&p_full[t], pn++ & 1u);
+                if (!ok) return;
+                tc_fence_after();
+                if (elect_one()) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    if (h == 1) ready = peek(bar, parity);
-                    if (elect_one()) {
-                        const uint64_t b = dv + (uint64_t)((uint32_t)(place(st + h) * kHalf) >> 4);
+                    for (int h = 0; h < 2; ++h) {
+                        const uint64_t b = dv + (uint64_t)((uint32_t)(place(slot + h) * kHalf) >> 4);
 #pragma unroll
                         for (int c = 0; c < 4; ++c)  // 16 keys: 8 columns of P, 2 KB of V
-                            mma_ts(tm + 2 * kTile + t * kTile, tm + t * kTile + 8 * (4 * h + c), b + (uint64_t)(c * 2048 >> 4), id_o,
-                                   h + c != 0 || !first);
-                        if (h == 1) {
-                            if (free) mma_commit(&done[tile % kSlots]);
-                            if (last) mma_commit(&o_full[t]);
-                        }
+                            mma_ts(tO, tS + 8 * (4 * h + c), b + (uint64_t)(c * 2048 >> 4), id_o, h + c != 0 || !first);
                     }
-                    __syncwarp();
+                    mma_commit(&done[seq % kSlots]);
+                    if (last) mma_commit(&o_full[t]);
                 }
-                return ready;
+                __syncwarp();
+                advance(2);
             };
-            auto bar_of = [&](bool there, uint32_t tile) { return there ? &full[tile % kSlots] : nullptr; };
-            auto parity_of = [&](uint32_t tile) { return (tile / kSlots) & 1u; };
-            for (int k = 0;; ++k) {
-                if (!wait_warp(&w_full[k & 1], (uint32_t)(k >> 1) & 1u)) break;
+            for (int k = 0; ok; ++k) {
+                ok = wait_warp(&w_full[k & 1], (uint32_t)(k >> 1) & 1u);
+                if (!ok) break;
                 const int n0 = __reduce_max_sync(0xffffffffu, work_slots[k & 1].n[0]);
                 const int n1 = __reduce_max_sync(0xffffffffu, work_slots[k & 1].n[1]);
                 const int end = __reduce_max_sync(0xffffffffu, work_slots[k & 1].end);
                 if (lane == 0) mbar_arrive(&w_empty[k & 1]);
                 if (end) break;
-                const int n_max = max(n0, n1);
-                if (n_max == 0) continue;
-                if constexpr (kDeal) {
-                    const int n = n0 + n1;
-                    bool ok = wait_warp(&q_full[0], qn0++ & 1u), ready = false;
-                    for (int i = 0; i < min(n, 2) && ok; ++i) {
-                        ok = landed(seq, false);
-                        if (!ok) break;
-                        scores(i, slot, seq, i + 1 == n, true, nullptr, 0);
-                        advance(k_chunks);
+                const int mine = t ? n1 : n0, n = kDeal ? n0 + n1 : max(n0, n1);
+                if (n == 0) continue;
+                if (kDeal || mine > 0) ok = wait_warp(&q_full[kDeal ? 0 : t], qn++ & 1u);
+                if (kDeal) {
+                    if (mine == 0) {
+                        if (lane == 0) mbar_arrive(&q_empty[0]);
+                        __syncwarp();
                     }
+                    auto key = [&](int i) {
+                        if ((i & 1) == t) scores(i + 2 >= n);
+                        else skip(k_chunks);
+                    };
+                    for (int i = 0; i < min(n, 2) && ok; ++i) key(i);
                     for (int i = 0; i < n && ok; ++i) {
-                        const int t = i & 1;
-                        ok = ready || wait_warp(&p_full[t], (t ? pn1 : pn0) & 1u);
-                        if (!ok) break;
-                        if (t) ++pn1;
-                        else ++pn0;
-                        tc_fence_after();
-                        // V_i, then K_i+2
-                        const bool more = i + 2 < n;
-                        ready = values(t, slot, seq, i < 2, !more, true, bar_of(more, seq + 1), parity_of(seq + 1));
-                        advance(2);
-                        if (more) {
-                            ok = landed(seq, ready);
-                            if (!ok) break;
-                            ready = scores(t, slot, seq, i + 3 == n, true, &p_full[t ^ 1], (t ? pn0 : pn1) & 1u);
-                            advance(k_chunks);
-                        }
+                        if ((i & 1) == t) values(i < 2, i + 2 >= n);
+                        else skip(2);
+                        if (ok && i + 2 < n) key(i + 2);
                     }
-                    if (!ok) break;
                     continue;
                 }
-                if (n0 > 0 && !wait_warp(&q_full[0], qn0++ & 1u)) break;
-                if (n1 > 0 && !wait_warp(&q_full[1], qn1++ & 1u)) break;
-                if (!landed(seq, false)) break;
-                if (n0 > 0) scores(0, slot, seq, n0 == 1, n1 == 0, nullptr, 0);
-                if (n1 > 0) scores(1, slot, seq, n1 == 1, true, nullptr, 0);
-                advance(k_chunks);
-                bool ok = true, ready = false;  // ready: the next wait's barrier was complete at the peek
-                for (int j = 0; j < n_max; ++j) {
-                    // V_j from slot sv on, K_j+1 from slot sk on
-                    const int sv = slot;
-                    const uint32_t tv = seq;
-                    advance(2);
-                    const int sk = slot;
-                    const uint32_t tk = seq;
-                    if (j + 1 < n_max) advance(k_chunks);
-                    if (j < n0) {
-                        ok = ready || wait_warp(&p_full[0], pn0 & 1u);
+                for (int j = 0; j < n && ok; ++j) {
+                    if (j == 0) {
+                        if (mine > 0) scores(mine == 1);
+                        else skip(k_chunks);
                         if (!ok) break;
-                        ++pn0;
-                        tc_fence_after();
-                        const bool more = j + 1 < n0;
-                        ready = values(0, sv, tv, j == 0, !more, j >= n1, bar_of(more, tk), parity_of(tk));
-                        if (more) {
-                            ok = landed(tk, ready);
-                            if (!ok) break;
-                            ready = scores(0, sk, tk, j + 2 == n0, j + 1 >= n1, j < n1 ? &p_full[1] : nullptr, pn1 & 1u);
-                        }
                     }
-                    if (j < n1) {
-                        ok = ready || wait_warp(&p_full[1], pn1 & 1u);
-                        if (!ok) break;
-                        ++pn1;
-                        tc_fence_after();
-                        const bool more = j + 1 < n1;
-                        ready = values(1, sv, tv, j == 0, !more, true, bar_of(more, tk), parity_of(tk));
-                        if (more) {
-                            ok = landed(tk, ready);
-                            if (!ok) break;
-                            ready = scores(1, sk, tk, j + 2 == n1, true, j + 1 < n0 ? &p_full[0] : nullptr, pn0 & 1u);
-                        }
-                    }
+                    if (j < mine) values(j == 0, j + 1 == mine);
+                    else skip(2);
+                    if (!ok || j + 1 == n) break;
+                    if (j + 1 < mine) scores(j + 2 == mine);
+                    else skip(k_chunks);
                 }
-                if (!ok) break;
             }
             if (issued) {  // no MMA is in flight when TMEM is released
-                if (elect_one()) mma_commit(drain);
+                if (elect_one()) mma_commit(&drain[t]);
                 __syncwarp();
-                drain_wait(drain, 0);
-            }
-        } else if (warp == 11 && lane == 0) {
-            // ------------------------------------------------------- tile watcher
-            // Waits for the V tiles in the MMA warp's stead. (For K as well, and so that the products of V wait for them:
-            // 2059 us for 16384 tokens of 32 heads.)
-            uint32_t seq = 0, pn[2] = {0, 0};
-            bool ok = true;
-            for (int k = 0; ok; ++k) {
-                if (!wait(&w_full[k & 1], (uint32_t)(k >> 1) & 1u)) break;
-                const int n0 = work_slots[k & 1].n[0], n1 = work_slots[k & 1].n[1], end = work_slots[k & 1].end;
-                mbar_arrive(&w_empty[k & 1]);
-                if (end) break;
-                const int n = kDeal ? n0 + n1 : max(n0, n1);
-                for (int j = 0; j < n && ok; ++j) {
-                    const uint32_t tile = seq + (kDeal && j < n - 1 ? 2 * j + 2 : 2 * j + 1);
-                    ok = wait(&full[tile % kSlots], (tile / kSlots) & 1u);
-                    for (int t = 0; t < 2 && ok; ++t) {
-                        if (kDeal ? t != (j & 1) : j >= (t ? n1 : n0)) continue;
-                        if (pn[t] > 0) ok = wait(&p_full[t], (pn[t] - 1) & 1u);  // one arrival in a phase
-                        ++pn[t];
-                        if (ok) mbar_arrive(&p_full[t]);
-                    }
-                }
-                seq += 2 * n;
+                drain_wait(&drain[t], 0);
             }
         }
     }
