@@ -3,25 +3,27 @@
 // the key axis (Walk).
 //
 // A cached row serves every head, as key whole and as value in its first R elements, so
-// a tile of 128 rows is loaded once and enters both products from the same place in
+// a tile of 64 rows is loaded once and enters both products from the same place in
 // shared memory. The products are transposed: the keys, and then the latent's elements,
-// are the 128 rows of the MMA and N query rows (token and head; 16, 32 or 64) its
+// are the rows of the MMA and N query rows (token and head; 16, 32 or 64) its
 // columns, because the sums of 128 heads would fill all of TMEM (128 lanes x 512 fp32)
-// and leave no place for scores. Per tile of 128 keys:
-//   S^T = K Q^T      K-major tiles of 64 elements; N columns of TMEM, a lane is a key
-//   P^T = exp2(scale S^T - m)   a thread has one key and half of the columns
-//   O^T += C^T P^T   the same tiles, read MN-major; P^T in shared memory, in the place of
+// and leave no place for scores. Per tile of 64 keys:
+//   S^T = K Q^T      K-major tiles of 64 elements, M 64: 16 keys in 16 lanes of each warp's quarter
+//   P^T = exp2(scale S^T - m)   a thread has two keys and every fourth pair of half of the columns
+//   O^T += C^T P^T   the same tiles, read MN-major, M 128; P^T in shared memory, in the place of
 //                    the rotary keys, which the second product does not need
+// The scores of the next tile are multiplied while the softmax of this one runs, and the
+// tile after that is on its way: queries of 64 rows and two tiles fill shared memory.
 // The columns' maxima m are shared by all keys of a tile. They come from a segment's first
 // tile and are raised, and O^T rescaled, only when a score passes its column's by 2^16:
-// fp32 and bf16 weights lose nothing by that (their exponents reach 2^127), and tiles
-// need no exchange between threads. The thread that finds such a score leaves a note, the
-// MMA warp, which meets all of them anyway, sends the tile back once more.
-// A thread sums its own key's weights, and the threads' sums are joined at the end of a segment.
+// fp32 and bf16 weights lose nothing by that (their exponents reach 2^127). The four warps
+// of half of the columns tell each other of such a score while the weights are computed, which
+// is done once more then. A thread sums its own keys' weights; the threads' sums are joined at
+// the end of a segment.
 // More rows than N: up to kMostSides CTAs beside each other take the same keys with N rows
 // each, at about the same time, so that HBM is read once.
 // Warps 0-3 and 4-7: softmax of the first and second half of the columns, queries and
-// results; warp 8: TMA; warp 9: MMA.
+// results; warp 8: TMA; warps 9 and 10: MMA.
 //
 // P is rounded to bf16, an error of up to 2^-8 of each weight beside the result's own
 // rounding: the MMA takes both operands in one 16-bit type, and the cache is bf16. The
@@ -42,9 +44,9 @@ namespace {
 
 using namespace tc;
 
-constexpr int kKeys = 128;                // keys of a tile
-constexpr int kThreads = 320;
-constexpr int kChunk = kKeys * 128;       // bytes of 128 rows x 64 elements
+constexpr int kKeys = 64;                 // keys of a tile
+constexpr int kThreads = 352;
+constexpr int kChunk = kKeys * 128;       // bytes of 64 rows x 64 elements
 constexpr unsigned kFull = 0xffffffffu;
 constexpr float kGrow = 16.0f;            // log2 of how far a column's maximum may run ahead of m
 constexpr float kMost = 3.402823466e38f;  // -kMost: a maximum of nothing
@@ -54,12 +56,13 @@ constexpr int kMostSides = 8;
 // N: query rows of a CTA. Rings of pairs of chunks (128 latent elements) and of the rotary chunks.
 template <int N>
 struct Shape {
-    static constexpr int COLS = N / 2;                       // columns of a thread
-    static constexpr int PAIRS = N == 64 ? 4 : 5, TAILS = N == 16 ? 2 : 1;
+    static constexpr int COLS = N / 2;                       // columns of a warp
+    static constexpr int G = COLS / 8;                       // groups of eight: a thread has two of each, of two keys
+    static constexpr int PAIRS = N == 64 ? 8 : N == 32 ? 10 : 11, TAILS = N == 64 ? 2 : 3;
     static constexpr int Q = 9 * N * 128;
     static constexpr int BODY = Q + PAIRS * 2 * kChunk + TAILS * kChunk;
     static constexpr int BYTES = 1024 + BODY;
-    static_assert(BYTES + 4096 <= 227 * 1024, "shared memory");
+    static_assert(BYTES + 4096 <= 227 * 1024 && 8 * N <= 512, "shared and tensor memory");
 };
 
 template <int C>
@@ -84,6 +87,33 @@ __device__ __forceinline__ void tmem_load(uint32_t taddr, uint32_t (&r)[C]) {
                      : "memory");
     }
 }
+// C columns of 16 lanes: this thread's u[4 g ..] are columns 8 g + 2 (lane % 4) + {0, 1} of row lane / 4, then of row
+// lane / 4 + 8.
+template <int C>
+__device__ __forceinline__ void tmem_load16(uint32_t taddr, uint32_t (&r)[C / 2]) {
+    if constexpr (C == 32) {
+        asm volatile(
+            "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+            : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+              "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+            : "r"(taddr));
+    } else if constexpr (C == 16) {
+        asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                     : "r"(taddr));
+    } else {
+        static_assert(C == 8, "columns");
+        asm volatile("tcgen05.ld.sync.aligned.16x256b.x1.b32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                     : "r"(taddr));
+    }
+}
+template <int n>
+__device__ __forceinline__ void pin(uint32_t (&r)[n]) {  // no use moves above the wait before
+#pragma unroll
+    for (int i = 0; i < n; ++i) asm volatile("" : "+r"(r[i]));
+}
+
 template <int C>
 __device__ __forceinline__ void tmem_store(uint32_t taddr, const uint32_t (&r)[C]) {
     if constexpr (C == 32) {
@@ -153,51 +183,57 @@ __global__ void __launch_bounds__(kThreads, 1)
 latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_constant__ Params pp) {
     pdl_enter();
     using L = Shape<N>;
-    constexpr int COLS = L::COLS, PAIRS = L::PAIRS, TAILS = L::TAILS;
+    constexpr int COLS = L::COLS, G = L::G, PAIRS = L::PAIRS, TAILS = L::TAILS;
     const AttnProblem& p = pp.l.a;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* sq = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint8_t* pairs = sq + L::Q;
     uint8_t* tails = pairs + PAIRS * 2 * kChunk;
-    __shared__ uint64_t bars[2 * (PAIRS + TAILS) + 12];
+    __shared__ uint64_t bars[2 * (PAIRS + TAILS) + 14];
     __shared__ Job jobs[2];
     uint64_t* full = bars;              // a pair landed
     uint64_t* empty = full + PAIRS;     // the products that read it finished
     uint64_t* tfull = empty + PAIRS;
     uint64_t* tempty = tfull + TAILS;
     uint64_t* q_full = tempty + TAILS;  // the queries are in shared memory
-    uint64_t* s_full = q_full + 1;
-    uint64_t* p_full = s_full + 1;      // P is written, O rescaled, unseen rows are 0
+    uint64_t* s_full = q_full + 1;      // scores of even and odd tiles
+    uint64_t* p_full = s_full + 2;      // P is written, O rescaled, unseen rows are 0
     uint64_t* o_full = p_full + 1;      // O holds this tile too
     uint64_t* drain = o_full + 1;
-    uint64_t* half = drain + 1;         // the four warps of half of the columns meet
+    uint64_t* half = drain + 2;         // the four warps of half of the columns meet
     uint64_t* both = half + 2;          // all eight
     uint64_t* j_full = both + 1;        // a job is in its slot
     uint64_t* j_empty = j_full + 2;     // every role has read it
     __shared__ uint32_t tmem_slot, good[TAILS];  // good: pages of the tile that are in the pool
     __shared__ int abort_word, row_hi[N];
-    __shared__ uint32_t raised, again;  // a score far above its maximum was found in tile .. - 1; that tile is to be done once more
-    __shared__ float sums[8][COLS];
+    __shared__ uint32_t raised[2];      // tile number (from 1 on) in which a score far above its maximum was found
+    __shared__ uint32_t poisoned[kKeys];  // the same for a key that holds what is no number
+    __shared__ __align__(8) float sums[8][COLS];
     __shared__ __align__(16) float low[N], factor[N];  // the columns' -m, and what a raise multiplies by
     __shared__ int64_t plan[plan_words(kThreads)];
     volatile int* abort_flag = &abort_word;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int R = p.D, pairs_of_tile = R / 128, W = pp.l.K;
+    const bool two = pairs_of_tile > 1 || W > R;  // scores in two parts
+    const int box_log2 = min(p.page_log2, 6), per_tile = kKeys >> box_log2;  // rows of a copy, copies of a chunk
     const int share = blockIdx.x / pp.sides, side = blockIdx.x - share * pp.sides;
     if (tid == 0) {
         for (int i = 0; i < PAIRS; ++i) mbar_init(&full[i], 1), mbar_init(&empty[i], 1);
-        for (int i = 0; i < TAILS; ++i) mbar_init(&tfull[i], 1), mbar_init(&tempty[i], 1);
+        for (int i = 0; i < TAILS; ++i) mbar_init(&tfull[i], 1), mbar_init(&tempty[i], 2);
         mbar_init(q_full, 8);
-        mbar_init(s_full, 1);
+        mbar_init(&s_full[0], 2);   // (here and below: both MMA warps)
+        mbar_init(&s_full[1], 2);
         mbar_init(p_full, 8);
-        mbar_init(o_full, 1);
-        mbar_init(drain, 1);
+        mbar_init(o_full, 2);
+        mbar_init(&drain[0], 1);
+        mbar_init(&drain[1], 1);
         mbar_init(&half[0], 4);
         mbar_init(&half[1], 4);
         mbar_init(both, 8);
-        for (int i = 0; i < 2; ++i) mbar_init(&j_full[i], 1), mbar_init(&j_empty[i], 9);  // (softmax warps, MMA)
+        for (int i = 0; i < 2; ++i) mbar_init(&j_full[i], 1), mbar_init(&j_empty[i], 10);  // (softmax warps, MMA warps)
         abort_word = 0;
-        raised = again = 0;
+        raised[0] = raised[1] = 0;
+        for (int i = 0; i < kKeys; ++i) poisoned[i] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 9) {
@@ -209,7 +245,7 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
     const bool any = __any_sync(kFull, walk.begin(p, share, plan));
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = tmem_slot, tS = tmem, tO = tmem + 128;  // O: pairs_of_tile times N columns
+    const uint32_t tmem = tmem_slot, tS = tmem, tO = tmem + 4 * N;  // S: two parts for even and odd tiles; O: pairs_of_tile times N columns
     auto wait_warp = [&](uint64_t* bar, uint32_t parity) { return warp_wait(bar, parity, abort_flag, p.err, pp.wait_limit_ns); };
 
     if (!any) {
@@ -219,10 +255,11 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
         const int wg = warp >> 2, r = (warp & 3) * 32 + lane, c0 = wg * COLS, wt = tid & 127;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t mS = tS + lanes + c0, mO = tO + lanes + c0;
+        const int key_a = (warp & 3) * 16 + (lane >> 2), col = c0 + 2 * (lane & 3);  // keys key_a, key_a + 8; columns col + 8 g + {0, 1}
         const float scale = p.scale_log2;
         uint32_t n_tiles = 0;  // so far
         int tail = 0, pair = 0;
-        uint32_t tphase = 0, sn = 0;
+        uint32_t tphase = 0;
         uint32_t meets = 0, meets_both = 0;
         // (mbarriers, not bar.sync: a warp whose wait gave up does not come)
         auto meet = [&](uint64_t* bar, uint32_t& n) {
@@ -266,141 +303,160 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
                 ok = meet(&half[wg], meets);
                 if (!ok) break;
             }
-            uint64_t l[COLS / 2];  // sums of the weights of this thread's keys, two columns each
+            uint64_t l[G];  // sums of the weights of this thread's keys
 #pragma unroll
-            for (int c = 0; c < COLS / 2; ++c) l[c] = pack2(0.0f, 0.0f);
-            if (x.tiles > 0) ok = wait_warp(s_full, sn++ & 1u);
+            for (int c = 0; c < G; ++c) l[c] = pack2(0.0f, 0.0f);
             for (int t = 0; t < x.tiles && ok; ++t) {
-                const int key = x.key0 + t * kKeys + r;
-                ok = wait_warp(&tfull[tail], tphase);
+                ok = wait_warp(&s_full[n_tiles & 1u], (n_tiles >> 1) & 1u) && wait_warp(&tfull[tail], tphase);
                 if (!ok) break;
+                tc_fence_after();
+                uint32_t u[2 * G * 2];
+                const uint32_t mine_s = mS + (n_tiles & 1u) * 2 * N;
+                auto load = [&] {
+                    tmem_load16<COLS>(mine_s, u);
+                    uint32_t v[2 * G * 2];
+                    if (two) tmem_load16<COLS>(mine_s + N, v);
+                    ld_wait();
+                    pin(u);
+                    if (!two) return;
+                    pin(v);
+#pragma unroll
+                    for (int c = 0; c < 4 * G; ++c) u[c] = __float_as_uint(__uint_as_float(u[c]) + __uint_as_float(v[c]));
+                };
+                load();
+                const int key0 = x.key0 + t * kKeys;
                 const uint32_t pages = *const_cast<volatile uint32_t*>(&good[tail]);
-                const bool all = x.key0 + (t + 1) * kKeys - 1 <= x.all_hi && pages == (1u << (kKeys >> p.page_log2)) - 1u;
-                const bool mine = pages >> (r >> p.page_log2) & 1u;
-                bool poison = false;
+                const bool all = key0 + kKeys - 1 <= x.all_hi && pages == (1u << per_tile) - 1u;
+                bool there[2] = {true, true}, poison[2] = {false, false};  // of the two keys
                 if (!all) {
-                    auto at = [&](int i) {  // piece i of this key's latent
+#pragma unroll
+                    for (int z = 0; z < 2; ++z) there[z] = pages >> ((key_a + 8 * z) >> box_log2) & 1u;
+                    // four threads for a key: what is no number where some rows see it and others do not, rows that none sees
+                    const int k = tid >> 2, key = key0 + k;
+                    auto at = [&](int i) {  // piece i of its latent
                         int slot = pair + (i >> 4);
                         if (slot >= PAIRS) slot -= PAIRS;
-                        return reinterpret_cast<uint4*>(pairs + slot * 2 * kChunk + (i >> 3 & 1) * kChunk + sw128_off(r, i & 7));
+                        return reinterpret_cast<uint4*>(pairs + slot * 2 * kChunk + (i >> 3 & 1) * kChunk + sw128_off(k, i & 7));
                     };
-                    if (mine && key > x.all_hi && key <= x.most_hi) {
-                        for (int i = 0; i < R / 8; ++i) {
+                    if (key > x.all_hi && key <= x.most_hi) {
+                        bool bad = false;
+                        for (int i = tid & 3; i < R / 8; i += 4) {
                             const uint4 v = *at(i);
-                            poison = poison || (__vcmpgeu2(v.x & 0x7fff7fffu, 0x7f807f80u) | __vcmpgeu2(v.y & 0x7fff7fffu, 0x7f807f80u) |
-                                                __vcmpgeu2(v.z & 0x7fff7fffu, 0x7f807f80u) | __vcmpgeu2(v.w & 0x7fff7fffu, 0x7f807f80u)) != 0;
+                            bad = bad || (__vcmpgeu2(v.x & 0x7fff7fffu, 0x7f807f80u) | __vcmpgeu2(v.y & 0x7fff7fffu, 0x7f807f80u) |
+                                          __vcmpgeu2(v.z & 0x7fff7fffu, 0x7f807f80u) | __vcmpgeu2(v.w & 0x7fff7fffu, 0x7f807f80u)) != 0;
                         }
+                        if (bad) *const_cast<volatile uint32_t*>(&poisoned[k]) = n_tiles + 1;
                     }
-                    ok = meet(both, meets_both);  // both threads of the key have looked
+                    ok = meet(both, meets_both);
                     if (!ok) break;
-                    if (poison || key > x.most_hi)
-                        for (int i = wg * (R / 16); i < (wg + 1) * (R / 16); ++i) *at(i) = make_uint4(0, 0, 0, 0);
+                    if (key > x.most_hi || *const_cast<volatile uint32_t*>(&poisoned[k]) == n_tiles + 1)
+                        for (int i = tid & 3; i < R / 8; i += 4) *at(i) = make_uint4(0, 0, 0, 0);
+#pragma unroll
+                    for (int z = 0; z < 2; ++z) poison[z] = *const_cast<volatile uint32_t*>(&poisoned[key_a + 8 * z]) == n_tiles + 1;
                 }
+                auto unseen = [&](int c, int z) { return !all && (!there[z] || key0 + key_a + 8 * z > row_hi[c]); };
                 uint8_t* dst = tails + tail * kChunk;
-                // One pass over the tile's scores. raise: the maxima are brought up to them first (the first tile, and
-                // where a pass before found one too far above); else, whether one is. count: the weights enter the sums.
-                auto pass = [&](bool raise, bool count) {
-                    tc_fence_after();
-                    uint32_t u[COLS];
-                    tmem_load<COLS>(mS, u);
-                    auto unseen = [&](int c) { return !all && (!mine || key > row_hi[c0 + c]); };
-                    if (raise) {
-                        // each column's largest score: over the warp's keys by a transposing maximum (lane: column), then
-                        // over the four warps
-                        float best[COLS];
+                // The maxima are brought up to this tile's scores, the sums so far to the maxima.
+                auto raise = [&] {
 #pragma unroll
-                        for (int c = 0; c < COLS; ++c) best[c] = unseen(c) ? -kMost : fmaxf(__uint_as_float(u[c]) * scale, -kMost);
+                    for (int g = 0; g < G; ++g)
 #pragma unroll
-                        for (int d = 16; d >= COLS; d >>= 1)
+                        for (int e = 0; e < 2; ++e) {
+                            float best = -kMost;
 #pragma unroll
-                            for (int c = 0; c < COLS; ++c) best[c] = fmaxf(best[c], __shfl_xor_sync(kFull, best[c], d));
+                            for (int z = 0; z < 2; ++z)
+                                if (!unseen(col + 8 * g + e, z)) best = fmaxf(best, __uint_as_float(u[4 * g + 2 * z + e]) * scale);
 #pragma unroll
-                        for (int d = COLS / 2; d; d >>= 1)
-#pragma unroll
-                            for (int c = 0; c < d; ++c) {
-                                const bool up = lane & d;
-                                const float give = up ? best[c] : best[c + d], keep = up ? best[c + d] : best[c];
-                                best[c] = fmaxf(keep, __shfl_xor_sync(kFull, give, d));
-                            }
-                        if (lane < COLS) sums[warp][lane] = best[0];
-                        ok = meet(&half[wg], meets);
-                        if (!ok) return false;
-                        if (wt < COLS) {
-                            float m = -low[c0 + wt];
-#pragma unroll
-                            for (int w = 0; w < 4; ++w) m = fmaxf(m, sums[4 * wg + w][wt]);
-                            factor[c0 + wt] = ex2(-low[c0 + wt] - m);  // (nothing yet: 0)
-                            low[c0 + wt] = -m;
+                            for (int d = 4; d < 32; d <<= 1) best = fmaxf(best, __shfl_xor_sync(kFull, best, d));
+                            if (lane < 4) sums[warp][8 * g + 2 * lane + e] = best;
                         }
-                        ok = meet(&half[wg], meets) && (t == 0 || wait_warp(o_full, (n_tiles - 1) & 1u));
-                        if (!ok) return false;
-                        if (t > 0) {
-                            tc_fence_after();
+                    ok = meet(&half[wg], meets);
+                    if (!ok) return;
+                    if (wt < COLS) {
+                        float m = -low[c0 + wt];
 #pragma unroll
-                            for (int c = 0; c < COLS / 2; ++c) {
-                                const float2 f = *reinterpret_cast<const float2*>(&factor[c0 + 2 * c]);
-                                l[c] = fma2(l[c], pack2(f.x, f.y), pack2(0.0f, 0.0f));
-                            }
-#pragma unroll 1
-                            for (int i = 0; i < pairs_of_tile; ++i) {
-                                uint32_t o[COLS];
-                                tmem_load<COLS>(mO + i * N, o);
-#pragma unroll
-                                for (int c = 0; c < COLS; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * factor[c0 + c]);
-                                tmem_store<COLS>(mO + i * N, o);
-                            }
-                            st_wait();
-                        }
+                        for (int w = 0; w < 4; ++w) m = fmaxf(m, sums[4 * wg + w][wt]);
+                        factor[c0 + wt] = ex2(-low[c0 + wt] - m);  // (nothing yet: 0)
+                        low[c0 + wt] = -m;
                     }
+                    ok = meet(&half[wg], meets);
+                    if (!ok || t == 0) return;
+                    ok = wait_warp(o_full, (n_tiles - 1) & 1u);
+                    if (!ok) return;
+                    tc_fence_after();
+#pragma unroll
+                    for (int g = 0; g < G; ++g) {
+                        const float2 f = *reinterpret_cast<const float2*>(&factor[col + 8 * g]);
+                        l[g] = fma2(l[g], pack2(f.x, f.y), pack2(0.0f, 0.0f));
+                    }
+#pragma unroll 1
+                    for (int i = 0; i < pairs_of_tile; ++i) {
+                        uint32_t o[COLS];
+                        tmem_load<COLS>(mO + i * N, o);
+#pragma unroll
+                        for (int c = 0; c < COLS; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * factor[c0 + c]);
+                        tmem_store<COLS>(mO + i * N, o);
+                    }
+                    st_wait();
+                };
+                // Scores relative to the maxima, base 2, and the largest of them.
+                float r2[4 * G];
+                auto relative = [&] {
                     const uint64_t sc2 = pack2(scale, scale);
                     float most = -kMost;
 #pragma unroll
-                    for (int c = 0; c < COLS; c += 4) {
-                        const float4 m = *reinterpret_cast<const float4*>(&low[c0 + c]);
-                        float2 a = unpack2(fma2(pack2(__uint_as_float(u[c]), __uint_as_float(u[c + 1])), sc2, pack2(m.x, m.y)));
-                        float2 b = unpack2(fma2(pack2(__uint_as_float(u[c + 2]), __uint_as_float(u[c + 3])), sc2, pack2(m.z, m.w)));
-                        if (!all) {
-                            a.x = unseen(c) ? neg_inf() : a.x, a.y = unseen(c + 1) ? neg_inf() : a.y;
-                            b.x = unseen(c + 2) ? neg_inf() : b.x, b.y = unseen(c + 3) ? neg_inf() : b.y;
-                        }
-                        most = max3(most, fmaxf(a.x, a.y), fmaxf(b.x, b.y));
-                        u[c] = __float_as_uint(a.x), u[c + 1] = __float_as_uint(a.y);
-                        u[c + 2] = __float_as_uint(b.x), u[c + 3] = __float_as_uint(b.y);
-                    }
-                    const bool over = __any_sync(kFull, most > kGrow) && !raise;
-                    if (over) {
-                        if (lane == 0) *const_cast<volatile uint32_t*>(&raised) = n_tiles + 1;
-                    } else {
+                    for (int g = 0; g < G; ++g) {
+                        const float2 m = *reinterpret_cast<const float2*>(&low[col + 8 * g]);
 #pragma unroll
-                        for (int c = 0; c < COLS; c += 8) {
-                            uint32_t w[4];
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const int k = c + 2 * i;
-                                float e0 = ex2(__uint_as_float(u[k])), e1 = ex2(__uint_as_float(u[k + 1]));
-                                if (poison) {
-                                    if (key <= row_hi[c0 + k]) e0 = __uint_as_float(0x7fc00000u);
-                                    if (key <= row_hi[c0 + k + 1]) e1 = __uint_as_float(0x7fc00000u);
-                                }
-                                if (count) l[k >> 1] = add2(l[k >> 1], pack2(e0, e1));
-                                w[i] = pack_bf16x2(e0, e1);
-                            }
-                            *reinterpret_cast<uint4*>(dst + sw128_off(r, (c0 + c) >> 3)) = make_uint4(w[0], w[1], w[2], w[3]);
+                        for (int z = 0; z < 2; ++z) {
+                            float2 a = unpack2(fma2(pack2(__uint_as_float(u[4 * g + 2 * z]), __uint_as_float(u[4 * g + 2 * z + 1])), sc2, pack2(m.x, m.y)));
+                            if (unseen(col + 8 * g, z)) a.x = neg_inf();
+                            if (unseen(col + 8 * g + 1, z)) a.y = neg_inf();
+                            most = max3(most, a.x, a.y);
+                            r2[4 * g + 2 * z] = a.x, r2[4 * g + 2 * z + 1] = a.y;
                         }
-                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     }
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(p_full);
-                    return over;
+                    return most;
                 };
-                const bool over = pass(t == 0, true);
-                // the next tile's scores, or the last tile's results, or this tile once more
-                ok = ok && wait_warp(s_full, sn++ & 1u);
-                if (ok && *const_cast<volatile uint32_t*>(&again) == n_tiles + 1) {
-                    pass(true, over);
-                    ok = ok && wait_warp(s_full, sn++ & 1u);
+                auto weights = [&](bool count) {
+#pragma unroll
+                    for (int g = 0; g < G; ++g)
+#pragma unroll
+                        for (int z = 0; z < 2; ++z) {
+                            float e0 = ex2(r2[4 * g + 2 * z]), e1 = ex2(r2[4 * g + 2 * z + 1]);
+                            if (poison[z]) {
+                                if (key0 + key_a + 8 * z <= row_hi[col + 8 * g]) e0 = __uint_as_float(0x7fc00000u);
+                                if (key0 + key_a + 8 * z <= row_hi[col + 8 * g + 1]) e1 = __uint_as_float(0x7fc00000u);
+                            }
+                            if (count) l[g] = add2(l[g], pack2(e0, e1));
+                            *reinterpret_cast<uint32_t*>(dst + sw128_off(key_a + 8 * z, (c0 >> 3) + g) + 4 * (lane & 3)) = pack_bf16x2(e0, e1);
+                        }
+                };
+                if (t == 0) {
+                    raise();
+                    if (!ok) break;
+                    relative();
+                    weights(true);
+                } else {
+                    const bool over = __any_sync(kFull, relative() > kGrow);
+                    if (lane == 0) {
+                        if (over) *const_cast<volatile uint32_t*>(&raised[wg]) = n_tiles + 1;
+                        mbar_arrive(&half[wg]);
+                    }
+                    if (!over) weights(true);
+                    ok = wait_warp(&half[wg], meets++ & 1u);
+                    if (!ok) break;
+                    if (*const_cast<volatile uint32_t*>(&raised[wg]) == n_tiles + 1) {
+                        raise();
+                        if (!ok) break;
+                        relative();
+                        weights(over);  // (the others have counted theirs, rescaled since)
+                    }
                 }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p_full);
                 ++n_tiles;
                 pair += pairs_of_tile;
                 while (pair >= PAIRS) pair -= PAIRS;
@@ -409,23 +465,18 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
             if (!ok) break;
             // ------------------------------------------------------------ result
             if (x.rows > 0) {
-                // each column's sum of weights over the keys, a transposing sum within the warp first
-                float lc[COLS];
+                // each column's sum of weights over the keys
 #pragma unroll
-                for (int c = 0; c < COLS / 2; ++c) lc[2 * c] = unpack2(l[c]).x, lc[2 * c + 1] = unpack2(l[c]).y;
+                for (int g = 0; g < G; ++g) {
+                    float2 v = unpack2(l[g]);
 #pragma unroll
-                for (int d = 16; d >= COLS; d >>= 1)
-#pragma unroll
-                    for (int c = 0; c < COLS; ++c) lc[c] += __shfl_xor_sync(kFull, lc[c], d);
-#pragma unroll
-                for (int d = COLS / 2; d; d >>= 1)
-#pragma unroll
-                    for (int c = 0; c < d; ++c) {
-                        const bool up = lane & d;
-                        const float give = up ? lc[c] : lc[c + d], keep = up ? lc[c + d] : lc[c];
-                        lc[c] = keep + __shfl_xor_sync(kFull, give, d);
-                    }
-                if (lane < COLS) sums[warp][lane] = lc[0];
+                    for (int d = 4; d < 32; d <<= 1) v.x += __shfl_xor_sync(kFull, v.x, d), v.y += __shfl_xor_sync(kFull, v.y, d);
+                    if (lane < 4) *reinterpret_cast<float2*>(&sums[warp][8 * g + 2 * lane]) = v;
+                }
+                if (x.tiles > 0) {
+                    ok = wait_warp(o_full, (n_tiles - 1) & 1u);
+                    if (!ok) break;
+                }
                 tc_fence_after();
                 ok = meet(&half[wg], meets);
                 if (!ok) break;
@@ -484,7 +535,7 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
         uint32_t inflight = 0, par = 0, tinflight = 0, tpar = 0;
         int slot = 0, tail = 0;
         uint32_t phase = 0, tphase = 0;
-        const int per_tile = kKeys >> p.page_log2, box = p.page * 128;
+        const int box = 128 << box_log2;
         const int nowhere = p.n_pages << p.page_log2;  // rows past the pool: the copy brings zeros
         bool ok = true, more = true;
         for (int j = 0; ok; ++j) {
@@ -501,16 +552,16 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
             if (!more) break;
             const int32_t* ids = p.page_table + (int64_t)x.b * p.max_pages;
             auto first_row = [&](int t) {  // of this lane's page of tile t
-                const int at = x.key0 + t * kKeys + (lane << p.page_log2);
+                const int at = x.key0 + t * kKeys + (lane << box_log2);
                 if (lane >= per_tile || t >= x.tiles || at > x.most_hi) return nowhere;
                 const int id = ids[at >> p.page_log2];
-                return id >= 0 && id < p.n_pages ? id << p.page_log2 : nowhere;
+                return id >= 0 && id < p.n_pages ? (id << p.page_log2) + (at & (p.page - 1)) : nowhere;
             };
             int row = first_row(0);
             for (int t = 0; t < x.tiles && ok; ++t) {
                 const int ahead = first_row(t + 1);
                 const uint32_t mask = __ballot_sync(kFull, row != nowhere);
-                // lane: page lane % per_tile of the first or second chunk of a pair
+                // lane: copy lane % per_tile of the first or second chunk of a pair
                 const int from = __shfl_sync(kFull, row, lane & (per_tile - 1)), chunk = lane / per_tile;
                 for (int i = 0; i < pairs_of_tile; ++i) {
                     ok = wait_warp(&empty[slot], phase ^ 1);
@@ -548,15 +599,19 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
                 if ((tinflight >> i) & 1u) drain_wait(&tfull[i], (tpar >> i) & 1u, t0);
         }
     } else {
-        // ------------------------- MMA issuer (the whole warp, one lane issues)
-        constexpr uint32_t kId = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(kKeys >> 4) << 24);
-        constexpr uint32_t kIdO = kId | (1u << 15) | (1u << 16);  // both operands MN-major
-        const uint32_t tm = __reduce_max_sync(kFull, tmem);
+        // ------------------------- MMA issuers (two whole warps, one lane of each issues)
+        // What a warp's wait or commit takes between two of its MMAs its own MMAs stand still (some 100 and 50 cycles); two
+        // warps fill each other's gaps. Warp 9 has the pairs 0, 2, .. of a tile, warp 10 the pairs 1, 3, .. and the rotary
+        // chunk: two parts of the scores, and row tiles of O^T of their own.
+        const int w2 = __reduce_max_sync(kFull, warp == 10);
+        constexpr uint32_t kId = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | (64u >> 4 << 24);
+        constexpr uint32_t kIdO = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | (128u >> 4 << 24) | (1u << 15) | (1u << 16);  // both operands MN-major
+        const uint32_t tm = __reduce_max_sync(kFull, tmem), tSw = tm + w2 * N;
         const uint64_t dq = sw128_desc(smem_u32(sq)), dk = sw128_desc(smem_u32(pairs)), dt = sw128_desc(smem_u32(tails));
         const uint64_t dv = mn_desc(smem_u32(pairs)), dp = mn_desc(smem_u32(tails));
-        const int tail_steps = (W - R + 15) / 16;
-        int slot = 0, tail = 0;
-        uint32_t phase = 0, tphase = 0, qn = 0, pn = 0, tile = 0;
+        const int tail_steps = w2 ? (W - R + 15) / 16 : 0;
+        int slot = 0, tail = 0, v_slot = 0, v_tail = 0;  // of the tile whose scores, whose values are next
+        uint32_t phase = 0, tphase = 0, qn = 0, pn = 0, scored = 0;
         bool ok = true, issued = false;
         for (int j = 0; ok; ++j) {
             ok = wait_warp(&j_full[j & 1], (uint32_t)(j >> 1) & 1u);
@@ -568,80 +623,72 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
             if (end) break;
             if (tiles <= 0) continue;
             ok = wait_warp(q_full, qn++ & 1u);
-            for (int t = 0; t < tiles && ok; ++t) {
-                const int slot0 = slot;
-                // The issue queue is shallow: what a wait takes after a batch of MMAs the tensor cores stand still. So the
-                // next batch's barrier is looked at before the last MMAs of this one.
-                auto peek = [&](uint64_t* bar, uint32_t parity) { return __all_sync(kFull, mbar_test_wait(bar, parity)); };
-                bool ready = false;
+            // the scores of the next tile, with its slots from `slot` and `tail` on
+            auto scores = [&] {
+                const uint32_t d = tSw + (scored & 1u) * 2 * N;
                 for (int i = 0; i < pairs_of_tile; ++i) {
-                    ok = ready || wait_warp(&full[slot], phase);
-                    if (!ok) break;
-                    tc_fence_after();
-                    const uint64_t a = dk + (uint64_t)((uint32_t)(slot * 2 * kChunk) >> 4), b = dq + (uint64_t)((uint32_t)(i * 2 * N * 128) >> 4);
+                    if ((i & 1) == w2) {
+                        ok = wait_warp(&full[slot], phase);
+                        if (!ok) return;
+                        tc_fence_after();
+                        if (elect_one()) {
+                            const uint64_t a = dk + (uint64_t)((uint32_t)(slot * 2 * kChunk) >> 4), b = dq + (uint64_t)((uint32_t)(i * 2 * N * 128) >> 4);
+#pragma unroll
+                            for (int k = 0; k < 8; ++k)
+                                mma_ss(d, a + (((k >> 2) * kChunk + (k & 3) * 32) >> 4), b + (((k >> 2) * N * 128 + (k & 3) * 32) >> 4), kId,
+                                       i > 1 || k > 0);
+                        }
+                        __syncwarp();
+                    }
                     if (++slot == PAIRS) slot = 0, phase ^= 1;
-                    if (elect_one()) {
-#pragma unroll
-                        for (int k = 0; k < 5; ++k)
-                            mma_ss(tm, a + (((k >> 2) * kChunk + (k & 3) * 32) >> 4), b + (((k >> 2) * N * 128 + (k & 3) * 32) >> 4), kId, i > 0 || k > 0);
-                    }
-                    __syncwarp();
-                    ready = i + 1 < pairs_of_tile ? peek(&full[slot], phase) : peek(&tfull[tail], tphase);
-                    if (elect_one()) {
-#pragma unroll
-                        for (int k = 5; k < 8; ++k)
-                            mma_ss(tm, a + (((k >> 2) * kChunk + (k & 3) * 32) >> 4), b + (((k >> 2) * N * 128 + (k & 3) * 32) >> 4), kId, 1);
-                    }
-                    __syncwarp();
-                    issued = true;
                 }
-                if (!ok) break;
-                ok = ready || wait_warp(&tfull[tail], tphase);
-                if (!ok) break;
-                tc_fence_after();
+                if (w2) {
+                    ok = wait_warp(&tfull[tail], tphase);
+                    if (!ok) return;
+                    tc_fence_after();
+                }
                 if (elect_one()) {
                     const uint64_t a = dt + (uint64_t)((uint32_t)(tail * kChunk) >> 4), b = dq + (uint64_t)((uint32_t)(pairs_of_tile * 2 * N * 128) >> 4);
-                    for (int k = 0; k < tail_steps; ++k) mma_ss(tm, a + (uint64_t)(k * 2), b + (uint64_t)(k * 2), kId, 1);
-                    mma_commit(s_full);
+                    for (int k = 0; k < tail_steps; ++k) mma_ss(d, a + (uint64_t)(k * 2), b + (uint64_t)(k * 2), kId, pairs_of_tile > 1 || k > 0);
+                    mma_commit(&s_full[scored & 1u]);
                 }
                 __syncwarp();
+                ++scored;
+                issued = true;
+                if (++tail == TAILS) tail = 0, tphase ^= 1;
+            };
+            if (ok) scores();
+            for (int t = 0; t < tiles && ok; ++t) {
+                if (t + 1 < tiles) scores();
+                if (!ok) break;
                 ok = wait_warp(p_full, pn++ & 1u);
                 if (!ok) break;
-                ++tile;
-                if (__any_sync(kFull, *const_cast<volatile uint32_t*>(&raised) == tile)) {
-                    if (lane == 0) {
-                        *const_cast<volatile uint32_t*>(&again) = tile;
-                        mbar_arrive(s_full);
-                    }
-                    __syncwarp();
-                    ok = wait_warp(p_full, pn++ & 1u);
-                    if (!ok) break;
-                }
                 tc_fence_after();
-                int sv = slot0;
                 for (int i = 0; i < pairs_of_tile; ++i) {
-                    if (elect_one()) {
-                        const uint64_t a = dv + (uint64_t)((uint32_t)(sv * 2 * kChunk) >> 4), b = dp + (uint64_t)((uint32_t)(tail * kChunk) >> 4);
+                    if ((i & 1) == w2) {
+                        if (elect_one()) {
+                            const uint64_t a = dv + (uint64_t)((uint32_t)(v_slot * 2 * kChunk) >> 4), b = dp + (uint64_t)((uint32_t)(v_tail * kChunk) >> 4);
 #pragma unroll
-                        for (int k = 0; k < kKeys / 16; ++k)
-                            mma_ss(tm + 128 + i * N, a + (uint64_t)(k * 2048 >> 4), b + (uint64_t)(k * 2048 >> 4), kIdO, t > 0 || k > 0);
-                        mma_commit(&empty[sv]);
-                        if (i == pairs_of_tile - 1) {
-                            mma_commit(&tempty[tail]);
-                            mma_commit(o_full);
-                            if (t == tiles - 1) mma_commit(s_full);
+                            for (int k = 0; k < kKeys / 16; ++k)
+                                mma_ss(tm + 4 * N + i * N, a + (uint64_t)(k * 2048 >> 4), b + (uint64_t)(k * 2048 >> 4), kIdO, t > 0 || k > 0);
+                            mma_commit(&empty[v_slot]);
                         }
+                        __syncwarp();
                     }
-                    __syncwarp();
-                    if (++sv == PAIRS) sv = 0;
+                    if (++v_slot == PAIRS) v_slot = 0;
                 }
-                if (++tail == TAILS) tail = 0, tphase ^= 1;
+                if (elect_one()) {
+                    mma_commit(&tempty[v_tail]);
+                    mma_commit(o_full);
+                }
+                __syncwarp();
+                if (++v_tail == TAILS) v_tail = 0;
             }
         }
         if (issued) {  // no MMA is in flight when TMEM is released
-            if (elect_one()) mma_commit(drain);
+            if (elect_one()) mma_commit(&drain[w2]);
             __syncwarp();
-            drain_wait(drain, 0);
+            drain_wait(&drain[w2], 0);
         }
     }
     tc_fence_before();
@@ -660,10 +707,10 @@ cudaError_t cached_as(LatentProblem p, int sides, cudaStream_t stream) {
     EncodeTiled fn = encode_fn();
     if (!fn) return cudaErrorInvalidValue;
     AttnProblem& a = p.a;
-    // the pool as rows of R + P elements, in boxes of 64 elements (128-byte swizzled, zeros past a row's end) of a page
+    // the pool as rows of R + P elements, in boxes of 64 elements (128-byte swizzled, zeros past a row's end) of a page's rows, up to a tile's
     CUtensorMap map;
     cuuint64_t dims[2] = {(cuuint64_t)p.K, (cuuint64_t)a.n_pages * a.page}, strides[1] = {(cuuint64_t)(2 * p.K)};
-    cuuint32_t box[2] = {64, (cuuint32_t)a.page}, estr[2] = {1, 1};
+    cuuint32_t box[2] = {64, (cuuint32_t)(a.page < kKeys ? a.page : kKeys)}, estr[2] = {1, 1};
     if (fn(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(a.k_pool), dims, strides, box, estr,
            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
