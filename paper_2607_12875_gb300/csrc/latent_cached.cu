@@ -23,7 +23,7 @@
 // More rows than N: up to kMostSides CTAs beside each other take the same keys with N rows
 // each, at about the same time, so that HBM is read once.
 // Warps 0-3 and 4-7: softmax of the first and second half of the columns, queries and
-// results; warp 8: TMA; warps 9 and 10: MMA.
+// results; warp 8: TMA; warps 9 and 10: MMA of the scores and of the values.
 //
 // P is rounded to bf16, an error of up to 2^-8 of each weight beside the result's own
 // rounding: the MMA takes both operands in one 16-bit type, and the cache is bf16. The
@@ -52,6 +52,7 @@ constexpr float kGrow = 16.0f;            // log2 of how far a column's maximum 
 constexpr float kMost = 3.402823466e38f;  // -kMost: a maximum of nothing
 constexpr int kMinBlocks = 1, kTileCost = 0;
 constexpr int kMostSides = 8;
+constexpr int kAhead = 3;                 // tiles that L2 is ahead of the copies
 
 // N: query rows of a CTA. Rings of pairs of chunks (128 latent elements) and of the rotary chunks.
 template <int N>
@@ -62,7 +63,7 @@ struct Shape {
     static constexpr int Q = 9 * N * 128;
     static constexpr int BODY = Q + PAIRS * 2 * kChunk + TAILS * kChunk;
     static constexpr int BYTES = 1024 + BODY;
-    static_assert(BYTES + 4096 <= 227 * 1024 && 8 * N <= 512, "shared and tensor memory");
+    static_assert(BYTES + 4096 <= 227 * 1024 && 6 * N <= 512, "shared and tensor memory");
 };
 
 template <int C>
@@ -180,7 +181,7 @@ struct Params {
 
 template <int N>
 __global__ void __launch_bounds__(kThreads, 1)
-latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_constant__ Params pp) {
+latent_cached_kernel(const __grid_constant__ CUtensorMap latents, const __grid_constant__ CUtensorMap pool, const __grid_constant__ Params pp) {
     pdl_enter();
     using L = Shape<N>;
     constexpr int COLS = L::COLS, G = L::G, PAIRS = L::PAIRS, TAILS = L::TAILS;
@@ -189,7 +190,7 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
     uint8_t* sq = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint8_t* pairs = sq + L::Q;
     uint8_t* tails = pairs + PAIRS * 2 * kChunk;
-    __shared__ uint64_t bars[2 * (PAIRS + TAILS) + 14];
+    __shared__ uint64_t bars[2 * (PAIRS + TAILS) + 15];
     __shared__ Job jobs[2];
     uint64_t* full = bars;              // a pair landed
     uint64_t* empty = full + PAIRS;     // the products that read it finished
@@ -198,7 +199,7 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
     uint64_t* q_full = tempty + TAILS;  // the queries are in shared memory
     uint64_t* s_full = q_full + 1;      // scores of even and odd tiles
     uint64_t* p_full = s_full + 2;      // P is written, O rescaled, unseen rows are 0
-    uint64_t* o_full = p_full + 1;      // O holds this tile too
+    uint64_t* o_full = p_full + 2;      // O holds this tile too
     uint64_t* drain = o_full + 1;
     uint64_t* half = drain + 2;         // the four warps of half of the columns meet
     uint64_t* both = half + 2;          // all eight
@@ -214,17 +215,14 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
     volatile int* abort_flag = &abort_word;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int R = p.D, pairs_of_tile = R / 128, W = pp.l.K;
-    const bool two = pairs_of_tile > 1 || W > R;  // scores in two parts
     const int box_log2 = min(p.page_log2, 6), per_tile = kKeys >> box_log2;  // rows of a copy, copies of a chunk
     const int share = blockIdx.x / pp.sides, side = blockIdx.x - share * pp.sides;
     if (tid == 0) {
         for (int i = 0; i < PAIRS; ++i) mbar_init(&full[i], 1), mbar_init(&empty[i], 1);
-        for (int i = 0; i < TAILS; ++i) mbar_init(&tfull[i], 1), mbar_init(&tempty[i], 2);
+        for (int i = 0; i < TAILS; ++i) mbar_init(&tfull[i], 1), mbar_init(&tempty[i], 1);
         mbar_init(q_full, 8);
-        mbar_init(&s_full[0], 2);   // (here and below: both MMA warps)
-        mbar_init(&s_full[1], 2);
-        mbar_init(p_full, 8);
-        mbar_init(o_full, 2);
+        for (int i = 0; i < 2; ++i) mbar_init(&s_full[i], 1), mbar_init(&p_full[i], 8);
+        mbar_init(o_full, 1);
         mbar_init(&drain[0], 1);
         mbar_init(&drain[1], 1);
         mbar_init(&half[0], 4);
@@ -245,7 +243,7 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
     const bool any = __any_sync(kFull, walk.begin(p, share, plan));
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = tmem_slot, tS = tmem, tO = tmem + 4 * N;  // S: two parts for even and odd tiles; O: pairs_of_tile times N columns
+    const uint32_t tmem = tmem_slot, tS = tmem, tO = tmem + 2 * N;  // S: even and odd tiles; O: pairs_of_tile times N columns
     auto wait_warp = [&](uint64_t* bar, uint32_t parity) { return warp_wait(bar, parity, abort_flag, p.err, pp.wait_limit_ns); };
 
     if (!any) {
@@ -311,19 +309,10 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
                 if (!ok) break;
                 tc_fence_after();
                 uint32_t u[2 * G * 2];
-                const uint32_t mine_s = mS + (n_tiles & 1u) * 2 * N;
-                auto load = [&] {
-                    tmem_load16<COLS>(mine_s, u);
-                    uint32_t v[2 * G * 2];
-                    if (two) tmem_load16<COLS>(mine_s + N, v);
-                    ld_wait();
-                    pin(u);
-                    if (!two) return;
-                    pin(v);
-#pragma unroll
-                    for (int c = 0; c < 4 * G; ++c) u[c] = __float_as_uint(__uint_as_float(u[c]) + __uint_as_float(v[c]));
-                };
-                load();
+                const uint32_t mine_s = mS + (n_tiles & 1u) * N;
+                tmem_load16<COLS>(mine_s, u);
+                ld_wait();
+                pin(u);
                 const int key0 = x.key0 + t * kKeys;
                 const uint32_t pages = *const_cast<volatile uint32_t*>(&good[tail]);
                 const bool all = key0 + kKeys - 1 <= x.all_hi && pages == (1u << per_tile) - 1u;
@@ -354,7 +343,7 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
 #pragma unroll
                     for (int z = 0; z < 2; ++z) poison[z] = *const_cast<volatile uint32_t*>(&poisoned[key_a + 8 * z]) == n_tiles + 1;
                 }
-                auto unseen = [&](int c, int z) { return !all && (!there[z] || key0 + key_a + 8 * z > row_hi[c]); };
+                auto unseen = [&](int c, int z) { return !there[z] || key0 + key_a + 8 * z > row_hi[c]; };
                 uint8_t* dst = tails + tail * kChunk;
                 // The maxima are brought up to this tile's scores, the sums so far to the maxima.
                 auto raise = [&] {
@@ -365,7 +354,7 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
                             float best = -kMost;
 #pragma unroll
                             for (int z = 0; z < 2; ++z)
-                                if (!unseen(col + 8 * g + e, z)) best = fmaxf(best, __uint_as_float(u[4 * g + 2 * z + e]) * scale);
+                                if (all || !unseen(col + 8 * g + e, z)) best = fmaxf(best, __uint_as_float(u[4 * g + 2 * z + e]) * scale);
 #pragma unroll
                             for (int d = 4; d < 32; d <<= 1) best = fmaxf(best, __shfl_xor_sync(kFull, best, d));
                             if (lane < 4) sums[warp][8 * g + 2 * lane + e] = best;
@@ -409,25 +398,30 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
                         const float2 m = *reinterpret_cast<const float2*>(&low[col + 8 * g]);
 #pragma unroll
                         for (int z = 0; z < 2; ++z) {
-                            float2 a = unpack2(fma2(pack2(__uint_as_float(u[4 * g + 2 * z]), __uint_as_float(u[4 * g + 2 * z + 1])), sc2, pack2(m.x, m.y)));
-                            if (unseen(col + 8 * g, z)) a.x = neg_inf();
-                            if (unseen(col + 8 * g + 1, z)) a.y = neg_inf();
-                            most = max3(most, a.x, a.y);
+                            const float2 a = unpack2(fma2(pack2(__uint_as_float(u[4 * g + 2 * z]), __uint_as_float(u[4 * g + 2 * z + 1])), sc2, pack2(m.x, m.y)));
                             r2[4 * g + 2 * z] = a.x, r2[4 * g + 2 * z + 1] = a.y;
                         }
                     }
+                    if (!all) {
+#pragma unroll
+                        for (int i = 0; i < 4 * G; ++i)
+                            if (unseen(col + 8 * (i >> 2) + (i & 1), i >> 1 & 1)) r2[i] = neg_inf();
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4 * G; i += 2) most = max3(most, r2[i], r2[i + 1]);
                     return most;
                 };
                 auto weights = [&](bool count) {
+                    if (poison[0] || poison[1]) {  // (a NaN's weight is a NaN)
+#pragma unroll
+                        for (int i = 0; i < 4 * G; ++i)
+                            if (poison[i >> 1 & 1] && !unseen(col + 8 * (i >> 2) + (i & 1), i >> 1 & 1)) r2[i] = __uint_as_float(0x7fc00000u);
+                    }
 #pragma unroll
                     for (int g = 0; g < G; ++g)
 #pragma unroll
                         for (int z = 0; z < 2; ++z) {
-                            float e0 = ex2(r2[4 * g + 2 * z]), e1 = ex2(r2[4 * g + 2 * z + 1]);
-                            if (poison[z]) {
-                                if (key0 + key_a + 8 * z <= row_hi[col + 8 * g]) e0 = __uint_as_float(0x7fc00000u);
-                                if (key0 + key_a + 8 * z <= row_hi[col + 8 * g + 1]) e1 = __uint_as_float(0x7fc00000u);
-                            }
+                            const float e0 = ex2(r2[4 * g + 2 * z]), e1 = ex2(r2[4 * g + 2 * z + 1]);
                             if (count) l[g] = add2(l[g], pack2(e0, e1));
                             *reinterpret_cast<uint32_t*>(dst + sw128_off(key_a + 8 * z, (c0 >> 3) + g) + 4 * (lane & 3)) = pack_bf16x2(e0, e1);
                         }
@@ -456,7 +450,7 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(p_full);
+                if (lane == 0) mbar_arrive(&p_full[n_tiles & 1u]);
                 ++n_tiles;
                 pair += pairs_of_tile;
                 while (pair >= PAIRS) pair -= PAIRS;
@@ -557,36 +551,66 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
                 const int id = ids[at >> p.page_log2];
                 return id >= 0 && id < p.n_pages ? (id << p.page_log2) + (at & (p.page - 1)) : nowhere;
             };
-            int row = first_row(0);
+            // Rows on their way to L2, in one piece as they lie: the copies take 128 bytes of each row at a time, an order
+            // that HBM is slow in. The CTAs beside each other take turns.
+            const uint8_t* rows = static_cast<const uint8_t*>(p.k_pool);
+            const uint32_t piece = (uint32_t)(2 * W) << box_log2;
+            auto prefetch = [&](int t, int row) {
+                if (row != nowhere && (uint32_t)t % (uint32_t)pp.sides == (uint32_t)side)
+                    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(rows + (int64_t)row * (2 * W)), "r"(piece) : "memory");
+            };
+            int next_rows[kAhead + 1];  // of this tile and the next ones
+#pragma unroll
+            for (int i = 0; i <= kAhead; ++i) next_rows[i] = first_row(i);
+#pragma unroll
+            for (int i = 1; i < kAhead; ++i) prefetch(i, next_rows[i]);
             for (int t = 0; t < x.tiles && ok; ++t) {
-                const int ahead = first_row(t + 1);
+                const int row = next_rows[0];
+                prefetch(t + kAhead, next_rows[kAhead]);
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) next_rows[i] = next_rows[i + 1];
+                next_rows[kAhead] = first_row(t + kAhead + 1);
                 const uint32_t mask = __ballot_sync(kFull, row != nowhere);
-                // lane: copy lane % per_tile of the first or second chunk of a pair
-                const int from = __shfl_sync(kFull, row, lane & (per_tile - 1)), chunk = lane / per_tile;
-                for (int i = 0; i < pairs_of_tile; ++i) {
-                    ok = wait_warp(&empty[slot], phase ^ 1);
-                    if (!ok) break;
-                    if (lane == 0) mbar_expect_tx(&full[slot], 2 * kChunk);
-                    __syncwarp();
-                    if (chunk < 2)
-                        tma_load_2d(pairs + (2 * slot + chunk) * kChunk + (lane & (per_tile - 1)) * box, &pool, 128 * i + 64 * chunk, from, &full[slot]);
-                    inflight |= 1u << slot;
-                    par = (par & ~(1u << slot)) | (phase << slot);
-                    if (++slot == PAIRS) slot = 0, phase ^= 1;
-                }
-                if (!ok) break;
-                ok = wait_warp(&tempty[tail], tphase ^ 1);
-                if (!ok) break;
+                int from[4];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) from[c] = __shfl_sync(kFull, row, c & (per_tile - 1));
+                // (by one lane from here on, and in as few copies as there can be: with a warp's meetings around each of
+                // them a pair took 590 cycles, which set the pace)
                 if (lane == 0) {
-                    *const_cast<volatile uint32_t*>(&good[tail]) = mask;
-                    mbar_expect_tx(&tfull[tail], W > R ? kChunk : 0);
+                    for (int i = 0; i < pairs_of_tile; ++i) {
+                        ok = mbar_wait(&empty[slot], phase ^ 1, abort_flag, p.err, pp.wait_limit_ns);
+                        if (!ok) break;
+                        uint8_t* dst = pairs + slot * 2 * kChunk;
+                        mbar_expect_tx(&full[slot], 2 * kChunk);
+                        if (per_tile == 1) {
+                            tma_load_3d(dst, &latents, 0, from[0], 2 * i, &full[slot]);
+                        } else {
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) {
+                                if (c >= per_tile) break;
+                                tma_load_3d(dst + c * box, &latents, 0, from[c], 2 * i, &full[slot]);
+                                tma_load_3d(dst + kChunk + c * box, &latents, 0, from[c], 2 * i + 1, &full[slot]);
+                            }
+                        }
+                        inflight |= 1u << slot;
+                        par = (par & ~(1u << slot)) | (phase << slot);
+                        if (++slot == PAIRS) slot = 0, phase ^= 1;
+                    }
+                    if (ok) ok = mbar_wait(&tempty[tail], tphase ^ 1, abort_flag, p.err, pp.wait_limit_ns);
+                    if (ok) {
+                        *const_cast<volatile uint32_t*>(&good[tail]) = mask;
+                        mbar_expect_tx(&tfull[tail], W > R ? kChunk : 0);
+                        if (W > R) {
+#pragma unroll
+                            for (int c = 0; c < 4; ++c)
+                                if (c < per_tile) tma_load_2d(tails + tail * kChunk + c * box, &pool, R, from[c], &tfull[tail]);
+                        }
+                        tinflight |= 1u << tail;
+                        tpar = (tpar & ~(1u << tail)) | (tphase << tail);
+                        if (++tail == TAILS) tail = 0, tphase ^= 1;
+                    }
                 }
-                __syncwarp();
-                if (chunk < 1 && W > R) tma_load_2d(tails + tail * kChunk + lane * box, &pool, R, from, &tfull[tail]);
-                tinflight |= 1u << tail;
-                tpar = (tpar & ~(1u << tail)) | (tphase << tail);
-                if (++tail == TAILS) tail = 0, tphase ^= 1;
-                row = ahead;
+                ok = __shfl_sync(kFull, ok, 0);
             }
             more = walk.next(p);
         }
@@ -599,96 +623,85 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap pool, const __grid_cons
                 if ((tinflight >> i) & 1u) drain_wait(&tfull[i], (tpar >> i) & 1u, t0);
         }
     } else {
-        // ------------------------- MMA issuers (two whole warps, one lane of each issues)
+        // ------------------------- MMA issuers (two whole warps, one lane of each issues): scores, and values
         // What a warp's wait or commit takes between two of its MMAs its own MMAs stand still (some 100 and 50 cycles); two
-        // warps fill each other's gaps. Warp 9 has the pairs 0, 2, .. of a tile, warp 10 the pairs 1, 3, .. and the rotary
-        // chunk: two parts of the scores, and row tiles of O^T of their own.
-        const int w2 = __reduce_max_sync(kFull, warp == 10);
-        constexpr uint32_t kId = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | (64u >> 4 << 24);
-        constexpr uint32_t kIdO = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | (128u >> 4 << 24) | (1u << 15) | (1u << 16);  // both operands MN-major
-        const uint32_t tm = __reduce_max_sync(kFull, tmem), tSw = tm + w2 * N;
+        // warps fill each other's gaps, and the values of a tile wait for no loads of the one after the next.
+        // (What the loops run to comes from warp-wide reductions, so that the MMA's operands stay in uniform registers.)
+        const int values = __reduce_max_sync(kFull, warp == 10);
+        constexpr uint32_t kId = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17);
+        constexpr uint32_t kIdS = kId | 64u >> 4 << 24, kIdO = kId | 128u >> 4 << 24 | 1u << 15 | 1u << 16;  // O: both operands MN-major
+        const uint32_t tm = __reduce_max_sync(kFull, tmem);
         const uint64_t dq = sw128_desc(smem_u32(sq)), dk = sw128_desc(smem_u32(pairs)), dt = sw128_desc(smem_u32(tails));
         const uint64_t dv = mn_desc(smem_u32(pairs)), dp = mn_desc(smem_u32(tails));
-        const int tail_steps = w2 ? (W - R + 15) / 16 : 0;
-        int slot = 0, tail = 0, v_slot = 0, v_tail = 0;  // of the tile whose scores, whose values are next
-        uint32_t phase = 0, tphase = 0, qn = 0, pn = 0, scored = 0;
+        const int tail_steps = (W - R + 15) / 16;
+        int slot = 0, tail = 0;
+        uint32_t phase = 0, tphase = 0, qn = 0, tile = 0;
         bool ok = true, issued = false;
+        auto weights_of = [&](uint32_t n) { return wait_warp(&p_full[n & 1u], n >> 1 & 1u); };
         for (int j = 0; ok; ++j) {
             ok = wait_warp(&j_full[j & 1], (uint32_t)(j >> 1) & 1u);
             if (!ok) break;
-            // (what the loops run to comes from warp-wide reductions, so that the MMA's operands stay in uniform registers)
             const int tiles = __reduce_max_sync(kFull, jobs[j & 1].tiles), end = __reduce_max_sync(kFull, jobs[j & 1].end);
             __syncwarp();
             if (lane == 0) mbar_arrive(&j_empty[j & 1]);
             if (end) break;
             if (tiles <= 0) continue;
-            ok = wait_warp(q_full, qn++ & 1u);
-            // the scores of the next tile, with its slots from `slot` and `tail` on
-            auto scores = [&] {
-                const uint32_t d = tSw + (scored & 1u) * 2 * N;
-                for (int i = 0; i < pairs_of_tile; ++i) {
-                    if ((i & 1) == w2) {
+            if (!values) ok = wait_warp(q_full, qn++ & 1u);
+            for (int t = 0; t < tiles && ok; ++t, ++tile) {
+                if (values) {
+                    ok = weights_of(tile);
+                    if (!ok) break;
+                    tc_fence_after();
+                    for (int i = 0; i < pairs_of_tile; ++i) {
+                        if (elect_one()) {
+                            const uint64_t a = dv + (uint64_t)((uint32_t)(slot * 2 * kChunk) >> 4), b = dp + (uint64_t)((uint32_t)(tail * kChunk) >> 4);
+#pragma unroll
+                            for (int k = 0; k < kKeys / 16; ++k)
+                                mma_ss(tm + 2 * N + i * N, a + (uint64_t)(k * 2048 >> 4), b + (uint64_t)(k * 2048 >> 4), kIdO, t > 0 || k > 0);
+                            mma_commit(&empty[slot]);
+                        }
+                        __syncwarp();
+                        if (++slot == PAIRS) slot = 0;
+                    }
+                    if (elect_one()) {
+                        mma_commit(&tempty[tail]);
+                        mma_commit(o_full);
+                    }
+                } else {
+                    if (tile >= 2) ok = weights_of(tile - 2);  // the scores that lay there have been read
+                    const uint32_t d = tm + (tile & 1u) * N;
+                    for (int i = 0; i < pairs_of_tile && ok; ++i) {
                         ok = wait_warp(&full[slot], phase);
-                        if (!ok) return;
+                        if (!ok) break;
                         tc_fence_after();
                         if (elect_one()) {
                             const uint64_t a = dk + (uint64_t)((uint32_t)(slot * 2 * kChunk) >> 4), b = dq + (uint64_t)((uint32_t)(i * 2 * N * 128) >> 4);
 #pragma unroll
                             for (int k = 0; k < 8; ++k)
-                                mma_ss(d, a + (((k >> 2) * kChunk + (k & 3) * 32) >> 4), b + (((k >> 2) * N * 128 + (k & 3) * 32) >> 4), kId,
-                                       i > 1 || k > 0);
+                                mma_ss(d, a + (((k >> 2) * kChunk + (k & 3) * 32) >> 4), b + (((k >> 2) * N * 128 + (k & 3) * 32) >> 4), kIdS,
+                                       i > 0 || k > 0);
                         }
                         __syncwarp();
+                        if (++slot == PAIRS) slot = 0, phase ^= 1;
                     }
-                    if (++slot == PAIRS) slot = 0, phase ^= 1;
-                }
-                if (w2) {
-                    ok = wait_warp(&tfull[tail], tphase);
-                    if (!ok) return;
+                    ok = ok && wait_warp(&tfull[tail], tphase);
+                    if (!ok) break;
                     tc_fence_after();
-                }
-                if (elect_one()) {
-                    const uint64_t a = dt + (uint64_t)((uint32_t)(tail * kChunk) >> 4), b = dq + (uint64_t)((uint32_t)(pairs_of_tile * 2 * N * 128) >> 4);
-                    for (int k = 0; k < tail_steps; ++k) mma_ss(d, a + (uint64_t)(k * 2), b + (uint64_t)(k * 2), kId, pairs_of_tile > 1 || k > 0);
-                    mma_commit(&s_full[scored & 1u]);
+                    if (elect_one()) {
+                        const uint64_t a = dt + (uint64_t)((uint32_t)(tail * kChunk) >> 4), b = dq + (uint64_t)((uint32_t)(pairs_of_tile * 2 * N * 128) >> 4);
+                        for (int k = 0; k < tail_steps; ++k) mma_ss(d, a + (uint64_t)(k * 2), b + (uint64_t)(k * 2), kIdS, 1);
+                        mma_commit(&s_full[tile & 1u]);
+                    }
                 }
                 __syncwarp();
-                ++scored;
                 issued = true;
                 if (++tail == TAILS) tail = 0, tphase ^= 1;
-            };
-            if (ok) scores();
-            for (int t = 0; t < tiles && ok; ++t) {
-                if (t + 1 < tiles) scores();
-                if (!ok) break;
-                ok = wait_warp(p_full, pn++ & 1u);
-                if (!ok) break;
-                tc_fence_after();
-                for (int i = 0; i < pairs_of_tile; ++i) {
-                    if ((i & 1) == w2) {
-                        if (elect_one()) {
-                            const uint64_t a = dv + (uint64_t)((uint32_t)(v_slot * 2 * kChunk) >> 4), b = dp + (uint64_t)((uint32_t)(v_tail * kChunk) >> 4);
-#pragma unroll
-                            for (int k = 0; k < kKeys / 16; ++k)
-                                mma_ss(tm + 4 * N + i * N, a + (uint64_t)(k * 2048 >> 4), b + (uint64_t)(k * 2048 >> 4), kIdO, t > 0 || k > 0);
-                            mma_commit(&empty[v_slot]);
-                        }
-                        __syncwarp();
-                    }
-                    if (++v_slot == PAIRS) v_slot = 0;
-                }
-                if (elect_one()) {
-                    mma_commit(&tempty[v_tail]);
-                    mma_commit(o_full);
-                }
-                __syncwarp();
-                if (++v_tail == TAILS) v_tail = 0;
             }
         }
         if (issued) {  // no MMA is in flight when TMEM is released
-            if (elect_one()) mma_commit(&drain[w2]);
+            if (elect_one()) mma_commit(&drain[values]);
             __syncwarp();
-            drain_wait(&drain[w2], 0);
+            drain_wait(&drain[values], 0);
         }
     }
     tc_fence_before();
@@ -707,18 +720,24 @@ cudaError_t cached_as(LatentProblem p, int sides, cudaStream_t stream) {
     EncodeTiled fn = encode_fn();
     if (!fn) return cudaErrorInvalidValue;
     AttnProblem& a = p.a;
-    // the pool as rows of R + P elements, in boxes of 64 elements (128-byte swizzled, zeros past a row's end) of a page's rows, up to a tile's
-    CUtensorMap map;
-    cuuint64_t dims[2] = {(cuuint64_t)p.K, (cuuint64_t)a.n_pages * a.page}, strides[1] = {(cuuint64_t)(2 * p.K)};
-    cuuint32_t box[2] = {64, (cuuint32_t)(a.page < kKeys ? a.page : kKeys)}, estr[2] = {1, 1};
-    if (fn(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(a.k_pool), dims, strides, box, estr,
-           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-        return cudaErrorInvalidValue;
+    // The pool as rows of R + P elements: its latents in boxes of one or two chunks of 64 elements (128-byte swizzled) of
+    // a page's rows, up to a tile's, and the rest in boxes of one chunk, with zeros past a row's end.
+    CUtensorMap latents, pool;
+    const cuuint32_t rows = (cuuint32_t)(a.page < kKeys ? a.page : kKeys);
+    cuuint64_t dims[3] = {64, (cuuint64_t)a.n_pages * a.page, (cuuint64_t)(a.D / 64)}, strides[2] = {(cuuint64_t)(2 * p.K), 128};
+    cuuint32_t box[3] = {64, rows, rows == kKeys ? 2u : 1u}, estr[3] = {1, 1, 1};
+    auto encode = [&](CUtensorMap* m, int rank) {
+        return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(a.k_pool), dims, strides, box, estr,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    };
+    if (!encode(&latents, 3)) return cudaErrorInvalidValue;
+    dims[0] = (cuuint64_t)p.K;
+    if (!encode(&pool, 2)) return cudaErrorInvalidValue;
     const int ctas = min(sm_count(), kLatentMaxParts / (2 * kLatentMaxRows));
     set_shares(a, sides * N, 1, ctas / sides, kMinBlocks, kTileCost, kKeys);
     Params pp{p, sides, tc_wait_limit_ns()};
-    if (cudaError_t e = launch_k(kernel, dim3(a.shares * sides), dim3(kThreads), Shape<N>::BYTES, stream, map, pp); e != cudaSuccess) return e;
+    if (cudaError_t e = launch_k(kernel, dim3(a.shares * sides), dim3(kThreads), Shape<N>::BYTES, stream, latents, pool, pp); e != cudaSuccess) return e;
     return a.shares > 1 ? launch_attn_join(a, stream) : cudaSuccess;
 }
 
