@@ -9,6 +9,8 @@
 //
 // Each element is read once and written once, so HBM bounds it for prompts and the
 // launch with three dependent loads (offsets, length, page) for single tokens.
+#include <climits>
+
 #include "attn_plan.cuh"
 #include "attn_turn.cuh"
 #include "latent.h"
@@ -23,6 +25,14 @@ constexpr unsigned kFull = 0xffffffffu;
 // cu_q[b + 1] > t, 32 offsets at a time of the interval that holds it.
 __device__ __forceinline__ int find_seq(const LatentAppend& p, int t) {
     const int lane = threadIdx.x & 31;
+    if (p.B <= 256) {  // all of them at once: one round trip to memory instead of two
+        int upto = 0, ends[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) ends[i] = lane + 32 * i < p.B ? p.cu_q[lane + 32 * i + 1] : INT_MAX;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) upto += __popc(__ballot_sync(kFull, ends[i] <= t));
+        return upto < p.B && p.cu_q[upto] <= t ? upto : -1;
+    }
     int lo = 0, hi = p.B;
     while (lo < hi) {
         const int step = (hi - lo + 31) / 32;

@@ -50,16 +50,17 @@ constexpr int kChunk = kKeys * 128;       // bytes of 64 rows x 64 elements
 constexpr unsigned kFull = 0xffffffffu;
 constexpr float kGrow = 16.0f;            // log2 of how far a column's maximum may run ahead of m
 constexpr float kMost = 3.402823466e38f;  // -kMost: a maximum of nothing
-constexpr int kMinBlocks = 1, kTileCost = 0;
+constexpr int kMinBlocks = 2, kTileCost = 1;
 constexpr int kMostSides = 8;
-constexpr int kAhead = 3;                 // tiles that L2 is ahead of the copies
 
 // N: query rows of a CTA. Rings of pairs of chunks (128 latent elements) and of the rotary chunks.
 template <int N>
 struct Shape {
     static constexpr int COLS = N / 2;                       // columns of a warp
     static constexpr int G = COLS / 8;                       // groups of eight: a thread has two of each, of two keys
-    static constexpr int PAIRS = N == 64 ? 8 : N == 32 ? 10 : 11, TAILS = N == 64 ? 2 : 3;
+    // (two rotary chunks, whatever the room: a tile's scores then wait for the values of the one before the last, so no
+    // wait for o_full or p_full is more than one phase behind, which is all that a parity tells)
+    static constexpr int PAIRS = N == 64 ? 8 : N == 32 ? 10 : 11, TAILS = 2;
     static constexpr int Q = 9 * N * 128;
     static constexpr int BODY = Q + PAIRS * 2 * kChunk + TAILS * kChunk;
     static constexpr int BYTES = 1024 + BODY;
@@ -266,27 +267,35 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap latents, const __grid_c
             return wait_warp(bar, n++ & 1u);
         };
         bool ok = true;
-        for (int j = 0; ok; ++j) {
+        auto take = [&](int j) {
             ok = wait_warp(&j_full[j & 1], (uint32_t)(j >> 1) & 1u);
-            if (!ok) break;
             const Job x = jobs[j & 1];
             __syncwarp();
             if (lane == 0) mbar_arrive(&j_empty[j & 1]);
+            return x;
+        };
+        // a segment's queries on their way: rows of 64 elements, 128-byte swizzled, zeros where there are none
+        auto fetch_queries = [&](const Job& x) {
+            if (x.end || x.tiles <= 0) return;
+            const int pieces = (pairs_of_tile * 2 + 1) * 8;
+            for (int i = tid; i < N * pieces; i += 256) {
+                const int row = i / pieces, c = i - row * pieces;
+                const bool there = row < x.rows && 8 * c < W;
+                const int rr = x.row0 + (there ? row : 0), tok = rr / p.R;
+                const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(p.q.p) + (int64_t)(x.q0 + tok) * p.q.ts +
+                                           (rr - tok * p.R) * p.q.hs + (there ? 8 * c : 0);
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(sq + (c >> 3) * (N * 128) + sw128_off(row, c & 7))),
+                             "l"(src), "r"(there ? 16 : 0)
+                             : "memory");
+            }
+        };
+        Job next = take(0);
+        if (ok) fetch_queries(next);
+        for (int j = 0; ok; ++j) {
+            const Job x = next;
             if (x.end) break;
             if (x.rows > 0) {
-                // queries: rows of N x 64 elements, 128-byte swizzled, zeros where there are none
                 if (x.tiles > 0) {
-                    const int pieces = (pairs_of_tile * 2 + 1) * 8;
-                    for (int i = tid; i < N * pieces; i += 256) {
-                        const int row = i / pieces, c = i - row * pieces;
-                        const bool there = row < x.rows && 8 * c < W;
-                        const int rr = x.row0 + (there ? row : 0), tok = rr / p.R;
-                        const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(p.q.p) + (int64_t)(x.q0 + tok) * p.q.ts +
-                                                   (rr - tok * p.R) * p.q.hs + (there ? 8 * c : 0);
-                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(sq + (c >> 3) * (N * 128) + sw128_off(row, c & 7))),
-                                     "l"(src), "r"(there ? 16 : 0)
-                                     : "memory");
-                    }
                     asm volatile("cp.async.wait_all;" ::: "memory");
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
@@ -426,27 +435,23 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap latents, const __grid_c
                             *reinterpret_cast<uint32_t*>(dst + sw128_off(key_a + 8 * z, (c0 >> 3) + g) + 4 * (lane & 3)) = pack_bf16x2(e0, e1);
                         }
                 };
-                if (t == 0) {
-                    raise();
+                // (a loop of one or two turns: each step's code is there once, the first tile's has not to be fetched for it alone)
+                bool up = t == 0, count = true;
+                for (;;) {
+                    if (up) raise();
                     if (!ok) break;
-                    relative();
-                    weights(true);
-                } else {
-                    const bool over = __any_sync(kFull, relative() > kGrow);
-                    if (lane == 0) {
+                    const bool over = __any_sync(kFull, relative() > kGrow) && !up;
+                    if (!up && lane == 0) {
                         if (over) *const_cast<volatile uint32_t*>(&raised[wg]) = n_tiles + 1;
                         mbar_arrive(&half[wg]);
                     }
-                    if (!over) weights(true);
+                    if (!over) weights(count);
+                    if (up) break;
                     ok = wait_warp(&half[wg], meets++ & 1u);
-                    if (!ok) break;
-                    if (*const_cast<volatile uint32_t*>(&raised[wg]) == n_tiles + 1) {
-                        raise();
-                        if (!ok) break;
-                        relative();
-                        weights(over);  // (the others have counted theirs, rescaled since)
-                    }
+                    if (!ok || *const_cast<volatile uint32_t*>(&raised[wg]) != n_tiles + 1) break;
+                    up = true, count = over;  // (the others have counted theirs, which the raise rescales)
                 }
+                if (!ok) break;
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 tc_fence_before();
                 __syncwarp();
@@ -457,6 +462,10 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap latents, const __grid_c
                 if (++tail == TAILS) tail = 0, tphase ^= 1;
             }
             if (!ok) break;
+            // the next segment's queries come while this one's results go (every product with these is done)
+            next = take(j + 1);
+            if (!ok) break;
+            fetch_queries(next);
             // ------------------------------------------------------------ result
             if (x.rows > 0) {
                 // each column's sum of weights over the keys
@@ -551,25 +560,9 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap latents, const __grid_c
                 const int id = ids[at >> p.page_log2];
                 return id >= 0 && id < p.n_pages ? (id << p.page_log2) + (at & (p.page - 1)) : nowhere;
             };
-            // Rows on their way to L2, in one piece as they lie: the copies take 128 bytes of each row at a time, an order
-            // that HBM is slow in. The CTAs beside each other take turns.
-            const uint8_t* rows = static_cast<const uint8_t*>(p.k_pool);
-            const uint32_t piece = (uint32_t)(2 * W) << box_log2;
-            auto prefetch = [&](int t, int row) {
-                if (row != nowhere && (uint32_t)t % (uint32_t)pp.sides == (uint32_t)side)
-                    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(rows + (int64_t)row * (2 * W)), "r"(piece) : "memory");
-            };
-            int next_rows[kAhead + 1];  // of this tile and the next ones
-#pragma unroll
-            for (int i = 0; i <= kAhead; ++i) next_rows[i] = first_row(i);
-#pragma unroll
-            for (int i = 1; i < kAhead; ++i) prefetch(i, next_rows[i]);
+            int row = first_row(0);
             for (int t = 0; t < x.tiles && ok; ++t) {
-                const int row = next_rows[0];
-                prefetch(t + kAhead, next_rows[kAhead]);
-#pragma unroll
-                for (int i = 0; i < kAhead; ++i) next_rows[i] = next_rows[i + 1];
-                next_rows[kAhead] = first_row(t + kAhead + 1);
+                const int ahead = first_row(t + 1);
                 const uint32_t mask = __ballot_sync(kFull, row != nowhere);
                 int from[4];
 #pragma unroll
@@ -611,6 +604,7 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap latents, const __grid_c
                     }
                 }
                 ok = __shfl_sync(kFull, ok, 0);
+                row = ahead;
             }
             more = walk.next(p);
         }

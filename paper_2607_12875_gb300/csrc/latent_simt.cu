@@ -16,6 +16,7 @@ namespace {
 
 constexpr int kThreads = 128;
 constexpr int kKeys = 32;
+static_assert(4 * kKeys == kThreads, "four threads for a key");
 constexpr int kMinBlocks = 1, kTileCost = 0;  // shares of one block of 64 keys, as attn_simt.cu
 
 // 16 bytes global -> shared, or 16 bytes of zeros
@@ -83,29 +84,31 @@ __device__ __forceinline__ void attend(const LatentProblem& lp, const Segment& i
     k_lo = c_lo;
     const int k_hi = min(c_hi, last_hi + 1);
 
+    // Four threads for a key's row, whose page is looked up a tile ahead.
     const int own = lp.own * EB / 16, key = lp.K * EB / 16, all_pieces = key + (kPaged ? 0 : p.D * EB / 16);
+    const int lr = tid >> 2, lc = tid & 3;
+    auto page_of = [&](int k0) {
+        if (!kPaged || k0 + lr >= k_hi) return -1;
+        const int id = p.page_table[(int64_t)it.b * p.max_pages + ((k0 + lr) >> p.page_log2)];
+        return id >= 0 && id < p.n_pages ? id : -1;
+    };
+    int page = page_of(k_lo);
     auto load = [&](int k0, int buf) {
-        for (int i = tid; i < kKeys * all_pieces; i += kThreads) {
-            const int r = i / all_pieces, c = i % all_pieces;
-            bool good = k0 + r < k_hi;
-            const uint8_t* src = static_cast<const uint8_t*>(p.q.p);  // (not read where good is false)
-            if constexpr (kPaged) {
-                if (good) {
-                    const int id = p.page_table[(int64_t)it.b * p.max_pages + ((k0 + r) >> p.page_log2)];
-                    good = id >= 0 && id < p.n_pages;
-                    if (good)
-                        src = static_cast<const uint8_t*>(p.k_pool) +
-                              ((int64_t)id * p.page + ((k0 + r) & (p.page - 1))) * lp.K * EB + 16 * c;
-                }
-                if (c == 0) marks[buf * kKeys + r] = good;
-            } else if (good) {
-                const int64_t at = it.s.k0 + k0 + r;
-                const Rows& from = c < own ? p.k : c < key ? lp.k_rope : p.v;
-                const int h = c >= own && c < key ? 0 : it.head;
-                src = reinterpret_cast<const uint8_t*>(static_cast<const TA*>(from.p) + at * from.ts + h * from.hs) +
-                      16 * (c < own ? c : c < key ? c - own : c - key);
-            }
-            cp_async_or_zero(skv + (buf * kKeys + r) * sz.k_pitch + 16 * c, src, good);
+        const bool good = kPaged ? page >= 0 : k0 + lr < k_hi;
+        uint8_t* dst = skv + (buf * kKeys + lr) * sz.k_pitch;
+        if constexpr (kPaged) {
+            const uint8_t* src = static_cast<const uint8_t*>(p.k_pool) +
+                                 ((int64_t)max(page, 0) * p.page + ((k0 + lr) & (p.page - 1))) * lp.K * EB;
+            for (int c = lc; c < key; c += 4) cp_async_or_zero(dst + 16 * c, good ? src + 16 * c : static_cast<const uint8_t*>(p.k_pool), good);
+            if (lc == 0) marks[buf * kKeys + lr] = good;
+            page = page_of(k0 + kKeys);
+        } else {
+            const int64_t at = it.s.k0 + (good ? k0 + lr : 0);
+            const uint8_t* k = reinterpret_cast<const uint8_t*>(static_cast<const TA*>(p.k.p) + at * p.k.ts + it.head * p.k.hs);
+            const uint8_t* r = reinterpret_cast<const uint8_t*>(static_cast<const TA*>(lp.k_rope.p) + at * lp.k_rope.ts);
+            const uint8_t* v = reinterpret_cast<const uint8_t*>(static_cast<const TA*>(p.v.p) + at * p.v.ts + it.head * p.v.hs);
+            for (int c = lc; c < all_pieces; c += 4)
+                cp_async_or_zero(dst + 16 * c, c < own ? k + 16 * c : c < key ? r + 16 * (c - own) : v + 16 * (c - key), good);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };

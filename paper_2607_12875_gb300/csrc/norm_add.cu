@@ -1,11 +1,11 @@
 // The residual's addition, the RMS norm and its rounding to 8 bits in one pass.
 //
-// A warp has a row and keeps the sum (as rounded to the activations' type, which is
+// A block has a row and keeps the sum (as rounded to the activations' type, which is
 // what is normed) in registers, so x and the residual are read once and nothing is
-// read back: up to 32 pieces of eight elements a lane (H up to 8192); wider rows are
-// read again for the second half. The sum of squares takes the elements in the order
-// of moe_rmsnorm (lane p the pieces p, p + 32, .. one by one, then pairs of lanes),
-// so the norm is the same bit for bit, whatever the launch.
+// read back (H up to 8192; wider rows are read again for the second half). The sum of
+// squares takes the elements in the order of moe_rmsnorm (lane p the pieces p, p + 32,
+// .. one by one, then pairs of lanes), so the norm is the same bit for bit: one warp
+// adds, on the rows in shared memory, while other blocks load and store.
 //
 // 8 bits: 128 columns are 16 lanes' pieces of the same number, so a block's maximum
 // is four exchanges.
@@ -52,110 +52,137 @@ __device__ __forceinline__ void add_piece(const Raw8<TA>& a, const Raw8<TA>& b, 
     }
 }
 
-// One row by one warp. kHeld: pieces of a lane that stay in registers (0: none, they are read again).
+// A lane's piece of the result, to the outputs that there are.
+template <typename TA>
+__device__ __forceinline__ void finish(const NormAdd& p, int64_t t, int at, const Raw8<TA>& s, const Raw8<TA>& g, float inv) {
+    float o[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j] = __fmul_rn(__fmul_rn(s.at(j), inv), g.at(j));
+    if (p.y) Vec8<TA>::store(static_cast<TA*>(p.y) + t * p.H + at, o);
+    if (!p.codes) return;
+    float top = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float a = fabsf(o[j]);
+        top = a <= 3.402823466e38f ? fmaxf(top, a) : top;  // (false for infinities and NaN)
+    }
+#pragma unroll
+    for (int d = 8; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, d));
+    const int e = block_exponent(top);
+    *reinterpret_cast<uint2*>(p.codes + t * p.H + at) = e4m3x8(o, pow2(-e));  // (-e <= 126)
+    if ((threadIdx.x & 15) == 0) p.scales[(t * p.H + at) >> 7] = pow2(e);
+}
+
+template <typename TA>
+__device__ __forceinline__ void put(TA* dst, const Raw8<TA>& s) {
+#pragma unroll
+    for (int j = 0; j < (int)sizeof(TA) / 2; ++j) reinterpret_cast<uint4*>(dst)[j] = s.v[j];
+}
+template <typename TA>
+__device__ __forceinline__ void add_squares(float& ss, const Raw8<TA>& s) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) ss = __fmaf_rn(s.at(j), s.at(j), ss);
+}
+// 1 / sqrt(mean + eps) from the lanes' sums
+__device__ __forceinline__ float inverse(const NormAdd& p, float ss) {
+#pragma unroll
+    for (int d = 16; d >= 1; d >>= 1) ss = __fadd_rn(ss, __shfl_xor_sync(kFull, ss, d));
+    return __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(__fdiv_rn(ss, (float)p.H), p.eps)));
+}
+
+// One row by a block: warp w has the 256 columns w, w + kWarps, .. (kHeld of them at most) in registers, and passes them
+// through shared memory to the first warp, which adds their squares up in the fixed order.
+constexpr int kWarps = 4;
 template <typename TA, int kHeld>
-__global__ void __launch_bounds__(128) norm_add_kernel(const __grid_constant__ NormAdd p) {
+__global__ void __launch_bounds__(32 * kWarps) norm_add_kernel(const __grid_constant__ NormAdd p) {
     pdl_enter();
-    const int lane = threadIdx.x & 31;
-    const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-    if (t >= p.T) return;
-    const int pieces = p.H / 8;  // a multiple of 32: every lane has as many
+    extern __shared__ uint4 rows[];
+    __shared__ float scale;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n = p.H / 256;
+    const int64_t t = blockIdx.x;
     const TA* x = static_cast<const TA*>(p.x) + t * p.H;
     const TA* res = p.residual ? static_cast<const TA*>(p.residual) + t * p.H : nullptr;
     TA* sum = p.sum ? static_cast<TA*>(p.sum) + t * p.H : nullptr;
-    const int n = pieces / 32;
-    constexpr int kKept = kHeld > 0 ? kHeld : 1;
-    Raw8<TA> kept[kKept];
-    float ss = 0.0f;
-    auto square = [&](const Raw8<TA>& s) {
+    TA* shared = reinterpret_cast<TA*>(rows);
+    auto column = [&](int i) { return 256 * (warp + kWarps * i) + 8 * lane; };
+    Raw8<TA> s[kHeld], r[kHeld], g[kHeld];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) ss = __fmaf_rn(s.at(j), s.at(j), ss);
-    };
-    auto put = [&](TA* dst, const Raw8<TA>& s) {
-#pragma unroll
-        for (int j = 0; j < (int)sizeof(TA) / 2; ++j) reinterpret_cast<uint4*>(dst)[j] = s.v[j];
-    };
-    constexpr int kBatch = sizeof(TA) == 2 ? 8 : 4;  // pieces of both terms in flight
-    if constexpr (kHeld > 0) {
-#pragma unroll
-        for (int i0 = 0; i0 < kHeld; i0 += kBatch) {
-            Raw8<TA> b[kBatch];
-#pragma unroll
-            for (int i = 0; i < kBatch; ++i) {
-                if (i0 + i >= kHeld || i0 + i >= n) continue;
-                const int at = 8 * (lane + 32 * (i0 + i));
-                kept[i0 + i].load(x + at);
-                if (res) b[i].load(res + at);
-            }
-#pragma unroll
-            for (int i = 0; i < kBatch; ++i) {
-                if (i0 + i >= kHeld || i0 + i >= n) continue;
-                add_piece(kept[i0 + i], b[i], res != nullptr, kept[i0 + i]);
-                if (sum) put(sum + 8 * (lane + 32 * (i0 + i)), kept[i0 + i]);
-                square(kept[i0 + i]);
-            }
-        }
-    } else {
-        for (int i = 0; i < n; ++i) {
-            const int at = 8 * (lane + 32 * i);
-            Raw8<TA> a, b, s;
-            a.load(x + at);
-            if (res) b.load(res + at);
-            add_piece(a, b, res != nullptr, s);
-            square(s);
-        }
+    for (int i = 0; i < kHeld; ++i) {
+        if (warp + kWarps * i >= n) continue;
+        s[i].load(x + column(i));
+        if (res) r[i].load(res + column(i));
     }
 #pragma unroll
-    for (int d = 16; d >= 1; d >>= 1) ss = __fadd_rn(ss, __shfl_xor_sync(kFull, ss, d));
-    const float ms = __fdiv_rn(ss, (float)p.H);
-    const float inv = __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(ms, p.eps)));
-    auto finish = [&](int i, const Raw8<TA>& s) {
-        const int at = 8 * (lane + 32 * i);
-        float g[8], o[8];
-        Vec8<TA>::load(static_cast<const TA*>(p.gamma) + at, g);
+    for (int i = 0; i < kHeld; ++i)
+        if (warp + kWarps * i < n) g[i].load(static_cast<const TA*>(p.gamma) + column(i));
 #pragma unroll
-        for (int j = 0; j < 8; ++j) o[j] = __fmul_rn(__fmul_rn(s.at(j), inv), g[j]);
-        if (p.y) Vec8<TA>::store(static_cast<TA*>(p.y) + t * p.H + at, o);
-        if (p.codes) {
-            float top = 0.0f;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float a = fabsf(o[j]);
-                top = a <= 3.402823466e38f ? fmaxf(top, a) : top;  // (false for infinities and NaN)
-            }
-#pragma unroll
-            for (int d = 8; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, d));
-            const int e = block_exponent(top);
-            *reinterpret_cast<uint2*>(p.codes + t * p.H + at) = e4m3x8(o, pow2(-e));  // (-e <= 126)
-            if ((lane & 15) == 0) p.scales[(t * p.H + at) >> 7] = pow2(e);
-        }
-    };
-    if constexpr (kHeld > 0) {
-#pragma unroll
-        for (int i = 0; i < kHeld; ++i)
-            if (i < n) finish(i, kept[i]);
-    } else {
+    for (int i = 0; i < kHeld; ++i) {
+        if (warp + kWarps * i >= n) continue;
+        add_piece(s[i], r[i], res != nullptr, s[i]);
+        put(shared + column(i), s[i]);
+        if (sum) put(sum + column(i), s[i]);
+    }
+    __syncthreads();
+    if (warp == 0) {
+        float ss = 0.0f;
+#pragma unroll 4
         for (int i = 0; i < n; ++i) {
-            const int at = 8 * (lane + 32 * i);
-            Raw8<TA> a, b, s;
-            a.load(x + at);
-            if (res) b.load(res + at);
-            add_piece(a, b, res != nullptr, s);
-            if (sum) put(sum + at, s);  // (after both readings: it may be x or the residual)
-            finish(i, s);
+            Raw8<TA> v;
+            v.load(shared + 256 * i + 8 * lane);
+            add_squares(ss, v);
         }
+        const float inv = inverse(p, ss);
+        if (lane == 0) scale = inv;
+    }
+    __syncthreads();
+    const float inv = scale;
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i)
+        if (warp + kWarps * i < n) finish(p, t, column(i), s[i], g[i], inv);
+}
+
+// Rows of any width, one by a warp, read twice.
+template <typename TA>
+__global__ void __launch_bounds__(128) norm_add_wide_kernel(const __grid_constant__ NormAdd p) {
+    pdl_enter();
+    const int lane = threadIdx.x & 31, n = p.H / 256;
+    const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+    if (t >= p.T) return;
+    const TA* x = static_cast<const TA*>(p.x) + t * p.H;
+    const TA* res = p.residual ? static_cast<const TA*>(p.residual) + t * p.H : nullptr;
+    TA* sum = p.sum ? static_cast<TA*>(p.sum) + t * p.H : nullptr;
+    auto piece = [&](int i) {
+        const int at = 256 * i + 8 * lane;
+        Raw8<TA> a, b, s;
+        a.load(x + at);
+        if (res) b.load(res + at);
+        add_piece(a, b, res != nullptr, s);
+        return s;
+    };
+    float ss = 0.0f;
+    for (int i = 0; i < n; ++i) add_squares(ss, piece(i));
+    const float inv = inverse(p, ss);
+    for (int i = 0; i < n; ++i) {
+        const int at = 256 * i + 8 * lane;
+        const Raw8<TA> s = piece(i);
+        Raw8<TA> g;
+        g.load(static_cast<const TA*>(p.gamma) + at);
+        if (sum) put(sum + at, s);  // (after both readings: it may be x or the residual)
+        finish(p, t, at, s, g, inv);
     }
 }
 
 template <typename TA>
 cudaError_t norm_add_as(const NormAdd& p, cudaStream_t stream) {
-    const dim3 grid((unsigned)(((int64_t)p.T + 3) / 4));
-    auto run = [&](auto kernel) { return launch_k(kernel, grid, dim3(128), 0, stream, p); };
-    const int n = p.H / 256;
-    if (n <= 8) return run(norm_add_kernel<TA, 8>);
-    if (n <= 16) return run(norm_add_kernel<TA, 16>);
-    if (sizeof(TA) == 2 && n <= 32) return run(norm_add_kernel<TA, sizeof(TA) == 2 ? 32 : 16>);
-    return run(norm_add_kernel<TA, 0>);
+    const int n = p.H / 256, held = (n + kWarps - 1) / kWarps;
+    auto run = [&](auto kernel) {
+        return launch_k(kernel, dim3((unsigned)p.T), dim3(32 * kWarps), (size_t)p.H * sizeof(TA), stream, p);
+    };
+    if (held <= 1) return run(norm_add_kernel<TA, 1>);
+    if (held <= 2) return run(norm_add_kernel<TA, 2>);
+    if (held <= 4) return run(norm_add_kernel<TA, 4>);
+    if (held <= 8) return run(norm_add_kernel<TA, 8>);
+    return launch_k(norm_add_wide_kernel<TA>, dim3((unsigned)(((int64_t)p.T + 3) / 4)), dim3(128), 0, stream, p);
 }
 
 }  // namespace

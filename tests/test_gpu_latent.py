@@ -311,7 +311,9 @@ def test_cached_masks_pages_outside_the_pool(act):
     more = torch.cat((q[:2], q, q[:2]))
     keep = (prefix(nq) + 2, i32(lens), i32(pool.table))
     gb.latent_cached(cfg, gb.attn_batch(*keep), more, gb.latent_cache(pool.rows), extra, workspace(cfg, 9, 4))
-    assert torch.equal(extra[2:7], out) and (extra[:2] == 7.0).all() and (extra[7:] == 7.0).all()
+    # (more rows in the call: its work may be divided otherwise, so its sums may differ in their last bits)
+    check(extra[2:7], None, want, act)
+    assert (extra[:2] == 7.0).all() and (extra[7:] == 7.0).all()
 
 
 @pytest.mark.parametrize("act", ["f32", "bf16"])
@@ -361,6 +363,27 @@ def test_cached_scores_far_apart(act):
         out = run_cached(cfg, pool, q, [1], lens)
         # scores up to some 10^4: fp32 sums are off by about 2^-24 of it times a few, which the weights feel as it is
         check(out, None, ref.absorbed(q, pool, 512, [1], lens, cfg.scale), act, terms=2e-2)
+
+
+@pytest.mark.parametrize("H", [3, 16, 30, 64, 128])
+@pytest.mark.parametrize("R,P", [(512, 64), (128, 16)])
+def test_cached_maxima_that_rise_in_every_tile(H, R, P):
+    """Keys that grow along the sequence, so that the running maximum rises by far more than the weights are let run ahead
+    in one tile after the other; 40 times, for tiles whose parts meet in any order."""
+    lens, nq = [4000, 1100], [1, 1]
+    pool, q, cfg = cached_case(12, "bf16", H, R, P, 64, nq, lens)
+    for b, m in enumerate(lens):
+        p = np.arange(m)
+        rows = (torch.from_numpy(pool.table[b, p // 64]).long().cuda(), torch.from_numpy(p % 64).cuda())
+        pool.rows[rows] = (pool.rows[rows].float() * torch.linspace(0.5, 12.0, m, device="cuda")[:, None]).to(torch.bfloat16)
+    q[:, ::2] *= 4.0
+    want = ref.absorbed(q, pool, R, nq, lens, cfg.scale)
+    ws = workspace(cfg, 2, 2)
+    outs = [run_cached(cfg, pool, q, nq, lens, ws=ws) for _ in range(40)]
+    # scores up to some 10^3, whose fp32 sums are off by about 2^-24 of the sum of their products' sizes (several times
+    # the score): up to 10^-3 of a weight
+    check(outs[0], None, want, "bf16", terms=2e-3)
+    assert all(torch.equal(o, outs[0]) for o in outs)
 
 
 @pytest.mark.parametrize("act", ["f32", "bf16"])
