@@ -49,9 +49,9 @@ __device__ __forceinline__ int find_seq(const LatentAppend& p, int t) {
 
 // Block x: tokens x * (256 / G) .., a group of G threads each. bits: log2 of the threads of a head's units.
 template <typename TA, int G>
-__global__ void __launch_bounds__(kThreads) latent_append_kernel(const __grid_constant__ LatentAppend p, int bits) {
+__global__ void __launch_bounds__(kThreads, 2) latent_append_kernel(const __grid_constant__ LatentAppend p, int bits) {
     pdl_enter();
-    constexpr int B = sizeof(TA) == 2 ? 4 : 2;  // heads of a thread whose loads are in flight
+    constexpr int B = sizeof(TA) == 2 ? 4 : 1;  // heads of a thread whose loads are in flight
     const int lane = threadIdx.x & 31, r = threadIdx.x % G;
     const int t = (int)min64((int64_t)blockIdx.x * (kThreads / G) + threadIdx.x / G, p.T);
     if (t >= p.T) return;  // (whole warps)
@@ -135,12 +135,15 @@ __global__ void __launch_bounds__(kThreads) latent_append_kernel(const __grid_co
     Angles angles;
     angles.set(p.r, unit, pos);
     for (int h = r >> bits; h < p.H; h += B * step) {
-        if (h != r >> bits) fetch(h);
+        Held<TA> now[B];
+#pragma unroll
+        for (int k = 0; k < B; ++k) now[k] = held[k];
+        fetch(h + B * step);  // the next heads' loads fly while these turn
 #pragma unroll
         for (int k = 0; k < B; ++k) {
             if (h + k * step >= p.H) break;
             Values v;
-            v.from(held[k], unit);
+            v.from(now[k], unit);
             v.turn(p.r, unit, angles);
             v.store(unit, row<TA>(p.q_out, t, h + k * step));
         }

@@ -58,8 +58,8 @@ template <int N>
 struct Shape {
     static constexpr int COLS = N / 2;                       // columns of a warp
     static constexpr int G = COLS / 8;                       // groups of eight: a thread has two of each, of two keys
-    // (two rotary chunks, whatever the room: a tile's scores then wait for the values of the one before the last, so no
-    // wait for o_full or p_full is more than one phase behind, which is all that a parity tells)
+    // (two rotary chunks, whatever the room: a tile's scores then wait for the values of the one before the last, so the
+    // pairs of barriers for even and odd tiles are never two phases ahead of who waits for them)
     static constexpr int PAIRS = N == 64 ? 8 : N == 32 ? 10 : 11, TAILS = 2;
     static constexpr int Q = 9 * N * 128;
     static constexpr int BODY = Q + PAIRS * 2 * kChunk + TAILS * kChunk;
@@ -191,7 +191,8 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap latents, const __grid_c
     uint8_t* sq = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint8_t* pairs = sq + L::Q;
     uint8_t* tails = pairs + PAIRS * 2 * kChunk;
-    __shared__ uint64_t bars[2 * (PAIRS + TAILS) + 15];
+    constexpr int kBars = 2 * (PAIRS + TAILS) + 16;
+    __shared__ uint64_t bars[kBars];
     __shared__ Job jobs[2];
     uint64_t* full = bars;              // a pair landed
     uint64_t* empty = full + PAIRS;     // the products that read it finished
@@ -200,8 +201,8 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap latents, const __grid_c
     uint64_t* q_full = tempty + TAILS;  // the queries are in shared memory
     uint64_t* s_full = q_full + 1;      // scores of even and odd tiles
     uint64_t* p_full = s_full + 2;      // P is written, O rescaled, unseen rows are 0
-    uint64_t* o_full = p_full + 2;      // O holds this tile too
-    uint64_t* drain = o_full + 1;
+    uint64_t* o_full = p_full + 2;      // O holds this tile too (even and odd ones: a parity tells one phase from the one before)
+    uint64_t* drain = o_full + 2;
     uint64_t* half = drain + 2;         // the four warps of half of the columns meet
     uint64_t* both = half + 2;          // all eight
     uint64_t* j_full = both + 1;        // a job is in its slot
@@ -218,23 +219,18 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap latents, const __grid_c
     const int R = p.D, pairs_of_tile = R / 128, W = pp.l.K;
     const int box_log2 = min(p.page_log2, 6), per_tile = kKeys >> box_log2;  // rows of a copy, copies of a chunk
     const int share = blockIdx.x / pp.sides, side = blockIdx.x - share * pp.sides;
-    if (tid == 0) {
-        for (int i = 0; i < PAIRS; ++i) mbar_init(&full[i], 1), mbar_init(&empty[i], 1);
-        for (int i = 0; i < TAILS; ++i) mbar_init(&tfull[i], 1), mbar_init(&tempty[i], 1);
-        mbar_init(q_full, 8);
-        for (int i = 0; i < 2; ++i) mbar_init(&s_full[i], 1), mbar_init(&p_full[i], 8);
-        mbar_init(o_full, 1);
-        mbar_init(&drain[0], 1);
-        mbar_init(&drain[1], 1);
-        mbar_init(&half[0], 4);
-        mbar_init(&half[1], 4);
-        mbar_init(both, 8);
-        for (int i = 0; i < 2; ++i) mbar_init(&j_full[i], 1), mbar_init(&j_empty[i], 10);  // (softmax warps, MMA warps)
-        abort_word = 0;
-        raised[0] = raised[1] = 0;
-        for (int i = 0; i < kKeys; ++i) poisoned[i] = 0;
+    // (each barrier by a thread of its own: one thread for all took over a microsecond)
+    if (tid < kBars) {
+        uint64_t* bar = bars + tid;
+        uint32_t count = 1;
+        if (bar == q_full || bar == both || (bar >= p_full && bar < p_full + 2)) count = 8;  // (softmax warps)
+        if (bar >= half && bar < half + 2) count = 4;
+        if (bar >= j_empty && bar < j_empty + 2) count = 10;  // (softmax warps, MMA warps)
+        mbar_init(bar, count);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (tid >= 64 && tid < 64 + kKeys) poisoned[tid - 64] = 0;
+    if (tid == 128) abort_word = 0, raised[0] = raised[1] = 0;
     if (warp == 9) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_slot)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -242,6 +238,7 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap latents, const __grid_c
     tc_fence_before();
     Walk<0, kKeys> walk;
     const bool any = __any_sync(kFull, walk.begin(p, share, plan));
+    const Job first = any ? job_of<N>(p, walk.g, side) : Job{};
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_slot, tS = tmem, tO = tmem + 2 * N;  // S: even and odd tiles; O: pairs_of_tile times N columns
@@ -266,6 +263,7 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap latents, const __grid_c
             if (lane == 0) mbar_arrive(bar);
             return wait_warp(bar, n++ & 1u);
         };
+        auto values_of = [&](uint32_t n) { return wait_warp(&o_full[n & 1u], n >> 1 & 1u); };
         bool ok = true;
         auto take = [&](int j) {
             ok = wait_warp(&j_full[j & 1], (uint32_t)(j >> 1) & 1u);
@@ -277,20 +275,20 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap latents, const __grid_c
         // a segment's queries on their way: rows of 64 elements, 128-byte swizzled, zeros where there are none
         auto fetch_queries = [&](const Job& x) {
             if (x.end || x.tiles <= 0) return;
-            const int pieces = (pairs_of_tile * 2 + 1) * 8;
-            for (int i = tid; i < N * pieces; i += 256) {
-                const int row = i / pieces, c = i - row * pieces;
+            constexpr int kOf = 256 / N;  // threads of a row
+            const int row = tid / kOf, rr = x.row0 + (row < x.rows ? row : 0), tok = rr / p.R;
+            const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(p.q.p) + (int64_t)(x.q0 + tok) * p.q.ts + (rr - tok * p.R) * p.q.hs;
+            const uint32_t dst = smem_u32(sq) + row * 128;
+#pragma unroll 6
+            for (int c = tid % kOf; c < pairs_of_tile * 16 + 8; c += kOf) {
                 const bool there = row < x.rows && 8 * c < W;
-                const int rr = x.row0 + (there ? row : 0), tok = rr / p.R;
-                const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(p.q.p) + (int64_t)(x.q0 + tok) * p.q.ts +
-                                           (rr - tok * p.R) * p.q.hs + (there ? 8 * c : 0);
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(sq + (c >> 3) * (N * 128) + sw128_off(row, c & 7))),
-                             "l"(src), "r"(there ? 16 : 0)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + (c >> 3) * (N * 128) + ((c ^ row) & 7) * 16),
+                             "l"(src + (there ? 8 * c : 0)), "r"(there ? 16 : 0)
                              : "memory");
             }
         };
-        Job next = take(0);
-        if (ok) fetch_queries(next);
+        Job next = first;
+        fetch_queries(next);
         for (int j = 0; ok; ++j) {
             const Job x = next;
             if (x.end) break;
@@ -379,7 +377,7 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap latents, const __grid_c
                     }
                     ok = meet(&half[wg], meets);
                     if (!ok || t == 0) return;
-                    ok = wait_warp(o_full, (n_tiles - 1) & 1u);
+                    ok = values_of(n_tiles - 1);
                     if (!ok) return;
                     tc_fence_after();
 #pragma unroll
@@ -463,7 +461,7 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap latents, const __grid_c
             }
             if (!ok) break;
             // the next segment's queries come while this one's results go (every product with these is done)
-            next = take(j + 1);
+            next = take(j);
             if (!ok) break;
             fetch_queries(next);
             // ------------------------------------------------------------ result
@@ -477,7 +475,7 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap latents, const __grid_c
                     if (lane < 4) *reinterpret_cast<float2*>(&sums[warp][8 * g + 2 * lane]) = v;
                 }
                 if (x.tiles > 0) {
-                    ok = wait_warp(o_full, (n_tiles - 1) & 1u);
+                    ok = values_of(n_tiles - 1);
                     if (!ok) break;
                 }
                 tc_fence_after();
@@ -541,16 +539,24 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap latents, const __grid_c
         const int box = 128 << box_log2;
         const int nowhere = p.n_pages << p.page_log2;  // rows past the pool: the copy brings zeros
         bool ok = true, more = true;
+        auto on_its_way = [&] {
+            inflight |= 1u << slot;
+            par = (par & ~(1u << slot)) | (phase << slot);
+            if (++slot == PAIRS) slot = 0, phase ^= 1;
+        };
         for (int j = 0; ok; ++j) {
-            ok = wait_warp(&j_empty[j & 1], ((uint32_t)(j >> 1) & 1u) ^ 1u);
-            if (!ok) break;
-            Job x = job_of<N>(p, walk.g, side);
-            if (!more) x.end = 1;
-            if (lane == 0) {
-                jobs[j & 1] = x;
-                mbar_arrive(&j_full[j & 1]);
-                if (more && side == 0) walk.note(p);
+            Job x = first;
+            if (j > 0) {  // (which every thread has)
+                ok = wait_warp(&j_empty[(j - 1) & 1], ((uint32_t)((j - 1) >> 1) & 1u) ^ 1u);
+                if (!ok) break;
+                if (more) x = job_of<N>(p, walk.g, side);
+                else x.end = 1;
+                if (lane == 0) {
+                    jobs[(j - 1) & 1] = x;
+                    mbar_arrive(&j_full[(j - 1) & 1]);
+                }
             }
+            if (lane == 0 && more && side == 0) walk.note(p);
             __syncwarp();
             if (!more) break;
             const int32_t* ids = p.page_table + (int64_t)x.b * p.max_pages;
@@ -569,7 +575,18 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap latents, const __grid_c
                 for (int c = 0; c < 4; ++c) from[c] = __shfl_sync(kFull, row, c & (per_tile - 1));
                 // (by one lane from here on, and in as few copies as there can be: with a warp's meetings around each of
                 // them a pair took 590 cycles, which set the pace)
-                if (lane == 0) {
+                if (per_tile == 4) {  // (pages of 16: eight copies of a pair, a lane for each)
+                    for (int i = 0; i < pairs_of_tile && ok; ++i) {
+                        ok = wait_warp(&empty[slot], phase ^ 1);
+                        if (!ok) break;
+                        if (lane == 0) mbar_expect_tx(&full[slot], 2 * kChunk);
+                        __syncwarp();
+                        const int mine = __shfl_sync(kFull, row, lane & 3);
+                        if (lane < 8)
+                            tma_load_3d(pairs + (2 * slot + (lane >> 2)) * kChunk + (lane & 3) * box, &latents, 0, mine, 2 * i + (lane >> 2), &full[slot]);
+                        on_its_way();
+                    }
+                } else if (lane == 0) {
                     for (int i = 0; i < pairs_of_tile; ++i) {
                         ok = mbar_wait(&empty[slot], phase ^ 1, abort_flag, p.err, pp.wait_limit_ns);
                         if (!ok) break;
@@ -579,16 +596,15 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap latents, const __grid_c
                             tma_load_3d(dst, &latents, 0, from[0], 2 * i, &full[slot]);
                         } else {
 #pragma unroll
-                            for (int c = 0; c < 4; ++c) {
-                                if (c >= per_tile) break;
+                            for (int c = 0; c < 2; ++c) {
                                 tma_load_3d(dst + c * box, &latents, 0, from[c], 2 * i, &full[slot]);
                                 tma_load_3d(dst + kChunk + c * box, &latents, 0, from[c], 2 * i + 1, &full[slot]);
                             }
                         }
-                        inflight |= 1u << slot;
-                        par = (par & ~(1u << slot)) | (phase << slot);
-                        if (++slot == PAIRS) slot = 0, phase ^= 1;
+                        on_its_way();
                     }
+                }
+                if (lane == 0) {
                     if (ok) ok = mbar_wait(&tempty[tail], tphase ^ 1, abort_flag, p.err, pp.wait_limit_ns);
                     if (ok) {
                         *const_cast<volatile uint32_t*>(&good[tail]) = mask;
@@ -633,12 +649,16 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap latents, const __grid_c
         bool ok = true, issued = false;
         auto weights_of = [&](uint32_t n) { return wait_warp(&p_full[n & 1u], n >> 1 & 1u); };
         for (int j = 0; ok; ++j) {
-            ok = wait_warp(&j_full[j & 1], (uint32_t)(j >> 1) & 1u);
-            if (!ok) break;
-            const int tiles = __reduce_max_sync(kFull, jobs[j & 1].tiles), end = __reduce_max_sync(kFull, jobs[j & 1].end);
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&j_empty[j & 1]);
-            if (end) break;
+            int tiles = __reduce_max_sync(kFull, first.tiles);
+            if (j > 0) {
+                ok = wait_warp(&j_full[(j - 1) & 1], (uint32_t)((j - 1) >> 1) & 1u);
+                if (!ok) break;
+                tiles = __reduce_max_sync(kFull, jobs[(j - 1) & 1].tiles);
+                const int end = __reduce_max_sync(kFull, jobs[(j - 1) & 1].end);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&j_empty[(j - 1) & 1]);
+                if (end) break;
+            }
             if (tiles <= 0) continue;
             if (!values) ok = wait_warp(q_full, qn++ & 1u);
             for (int t = 0; t < tiles && ok; ++t, ++tile) {
@@ -659,7 +679,7 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap latents, const __grid_c
                     }
                     if (elect_one()) {
                         mma_commit(&tempty[tail]);
-                        mma_commit(o_full);
+                        mma_commit(&o_full[tile & 1u]);
                     }
                 } else {
                     if (tile >= 2) ok = weights_of(tile - 2);  // the scores that lay there have been read

@@ -386,6 +386,25 @@ def test_cached_maxima_that_rise_in_every_tile(H, R, P):
     assert all(torch.equal(o, outs[0]) for o in outs)
 
 
+def test_cached_after_other_kernels():
+    """Contexts of one to four tiles, each call after kernels of other code and sizes, so that the CTA's warps come to
+    their first instructions at different times."""
+    cases = [cached_case(20 + i, "bf16", H, R, P, page, [1] * len(lens), lens)
+             for i, (H, R, P, page, lens) in enumerate([(1, 512, 64, 32, [127, 128]), (5, 256, 32, 16, [200, 17, 130]), (64, 512, 64, 64, [128]),
+                                                        (30, 128, 16, 64, [250, 129, 64]), (128, 384, 64, 128, [190, 128])])]
+    wants = [ref.absorbed(q, pool, cfg.latent_dim, [1] * q.shape[0], pool.lens, cfg.scale) for pool, q, cfg in cases]
+    big = torch.empty(1 << 26, device="cuda")
+    q, k, kr, v = prompt_inputs(1, "bf16", 8, 128, 64, 128, [300], [300])
+    pc, o = gb.latent_config(8), torch.empty((300, 8, 128), dtype=torch.bfloat16, device="cuda")
+    pws = workspace(pc, 300, 1)
+    for _ in range(12):
+        for (pool, cq, cfg), want in zip(cases, wants):
+            big.fill_(1.0)
+            gb.latent_prompt(pc, q, k, kr, v, prefix([300]), prefix([300]), o, pws)
+            (big[: 1 << 20].view(1024, 1024) @ big[: 1 << 20].view(1024, 1024)).sum()
+            check(run_cached(cfg, pool, cq, [1] * cq.shape[0], pool.lens), None, want, "bf16")
+
+
 @pytest.mark.parametrize("act", ["f32", "bf16"])
 def test_pool_past_32_bit_offsets(act):
     """A sequence's pages at the end of a pool of more than 2^32 bytes (and elements, bf16)."""
