@@ -762,12 +762,16 @@ bool latent_cached_tc_supported(const LatentProblem& p) {
 }
 
 cudaError_t launch_latent_cached_tc(const LatentProblem& p, cudaStream_t stream) {
-    // rows of a sequence, on average
-    const int64_t rows = ((int64_t)p.a.T * p.a.R + p.a.B - 1) / p.a.B;
-    auto sides = [&](int n) { return (int)min64(kMostSides, (rows + n - 1) / n); };
-    if (rows <= 16) return cached_as<16>(p, 1, stream);
-    if (rows <= 32) return cached_as<32>(p, 1, stream);
-    return cached_as<64>(p, sides(64), stream);
+    // Rows of a sequence, on average. As many of them in a CTA as there are, up to 64; fewer, and more CTAs beside each
+    // other, where the key axis has too few blocks for every SM: a CTA's queries and results are then less (one sequence
+    // of 4000 keys and 128 heads).
+    const AttnProblem& a = p.a;
+    const int64_t rows = ((int64_t)a.T * a.R + a.B - 1) / a.B;
+    int n = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+    auto sides = [&] { return (int)min64(kMostSides, (rows + n - 1) / n); };
+    const int64_t blocks = a.B * (((int64_t)a.max_pages * a.page + kKeys - 1) / kKeys + kTileCost);
+    while (n > 16 && 2 * sides() <= kMostSides && 2 * sides() * ((blocks + kMinBlocks - 1) / kMinBlocks) <= sm_count()) n /= 2;
+    return n == 16 ? cached_as<16>(p, sides(), stream) : n == 32 ? cached_as<32>(p, sides(), stream) : cached_as<64>(p, sides(), stream);
 }
 
 }  // namespace gbmoe
