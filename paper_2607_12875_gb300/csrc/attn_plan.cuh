@@ -165,6 +165,10 @@ struct Segment {
 template <int kRows, int kBlock = kBlockKeys>
 struct Walk {
     __device__ __forceinline__ static int tile_rows(const AttnProblem& p) { return kRows > 0 ? kRows : p.tile_rows; }
+    __device__ __forceinline__ static int64_t tiles_of(const AttnProblem& p, const Seq& s) {
+        if constexpr (kRows > 0) return row_tiles(p, s, kRows);
+        return div64((int64_t)s.nq * p.R + p.tile_rows - 1, p.tile_rows);
+    }
     Shares sh;
     int64_t u, u0, u1;  // where the segment begins; the share's begin and end
     int64_t share;
@@ -176,7 +180,7 @@ struct Walk {
         share = index;
         const Place at = find_place(
             p.B,
-            [&](int b) { const Seq s = load_seq(p, b); return row_tiles(p, s, tile_rows(p)) * (key_blocks<kBlock>(s) + p.tile_cost) * p.Hkv; },
+            [&](int b) { const Seq s = load_seq(p, b); return tiles_of(p, s) * (key_blocks<kBlock>(s) + p.tile_cost) * p.Hkv; },
             [&](int64_t total) { sh.set(p, total); return index * sh.each; }, sm);
         if (at.b < 0) return false;
         u = u0 = index * sh.each;
@@ -226,7 +230,7 @@ struct Walk {
     __device__ __forceinline__ void enter(const AttnProblem& p, int b) {
         g.b = b;
         g.s = load_seq(p, b);
-        tiles = (int)row_tiles(p, g.s, tile_rows(p));
+        tiles = (int)tiles_of(p, g.s);
         g.nb = key_blocks<kBlock>(g.s);
     }
     __device__ __forceinline__ void cut(const AttnProblem& p) {

@@ -183,7 +183,6 @@ struct Params {
 template <int N>
 __global__ void __launch_bounds__(kThreads, 1)
 latent_cached_kernel(const __grid_constant__ CUtensorMap latents, const __grid_constant__ CUtensorMap pool, const __grid_constant__ Params pp) {
-    pdl_enter();
     using L = Shape<N>;
     constexpr int COLS = L::COLS, G = L::G, PAIRS = L::PAIRS, TAILS = L::TAILS;
     const AttnProblem& p = pp.l.a;
@@ -235,6 +234,8 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap latents, const __grid_c
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_slot)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
+    // (up to here nothing in memory is read: barriers and TMEM are set up while the kernel before still runs)
+    pdl_enter();
     tc_fence_before();
     Walk<0, kKeys> walk;
     const bool any = __any_sync(kFull, walk.begin(p, share, plan));
