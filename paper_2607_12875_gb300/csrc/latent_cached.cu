@@ -532,6 +532,7 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap latents, const __grid_c
                 if (!ok) break;
             }
         }
+        asm volatile("cp.async.wait_all;" ::: "memory");  // (a wait gave up: queries may be on their way)
     } else if (warp == 8) {
         // ------------------------------------------------------------ TMA producer
         uint32_t inflight = 0, par = 0, tinflight = 0, tpar = 0;
@@ -667,6 +668,7 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap latents, const __grid_c
                     ok = weights_of(tile);
                     if (!ok) break;
                     tc_fence_after();
+                    issued = true;
                     for (int i = 0; i < pairs_of_tile; ++i) {
                         if (elect_one()) {
                             const uint64_t a = dv + (uint64_t)((uint32_t)(slot * 2 * kChunk) >> 4), b = dp + (uint64_t)((uint32_t)(tail * kChunk) >> 4);
@@ -689,6 +691,7 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap latents, const __grid_c
                         ok = wait_warp(&full[slot], phase);
                         if (!ok) break;
                         tc_fence_after();
+                        issued = true;
                         if (elect_one()) {
                             const uint64_t a = dk + (uint64_t)((uint32_t)(slot * 2 * kChunk) >> 4), b = dq + (uint64_t)((uint32_t)(i * 2 * N * 128) >> 4);
 #pragma unroll
@@ -709,7 +712,6 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap latents, const __grid_c
                     }
                 }
                 __syncwarp();
-                issued = true;
                 if (++tail == TAILS) tail = 0, tphase ^= 1;
             }
         }

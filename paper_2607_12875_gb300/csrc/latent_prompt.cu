@@ -49,6 +49,11 @@ constexpr float kGrow = 8.0f;          // log2 of how far a row's maximum may ru
 constexpr int kSmem = 1024 + 2 * kQTile + kSlots * kHalf + 512;
 static_assert((2 * kSlots + 24) * 8 <= 512 && kSmem + 1024 <= 227 * 1024, "shared memory");
 
+// bytes that are to come, without an arrival
+__device__ __forceinline__ void mbar_expect_only(uint64_t* bar, uint32_t bytes) {
+    asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
+}
+
 struct Params {
     LatentProblem l;
     uint64_t wait_limit_ns;
@@ -398,6 +403,7 @@ latent_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             int slot = 0, used = 0;       // next slot, slots that are not free
             uint32_t seq = 0, oldest = 0;  // tiles begun, and of those the first whose slots are not free
             uint64_t sizes = 0;           // slots of the latest tiles, four bits each
+            bool open = false;            // the last tile's chunks are not all asked for
             bool ok = true;
             const int v_boxes = (p.D + 63) / 64;
             for (int k = 0; ok; ++k) {
@@ -435,10 +441,8 @@ latent_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                             ++oldest;
                         }
                         if (!ok) break;
-                        if (c == 0) {
-                            mbar_expect_tx(bar, value ? v_boxes * kHalf : k_chunks * kHalf);
-                            ++seq;
-                        }
+                        if (c == 0) ++seq;
+                        mbar_expect_only(bar, value ? v_boxes * kHalf / 2 : kHalf);
                         uint8_t* dst = sKV + slot * kHalf;
                         if (value)
                             for (int x = 0; x < v_boxes; ++x) tma_load_3d(dst + x * kHalf / 2, &tm_v, 64 * x, w.head0, key + 64 * c, bar);
@@ -448,10 +452,13 @@ latent_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                             tma_load_3d(dst, &tm_r, 0, 0, key, bar);
                         ++used;
                         if (++slot == kSlots) slot = 0;
+                        open = c + 1 < chunks;
+                        if (!open) mbar_arrive(bar);
                     }
                 }
             }
-            // every copy has landed before the CTA leaves
+            // every copy has landed before the CTA leaves (a wait that gave up inside a tile: those that were asked for)
+            if (open) mbar_arrive(&full[(seq - 1) % kSlots]);
             const uint64_t t0 = global_ns();
             for (int t = 0; t < 2; ++t)
                 if (qn[t] > 0) drain_wait(&q_full[t], (qn[t] - 1) & 1u, t0);

@@ -226,6 +226,22 @@ def test_prompt_ignores_what_no_query_sees(act, bad):
     check(torch.where(seen | rows, out, out2), None, want, act)
 
 
+@pytest.mark.parametrize("H,lens", [(4, [700]), (100, [300, 200])])   # keys dealt to both tiles; each CTA takes several items
+def test_prompt_waits_that_run_out(monkeypatch, H, lens):
+    """With a limit of 0 ns on the pipeline waits a call gives up, the error word says so, and the next is right again."""
+    T = sum(lens)
+    q, k, kr, v = prompt_inputs(13, "bf16", H, 128, 64, 128, lens, lens)
+    cfg = gb.latent_config(H)
+    ws, cu, out = workspace(cfg, T, len(lens)), prefix(lens), torch.zeros((T, H, 128), dtype=torch.bfloat16, device="cuda")
+    monkeypatch.setenv("GBMOE_TC_WAIT_LIMIT_NS", "0")
+    gb.latent_prompt(cfg, q, k, kr, v, cu, cu, out, ws)
+    assert gb.moe_device_status(ws) == gb.EDEVICE_TIMEOUT
+    monkeypatch.delenv("GBMOE_TC_WAIT_LIMIT_NS")
+    gb.latent_prompt(cfg, q, k, kr, v, cu, cu, out, ws)
+    assert gb.moe_device_status(ws) == gb.OK
+    check(out, None, ref.expanded(q, k, kr, v, lens, lens, cfg.scale), "bf16")
+
+
 # ------------------------------------------------------------------- absorbed
 
 
@@ -384,6 +400,19 @@ def test_cached_maxima_that_rise_in_every_tile(H, R, P):
     # the score): up to 10^-3 of a weight
     check(outs[0], None, want, "bf16", terms=2e-3)
     assert all(torch.equal(o, outs[0]) for o in outs)
+
+
+@pytest.mark.parametrize("H,page", [(16, 16), (128, 64)])
+def test_cached_waits_that_run_out(monkeypatch, H, page):
+    nq, lens = [1, 2], [3000, 500]
+    pool, q, cfg = cached_case(14, "bf16", H, 512, 64, page, nq, lens)
+    keep, ws = (prefix(nq), i32(lens), i32(pool.table)), workspace(cfg, 3, 2)
+    out = torch.zeros((3, H, 512), dtype=torch.bfloat16, device="cuda")
+    monkeypatch.setenv("GBMOE_TC_WAIT_LIMIT_NS", "0")
+    gb.latent_cached(cfg, gb.attn_batch(*keep), q, gb.latent_cache(pool.rows), out, ws)
+    assert gb.moe_device_status(ws) == gb.EDEVICE_TIMEOUT
+    monkeypatch.delenv("GBMOE_TC_WAIT_LIMIT_NS")
+    check(run_cached(cfg, pool, q, nq, lens, ws=ws), None, ref.absorbed(q, pool, 512, nq, lens, cfg.scale), "bf16")
 
 
 def test_cached_after_other_kernels():
