@@ -255,8 +255,8 @@ int moe_rmsnorm(const gbmoe_config* cfg, const void* x, const void* gamma, float
  *   s = x + residual          rounded to act_dtype (residual NULL: s = x)
  *   y = moe_rmsnorm(s)        bit for bit
  * sum_out [T, H] takes s (NULL: not wanted; it may be x or residual). y [T, H] may
- * be NULL where codes and scales are given: the norm before its rounding to
- * act_dtype as e4m3 codes [T, H] with one fp32 scale per row and 128 columns [T, H
+ * be NULL where codes and scales are given: the norm, not rounded to act_dtype
+ * in between, as e4m3 codes [T, H] with one fp32 scale per row and 128 columns [T, H
  * / 128], the smallest power of two 2^e >= 2^-126 with max |y in the block| <= 448
  * * 2^e; element = e4m3(code) * scale, rounded to the nearest code, ties to even. A
  * NaN gives the NaN code and an infinity +-448 (both are left out of the maximum).

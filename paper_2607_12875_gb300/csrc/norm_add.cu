@@ -54,12 +54,17 @@ __device__ __forceinline__ void add_piece(const Raw8<TA>& a, const Raw8<TA>& b, 
 
 // A lane's piece of the result, to the outputs that there are.
 template <typename TA>
-__device__ __forceinline__ void finish(const NormAdd& p, int64_t t, int at, const Raw8<TA>& s, const Raw8<TA>& g, float inv) {
+__device__ __forceinline__ void finish(const NormAdd& p, int64_t t, int at, const Raw8<TA>& s, const Raw8<TA>& g, float inv, float close) {
     float o[8];
+    if (p.y) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) o[j] = __fmul_rn(__fmul_rn(s.at(j), inv), g.at(j));
-    if (p.y) Vec8<TA>::store(static_cast<TA*>(p.y) + t * p.H + at, o);
+        for (int j = 0; j < 8; ++j) o[j] = __fmul_rn(__fmul_rn(s.at(j), inv), g.at(j));
+        Vec8<TA>::store(static_cast<TA*>(p.y) + t * p.H + at, o);
+    }
     if (!p.codes) return;
+    // (bf16: the first product is exact, so there is one rounding before the code's)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j] = __fmul_rn(__fmul_rn(s.at(j), g.at(j)), close);
     float top = 0.0f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -83,6 +88,20 @@ __device__ __forceinline__ void add_squares(float& ss, const Raw8<TA>& s) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) ss = __fmaf_rn(s.at(j), s.at(j), ss);
 }
+// The squares once more, for the codes: eight sums and then a tree, whose roundings do not add up as those of the fixed
+// order do (of 33.5 million codes 19 to 32 came out one step off the nearest with that order's sum).
+template <typename TA>
+__device__ __forceinline__ void add_squares8(float (&ss)[8], const Raw8<TA>& s) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) ss[j] = fmaf(s.at(j), s.at(j), ss[j]);
+}
+__device__ __forceinline__ float tree(const float (&ss)[8]) {
+    float v = ((ss[0] + ss[1]) + (ss[2] + ss[3])) + ((ss[4] + ss[5]) + (ss[6] + ss[7]));
+#pragma unroll
+    for (int d = 16; d >= 1; d >>= 1) v += __shfl_xor_sync(kFull, v, d);
+    return v;
+}
+__device__ __forceinline__ float close_inverse(const NormAdd& p, float sum) { return __frsqrt_rn(sum / (float)p.H + p.eps); }
 // 1 / sqrt(mean + eps) from the lanes' sums
 __device__ __forceinline__ float inverse(const NormAdd& p, float ss) {
 #pragma unroll
@@ -97,7 +116,7 @@ template <typename TA, int kHeld>
 __global__ void __launch_bounds__(32 * kWarps) norm_add_kernel(const __grid_constant__ NormAdd p) {
     pdl_enter();
     extern __shared__ uint4 rows[];
-    __shared__ float scale;
+    __shared__ float scale, sums[kWarps];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n = p.H / 256;
     const int64_t t = blockIdx.x;
     const TA* x = static_cast<const TA*>(p.x) + t * p.H;
@@ -122,8 +141,16 @@ __global__ void __launch_bounds__(32 * kWarps) norm_add_kernel(const __grid_cons
         put(shared + column(i), s[i]);
         if (sum) put(sum + column(i), s[i]);
     }
+    if (p.codes) {
+        float ss[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i)
+            if (warp + kWarps * i < n) add_squares8(ss, s[i]);
+        const float v = tree(ss);
+        if (lane == 0) sums[warp] = v;
+    }
     __syncthreads();
-    if (warp == 0) {
+    if (warp == 0 && p.y) {
         float ss = 0.0f;
 #pragma unroll 4
         for (int i = 0; i < n; ++i) {
@@ -134,11 +161,11 @@ __global__ void __launch_bounds__(32 * kWarps) norm_add_kernel(const __grid_cons
         const float inv = inverse(p, ss);
         if (lane == 0) scale = inv;
     }
-    __syncthreads();
-    const float inv = scale;
+    if (p.y) __syncthreads();
+    const float inv = p.y ? scale : 0.0f, close = p.codes ? close_inverse(p, (sums[0] + sums[1]) + (sums[2] + sums[3])) : 0.0f;
 #pragma unroll
     for (int i = 0; i < kHeld; ++i)
-        if (warp + kWarps * i < n) finish(p, t, column(i), s[i], g[i], inv);
+        if (warp + kWarps * i < n) finish(p, t, column(i), s[i], g[i], inv, close);
 }
 
 // Rows of any width, one by a warp, read twice.
@@ -159,16 +186,20 @@ __global__ void __launch_bounds__(128) norm_add_wide_kernel(const __grid_constan
         add_piece(a, b, res != nullptr, s);
         return s;
     };
-    float ss = 0.0f;
-    for (int i = 0; i < n; ++i) add_squares(ss, piece(i));
-    const float inv = inverse(p, ss);
+    float ss = 0.0f, ss8[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < n; ++i) {
+        const Raw8<TA> s = piece(i);
+        add_squares(ss, s);
+        add_squares8(ss8, s);
+    }
+    const float inv = inverse(p, ss), close = close_inverse(p, tree(ss8));
     for (int i = 0; i < n; ++i) {
         const int at = 256 * i + 8 * lane;
         const Raw8<TA> s = piece(i);
         Raw8<TA> g;
         g.load(static_cast<const TA*>(p.gamma) + at);
         if (sum) put(sum + at, s);  // (after both readings: it may be x or the residual)
-        finish(p, t, at, s, g, inv);
+        finish(p, t, at, s, g, inv, close);
     }
 }
 
