@@ -2,7 +2,7 @@
 // kernels do not take. Both forms.
 //
 // One pass over the keys with the running maximum and sum of the softmax: a block
-// holds 16 rows, token and head (absorbed), or 32 tokens of one head (expanded), walks
+// holds 8 or 16 rows, token and head (absorbed), or 16 or 32 tokens of one head (expanded), walks
 // its keys in tiles of 32 through two buffers in shared memory (cp.async) and keeps
 // the weighted sums in registers. Absorbed: a tile's rows are keys and values at once.
 #include <type_traits>
@@ -17,7 +17,7 @@ namespace {
 constexpr int kThreads = 128;
 constexpr int kKeys = 32;
 static_assert(4 * kKeys == kThreads, "four threads for a key");
-constexpr int kMinBlocks = 1, kTileCost = 0;  // shares of one block of 64 keys, as attn_simt.cu
+constexpr int kBlock = kKeys, kMinBlocks = 1, kTileCost = 0;  // absorbed: shares of one tile at least
 
 // 16 bytes global -> shared, or 16 bytes of zeros
 __device__ __forceinline__ void cp_async_or_zero(void* dst, const void* src, bool good) {
@@ -44,12 +44,15 @@ __host__ __device__ __forceinline__ Sizes sizes_of(int key, int value, int eb, i
     return s;
 }
 
-// N: rows of a thread, 2 (expanded) or 1 (absorbed); NC: its float4 columns. Thread
-// (ty, tx) = (tid / 8, tid % 8) holds rows N ty .., of the scores the keys tx + 8 j,
-// of the result the columns 4 tx + 32 j ..; a row's eight threads lie in one warp.
-template <typename TA, int N, int NC>
+// N: rows of a thread, 2 (expanded) or 1 (absorbed); TX: threads of its rows, 8 or 16
+// (all in one warp); NC: its float4 columns. Thread (ty, tx) = (tid / TX, tid % TX)
+// holds rows N ty .., of the scores the keys tx + TX j, of the result the columns 4 tx +
+// 4 TX j ..
+template <int N, int TX>
+constexpr int kTileRows = kThreads / TX * N;
+template <typename TA, int N, int TX, int NC>
 __device__ __forceinline__ void attend(const LatentProblem& lp, const Segment& it) {
-    constexpr int kRows = 16 * N, EB = sizeof(TA);
+    constexpr int kRows = kTileRows<N, TX>, EB = sizeof(TA), JK = kKeys / TX;
     constexpr bool kPaged = N == 1;
     const AttnProblem& p = lp.a;
     extern __shared__ float4 smem4[];
@@ -60,10 +63,10 @@ __device__ __forceinline__ void attend(const LatentProblem& lp, const Segment& i
     int* marks = reinterpret_cast<int*>(sp + kRows * (kKeys + 1));
     const int R = p.R, head0 = kPaged ? 0 : it.head, row0 = it.tile * kRows;
     const int n_rows = (int)min64(kRows, (int64_t)it.s.nq * R - row0);
-    const int c_lo = (int)min64((int64_t)it.blk0 * kBlockKeys, it.s.len);
-    const int c_hi = (int)min64((int64_t)it.blk1 * kBlockKeys, it.s.len);
+    const int c_lo = (int)min64((int64_t)it.blk0 * kBlock, it.s.len);
+    const int c_hi = (int)min64((int64_t)it.blk1 * kBlock, it.s.len);
 
-    const int tid = threadIdx.x, ty = tid >> 3, tx = tid & 7;
+    const int tid = threadIdx.x, ty = tid / TX, tx = tid % TX;
     const int qp = lp.K * EB / 16;  // pieces of a query
     for (int i = tid; i < kRows * qp; i += kThreads) {
         const int r = i / qp, c = i % qp;
@@ -132,18 +135,18 @@ __device__ __forceinline__ void attend(const LatentProblem& lp, const Segment& i
         }
         __syncthreads();
         const uint8_t* tile = skv + buf * kKeys * sz.k_pitch;
-        if (N * 4 * (tid >> 5) < n_rows) {  // (else no row of this warp)
-            float s[N][4] = {};
+        if (N * (32 / TX) * (tid >> 5) < n_rows) {  // (else no row of this warp)
+            float s[N][JK] = {};
             for (int d = 0; d < lp.K; d += 4) {
-                float4 a[N], b[4];
+                float4 a[N], b[JK];
 #pragma unroll
                 for (int r = 0; r < N; ++r) a[r] = load4<TA>(sq + (N * ty + r) * sz.q_pitch + d * EB);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) b[j] = load4<TA>(tile + (tx + 8 * j) * sz.k_pitch + d * EB);
+                for (int j = 0; j < JK; ++j) b[j] = load4<TA>(tile + (tx + TX * j) * sz.k_pitch + d * EB);
 #pragma unroll
                 for (int r = 0; r < N; ++r)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
+                    for (int j = 0; j < JK; ++j)
                         s[r][j] = fmaf(a[r].x, b[j].x, fmaf(a[r].y, b[j].y, fmaf(a[r].z, b[j].z, fmaf(a[r].w, b[j].w, s[r][j]))));
             }
             bool all = true;  // this thread's rows see every key of the tile
@@ -151,25 +154,25 @@ __device__ __forceinline__ void attend(const LatentProblem& lp, const Segment& i
             for (int r = 0; r < N; ++r) {
                 float mx = neg_inf();
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int k = k0 + tx + 8 * j;
-                    const bool see = k >= lo[r] && k <= hi[r] && k < k_hi && (!kPaged || marks[buf * kKeys + tx + 8 * j]);
+                for (int j = 0; j < JK; ++j) {
+                    const int k = k0 + tx + TX * j;
+                    const bool see = k >= lo[r] && k <= hi[r] && k < k_hi && (!kPaged || marks[buf * kKeys + tx + TX * j]);
                     all &= see;
                     s[r][j] = see ? s[r][j] * p.scale_log2 : neg_inf();
                     mx = fmaxf(mx, s[r][j]);
                 }
 #pragma unroll
-                for (int d = 1; d < 8; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+                for (int d = 1; d < TX; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
                 const float m_new = fmaxf(m[r], mx);
                 const float base = m_new == neg_inf() ? 0.0f : m_new;
                 const float f = exp2f(m[r] - base);
                 m[r] = m_new;
                 float sum = 0.0f;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
+                for (int j = 0; j < JK; ++j) {
                     s[r][j] = exp2f(s[r][j] - base);
                     sum += s[r][j];
-                    sp[(N * ty + r) * (kKeys + 1) + tx + 8 * j] = s[r][j];
+                    sp[(N * ty + r) * (kKeys + 1) + tx + TX * j] = s[r][j];
                 }
                 l[r] = l[r] * f + sum;
 #pragma unroll
@@ -191,7 +194,7 @@ __device__ __forceinline__ void attend(const LatentProblem& lp, const Segment& i
                     }
 #pragma unroll
                     for (int c = 0; c < NC; ++c) {
-                        const int d = 4 * tx + 32 * c;
+                        const int d = 4 * tx + 4 * TX * c;
                         if (d >= p.D) break;
                         const float4 v = load4<TA>(values + j * sz.k_pitch + d * EB);
 #pragma unroll
@@ -212,7 +215,7 @@ __device__ __forceinline__ void attend(const LatentProblem& lp, const Segment& i
 #pragma unroll
     for (int r = 0; r < N; ++r) {
 #pragma unroll
-        for (int d = 1; d < 8; d <<= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], d);
+        for (int d = 1; d < TX; d <<= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], d);
         const int rr = N * ty + r;
         if (rr >= n_rows) continue;
         const int64_t t = it.s.q0 + (row0 + rr) / R;
@@ -225,7 +228,7 @@ __device__ __forceinline__ void attend(const LatentProblem& lp, const Segment& i
             if (tx == 0) reinterpret_cast<float4*>(p.part_s)[at] = make_float4(m[r], l[r], m[r], sees ? 1.0f : 0.0f);
 #pragma unroll
             for (int c = 0; c < NC; ++c)
-                if (4 * tx + 32 * c < p.D) *reinterpret_cast<float4*>(p.part_o + at * p.D + 4 * tx + 32 * c) = o[r][c];
+                if (4 * tx + 4 * TX * c < p.D) *reinterpret_cast<float4*>(p.part_o + at * p.D + 4 * tx + 4 * TX * c) = o[r][c];
             continue;
         }
         const bool empty = hi[r] < lo[r] || !sees;
@@ -234,7 +237,7 @@ __device__ __forceinline__ void attend(const LatentProblem& lp, const Segment& i
         TA* out = const_cast<TA*>(static_cast<const TA*>(p.out.p)) + t * p.out.ts + hq * p.out.hs;
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-            const int d = 4 * tx + 32 * c;
+            const int d = 4 * tx + 4 * TX * c;
             if (d >= p.D) continue;
             const float v[4] = {o[r][c].x * inv, o[r][c].y * inv, o[r][c].z * inv, o[r][c].w * inv};
             if constexpr (EB == 4)
@@ -245,50 +248,51 @@ __device__ __forceinline__ void attend(const LatentProblem& lp, const Segment& i
     }
 }
 
-template <typename TA, int N, int NC>
+template <typename TA, int N, int TX, int NC>
 __global__ void __launch_bounds__(kThreads) latent_simt_kernel(const __grid_constant__ LatentProblem lp) {
     pdl_enter();
     const AttnProblem& p = lp.a;
     __shared__ int64_t plan[plan_words(kThreads)];
     if constexpr (N == 1) {
-        Walk<16> w;
+        Walk<kTileRows<N, TX>, kBlock> w;
         if (!w.begin(p, blockIdx.x, plan)) {
             if (threadIdx.x == 0) w.note_idle(p, blockIdx.x);
             return;
         }
         do {
-            attend<TA, N, NC>(lp, w.g);
+            attend<TA, N, TX, NC>(lp, w.g);
             if (threadIdx.x == 0) w.note(p);
             __syncthreads();
         } while (w.next(p));
     } else {
         Segment g{};
         g.head = blockIdx.x % p.Hq;
-        const Place at = find_tile(p, blockIdx.x / p.Hq, 16 * N, plan);
+        const Place at = find_tile(p, blockIdx.x / p.Hq, kTileRows<N, TX>, plan);
         if (at.b < 0) return;
         g.b = at.b, g.s = load_seq(p, at.b), g.tile = (int)at.at;
-        g.blk1 = key_blocks(g.s), g.slot = -1;
-        attend<TA, N, NC>(lp, g);
+        g.blk1 = key_blocks<kBlock>(g.s), g.slot = -1;
+        attend<TA, N, TX, NC>(lp, g);
     }
 }
 
-template <typename TA, int N, int NC>
+template <typename TA, int N, int TX, int NC>
 cudaError_t simt_as(const LatentProblem& p, cudaStream_t stream) {
-    constexpr auto kernel = latent_simt_kernel<TA, N, NC>;
+    constexpr auto kernel = latent_simt_kernel<TA, N, TX, NC>;
+    constexpr int kRows = kTileRows<N, TX>;
     static DeviceOnce once;
     constexpr int kMost = 227 * 1024;
     if (cudaError_t e = once.run([] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost - 1024); });
         e != cudaSuccess)
         return e;
-    const int smem = sizes_of(p.K, N == 1 ? 0 : p.a.D, (int)sizeof(TA), 16 * N).total;
+    const int smem = sizes_of(p.K, N == 1 ? 0 : p.a.D, (int)sizeof(TA), kRows).total;
     if constexpr (N == 1) {
         LatentProblem a = p;
         const int fit = kMost / (smem + 2048);
-        set_shares(a.a, 16, fit < 1 ? 1 : fit > 4 ? 4 : fit, sm_count(), kMinBlocks, kTileCost);
+        set_shares(a.a, kRows, fit < 1 ? 1 : fit > 4 ? 4 : fit, sm_count(), kMinBlocks, kTileCost, kBlock);
         if (cudaError_t e = launch_k(kernel, dim3(a.a.shares), dim3(kThreads), smem, stream, a); e != cudaSuccess) return e;
         return a.a.shares > 1 ? launch_attn_join(a.a, stream) : cudaSuccess;
     } else {
-        const int64_t grid = ((int64_t)p.a.T / (16 * N) + p.a.B) * p.a.Hq;
+        const int64_t grid = ((int64_t)p.a.T / kRows + p.a.B) * p.a.Hq;
         if (grid > INT32_MAX) return cudaErrorInvalidConfiguration;
         return launch_k(kernel, dim3((unsigned)grid), dim3(kThreads), smem, stream, p);
     }
@@ -296,8 +300,16 @@ cudaError_t simt_as(const LatentProblem& p, cudaStream_t stream) {
 
 template <typename TA>
 cudaError_t simt_type(const LatentProblem& p, cudaStream_t stream) {
-    if (p.a.paged) return p.a.D <= 256 ? simt_as<TA, 1, 8>(p, stream) : simt_as<TA, 1, 16>(p, stream);
-    return p.a.D <= 64 ? simt_as<TA, 2, 2>(p, stream) : simt_as<TA, 2, 4>(p, stream);
+    if (p.a.paged) {
+        // eight rows where a sequence has no more, so that none of the warps stands idle
+        const bool few = (int64_t)p.a.T * p.a.R <= 8 * (int64_t)p.a.B;
+        if (p.a.D <= 256) return few ? simt_as<TA, 1, 16, 4>(p, stream) : simt_as<TA, 1, 8, 8>(p, stream);
+        return few ? simt_as<TA, 1, 16, 8>(p, stream) : simt_as<TA, 1, 8, 16>(p, stream);
+    }
+    // 16 tokens where 32 leave SMs without a block
+    const bool few = ((int64_t)p.a.T / 32 + p.a.B) * p.a.Hq <= sm_count();
+    if (p.a.D <= 64) return few ? simt_as<TA, 2, 16, 1>(p, stream) : simt_as<TA, 2, 8, 2>(p, stream);
+    return few ? simt_as<TA, 2, 16, 2>(p, stream) : simt_as<TA, 2, 8, 4>(p, stream);
 }
 
 }  // namespace
