@@ -648,9 +648,10 @@ bool latent_prompt_tc_supported(const LatentProblem& p) {
 }
 
 cudaError_t launch_latent_prompt_tc(const LatentProblem& p, cudaStream_t stream) {
-    // Too few items for every SM (or, of long prompts, to even out over them).
-    const int64_t items = items_of(p.a, 2 * kTile);
-    const bool deal = items <= sm_count() || (items <= 2 * sm_count() && p.a.T >= (int64_t)2 * kTile * p.a.B);
+    // Too few items for every SM. Us without and with: 1000 tokens of 4 heads 25.7 and 18.5; 4096 of 8 (136 items) 73.8 and
+    // 68.5; four prompts of 4000 in all, 8 heads (152 items) 38.3 and 40.1; 4096 of 16 92 and 112 (dealt keys are
+    // loaded for half as many rows).
+    const bool deal = items_of(p.a, 2 * kTile) < sm_count();
     return deal ? prompt_as<true>(p, stream) : prompt_as<false>(p, stream);
 }
 
