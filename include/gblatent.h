@@ -74,9 +74,10 @@ size_t latent_workspace_size(const gblatent_config* cfg, int32_t T, int32_t B);
  * in fp32, rounded once. Optional outputs: kv_out [T, R + P], the same rows (what
  * the expansion to keys and values takes; kv_out may be kv), and q_out, the
  * rotary parts of the queries q [T, heads, P] turned likewise (q_out may be q).
- * table: attn_rope_table of P. Tokens whose position is negative or beyond the
- * table, or whose page is outside the pool, are not stored; their outputs are
- * written. Two sequences may not append to the same slot in one call.
+ * table: attn_rope_table of P. Tokens whose place p is negative or beyond the
+ * page table, or whose page is outside the pool, are not stored; their outputs are
+ * written. Two sequences may not append to the same slot in one call. Only the
+ * rows of kv and q may be written by it, each in its own place (kv_out, q_out).
  */
 int latent_append(const gblatent_config* cfg, int32_t T, const gbattn_batch* batch, const gbattn_rows* kv,
                   const void* gamma, const gbattn_rows* q, const int32_t* positions, const uint64_t* table,

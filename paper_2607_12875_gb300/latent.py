@@ -4,7 +4,7 @@ over the cached latents themselves. Argument marshalling only, as in attn:
 tensors with heads are [tokens, heads, dim], without [tokens, dim] (any strides
 with contiguous last elements); handles are made once with latent_config,
 latent_cache and attn_batch. A tensor that has fewer tokens, heads or elements than
-the call says is refused here (ValueError)."""
+the call says, or elements of another size, is refused here (ValueError)."""
 from __future__ import annotations
 
 import ctypes
@@ -12,7 +12,7 @@ import math
 
 import paper_2607_12875_gb300 as _gb
 
-from .attn import LAYOUTS, AttnBatch, AttnRows, _rows, _words
+from .attn import LAYOUTS, AttnBatch, AttnRows, _rows
 
 # every function include/gblatent.h declares
 LATENT_EXPORTS = ("latent_check_config", "latent_workspace_size", "latent_append", "latent_prompt", "latent_cached")
@@ -63,14 +63,34 @@ def latent_cache(pool) -> LatentCache:
     if len(pool.shape) != 3 or not pool.is_contiguous():
         raise ValueError("a pool of pages is contiguous, [n_pages, page, latent_dim + rope_dim]")
     c = LatentCache(_gb._ptr(pool), pool.shape[0])
-    c.shape = tuple(pool.shape[1:])  # (the calls hold it against their config)
+    c.shape = (*pool.shape[1:], pool.element_size())  # (the calls hold it against their config)
     return c
 
 
+def _size(cfg):
+    """Bytes of an element of the config's tensors."""
+    return 4 if cfg.act_dtype == _gb.F32 else 2
+
+
 def _pool(cfg, cache):
-    if getattr(cache, "shape", None) not in (None, (cfg.page, cfg.latent_dim + cfg.rope_dim)):
-        raise ValueError(f"pages of {cache.shape} in a call of {cfg.page} tokens of {cfg.latent_dim + cfg.rope_dim}")
+    want = (cfg.page, cfg.latent_dim + cfg.rope_dim, _size(cfg))
+    if getattr(cache, "shape", want) != want:
+        raise ValueError(f"pages of {cache.shape} (tokens, elements, bytes of one) in a call of {want}")
     return cache
+
+
+def _sized(cfg, *tensors):
+    size = _size(cfg)
+    for t in tensors:
+        if t is not None and t.element_size() != size:
+            raise ValueError(f"elements of {t.element_size()} bytes in a call of {size}")
+
+
+def _vector(t, n, size):
+    """Address of an array of at least n entries of so many bytes (None: no array)."""
+    if t is not None and (t.numel() < n or t.element_size() != size or not t.is_contiguous()):
+        raise ValueError(f"{t.numel()} entries of {t.element_size()} bytes, or not contiguous, where the call takes {n} of {size}")
+    return _gb._ptr(t)
 
 
 def _flat(t, tokens, dim):
@@ -93,22 +113,25 @@ def latent_append(cfg, batch, kv, gamma, table, cache, q=None, q_out=None, kv_ou
     T, W, H, P = kv.shape[0], cfg.latent_dim + cfg.rope_dim, cfg.heads, cfg.rope_dim
     if q is not None and q_out is None:
         raise ValueError("queries are turned into q_out")
-    _gb._check(_gb.lib().latent_append(cfg, T, batch, _flat(kv, T, W), _words(gamma, cfg.latent_dim), _rows(q, T, H, P),
-                                       _words(positions, T), _words(table, P // 2), _pool(cfg, cache), _flat(kv_out, T, W),
-                                       _rows(q_out, T, H, P), _gb._stream(stream)), "latent_append")
+    _sized(cfg, kv, q, q_out, kv_out)
+    _gb._check(_gb.lib().latent_append(cfg, T, batch, _flat(kv, T, W), _vector(gamma, cfg.latent_dim, _size(cfg)),
+                                       _rows(q, T, H, P), _vector(positions, T, 4), _vector(table, P // 2, 8), _pool(cfg, cache),
+                                       _flat(kv_out, T, W), _rows(q_out, T, H, P), _gb._stream(stream)), "latent_append")
 
 
 def latent_prompt(cfg, q, k, k_rope, v, cu_q, cu_k, out, ws, lse=None, stream=None):
     """k_rope may be None where the config has no rotary elements."""
     Tq, Tk, B, H, N = q.shape[0], k.shape[0], cu_q.numel() - 1, cfg.heads, cfg.nope_dim
+    _sized(cfg, q, k, k_rope, v, out)
     _gb._check(_gb.lib().latent_prompt(cfg, Tq, Tk, B, _rows(q, Tq, H, N + cfg.rope_dim), _rows(k, Tk, H, N),
-                                       _flat(k_rope, Tk, cfg.rope_dim), _rows(v, Tk, H, cfg.value_dim), _gb._ptr(cu_q),
-                                       _words(cu_k, B + 1), _rows(out, Tq, H, cfg.value_dim), _words(lse, Tq * H), _gb._ptr(ws),
+                                       _flat(k_rope, Tk, cfg.rope_dim), _rows(v, Tk, H, cfg.value_dim), _vector(cu_q, B + 1, 4),
+                                       _vector(cu_k, B + 1, 4), _rows(out, Tq, H, cfg.value_dim), _vector(lse, Tq * H, 4), _gb._ptr(ws),
                                        ws.numel() * ws.element_size(), _gb._stream(stream)), "latent_prompt")
 
 
 def latent_cached(cfg, batch, q, cache, out, ws, lse=None, stream=None):
     T, H = q.shape[0], cfg.heads
+    _sized(cfg, q, out)
     _gb._check(_gb.lib().latent_cached(cfg, T, batch, _rows(q, T, H, cfg.latent_dim + cfg.rope_dim), _pool(cfg, cache),
-                                       _rows(out, T, H, cfg.latent_dim), _words(lse, T * H), _gb._ptr(ws),
+                                       _rows(out, T, H, cfg.latent_dim), _vector(lse, T * H, 4), _gb._ptr(ws),
                                        ws.numel() * ws.element_size(), _gb._stream(stream)), "latent_cached")

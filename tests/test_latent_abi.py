@@ -9,7 +9,7 @@ import torch
 
 import paper_2607_12875_gb300 as gb
 from paper_2607_12875_gb300 import attn, latent
-from test_attn_abi import Rows, Ws, changed, status_of
+from test_attn_abi import Rows as Anything, Ws, changed, status_of
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 HEADER = os.path.join(ROOT, "include", "gblatent.h")
@@ -61,6 +61,27 @@ def test_workspace_sizes(lib):
     assert gb.latent_workspace_size(cfg(), 0, 0) > 0
 
 
+class Rows(Anything):
+    """bf16 elements."""
+
+    def element_size(self):
+        return 2
+
+
+class Array(Anything):
+    """n entries of so many bytes at an address that is never read here."""
+
+    def __init__(self, n, size=4, at=0x1000):
+        super().__init__(n, 1, 1, at)
+        self.size = size
+
+    def element_size(self):
+        return self.size
+
+    def is_contiguous(self):
+        return True
+
+
 class Flat(Rows):
     def __init__(self, T=4, D=576, at=0x1000, strides=None):
         super().__init__(T, 1, D, at)
@@ -76,21 +97,21 @@ def pool(at=0x5000, n=10):
 
 
 def test_append_refusals(lib):
-    table, gamma = Rows(T=64), Rows(T=512)
+    table, gamma = Array(64, 8), Array(512, 2)
 
     def call(c=cfg(), b=batch(), kv=Flat(), gamma=gamma, table=table, cache=pool(), **kw):
         return status_of(gb.latent_append, c, b, kv, gamma, table, cache, **kw)
     q = Rows(D=64)
     assert call(table=None) == gb.EINVAL
-    assert call(table=Rows(T=64, at=0x1008)) == gb.EINVAL
-    assert call(gamma=Rows(T=512, at=0x1004)) == gb.EINVAL
+    assert call(table=Array(64, 8, 0x1008)) == gb.EINVAL
+    assert call(gamma=Array(512, 2, 0x1004)) == gb.EINVAL
     assert call(kv=Flat(at=0x1002)) == gb.EINVAL
     assert call(kv=Flat(strides=(577, 1))) == gb.EINVAL
     assert call(kv_out=Flat(strides=(64, 1))) == gb.EINVAL             # rows that overlap
     assert call(q_out=q) == gb.EINVAL                                  # no q to turn
     assert call(q=q, q_out=Rows(D=64, strides=(64, 64, 1))) == gb.EINVAL
     assert call(q=Rows(D=64, strides=(516, 64, 1)), q_out=q) == gb.EINVAL
-    assert call(positions=Rows(at=0x1001)) == gb.EINVAL
+    assert call(positions=Array(4, at=0x1001)) == gb.EINVAL
     assert call(cache=pool(None)) == gb.EINVAL and call(cache=pool(0x5004)) == gb.EINVAL and call(cache=pool(n=-1)) == gb.EINVAL
     assert call(cache=pool(n=(1 << 24) + 1)) == gb.EUNSUPPORTED
     for kw in (dict(cu_q=None), dict(kv_len=0x1001), dict(page_table=None), dict(B=-1), dict(max_pages=-1)):
@@ -108,16 +129,16 @@ def test_attention_refusals(lib):
     ws = Ws(gb.latent_workspace_size(c, 4, 2))
     q, k, kr, v, out = Rows(D=192), Rows(), Flat(D=64), Rows(), Rows()
 
-    def prompt(q=q, k=k, kr=kr, v=v, cu=Rows(T=3), out=out, ws=ws, c=c, **kw):
+    def prompt(q=q, k=k, kr=kr, v=v, cu=Array(3), out=out, ws=ws, c=c, **kw):
         return status_of(gb.latent_prompt, c, q, k, kr, v, cu, cu, out, ws, **kw)
     assert prompt(ws=Ws(64)) == gb.EWORKSPACE and prompt(ws=Ws(1 << 40, at=0x10010)) == gb.EINVAL
-    assert prompt(cu=Rows(T=3, at=0x1002)) == gb.EINVAL
+    assert prompt(cu=Array(3, at=0x1002)) == gb.EINVAL
     assert prompt(q=Rows(D=192, at=0x1008)) == gb.EINVAL
     assert prompt(out=Rows(strides=(1024, 64, 1))) == gb.EINVAL
     assert prompt(k=Rows(strides=(1028, 128, 1))) == gb.EINVAL
     assert prompt(kr=Flat(D=64, at=0x1004)) == gb.EINVAL and prompt(kr=None) == gb.EINVAL
-    assert prompt(v=Rows(at=0x1002)) == gb.EINVAL and prompt(lse=Rows(at=0x1002)) == gb.EINVAL
-    assert prompt(cu=Rows(T=1)) == gb.OK and prompt(q=Rows(T=0, D=192)) == gb.OK
+    assert prompt(v=Rows(at=0x1002)) == gb.EINVAL and prompt(lse=Array(32, at=0x1002)) == gb.EINVAL
+    assert prompt(cu=Array(1)) == gb.OK and prompt(q=Rows(T=0, D=192)) == gb.OK
     assert prompt(c=cfg(page=48)) == gb.EUNSUPPORTED
 
     wide, low = Rows(D=576), Rows(D=512)
@@ -127,7 +148,7 @@ def test_attention_refusals(lib):
     assert cached(ws=Ws(64)) == gb.EWORKSPACE
     assert cached(cache=pool(0x5008)) == gb.EINVAL and cached(b=batch(kv_len=None)) == gb.EINVAL
     assert cached(out=Rows(D=512, at=0x1004)) == gb.EINVAL and cached(out=Rows(D=512, strides=(4096, 256, 1))) == gb.EINVAL
-    assert cached(lse=Rows(at=0x1001)) == gb.EINVAL
+    assert cached(lse=Array(32, at=0x1001)) == gb.EINVAL
     assert cached(b=batch(B=0)) == gb.OK
     assert cached(b=batch(max_pages=(1 << 24) + 1)) == gb.EUNSUPPORTED
     assert cached(cache=pool(n=(1 << 24) + 1)) == gb.EUNSUPPORTED
