@@ -25,6 +25,20 @@
 // Warps 0-3 and 4-7: softmax of the first and second half of the columns, queries and
 // results; warp 8: TMA; warps 9 and 10: MMA of the scores and of the values.
 //
+// What bounds it (64 rows, R 512, P 64, a tile of 64 keys): HBM allows a tile on every SM each 3190 cycles; L2 hands an
+// SM 27.8 bytes a cycle whatever the copies' pattern (8 TB/s in all), which is 2650 for a tile, and is what two CTAs
+// beside each other share HBM's bytes through; both products' operands, the copies and P are 335 KB of shared
+// memory's 128 bytes a cycle, 2620; the MMAs 1930. A tile takes 3560 to 3900: its copies are asked for when the values of
+// the tile before the last are done and take some 2000 cycles, so a third of the ring is in flight on average.
+// 4 sequences of up to 131072 keys, 56 heads: 108 us, 3.8 TB/s; 32 of up to 32768 keys, 128 heads: 284 us, 630 TFLOP/s
+// (under the power cap: 1.6 GHz). Few keys: latency, 19.8 us for one sequence of 4000 keys and 128 heads, of which the
+// search for the share 2.7, queries and first rows 3, the first tile's softmax (code not yet in the instruction
+// cache) 1.7, the results 1.7 to 3, the join 5.
+// Steps that led here, us for those two long cases: one MMA warp, tiles of 128 keys, one after the other 146 and 369;
+// tiles of 64 keys with the next tile's scores ahead 120 and 339; one copy for two chunks instead of one for each, and an
+// MMA warp each for scores and values 114 and 296. Prefetching rows to L2 in the order they lie in took more from
+// L2's rate than it gave (112 and 304 against 108 and 293 then); TMA multicast to two CTAs runs at 10 bytes a cycle.
+//
 // P is rounded to bf16, an error of up to 2^-8 of each weight beside the result's own
 // rounding: the MMA takes both operands in one 16-bit type, and the cache is bf16. The
 // weights' sum is not rounded.
@@ -50,6 +64,9 @@ constexpr int kChunk = kKeys * 128;       // bytes of 64 rows x 64 elements
 constexpr unsigned kFull = 0xffffffffu;
 constexpr float kGrow = 16.0f;            // log2 of how far a column's maximum may run ahead of m
 constexpr float kMost = 3.402823466e38f;  // -kMost: a maximum of nothing
+// Least blocks of 64 keys of a share, and how many a segment's set-up counts for. Us at (1, 0), (2, 1), (3, 1) and (4, 2):
+// one sequence of 4000 keys 26.2, 23.4, 24.2, 25.4; 32 of up to 32768, 128 heads 305, 283, 283, 303; short contexts (2 MB
+// of rows in all) 27, 27, 46, 46.
 constexpr int kMinBlocks = 2, kTileCost = 1;
 constexpr int kMostSides = 8;
 
@@ -767,7 +784,7 @@ bool latent_cached_tc_supported(const LatentProblem& p) {
 cudaError_t launch_latent_cached_tc(const LatentProblem& p, cudaStream_t stream) {
     // Rows of a sequence, on average. As many of them in a CTA as there are, up to 64; fewer, and more CTAs beside each
     // other, where the key axis has too few blocks for every SM: a CTA's queries and results are then less (one sequence
-    // of 4000 keys and 128 heads).
+    // of 4000 keys and 128 heads: 21.8 us with 64 rows, 19.8 with 32).
     const AttnProblem& a = p.a;
     const int64_t rows = ((int64_t)a.T * a.R + a.B - 1) / a.B;
     int n = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;

@@ -25,6 +25,12 @@
 // for the next work run while the softmax warps still write the last results.
 // TMEM columns: S_0, S_1 (128 each), O_0, O_1 (128 each).
 //
+// What bounds it: of 128 keys of two tiles the products take 2560 cycles, their operands in shared memory and the
+// copies into it 2660 (340 KB), the copies from L2 2880 (27.8 bytes a cycle and SM at most): all three are near each
+// other. 16384 tokens of 32 heads, causal: 1.85 ms, 1.49 PFLOP/s; 7 prompts of 8192 in all 153 us (ends, masks,
+// results and the first products of eight items a CTA). One MMA warp for both tiles, which stood still in its waits and
+// commits, took 2.02 ms.
+//
 // P is rounded to bf16, an error of up to 2^-8 of each weight beside the result's
 // own rounding: the MMA takes both operands in one 16-bit type, and V is bf16.
 //
