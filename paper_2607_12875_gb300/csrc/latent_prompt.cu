@@ -418,18 +418,9 @@ latent_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 mbar_arrive(&w_empty[k & 1]);
                 if (w.end) break;
                 const int n_max = max(w.n[0], w.n[1]);
-                for (int t = 0; t < (kDeal ? 1 : 2) && ok; ++t) {
-                    if (w.n[t] == 0) continue;
-                    ok = wait(&q_empty[t], (qn[t] & 1u) ^ 1u);
-                    if (!ok) break;
-                    mbar_expect_tx(&q_full[t], k_chunks * kHalf);
-                    for (int c = 0; c < k_chunks; ++c)
-                        tma_load_3d(sQ + t * kQTile + c * kHalf, &tm_q, c < own_chunks ? 64 * c : own, w.head0, w.s.q0 + w.tok0[t], &q_full[t]);
-                    ++qn[t];
-                }
                 // K_0, V_0, K_1, V_1, ..; kDeal: K_0, K_1, V_0, K_2, V_1, .., K_n-1, V_n-2, V_n-1
                 const int n_all = kDeal ? w.n[0] + w.n[1] : n_max;
-                for (int i = 0; i < 2 * n_all && ok; ++i) {
+                auto tile = [&](int i) {
                     bool value = i & 1;
                     int at = i >> 1;
                     if constexpr (kDeal) {
@@ -461,7 +452,19 @@ latent_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                         open = c + 1 < chunks;
                         if (!open) mbar_arrive(bar);
                     }
+                };
+                // (the first keys before the queries, which wait for the last product with the item's before)
+                if (n_all > 0) tile(0);
+                for (int t = 0; t < (kDeal ? 1 : 2) && ok; ++t) {
+                    if (w.n[t] == 0) continue;
+                    ok = wait(&q_empty[t], (qn[t] & 1u) ^ 1u);
+                    if (!ok) break;
+                    mbar_expect_tx(&q_full[t], k_chunks * kHalf);
+                    for (int c = 0; c < k_chunks; ++c)
+                        tma_load_3d(sQ + t * kQTile + c * kHalf, &tm_q, c < own_chunks ? 64 * c : own, w.head0, w.s.q0 + w.tok0[t], &q_full[t]);
+                    ++qn[t];
                 }
+                for (int i = 1; i < 2 * n_all && ok; ++i) tile(i);
             }
             // every copy has landed before the CTA leaves (a wait that gave up inside a tile: those that were asked for)
             if (open) mbar_arrive(&full[(seq - 1) % kSlots]);

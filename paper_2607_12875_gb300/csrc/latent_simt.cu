@@ -6,7 +6,7 @@
 // its keys in tiles of 32 through two buffers in shared memory (cp.async) and keeps
 // the weighted sums in registers. Absorbed: a tile's rows are keys and values at once.
 // Bound by the latency of its loads and by shared-memory wavefronts of a few warps: 333 tokens of 8 heads (96 and 64
-// elements) 18.8 us, 11 sequences of up to 500 keys, 8 heads of 256 + 32 elements 15.8 us (tiles of 16 rows, half of
+// elements) 15.4 us, 11 sequences of up to 500 keys, 8 heads of 256 + 32 elements 15.8 us (tiles of 16 rows, half of
 // them empty, and shares of 64 keys: 27.5).
 #include <type_traits>
 
@@ -39,28 +39,39 @@ __device__ __forceinline__ float4 load4(const uint8_t* p) {
 struct Sizes {
     int q_pitch, k_pitch, total;
 };
-__host__ __device__ __forceinline__ Sizes sizes_of(int key, int value, int eb, int rows) {
-    Sizes s;
+__host__ __device__ constexpr Sizes sizes_of(int key, int value, int eb, int rows, int least = 0) {
+    Sizes s{};
     s.q_pitch = ((key * eb / 16) | 1) * 16;
     s.k_pitch = (((key + value) * eb / 16) | 1) * 16;
     s.total = rows * s.q_pitch + 2 * kKeys * s.k_pitch + rows * (kKeys + 1) * 4 + 2 * kKeys * 4;
+    if (s.total < least) s.total = least;
     return s;
 }
 
 // N: rows of a thread, 2 (expanded) or 1 (absorbed); TX: threads of its rows, 8 or 16
 // (all in one warp); NC: its float4 columns. Thread (ty, tx) = (tid / TX, tid % TX)
 // holds rows N ty .., of the scores the keys tx + TX j, of the result the columns 4 tx +
-// 4 TX j ..
+// 4 TX j .. KG: groups of 128 threads, with every KG-th tile of the keys and shared memory of their own, whose results
+// the first one joins.
 template <int N, int TX>
 constexpr int kTileRows = kThreads / TX * N;
-template <typename TA, int N, int TX, int NC>
+// bytes of what a group passes on
+template <int N, int NC, int KG>
+constexpr int kPart = KG > 1 ? N * (NC + 1) * kThreads * 16 : 0;
+template <typename TA, int N, int TX, int NC, int KG>
 __device__ __forceinline__ void attend(const LatentProblem& lp, const Segment& it) {
     constexpr int kRows = kTileRows<N, TX>, EB = sizeof(TA), JK = kKeys / TX;
     constexpr bool kPaged = N == 1;
+    static_assert(KG == 1 || !kPaged, "groups of the expanded form");
     const AttnProblem& p = lp.a;
     extern __shared__ float4 smem4[];
-    uint8_t* sq = reinterpret_cast<uint8_t*>(smem4);
-    const Sizes sz = sizes_of(lp.K, kPaged ? 0 : p.D, EB, kRows);
+    const Sizes sz = sizes_of(lp.K, kPaged ? 0 : p.D, EB, kRows, kPart<N, NC, KG>);
+    const int group = KG == 1 ? 0 : threadIdx.x / kThreads;
+    uint8_t* sq = reinterpret_cast<uint8_t*>(smem4) + group * sz.total;
+    auto sync = [&] {  // of the group
+        if constexpr (KG == 1) __syncthreads();
+        else asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(kThreads) : "memory");
+    };
     uint8_t* skv = sq + kRows * sz.q_pitch;
     float* sp = reinterpret_cast<float*>(skv + 2 * kKeys * sz.k_pitch);
     int* marks = reinterpret_cast<int*>(sp + kRows * (kKeys + 1));
@@ -69,7 +80,7 @@ __device__ __forceinline__ void attend(const LatentProblem& lp, const Segment& i
     const int c_lo = (int)min64((int64_t)it.blk0 * kBlock, it.s.len);
     const int c_hi = (int)min64((int64_t)it.blk1 * kBlock, it.s.len);
 
-    const int tid = threadIdx.x, ty = tid / TX, tx = tid % TX;
+    const int tid = threadIdx.x % kThreads, ty = tid / TX, tx = tid % TX;
     const int qp = lp.K * EB / 16;  // pieces of a query
     for (int i = tid; i < kRows * qp; i += kThreads) {
         const int r = i / qp, c = i % qp;
@@ -87,7 +98,7 @@ __device__ __forceinline__ void attend(const LatentProblem& lp, const Segment& i
     // keys that some row of the tile sees
     int k_lo, last_hi;
     seen_keys(p, it.s, (row0 + n_rows - 1) / R, k_lo, last_hi);
-    k_lo = c_lo;
+    k_lo = c_lo + group * kKeys;
     const int k_hi = min(c_hi, last_hi + 1);
 
     // Four threads for a key's row, whose page is looked up a tile ahead.
@@ -129,14 +140,14 @@ __device__ __forceinline__ void attend(const LatentProblem& lp, const Segment& i
     }
     if (k_lo < k_hi) load(k_lo, 0);
     int buf = 0;
-    for (int k0 = k_lo; k0 < k_hi; k0 += kKeys, buf ^= 1) {
-        if (k0 + kKeys < k_hi) {
-            load(k0 + kKeys, buf ^ 1);
+    for (int k0 = k_lo; k0 < k_hi; k0 += KG * kKeys, buf ^= 1) {
+        if (k0 + KG * kKeys < k_hi) {
+            load(k0 + KG * kKeys, buf ^ 1);
             asm volatile("cp.async.wait_group 1;" ::: "memory");
         } else {
             asm volatile("cp.async.wait_group 0;" ::: "memory");
         }
-        __syncthreads();
+        sync();
         const uint8_t* tile = skv + buf * kKeys * sz.k_pitch;
         if (N * (32 / TX) * (tid >> 5) < n_rows) {  // (else no row of this warp)
             float s[N][JK] = {};
@@ -212,13 +223,45 @@ __device__ __forceinline__ void attend(const LatentProblem& lp, const Segment& i
             if (all) products(std::false_type{});
             else products(std::true_type{});
         }
-        __syncthreads();
+        sync();
     }
     if (k_lo >= k_hi) asm volatile("cp.async.wait_all;" ::: "memory");
 #pragma unroll
-    for (int r = 0; r < N; ++r) {
+    for (int r = 0; r < N; ++r)
 #pragma unroll
         for (int d = 1; d < TX; d <<= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], d);
+    if constexpr (KG > 1) {
+        // a thread's maxima, sums and results in its group's shared memory, a row of all threads' for each
+        auto part = [&](int g, int i) { return reinterpret_cast<float4*>(reinterpret_cast<uint8_t*>(smem4) + g * sz.total) + i * kThreads + tid; };
+        if (group > 0) {
+            if (k_lo >= k_hi) sync();  // (the queries of all of the group's threads have landed)
+#pragma unroll
+            for (int r = 0; r < N; ++r) {
+                *part(group, r) = make_float4(m[r], l[r], 0.f, 0.f);
+#pragma unroll
+                for (int c = 0; c < NC; ++c) *part(group, N + r * NC + c) = o[r][c];
+            }
+        }
+        __syncthreads();
+        if (group > 0) return;
+#pragma unroll
+        for (int g = 1; g < KG; ++g)
+#pragma unroll
+            for (int r = 0; r < N; ++r) {
+                const float4 other = *part(g, r);
+                const float m_new = fmaxf(m[r], other.x), base = m_new == neg_inf() ? 0.0f : m_new;
+                const float a = exp2f(m[r] - base), b = exp2f(other.x - base);
+                m[r] = m_new, l[r] = l[r] * a + other.y * b;
+#pragma unroll
+                for (int c = 0; c < NC; ++c) {
+                    const float4 v = *part(g, N + r * NC + c);
+                    o[r][c].x = o[r][c].x * a + v.x * b, o[r][c].y = o[r][c].y * a + v.y * b;
+                    o[r][c].z = o[r][c].z * a + v.z * b, o[r][c].w = o[r][c].w * a + v.w * b;
+                }
+            }
+    }
+#pragma unroll
+    for (int r = 0; r < N; ++r) {
         const int rr = N * ty + r;
         if (rr >= n_rows) continue;
         const int64_t t = it.s.q0 + (row0 + rr) / R;
@@ -251,11 +294,11 @@ __device__ __forceinline__ void attend(const LatentProblem& lp, const Segment& i
     }
 }
 
-template <typename TA, int N, int TX, int NC>
-__global__ void __launch_bounds__(kThreads) latent_simt_kernel(const __grid_constant__ LatentProblem lp) {
+template <typename TA, int N, int TX, int NC, int KG>
+__global__ void __launch_bounds__(KG* kThreads) latent_simt_kernel(const __grid_constant__ LatentProblem lp) {
     pdl_enter();
     const AttnProblem& p = lp.a;
-    __shared__ int64_t plan[plan_words(kThreads)];
+    __shared__ int64_t plan[plan_words(KG * kThreads)];
     if constexpr (N == 1) {
         Walk<kTileRows<N, TX>, kBlock> w;
         if (!w.begin(p, blockIdx.x, plan)) {
@@ -263,7 +306,7 @@ __global__ void __launch_bounds__(kThreads) latent_simt_kernel(const __grid_cons
             return;
         }
         do {
-            attend<TA, N, TX, NC>(lp, w.g);
+            attend<TA, N, TX, NC, KG>(lp, w.g);
             if (threadIdx.x == 0) w.note(p);
             __syncthreads();
         } while (w.next(p));
@@ -272,22 +315,23 @@ __global__ void __launch_bounds__(kThreads) latent_simt_kernel(const __grid_cons
         g.head = blockIdx.x % p.Hq;
         const Place at = find_tile(p, blockIdx.x / p.Hq, kTileRows<N, TX>, plan);
         if (at.b < 0) return;
-        g.b = at.b, g.s = load_seq(p, at.b), g.tile = (int)at.at;
+        g.b = at.b, g.s = load_seq(p, at.b);
+        g.tile = (int)(row_tiles(p, g.s, kTileRows<N, TX>) - 1 - at.at);  // the last tiles, which see the most keys, first
         g.blk1 = key_blocks<kBlock>(g.s), g.slot = -1;
-        attend<TA, N, TX, NC>(lp, g);
+        attend<TA, N, TX, NC, KG>(lp, g);
     }
 }
 
-template <typename TA, int N, int TX, int NC>
+template <typename TA, int N, int TX, int NC, int KG>
 cudaError_t simt_as(const LatentProblem& p, cudaStream_t stream) {
-    constexpr auto kernel = latent_simt_kernel<TA, N, TX, NC>;
+    constexpr auto kernel = latent_simt_kernel<TA, N, TX, NC, KG>;
     constexpr int kRows = kTileRows<N, TX>;
     static DeviceOnce once;
     constexpr int kMost = 227 * 1024;
     if (cudaError_t e = once.run([] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost - 1024); });
         e != cudaSuccess)
         return e;
-    const int smem = sizes_of(p.K, N == 1 ? 0 : p.a.D, (int)sizeof(TA), kRows).total;
+    const int smem = sizes_of(p.K, N == 1 ? 0 : p.a.D, (int)sizeof(TA), kRows, kPart<N, NC, KG>).total;
     if constexpr (N == 1) {
         LatentProblem a = p;
         const int fit = kMost / (smem + 2048);
@@ -295,9 +339,12 @@ cudaError_t simt_as(const LatentProblem& p, cudaStream_t stream) {
         if (cudaError_t e = launch_k(kernel, dim3(a.a.shares), dim3(kThreads), smem, stream, a); e != cudaSuccess) return e;
         return a.a.shares > 1 ? launch_attn_join(a.a, stream) : cudaSuccess;
     } else {
+        // fewer groups where these do not fit (keys have up to 256 elements, values NC float4 of each thread)
+        if constexpr (KG * sizes_of(256, 4 * TX * NC, (int)sizeof(TA), kRows, kPart<N, NC, KG>).total > kMost - 1024)
+            if (KG * smem > kMost - 1024) return simt_as<TA, N, TX, NC, KG / 2>(p, stream);
         const int64_t grid = ((int64_t)p.a.T / kRows + p.a.B) * p.a.Hq;
         if (grid > INT32_MAX) return cudaErrorInvalidConfiguration;
-        return launch_k(kernel, dim3((unsigned)grid), dim3(kThreads), smem, stream, p);
+        return launch_k(kernel, dim3((unsigned)grid), dim3(KG * kThreads), KG * smem, stream, p);
     }
 }
 
@@ -306,13 +353,14 @@ cudaError_t simt_type(const LatentProblem& p, cudaStream_t stream) {
     if (p.a.paged) {
         // eight rows where a sequence has no more, so that none of the warps stands idle
         const bool few = (int64_t)p.a.T * p.a.R <= 8 * (int64_t)p.a.B;
-        if (p.a.D <= 256) return few ? simt_as<TA, 1, 16, 4>(p, stream) : simt_as<TA, 1, 8, 8>(p, stream);
-        return few ? simt_as<TA, 1, 16, 8>(p, stream) : simt_as<TA, 1, 8, 16>(p, stream);
+        if (p.a.D <= 256) return few ? simt_as<TA, 1, 16, 4, 1>(p, stream) : simt_as<TA, 1, 8, 8, 1>(p, stream);
+        return few ? simt_as<TA, 1, 16, 8, 1>(p, stream) : simt_as<TA, 1, 8, 16, 1>(p, stream);
     }
-    // 16 tokens where 32 leave SMs without a block
+    // Where 32 tokens for a block leave SMs without one: 16, and the keys dealt to four groups of threads. Us for 333 tokens
+    // of 8 heads with 32 tokens 23.4; with 16 and one, two and four groups 20.2, 17.3 and 15.4.
     const bool few = ((int64_t)p.a.T / 32 + p.a.B) * p.a.Hq <= sm_count();
-    if (p.a.D <= 64) return few ? simt_as<TA, 2, 16, 1>(p, stream) : simt_as<TA, 2, 8, 2>(p, stream);
-    return few ? simt_as<TA, 2, 16, 2>(p, stream) : simt_as<TA, 2, 8, 4>(p, stream);
+    if (p.a.D <= 64) return few ? simt_as<TA, 2, 16, 1, 4>(p, stream) : simt_as<TA, 2, 8, 2, 1>(p, stream);
+    return few ? simt_as<TA, 2, 16, 2, 4>(p, stream) : simt_as<TA, 2, 8, 4, 1>(p, stream);
 }
 
 }  // namespace
