@@ -126,6 +126,17 @@ __device__ __forceinline__ Place find_place(int B, Units units, Index index_of, 
     }
     return Place{(int)found[0], found[1]};
 }
+// The same of up to 32 sequences, by each warp for itself.
+template <typename Units, typename Index>
+__device__ __forceinline__ Place find_place_alone(int B, Units units, Index index_of) {
+    const int lane = threadIdx.x & 31;
+    const int64_t v = lane < B ? units(lane) : 0, pre = warp_scan(v);
+    const int64_t index = index_of(__shfl_sync(0xffffffffu, pre, 31));
+    const uint32_t hit = __ballot_sync(0xffffffffu, index < pre);
+    if (!hit) return Place{-1, 0};
+    const int b = __ffs(hit) - 1;
+    return Place{b, index - __shfl_sync(0xffffffffu, pre - v, b)};
+}
 constexpr int plan_words(int threads) { return threads / 32 + 2; }
 
 // Row tile `index` of packed queries (sequences in order, their tiles in order).
@@ -178,10 +189,9 @@ struct Walk {
     // whether share `index` holds anything (then g is its first segment)
     __device__ __forceinline__ bool begin(const AttnProblem& p, int64_t index, int64_t* sm) {
         share = index;
-        const Place at = find_place(
-            p.B,
-            [&](int b) { const Seq s = load_seq(p, b); return tiles_of(p, s) * (key_blocks<kBlock>(s) + p.tile_cost) * p.Hkv; },
-            [&](int64_t total) { sh.set(p, total); return index * sh.each; }, sm);
+        const auto units = [&](int b) { const Seq s = load_seq(p, b); return tiles_of(p, s) * (key_blocks<kBlock>(s) + p.tile_cost) * p.Hkv; };
+        const auto index_of = [&](int64_t total) { sh.set(p, total); return index * sh.each; };
+        const Place at = kRows == 0 && p.B <= 32 ? find_place_alone(p.B, units, index_of) : find_place(p.B, units, index_of, sm);
         if (at.b < 0) return false;
         u = u0 = index * sh.each;
         u1 = min64(u0 + sh.each, sh.total);

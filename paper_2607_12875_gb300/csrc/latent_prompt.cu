@@ -27,7 +27,7 @@
 //
 // What bounds it: of 128 keys of two tiles the products take 2560 cycles, their operands in shared memory and the
 // copies into it 2660 (340 KB), the copies from L2 2880 (27.8 bytes a cycle and SM at most): all three are near each
-// other. 16384 tokens of 32 heads, causal: 1.85 ms, 1.49 PFLOP/s; 7 prompts of 8192 in all 153 us (ends, masks,
+// other. 16384 tokens of 32 heads, causal: 1.85 ms, 1.49 PFLOP/s; 7 prompts of 8192 in all 131 us (ends, masks,
 // results and the first products of eight items a CTA). One MMA warp for both tiles, which stood still in its waits and
 // commits, took 2.02 ms.
 //
@@ -51,13 +51,21 @@ constexpr int kThreads = 384;
 constexpr int kHalf = kTile * 128;     // bytes of a chunk: 128 rows of 64 elements
 constexpr int kQTile = 3 * kHalf;
 constexpr int kSlots = 8;              // chunks of K and V in flight
+constexpr int kAhead = 4;              // tiles of K and V of an item still to be loaded when the CTA asks for its next item
 constexpr float kGrow = 8.0f;          // log2 of how far a row's maximum may run ahead of m
 constexpr int kSmem = 1024 + 2 * kQTile + kSlots * kHalf + 512;
-static_assert((2 * kSlots + 24) * 8 <= 512 && kSmem + 1024 <= 227 * 1024, "shared memory");
+static_assert((2 * kSlots + 26) * 8 <= 512 && kSmem + 1024 <= 227 * 1024, "shared memory");
 
 // bytes that are to come, without an arrival
 __device__ __forceinline__ void mbar_expect_only(uint64_t* bar, uint32_t bytes) {
     asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
+}
+
+// 32 bytes to a 32-byte aligned address
+__device__ __forceinline__ void store32(__nv_bfloat16* dst, const uint32_t (&a)[4], const uint32_t (&b)[4]) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst), "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]),
+                 "r"(b[0]), "r"(b[1]), "r"(b[2]), "r"(b[3])
+                 : "memory");
 }
 
 struct Params {
@@ -129,7 +137,8 @@ latent_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
     uint64_t* w_full = o_full + 2;    // a work item is in its slot
     uint64_t* w_empty = w_full + 2;   // every role has read it
     uint64_t* ans = w_empty + 2;      // the answer to try_cancel
-    uint64_t* drain = ans + 1;
+    uint64_t* ask = ans + 1;          // the loads of a work item are nearly all on their way
+    uint64_t* drain = ask + 1;
     uint64_t* pair = drain + 2;       // kDeal: the two warps of the same rows
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(pair + 4);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
@@ -150,6 +159,7 @@ latent_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             mbar_init(&w_empty[t], 11);  // softmax warps, TMA, MMA warps
         }
         mbar_init(ans, 1);
+        mbar_init(ask, 1);
         mbar_init(&drain[0], 1);
         mbar_init(&drain[1], 1);
         for (int i = 0; i < 4; ++i) mbar_init(&pair[i], 2);
@@ -183,6 +193,8 @@ latent_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             if (lane == 0) mbar_arrive(&pair[warp & 3]);
             return wait_warp(&pair[warp & 3], meets++ & 1u);
         };
+        // whole sectors of 32 bytes for a thread's stores, where the results lie so
+        const bool wide = ((reinterpret_cast<uintptr_t>(p.out.p) | (uintptr_t)(2 * p.out.ts) | (uintptr_t)(2 * p.out.hs) | (uintptr_t)(2 * p.D)) & 31) == 0;
         bool ok = true;
         for (int k = 0; ok; ++k) {
             if (!wait_warp(&w_full[k & 1], (uint32_t)(k >> 1) & 1u)) break;
@@ -317,6 +329,7 @@ latent_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                     ld_wait();
                     pin32(o);
                 }
+                uint32_t before[4];
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     uint32_t w[4];
@@ -327,8 +340,16 @@ latent_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                         if (c + 8 * q < p.D) check = fmaf(a, 0.0f, fmaf(b, 0.0f, check));
                         w[i] = pack_bf16x2(a, b);
                     }
-                    const uint4 v = make_uint4(w[0], w[1], w[2], w[3]);
-                    if (have && c + 8 * q < p.D) *reinterpret_cast<uint4*>(out + c + 8 * q) = v;
+                    if (q & 1) {
+                        if (wide) {
+                            if (have && c + 8 * q < p.D) store32(out + c + 8 * (q - 1), before, w);
+                            continue;
+                        }
+                        if (have && c + 8 * (q - 1) < p.D) *reinterpret_cast<uint4*>(out + c + 8 * (q - 1)) = make_uint4(before[0], before[1], before[2], before[3]);
+                        if (have && c + 8 * q < p.D) *reinterpret_cast<uint4*>(out + c + 8 * q) = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) before[i] = w[i];
                 }
             }
             if constexpr (kDeal) {
@@ -359,24 +380,24 @@ latent_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             uint32_t turn = 0;
             int k = 0;
             for (; more; ++turn) {
-                if (lane == 0) try_cancel(&answer, ans);
-                asked = true;
                 const Place at = tiles.find(p, block / p.Hq, toks);
                 if (at.b >= 0) {
                     if (!wait_warp(&w_empty[k & 1], ((uint32_t)(k >> 1) & 1u) ^ 1u)) break;
                     Work w;
                     w.s = load_seq(p, at.b);
-                    // the last tiles, which see the most keys, first
-                    const int first = ((w.s.nq + toks - 1) / toks - 1 - (int)at.at) * toks;
+                    // The last tiles, which see the most keys, first. Of an odd number the sequence's first is alone, as the
+                    // second of its CTA: a tile alone takes nearly as long as two (3000 and 3500 cycles for 128 keys).
+                    const int n_tiles = (w.s.nq + kTile - 1) / kTile, last = (w.s.nq + toks - 1) / toks - 1 - (int)at.at;
+                    const int first = kDeal ? last : 2 * last - (n_tiles & 1);
                     w.head0 = (int)(block % p.Hq);
                     w.end = 0;
                     int lo, hi;
-                    seen_keys(p, w.s, first, lo, hi);
+                    seen_keys(p, w.s, max(first, 0) * kTile, lo, hi);
                     w.k_first = hi < 0 ? 0 : lo & ~(kTile - 1);
 #pragma unroll
                     for (int t = 0; t < 2; ++t) {
-                        w.tok0[t] = first + (kDeal ? 0 : t * kTile);
-                        w.rows[t] = min(kTile, w.s.nq - w.tok0[t]);
+                        w.tok0[t] = (kDeal ? first : first + t) * kTile;
+                        w.rows[t] = w.tok0[t] < 0 ? 0 : min(kTile, w.s.nq - w.tok0[t]);
                         w.n[t] = 0;
                         if (w.rows[t] > 0) {
                             seen_keys(p, w.s, w.tok0[t] + w.rows[t] - 1, lo, hi);  // its last token sees the furthest
@@ -390,7 +411,12 @@ latent_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                     }
                     __syncwarp();
                     ++k;
+                    // (not before: a CTA that has work for long is not to hold more of it. Packed prompts of 8192 tokens, 32 heads:
+                    // 131 us; asked for when the item begins 143, an item earlier 152, with CTAs done after 82 to 156)
+                    if (!wait_warp(ask, (uint32_t)(k - 1) & 1u)) break;
                 }
+                if (lane == 0) try_cancel(&answer, ans);
+                asked = true;
                 if (!wait_warp(ans, turn & 1u)) break;
                 asked = false;
                 more = cancelled(&answer, block);
@@ -420,7 +446,9 @@ latent_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 const int n_max = max(w.n[0], w.n[1]);
                 // K_0, V_0, K_1, V_1, ..; kDeal: K_0, K_1, V_0, K_2, V_1, .., K_n-1, V_n-2, V_n-1
                 const int n_all = kDeal ? w.n[0] + w.n[1] : n_max;
+                if (n_all == 0) mbar_arrive(ask);
                 auto tile = [&](int i) {
+                    if (i == max(0, 2 * n_all - kAhead)) mbar_arrive(ask);
                     bool value = i & 1;
                     int at = i >> 1;
                     if constexpr (kDeal) {
@@ -453,18 +481,19 @@ latent_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                         if (!open) mbar_arrive(bar);
                     }
                 };
-                // (the first keys before the queries, which wait for the last product with the item's before)
-                if (n_all > 0) tile(0);
+                // (the first keys between the tiles' queries: the last product with the second tile's of the item before comes
+                // later than the ring has room for them)
                 for (int t = 0; t < (kDeal ? 1 : 2) && ok; ++t) {
+                    if (t == 1 && n_all > 0) tile(0);
                     if (w.n[t] == 0) continue;
-                    ok = wait(&q_empty[t], (qn[t] & 1u) ^ 1u);
+                    ok = ok && wait(&q_empty[t], (qn[t] & 1u) ^ 1u);
                     if (!ok) break;
                     mbar_expect_tx(&q_full[t], k_chunks * kHalf);
                     for (int c = 0; c < k_chunks; ++c)
                         tma_load_3d(sQ + t * kQTile + c * kHalf, &tm_q, c < own_chunks ? 64 * c : own, w.head0, w.s.q0 + w.tok0[t], &q_full[t]);
                     ++qn[t];
                 }
-                for (int i = 1; i < 2 * n_all && ok; ++i) tile(i);
+                for (int i = kDeal ? 0 : 1; i < 2 * n_all && ok; ++i) tile(i);
             }
             // every copy has landed before the CTA leaves (a wait that gave up inside a tile: those that were asked for)
             if (open) mbar_arrive(&full[(seq - 1) % kSlots]);
