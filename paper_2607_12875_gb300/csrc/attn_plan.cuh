@@ -126,17 +126,6 @@ __device__ __forceinline__ Place find_place(int B, Units units, Index index_of, 
     }
     return Place{(int)found[0], found[1]};
 }
-// The same of up to 32 sequences, by each warp for itself.
-template <typename Units, typename Index>
-__device__ __forceinline__ Place find_place_alone(int B, Units units, Index index_of) {
-    const int lane = threadIdx.x & 31;
-    const int64_t v = lane < B ? units(lane) : 0, pre = warp_scan(v);
-    const int64_t index = index_of(__shfl_sync(0xffffffffu, pre, 31));
-    const uint32_t hit = __ballot_sync(0xffffffffu, index < pre);
-    if (!hit) return Place{-1, 0};
-    const int b = __ffs(hit) - 1;
-    return Place{b, index - __shfl_sync(0xffffffffu, pre - v, b)};
-}
 constexpr int plan_words(int threads) { return threads / 32 + 2; }
 
 // Row tile `index` of packed queries (sequences in order, their tiles in order).
@@ -188,11 +177,17 @@ struct Walk {
 
     // whether share `index` holds anything (then g is its first segment)
     __device__ __forceinline__ bool begin(const AttnProblem& p, int64_t index, int64_t* sm) {
-        share = index;
-        const auto units = [&](int b) { const Seq s = load_seq(p, b); return tiles_of(p, s) * (key_blocks<kBlock>(s) + p.tile_cost) * p.Hkv; };
-        const auto index_of = [&](int64_t total) { sh.set(p, total); return index * sh.each; };
-        const Place at = kRows == 0 && p.B <= 32 ? find_place_alone(p.B, units, index_of) : find_place(p.B, units, index_of, sm);
+        const Place at = find_place(
+            p.B,
+            [&](int b) { const Seq s = load_seq(p, b); return tiles_of(p, s) * (key_blocks<kBlock>(s) + p.tile_cost) * p.Hkv; },
+            [&](int64_t total) { sh.set(p, total); return index * sh.each; }, sm);
         if (at.b < 0) return false;
+        start(p, index, at);
+        return true;
+    }
+    // the share that begins at this place
+    __device__ __forceinline__ void start(const AttnProblem& p, int64_t index, const Place& at) {
+        share = index;
         u = u0 = index * sh.each;
         u1 = min64(u0 + sh.each, sh.total);
         enter(p, at.b);
@@ -203,7 +198,6 @@ struct Walk {
         g.tile = (int)div64(rest, nx);
         x0 = (int)(rest - (int64_t)g.tile * nx);
         cut(p);
-        return true;
     }
     __device__ __forceinline__ bool next(const AttnProblem& p) {
         if (last(p)) return false;
@@ -225,10 +219,12 @@ struct Walk {
     __device__ __forceinline__ bool last(const AttnProblem& p) const { return u + (x1 - x0) + p.tile_cost >= u1; }
     // For one thread, at a segment's end (or, idle, where the share holds nothing): what the join is to know
     __device__ __forceinline__ void note(const AttnProblem& p) const {
-        if (!last(p)) return;
+        if (last(p)) note_parts(p, (int)div64(g.nb - g.blk1 + sh.each - 1, sh.each) + 1);
+    }
+    __device__ __forceinline__ void note_parts(const AttnProblem& p, int parts) const {
         CutTile c{};
         if (g.blk0 == 0 && g.blk1 < g.nb) {
-            c.parts = (int)div64(g.nb - g.blk1 + sh.each - 1, sh.each) + 1;
+            c.parts = parts;
             c.first = (int)g.slot;
             c.rows = (int)min64(tile_rows(p), (int64_t)g.s.nq * p.R - (int64_t)g.tile * tile_rows(p));
             c.head = g.head, c.tile = g.tile;

@@ -30,10 +30,10 @@
 // beside each other share HBM's bytes through; both products' operands, the copies and P are 335 KB of shared
 // memory's 128 bytes a cycle, 2620; the MMAs 1930. A tile takes 3560 to 3900: its copies are asked for when the values of
 // the tile before the last are done and take some 2000 cycles, so a third of the ring is in flight on average.
-// 4 sequences of up to 131072 keys, 56 heads: 108 us, 3.8 TB/s; 32 of up to 32768 keys, 128 heads: 284 us, 630 TFLOP/s
-// (under the power cap: 1.6 GHz). Few keys: latency, 19.8 us for one sequence of 4000 keys and 128 heads, of which the
-// search for the share 2.7, queries and first rows 3, the first tile's softmax (code not yet in the instruction
-// cache) 1.7, the results 1.7 to 3, the join 5.
+// 4 sequences of up to 131072 keys, 56 heads: 100 us, 4.1 TB/s; 32 of up to 32768 keys, 128 heads: 280 us, 640 TFLOP/s.
+// Few keys: latency, 19.1 us for one sequence of 4000 keys and 128 heads: 11 until the last CTA is done (search for the
+// share, queries and first rows, the first tile's softmax, whose code is not yet in the instruction cache, results) and
+// 8 of the join (1.5 until it runs and knows the parts, 4 for their sums, 1.5 for the results).
 // Steps that led here, us for those two long cases: one MMA warp, tiles of 128 keys, one after the other 146 and 369;
 // tiles of 64 keys with the next tile's scores ahead 120 and 339; one copy for two chunks instead of one for each, and an
 // MMA warp each for scores and values 114 and 296. Prefetching rows to L2 in the order they lie in took more from
@@ -68,6 +68,8 @@ constexpr float kMost = 3.402823466e38f;  // -kMost: a maximum of nothing
 // one sequence of 4000 keys 26.2, 23.4, 24.2, 25.4; 32 of up to 32768, 128 heads 305, 283, 283, 303; short contexts (2 MB
 // of rows in all) 27, 27, 46, 46.
 constexpr int kMinBlocks = 2, kTileCost = 1;
+// Us at 0, 3 and 8: 4 sequences of up to 131072 keys, 56 heads 111.5, 102.6, 102.8 (0: parts are longer than the shares).
+constexpr int kSetup = 3;
 constexpr int kMostSides = 8;
 
 // N: query rows of a CTA. Rings of pairs of chunks (128 latent elements) and of the rotary chunks.
@@ -191,6 +193,69 @@ __device__ __forceinline__ Job job_of(const AttnProblem& p, const Segment& g, in
     return x;
 }
 
+// A share of the key axis that is part of one tile, where every tile can be cut into equal parts that are hardly longer
+// than the shares of Walk (kSetup blocks at most): a share with the end of one tile and the beginning of the next sets up
+// and finishes twice, which takes as long as several blocks (17 sequences of up to 3000 keys: 23 us for such a CTA, 15
+// for the others; with parts 34.3 to 30.3 us, 4 long ones 110 to 100). Else the shares of Walk. Up to 32 sequences, a lane for each.
+struct Deal : Walk<0, kKeys> {
+    static constexpr int kAlone = 32;  // sequences that a warp looks through by itself
+    int per = 0;  // parts of this share's tile (0: a share of Walk)
+
+    // (Out of line: what the loops' code shares the instruction cache with counts. 32 sequences of up to 32768 keys, 128
+    // heads: 290 us inline, 280 so.)
+    __device__ __noinline__ bool begin_together(const AttnProblem& p, int64_t index, int64_t* sm) { return Walk::begin(p, index, sm); }
+    __device__ __forceinline__ bool begin(const AttnProblem& p, int64_t index, int64_t* sm) {
+        per = 0;
+        if (p.B > kAlone) return begin_together(p, index, sm);
+        const int lane = threadIdx.x & 31;
+        Seq s{};
+        if (lane < p.B) s = load_seq(p, lane);
+        const int64_t tiles_here = lane < p.B ? tiles_of(p, s) : 0;
+        const int nb = key_blocks<kKeys>(s);
+        const int64_t v = tiles_here * (nb + p.tile_cost), pre = warp_scan(v);
+        sh.set(p, __shfl_sync(kFull, pre, 31));
+        const uint32_t all = __reduce_add_sync(kFull, (uint32_t)tiles_here);  // (T heads is 2^30 at most)
+        const int shares = p.shares;
+        auto parts_of = [&](int blocks) { return (uint32_t)tiles_here * (uint32_t)max(1, (nb + blocks - 1) / blocks); };
+        if (all <= (uint32_t)shares) {
+            // (the shares hold all blocks, so the sums of parts are small)
+            int lo = p.min_blocks, hi = (int)sh.each + kSetup;
+            if (__reduce_add_sync(kFull, parts_of(hi)) <= (uint32_t)shares) {
+                lo = max(lo, (int)sh.each - p.tile_cost - 1);
+                while (lo < hi) {
+                    const int mid = (lo + hi) >> 1;
+                    if (__reduce_add_sync(kFull, parts_of(mid)) <= (uint32_t)shares) hi = mid;
+                    else lo = mid + 1;
+                }
+                const uint32_t mine = parts_of(hi);
+                const int end = (int)warp_scan(mine), i = (int)index;
+                const uint32_t hit = __ballot_sync(kFull, i < end);
+                if (!hit) return false;
+                const int b = __ffs(hit) - 1, at = i - __shfl_sync(kFull, end - (int)mine, b);
+                enter(p, b);
+                share = index;
+                per = max(1, (g.nb + hi - 1) / hi);
+                const int part = at % per, each = (g.nb + per - 1) / per;
+                g.head = 0, g.tile = at / per;
+                g.blk0 = part * each, g.blk1 = min(g.blk0 + each, g.nb);
+                g.slot = per == 1 ? -1 : 2 * share;
+                return true;
+            }
+        }
+        const int64_t want = index * sh.each;
+        const uint32_t hit = __ballot_sync(kFull, want < pre);
+        if (!hit) return false;
+        const int b = __ffs(hit) - 1;
+        start(p, index, Place{b, want - __shfl_sync(kFull, pre - v, b)});
+        return true;
+    }
+    __device__ __forceinline__ bool next(const AttnProblem& p) { return per == 0 && Walk::next(p); }
+    __device__ __forceinline__ void note(const AttnProblem& p) const {
+        if (per == 0) Walk::note(p);
+        else note_parts(p, per);
+    }
+};
+
 struct Params {
     LatentProblem l;
     int sides;
@@ -209,7 +274,7 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap latents, const __grid_c
     uint8_t* tails = pairs + PAIRS * 2 * kChunk;
     constexpr int kBars = 2 * (PAIRS + TAILS) + 16;
     __shared__ uint64_t bars[kBars];
-    __shared__ Job jobs[2];
+    __shared__ Job jobs[2], first_job;
     uint64_t* full = bars;              // a pair landed
     uint64_t* empty = full + PAIRS;     // the products that read it finished
     uint64_t* tfull = empty + PAIRS;
@@ -254,16 +319,22 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap latents, const __grid_c
     // (up to here nothing in memory is read: barriers and TMEM are set up while the kernel before still runs)
     pdl_enter();
     tc_fence_before();
-    Walk<0, kKeys> walk;
-    const bool any = __any_sync(kFull, walk.begin(p, share, plan));
-    const Job first = any ? job_of<N>(p, walk.g, side) : Job{};
+    Deal walk;
+    if (warp == 8 || p.B > Deal::kAlone) {
+        const bool some = __any_sync(kFull, walk.begin(p, share, plan));
+        Job x{};
+        if (some) x = job_of<N>(p, walk.g, side);
+        x.end = !some;
+        if (warp == 8 && lane == 0) first_job = x;
+    }
     __syncthreads();
+    const bool any = !first_job.end;
     tc_fence_after();
     const uint32_t tmem = tmem_slot, tS = tmem, tO = tmem + 2 * N;  // S: even and odd tiles; O: pairs_of_tile times N columns
     auto wait_warp = [&](uint64_t* bar, uint32_t parity) { return warp_wait(bar, parity, abort_flag, p.err, pp.wait_limit_ns); };
 
     if (!any) {
-        if (tid == 0 && side == 0) walk.note_idle(p, share);
+        if (tid == 0 && side == 0) Deal::note_idle(p, share);
     } else if (warp < 8) {
         // ------------------------------------------------------------ softmax
         const int wg = warp >> 2, r = (warp & 3) * 32 + lane, c0 = wg * COLS, wt = tid & 127;
@@ -297,7 +368,7 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap latents, const __grid_c
             const int row = tid / kOf, rr = x.row0 + (row < x.rows ? row : 0), tok = rr / p.R;
             const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(p.q.p) + (int64_t)(x.q0 + tok) * p.q.ts + (rr - tok * p.R) * p.q.hs;
             const uint32_t dst = smem_u32(sq) + row * 128;
-#pragma unroll 6
+#pragma unroll 9
             for (int c = tid % kOf; c < pairs_of_tile * 16 + 8; c += kOf) {
                 const bool there = row < x.rows && 8 * c < W;
                 asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + (c >> 3) * (N * 128) + ((c ^ row) & 7) * 16),
@@ -305,7 +376,7 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap latents, const __grid_c
                              : "memory");
             }
         };
-        Job next = first;
+        Job next = first_job;
         fetch_queries(next);
         for (int j = 0; ok; ++j) {
             const Job x = next;
@@ -564,7 +635,7 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap latents, const __grid_c
             if (++slot == PAIRS) slot = 0, phase ^= 1;
         };
         for (int j = 0; ok; ++j) {
-            Job x = first;
+            Job x = first_job;
             if (j > 0) {  // (which every thread has)
                 ok = wait_warp(&j_empty[(j - 1) & 1], ((uint32_t)((j - 1) >> 1) & 1u) ^ 1u);
                 if (!ok) break;
@@ -668,7 +739,7 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap latents, const __grid_c
         bool ok = true, issued = false;
         auto weights_of = [&](uint32_t n) { return wait_warp(&p_full[n & 1u], n >> 1 & 1u); };
         for (int j = 0; ok; ++j) {
-            int tiles = __reduce_max_sync(kFull, first.tiles);
+            int tiles = __reduce_max_sync(kFull, first_job.tiles);
             if (j > 0) {
                 ok = wait_warp(&j_full[(j - 1) & 1], (uint32_t)((j - 1) >> 1) & 1u);
                 if (!ok) break;
@@ -740,7 +811,7 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap latents, const __grid_c
     }
     tc_fence_before();
     __syncthreads();
-    if (tid == 0 && side == 0 && *abort_flag) Walk<0, kKeys>::note_idle(p, share);  // (the join leaves this share's tile alone)
+    if (tid == 0 && side == 0 && *abort_flag) Deal::note_idle(p, share);  // (the join leaves this share's tile alone)
     if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
 

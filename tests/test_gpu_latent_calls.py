@@ -248,3 +248,21 @@ def test_sizes_at_the_limits():
             out.fill_(7.0)
             gb.latent_prompt(cfg, q, k, kr, v, prefix([0, 0]), prefix([1, 0]), out, ws)
             assert bool((out == 7).all()) and gb.moe_device_status(ws) == gb.OK
+
+
+@pytest.mark.parametrize("H,nq,lens", [
+    (64, [200], [600]),                                   # more tiles of rows than shares
+    (16, [1] * 32, [900] * 31 + [64]), (16, [1] * 33, [900] * 32 + [64]),  # sequences that a warp looks through, and one more
+    (40, [1] * 5, [9000, 1, 0, 64, 65]),                  # one of them nearly all of the work
+    (24, [0, 3, 0, 1, 0], [500, 2000, 0, 1999, 7]),       # sequences without queries in between
+    (128, [1] * 3, [6400, 6464, 6336]),
+])
+def test_shares_of_the_key_axis(H, nq, lens):
+    """Parts of tiles, shares over several tiles, idle ones: every key is seen once."""
+    pool, q, cfg = cached_case(29, "bf16", H, 512, 64, 64, nq, lens)
+    out, lse = torch.full((sum(nq), H, 512), float("nan"), dtype=torch.bfloat16, device="cuda"), torch.empty((sum(nq), H), device="cuda")
+    ws = workspace(cfg, sum(nq), len(nq))
+    for _ in range(2):
+        gb.latent_cached(cfg, gb.attn_batch(prefix(nq), i32(lens), i32(pool.table)), q, gb.latent_cache(pool.rows), out, ws, lse=lse)
+        check(out, lse, ref.absorbed(q, pool, 512, nq, lens, cfg.scale), "bf16")
+    assert gb.moe_device_status(ws) == gb.OK
