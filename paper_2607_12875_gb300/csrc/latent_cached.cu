@@ -1,6 +1,6 @@
 // Absorbed latent attention of few query tokens over the paged cache on the tensor
 // cores (bf16, R a multiple of 128, P up to 64), the work dealt out in equal shares of
-// the key axis (Walk).
+// the key axis (Deal).
 //
 // A cached row serves every head, as key whole and as value in its first R elements, so
 // a tile of 64 rows is loaded once and enters both products from the same place in
