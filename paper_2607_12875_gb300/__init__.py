@@ -185,13 +185,22 @@ def moe_rmsnorm(cfg, x, gamma, eps, y, stream=None):
            "moe_rmsnorm")
 
 
+def _array(t, n, size):
+    if t is not None and (t.numel() < n or t.element_size() != size or not t.is_contiguous()):
+        raise ValueError(f"{t.numel()} elements of {t.element_size()} bytes, or not contiguous, where the call takes {n} of {size}")
+
+
 def moe_rmsnorm_add(cfg, x, residual, gamma, eps, sum_out, y, codes=None, scales=None, stream=None):
     """residual and sum_out may be None (the norm of x alone; no sum wanted), y too where codes and scales are given."""
-    n, act = cfg.T * cfg.H, 4 if cfg.act_dtype == F32 else 2
-    for t, least, size in ((x, n, act), (residual, n, act), (gamma, cfg.H, act), (sum_out, n, act), (y, n, act), (codes, n, 1),
-                           (scales, n // 128, 4)):
-        if t is not None and (t.numel() < least or t.element_size() != size or not t.is_contiguous()):
-            raise ValueError(f"{t.numel()} elements of {t.element_size()} bytes, or not contiguous, where the call takes {least} of {size}")
+    H, act = cfg.H, 4 if cfg.act_dtype == F32 else 2
+    n = cfg.T * H
+    for t in (x, residual, sum_out, y):
+        if t is not None and (t.nbytes != n * act or not t.is_contiguous()):
+            _array(t, n, act)
+    _array(gamma, H, act)
+    if codes is not None or scales is not None:
+        _array(codes, n, 1)
+        _array(scales, n // 128, 4)
     _check(lib().moe_rmsnorm_add(ctypes.byref(cfg), _ptr(x), _ptr(residual), _ptr(gamma), float(eps), _ptr(sum_out), _ptr(y),
                                  _ptr(codes), _ptr(scales), _stream(stream)), "moe_rmsnorm_add")
 

@@ -67,20 +67,14 @@ def latent_cache(pool) -> LatentCache:
     return c
 
 
-def _size(cfg):
-    """Bytes of an element of the config's tensors."""
-    return 4 if cfg.act_dtype == _gb.F32 else 2
-
-
-def _pool(cfg, cache):
-    want = (cfg.page, cfg.latent_dim + cfg.rope_dim, _size(cfg))
+def _pool(page, width, size, cache):
+    want = (page, width, size)
     if getattr(cache, "shape", want) != want:
         raise ValueError(f"pages of {cache.shape} (tokens, elements, bytes of one) in a call of {want}")
     return cache
 
 
-def _sized(cfg, *tensors):
-    size = _size(cfg)
+def _sized(size, *tensors):
     for t in tensors:
         if t is not None and t.element_size() != size:
             raise ValueError(f"elements of {t.element_size()} bytes in a call of {size}")
@@ -88,9 +82,11 @@ def _sized(cfg, *tensors):
 
 def _vector(t, n, size):
     """Address of an array of at least n entries of so many bytes (None: no array)."""
-    if t is not None and (t.numel() < n or t.element_size() != size or not t.is_contiguous()):
+    if t is None:
+        return None
+    if t.numel() < n or t.element_size() != size or not t.is_contiguous():
         raise ValueError(f"{t.numel()} entries of {t.element_size()} bytes, or not contiguous, where the call takes {n} of {size}")
-    return _gb._ptr(t)
+    return t.data_ptr()
 
 
 def _flat(t, tokens, dim):
@@ -110,19 +106,20 @@ def _flat(t, tokens, dim):
 
 def latent_append(cfg, batch, kv, gamma, table, cache, q=None, q_out=None, kv_out=None, positions=None, stream=None):
     """gamma None: the latent is stored as it is; q_out and kv_out are optional."""
-    T, W, H, P = kv.shape[0], cfg.latent_dim + cfg.rope_dim, cfg.heads, cfg.rope_dim
+    T, R, H, P, size = kv.shape[0], cfg.latent_dim, cfg.heads, cfg.rope_dim, 4 if cfg.act_dtype == _gb.F32 else 2
+    W = R + P
     if q is not None and q_out is None:
         raise ValueError("queries are turned into q_out")
-    _sized(cfg, kv, q, q_out, kv_out)
-    _gb._check(_gb.lib().latent_append(cfg, T, batch, _flat(kv, T, W), _vector(gamma, cfg.latent_dim, _size(cfg)),
-                                       _rows(q, T, H, P), _vector(positions, T, 4), _vector(table, P // 2, 8), _pool(cfg, cache),
+    _sized(size, kv, q, q_out, kv_out)
+    _gb._check(_gb.lib().latent_append(cfg, T, batch, _flat(kv, T, W), _vector(gamma, R, size),
+                                       _rows(q, T, H, P), _vector(positions, T, 4), _vector(table, P // 2, 8), _pool(cfg.page, W, size, cache),
                                        _flat(kv_out, T, W), _rows(q_out, T, H, P), _gb._stream(stream)), "latent_append")
 
 
 def latent_prompt(cfg, q, k, k_rope, v, cu_q, cu_k, out, ws, lse=None, stream=None):
     """k_rope may be None where the config has no rotary elements."""
     Tq, Tk, B, H, N = q.shape[0], k.shape[0], cu_q.numel() - 1, cfg.heads, cfg.nope_dim
-    _sized(cfg, q, k, k_rope, v, out)
+    _sized(4 if cfg.act_dtype == _gb.F32 else 2, q, k, k_rope, v, out)
     _gb._check(_gb.lib().latent_prompt(cfg, Tq, Tk, B, _rows(q, Tq, H, N + cfg.rope_dim), _rows(k, Tk, H, N),
                                        _flat(k_rope, Tk, cfg.rope_dim), _rows(v, Tk, H, cfg.value_dim), _vector(cu_q, B + 1, 4),
                                        _vector(cu_k, B + 1, 4), _rows(out, Tq, H, cfg.value_dim), _vector(lse, Tq * H, 4), _gb._ptr(ws),
@@ -130,8 +127,9 @@ def latent_prompt(cfg, q, k, k_rope, v, cu_q, cu_k, out, ws, lse=None, stream=No
 
 
 def latent_cached(cfg, batch, q, cache, out, ws, lse=None, stream=None):
-    T, H = q.shape[0], cfg.heads
-    _sized(cfg, q, out)
-    _gb._check(_gb.lib().latent_cached(cfg, T, batch, _rows(q, T, H, cfg.latent_dim + cfg.rope_dim), _pool(cfg, cache),
-                                       _rows(out, T, H, cfg.latent_dim), _vector(lse, T * H, 4), _gb._ptr(ws),
+    T, H, R, size = q.shape[0], cfg.heads, cfg.latent_dim, 4 if cfg.act_dtype == _gb.F32 else 2
+    W = R + cfg.rope_dim
+    _sized(size, q, out)
+    _gb._check(_gb.lib().latent_cached(cfg, T, batch, _rows(q, T, H, W), _pool(cfg.page, W, size, cache),
+                                       _rows(out, T, H, R), _vector(lse, T * H, 4), _gb._ptr(ws),
                                        ws.numel() * ws.element_size(), _gb._stream(stream)), "latent_cached")
