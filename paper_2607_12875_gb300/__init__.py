@@ -195,7 +195,7 @@ def moe_rmsnorm_add(cfg, x, residual, gamma, eps, sum_out, y, codes=None, scales
     H, act = cfg.H, 4 if cfg.act_dtype == F32 else 2
     n = cfg.T * H
     for t in (x, residual, sum_out, y):
-        if t is not None and (t.nbytes != n * act or not t.is_contiguous()):
+        if t is not None and (t.nbytes != n * act or t.element_size() != act or not t.is_contiguous()):
             _array(t, n, act)
     _array(gamma, H, act)
     if codes is not None or scales is not None:

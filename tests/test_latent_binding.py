@@ -108,3 +108,14 @@ def test_norm_of_elements_of_another_size_is_refused(dt, name, size):
         call(scales=zeros(torch.float64, 8))
     with pytest.raises(ValueError):
         call(codes=zeros(torch.int32, 1024))
+
+
+@pytest.mark.parametrize("dt,same", [(BF, zeros(F, 512)), (BF, zeros(torch.uint8, 4, 512)), (F, zeros(BF, 2048)), (F, zeros(torch.float64, 512))])
+@pytest.mark.parametrize("name", ["x", "residual", "sum_out", "y"])
+def test_norm_of_as_many_bytes_of_another_type_is_refused(dt, same, name):
+    """4 rows of 256: the bytes are right, the elements are not."""
+    cfg = gb.make_config(4, 256, 128, 8, 2, act="bf16" if dt is BF else "f32", w="bf16" if dt is BF else "f32")
+    t = {**dict(x=zeros(dt, 1024), residual=zeros(dt, 1024), gamma=zeros(dt, 256), eps=1e-6, sum_out=zeros(dt, 1024), y=zeros(dt, 1024)), name: same}
+    assert same.nbytes == 1024 * zeros(dt, 1).element_size()
+    with pytest.raises(ValueError):
+        gb.moe_rmsnorm_add(cfg, **t)
