@@ -291,7 +291,11 @@ latent_cached_kernel(const __grid_constant__ CUtensorMap latents, const __grid_c
     __shared__ uint32_t tmem_slot, good[TAILS];  // good: pages of the tile that are in the pool
     __shared__ int abort_word, row_hi[N];
     __shared__ uint32_t raised[2];      // tile number (from 1 on) in which a score far above its maximum was found
-    __shared__ uint32_t poisoned[kKeys];  // the same for a key that holds what is no number
+    // The same for a key that holds what is no number. The warps of one half of the columns may mark keys of the next tile
+    // before those of the other half have read this one's marks, but never the same word: keys that some rows see and others
+    // do not lie within N - 1 in a row, and the next segment begins when all warps' weights of this one are written.
+    static_assert(N <= kKeys, "no two tiles of a segment mark the same word");
+    __shared__ uint32_t poisoned[kKeys];
     __shared__ __align__(8) float sums[8][COLS];
     __shared__ __align__(16) float low[N], factor[N];  // the columns' -m, and what a raise multiplies by
     __shared__ int64_t plan[plan_words(kThreads)];
