@@ -54,7 +54,8 @@ class LatentLayer:
         order = torch.randperm(batch * per, generator=g, device=device).to(torch.int32)
         self.pages = order.view(batch, per)  # (an engine would hand pages out as sequences grow)
         self.lens = torch.zeros(batch, dtype=torch.int32, device=device)
-        self.ws = torch.zeros(gb.latent_workspace_size(self.attn, 1, batch), dtype=torch.uint8, device=device)
+        # (no call has more query tokens than whole prompts of all sequences)
+        self.ws = torch.zeros(gb.latent_workspace_size(self.attn, batch * context, batch), dtype=torch.uint8, device=device)
         self.moe_ws = {}
 
     def _norm(self, x, residual, which):
