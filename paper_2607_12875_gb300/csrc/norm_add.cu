@@ -53,9 +53,15 @@ __device__ __forceinline__ void add_piece(const Raw8<TA>& a, const Raw8<TA>& b, 
     }
 }
 
+// 1 / sqrt(mean + eps) = rest * power, a power of two. Taken first, the power brings a row to about 1 without a rounding, so
+// that its product with gamma leaves fp32's range only where the norm does too.
+struct Inverse {
+    float rest, power;
+};
+
 // A lane's piece of the result, to the outputs that there are.
 template <typename TA>
-__device__ __forceinline__ void finish(const NormAdd& p, int64_t t, int at, const Raw8<TA>& s, const Raw8<TA>& g, float inv, float close) {
+__device__ __forceinline__ void finish(const NormAdd& p, int64_t t, int at, const Raw8<TA>& s, const Raw8<TA>& g, float inv, const Inverse& close) {
     float o[8];
     if (p.y) {
 #pragma unroll
@@ -63,9 +69,9 @@ __device__ __forceinline__ void finish(const NormAdd& p, int64_t t, int at, cons
         Vec8<TA>::store(static_cast<TA*>(p.y) + t * p.H + at, o);
     }
     if (!p.codes) return;
-    // (bf16: the first product is exact, so there is one rounding before the code's)
+    // (bf16: the first two products are exact, so there is one rounding before the code's)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) o[j] = __fmul_rn(__fmul_rn(s.at(j), g.at(j)), close);
+    for (int j = 0; j < 8; ++j) o[j] = __fmul_rn(__fmul_rn(__fmul_rn(s.at(j), close.power), g.at(j)), close.rest);
     float top = 0.0f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -102,7 +108,12 @@ __device__ __forceinline__ float tree(const float (&ss)[8]) {
     for (int d = 16; d >= 1; d >>= 1) v += __shfl_xor_sync(kFull, v, d);
     return v;
 }
-__device__ __forceinline__ float close_inverse(const NormAdd& p, float sum) { return __frsqrt_rn(sum / (float)p.H + p.eps); }
+__device__ __forceinline__ Inverse close_inverse(const NormAdd& p, float sum) {
+    const float v = __frsqrt_rn(sum / (float)p.H + p.eps);
+    const float power = __uint_as_float(__float_as_uint(v) & 0x7f800000u);
+    if (!(power > 0.0f && power <= 3.402823466e38f)) return Inverse{v, 1.0f};  // (a row of zeros, of infinities, of NaN)
+    return Inverse{__uint_as_float((__float_as_uint(v) & 0x007fffffu) | 0x3f800000u), power};
+}
 // 1 / sqrt(mean + eps) from the lanes' sums
 __device__ __forceinline__ float inverse(const NormAdd& p, float ss) {
 #pragma unroll
@@ -163,7 +174,9 @@ __global__ void __launch_bounds__(32 * kWarps) norm_add_kernel(const __grid_cons
         if (lane == 0) scale = inv;
     }
     if (p.y) __syncthreads();
-    const float inv = p.y ? scale : 0.0f, close = p.codes ? close_inverse(p, (sums[0] + sums[1]) + (sums[2] + sums[3])) : 0.0f;
+    const float inv = p.y ? scale : 0.0f;
+    Inverse close{};
+    if (p.codes) close = close_inverse(p, (sums[0] + sums[1]) + (sums[2] + sums[3]));
 #pragma unroll
     for (int i = 0; i < kHeld; ++i)
         if (warp + kWarps * i < n) finish(p, t, column(i), s[i], g[i], inv, close);
@@ -193,7 +206,8 @@ __global__ void __launch_bounds__(128) norm_add_wide_kernel(const __grid_constan
         add_squares(ss, s);
         add_squares8(ss8, s);
     }
-    const float inv = inverse(p, ss), close = close_inverse(p, tree(ss8));
+    const float inv = inverse(p, ss);
+    const Inverse close = close_inverse(p, tree(ss8));
     for (int i = 0; i < n; ++i) {
         const int at = 256 * i + 8 * lane;
         const Raw8<TA> s = piece(i);

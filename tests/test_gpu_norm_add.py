@@ -102,3 +102,28 @@ def test_values_that_are_no_numbers_in_8_bits():
     gb.moe_rmsnorm_add(cfg, x, None, plain, 1e-6, None, y, c1, s1)
     assert torch.isnan(y[1]).all() and torch.isfinite(y[0]).all() and ((c1[1] & 0x7f) == 0x7f).all()
     assert (s1[1] == 2.0 ** -126).all()
+
+
+@pytest.mark.parametrize("act", ["bf16", "f32"])
+@pytest.mark.parametrize("H", [512, 7168, 8448])
+@pytest.mark.parametrize("power", [-60, 55])
+def test_codes_where_the_row_times_gamma_leaves_fp32s_range(act, H, power):
+    """Rows of about 2^power, whose products with gamma are no normal fp32 numbers though the norm's elements are: columns
+    with gammas of about 2^-85, 1 and 2^78. Against the definition, as above."""
+    x = rows(8, 3, H, act, 0.0) * 2.0 ** power
+    gamma = rows(9, 1, H, act, 0.0)[0]
+    gamma[:128] *= 2.0 ** -85
+    gamma[128:256] *= 2.0 ** 78
+    cfg = gb.make_config(3, H, 128, 8, 2, act=act, w=act)
+    codes = torch.empty((3, H), dtype=torch.uint8, device="cuda")
+    scales = torch.empty((3, H // 128), device="cuda")
+    gb.moe_rmsnorm_add(cfg, x, None, gamma, 0.0, None, None, codes, scales)
+    t = x.double().cpu().numpy()
+    want = (t / np.sqrt((t * t).mean(1, keepdims=True)) * gamma.double().cpu().numpy()).reshape(3, -1, 128)
+    got_s = scales.double().cpu().numpy()
+    top, near = np.abs(want).max(-1), 1 + 4e-6
+    assert (top <= 448 * got_s * near).all() and (top >= 224 * got_s / near).all()
+    v = want / got_s[..., None]
+    got = attn_reference.e4m3_values()[codes.cpu().numpy()].reshape(want.shape)
+    step = 2.0 ** (np.maximum(np.floor(np.log2(np.maximum(np.abs(v), 2.0 ** -40))), -6) - 3)
+    assert (np.abs(got - v) <= step / 2 + 4e-6 * np.abs(v)).all()
