@@ -266,3 +266,97 @@ def test_shares_of_the_key_axis(H, nq, lens):
         gb.latent_cached(cfg, gb.attn_batch(prefix(nq), i32(lens), i32(pool.table)), q, gb.latent_cache(pool.rows), out, ws, lse=lse)
         check(out, lse, ref.absorbed(q, pool, 512, nq, lens, cfg.scale), "bf16")
     assert gb.moe_device_status(ws) == gb.OK
+
+
+@pytest.mark.parametrize("act", ["f32", "bf16"])
+@pytest.mark.parametrize("page,R,P,H,new,lens", [
+    (16, 512, 64, 5, [1, 1, 1], [1, 17, 32]), (64, 512, 64, 128, [70, 0, 3], [200, 64, 3]), (128, 8, 128, 3, [300, 5], [300, 131]),
+    (32, 256, 32, 16, [1] * 70, list(range(1, 71))),
+])
+@pytest.mark.parametrize("queries,rows_out", [(False, False), (True, False), (False, True)])
+def test_append_stores_the_same_rows_whatever_else_is_wanted(act, page, R, P, H, new, lens, queries, rows_out):
+    """The rows that a call with every output gives (held to 64 bits elsewhere) in their slots bit for bit, and every other
+    slot as it was, with none or one of the optional outputs."""
+    T = sum(new)
+    pool = Pool(page, act, R + P, page, lens)
+    kv, gamma, q = normal(1, (T, R + P), act, 3.0), normal(2, (R,), act), normal(3, (T, H, P), act)
+    cfg, table = gb.latent_config(H, latent_dim=R, rope_dim=P, act=act, page=page), gb.attn_rope_table(P)
+    keep = (prefix(new), i32(lens), i32(pool.table))
+    want_kv, want_q = torch.empty_like(kv), torch.empty_like(q)
+    gb.latent_append(cfg, gb.attn_batch(*keep), kv, gamma, table, gb.latent_cache(pool.rows.clone()), q=q, q_out=want_q, kv_out=want_kv)
+    want, at = pool.rows.clone(), 0
+    for b, (n, m) in enumerate(zip(new, lens)):
+        for p in range(m - n, m):
+            want[pool.table[b, p // page], p % page] = want_kv[at]
+            at += 1
+    got_kv, got_q = torch.full_like(kv, 7.0), torch.full_like(q, 7.0)
+    outputs = {**(dict(q=q, q_out=got_q) if queries else {}), **(dict(kv_out=got_kv) if rows_out else {})}
+    gb.latent_append(cfg, gb.attn_batch(*keep), kv, gamma, table, gb.latent_cache(pool.rows), **outputs)
+    bits = torch.int32 if act == "f32" else torch.int16
+    assert torch.equal(pool.rows.view(bits), want.view(bits))
+    assert torch.equal(got_q, want_q) if queries else bool((got_q == 7).all())
+    assert torch.equal(got_kv, want_kv) if rows_out else bool((got_kv == 7).all())
+
+
+@pytest.mark.parametrize("act", ["f32", "bf16"])
+@pytest.mark.parametrize("bad", [float("inf"), -float("inf")])
+@pytest.mark.parametrize("shared", [True, False])
+def test_prompt_keys_with_an_infinity(act, bad, shared):
+    """One element of a key (of its rotary part, all heads', or of one head's own): for a query that sees it the score is
+    +inf or -inf by the sign of the query's element, so its result is no number, or the one without that key."""
+    lens, H, N, at = [100, 37, 129], 3, 128, 120                # position 20 of the second sequence
+    T = sum(lens)
+    q, k, kr, v = (normal(i + 31, s, act) for i, s in enumerate([(T, H, 192), (T, H, N), (T, 64), (T, H, 128)]))
+    cfg = gb.latent_config(H, act=act)
+    want = ref.expanded(q, k, kr, v, lens, lens, cfg.scale)
+    two = slice(100, 137)
+    present = torch.ones(37, dtype=torch.bool, device="cuda")
+    present[at - 100] = False
+    key = torch.cat((k, kr[:, None].expand(-1, H, -1)), -1)
+    without = ref.attention(q[two], key[two], v[two], 37, 37, cfg.scale, True, present)
+    if shared:
+        kr[at, 5] = bad
+        score = bad * q[two, :, N + 5].double()
+    else:
+        k[at, 1, 7] = bad
+        score = torch.zeros((37, H), dtype=torch.float64, device="cuda")
+        score[:, 1] = bad * q[two, 1, 7].double()
+    sees = torch.arange(37, device="cuda")[:, None] >= at - 100
+    up, down = sees & (score == torch.inf), sees & (score == -torch.inf)
+    assert bool(up.any()) and bool(down.any())
+    out, ws = torch.full((T, H, 128), 7.0, dtype=DT[act], device="cuda"), workspace(cfg, T, 3)
+    gb.latent_prompt(cfg, q, k, kr, v, prefix(lens), prefix(lens), out, ws)
+    assert gb.moe_device_status(ws) == gb.OK
+    mine = out[two]
+    assert bool(torch.isnan(mine[up]).all())
+    check(mine[down][:, None], None, tuple(w[down][:, None] if w.dim() == 3 else w[down] for w in without), act)
+    rest = torch.ones((T, H), dtype=torch.bool, device="cuda")
+    rest[two] = ~(up | down)
+    check(out[rest][:, None], None, tuple(w[rest][:, None] if w.dim() == 3 else w[rest] for w in want), act)
+
+
+@pytest.mark.parametrize("act", ["f32", "bf16"])
+@pytest.mark.parametrize("bad", [float("inf"), -float("inf")])
+@pytest.mark.parametrize("at", [0, 200, 298])
+def test_cached_rotary_keys_with_an_infinity(act, bad, at):
+    """The same over cached rows: draft tokens of which some do not see the row, and a sequence without it."""
+    nq, lens, H, R = [4, 2], [300, 77], 20, 512
+    pool, q, cfg = cached_case(17, act, H, R, 64, 64, nq, lens)
+    want = ref.absorbed(q, pool, R, nq, lens, cfg.scale)
+    rows, _ = pool.sequence(0, 300)
+    key = rows[:, None].expand(-1, H, -1)
+    present = torch.arange(300, device="cuda") != at
+    without = ref.attention(q[:4], key, key[..., :R], 4, 300, cfg.scale, True, present)
+    pool.rows[pool.table[0, at // 64], at % 64, R + 5] = bad
+    sees = (torch.arange(296, 300, device="cuda") >= at)[:, None]
+    score = bad * q[:4, :, R + 5].double()
+    up, down = sees & (score == torch.inf), sees & (score == -torch.inf)
+    assert bool(up.any()) and bool(down.any())
+    out, ws = torch.full((6, H, R), 7.0, dtype=DT[act], device="cuda"), workspace(cfg, 6, 2)
+    gb.latent_cached(cfg, gb.attn_batch(prefix(nq), i32(lens), i32(pool.table)), q, gb.latent_cache(pool.rows), out, ws)
+    assert gb.moe_device_status(ws) == gb.OK
+    assert bool(torch.isnan(out[:4][up]).all())
+    check(out[:4][down][:, None], None, tuple(w[down][:, None] if w.dim() == 3 else w[down] for w in without), act)
+    rest = torch.ones((6, H), dtype=torch.bool, device="cuda")
+    rest[:4] = ~(up | down)
+    check(out[rest][:, None], None, tuple(w[rest][:, None] if w.dim() == 3 else w[rest] for w in want), act)
