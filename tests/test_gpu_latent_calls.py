@@ -360,3 +360,36 @@ def test_cached_rotary_keys_with_an_infinity(act, bad, at):
     rest = torch.ones((6, H), dtype=torch.bool, device="cuda")
     rest[:4] = ~(up | down)
     check(out[rest][:, None], None, tuple(w[rest][:, None] if w.dim() == 3 else w[rest] for w in want), act)
+
+
+@pytest.mark.parametrize("act", ["f32", "bf16"])
+@pytest.mark.parametrize("B", [256, 257, 1100])
+def test_append_of_many_sequences(act, B):
+    """More sequences than are looked through at once, most of them with no or one token: each token's row in its own slot,
+    the values of a call without norm (the latent as it is), every other slot and row as it was."""
+    rng = np.random.default_rng(B)
+    new = [int(n) for n in rng.choice([0, 0, 1, 1, 2, 7], B)]
+    lens = [n + int(m) for n, m in zip(new, rng.integers(0, 40, B))]
+    R, P, page, T = 64, 16, 16, sum(new)
+    pool = Pool(31, act, R + P, page, lens)
+    kv, q = normal(1, (T + 5, R + P), act), normal(2, (T + 5, 2, P), act)
+    cfg, table = gb.latent_config(2, latent_dim=R, rope_dim=P, act=act, page=page), gb.attn_rope_table(P)
+    kv_out, q_out = torch.full_like(kv, 7.0), torch.full_like(q, 7.0)
+    want = pool.rows.clone()
+    keep = (prefix(new) + 2, i32(lens), i32(pool.table))
+    gb.latent_append(cfg, gb.attn_batch(*keep), kv, None, table, gb.latent_cache(pool.rows), q=q, q_out=q_out, kv_out=kv_out)
+    mine = slice(2, T + 2)
+    at = np.concatenate([np.arange(m - n, m) for n, m in zip(new, lens)])
+    seq = np.repeat(np.arange(B), new)
+    want[torch.from_numpy(pool.table[seq, at // page]).long().cuda(), torch.from_numpy(at % page).cuda()] = kv_out[mine]
+    bits = torch.int32 if act == "f32" else torch.int16
+    assert torch.equal(pool.rows.view(bits), want.view(bits)) and torch.equal(kv_out[mine, :R], kv[mine, :R])
+    # the turns are those of the tokens' places: one sequence with the same positions gives the same
+    flat_kv, flat_q = torch.empty_like(kv[mine]), torch.empty_like(q[mine])
+    one = torch.zeros((T // page + 1, page, R + P), dtype=DT[act], device="cuda")
+    keep = (prefix([T]), i32([T]), i32([list(range(T // page + 1))]), i32(at))
+    gb.latent_append(cfg, gb.attn_batch(*keep[:3]), kv[mine], None, table, gb.latent_cache(one), q=q[mine], q_out=flat_q, kv_out=flat_kv,
+                     positions=keep[3])
+    assert torch.equal(kv_out[mine], flat_kv) and torch.equal(q_out[mine], flat_q)
+    for t in (kv_out, q_out):
+        assert bool((t[:2] == 7).all()) and bool((t[T + 2:] == 7).all())
