@@ -89,8 +89,13 @@ int latent_append(const gblatent_config* cfg, int32_t T, const gbattn_batch* bat
  * heads, V], cu_q and cu_k [B+1] (equal for whole prompts; a sequence with more
  * keys than queries has its queries at the end), lse [Tq, heads] fp32 or NULL.
  * k_rope is not read when P is 0. out may not overlap the inputs. bf16 runs on the
- * tensor cores (P up to 64; weights rounded to bf16: off by 2^-8 of themselves),
- * else on CUDA cores.
+ * tensor cores (weights rounded to bf16: off by 2^-8 of themselves) where P is up
+ * to 64, scale is above 0 and no stride that is used is 0 (or 2^39 elements and
+ * more), else on CUDA cores, which are far slower. On the tensor cores a value that
+ * is no number costs time in queries that do not see it but lie in a tile that
+ * reaches its 128 keys (one behind a sequence's end, say): they are computed once
+ * more, 0.13 us a key and up to 32 after each other, so that past some 400 000 keys
+ * the waits may run out. Set such rows to something finite where that counts.
  */
 int latent_prompt(const gblatent_config* cfg, int32_t Tq, int32_t Tk, int32_t B, const gbattn_rows* q,
                   const gbattn_rows* k, const gbattn_rows* k_rope, const gbattn_rows* v, const int32_t* cu_q,
@@ -102,7 +107,9 @@ int latent_prompt(const gblatent_config* cfg, int32_t Tq, int32_t Tk, int32_t B,
  * own tokens already appended): q [T, heads, R + P], out [T, heads, R], lse [T,
  * heads] fp32 or NULL. Meant for few query tokens per sequence (decoding, draft
  * tokens); any number works. Long contexts are split over CTAs and joined by a
- * second launch, deterministically. bf16 with R a multiple of 128 and P up to 64
+ * second launch, deterministically; how many rows a CTA has follows from T, B and
+ * max_pages * page, so a table no wider than the longest context is fastest where
+ * keys are few. bf16 with R a multiple of 128 and P up to 64
  * runs on the tensor cores (weights rounded to bf16: off by 2^-8 of themselves),
  * else on CUDA cores. A token whose page is outside the pool is masked. out may
  * not overlap the inputs. T * heads, max_pages * page and n_pages * page up to

@@ -9,7 +9,7 @@
 //
 // Each element is read once and written once, so HBM bounds it for prompts (8192 tokens, 128 heads, rows also in
 // place: 58 us, 5.1 TB/s; the next heads' loads in flight while these turn: 64 without) and the launch with three
-// dependent loads (offsets, length, page) for single tokens: 128 in 6.7 us.
+// dependent loads (offsets, length, page) for single tokens: 128 in 7.1 us.
 #include <climits>
 
 #include "attn_plan.cuh"
@@ -162,7 +162,7 @@ template <typename TA>
 cudaError_t append_type(const LatentAppend& p, cudaStream_t stream) {
     // A token's search and angles cost as much as several of its heads, so it has as few threads as keep its loads in
     // flight. Us with 32, 64 and 128: 8192 tokens of 128 heads 59, 57 and 72, of 16 heads 20, 28 and 48; 128 tokens of
-    // 128 heads 9.6, 7.4 and 7.3.
+    // 128 heads 9.6, 7.4 and 7.3 (one session's figures).
     return (p.H << unit_bits(max(p.r.R >> 4, 1))) <= 128 ? append_as<TA, 32>(p, stream) : append_as<TA, 64>(p, stream);
 }
 

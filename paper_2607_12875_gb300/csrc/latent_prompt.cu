@@ -27,7 +27,7 @@
 //
 // What bounds it: of 128 keys of two tiles the products take 2560 cycles, their operands in shared memory and the
 // copies into it 2660 (340 KB), the copies from L2 2880 (27.8 bytes a cycle and SM at most): all three are near each
-// other. 16384 tokens of 32 heads, causal: 1.85 ms, 1.49 PFLOP/s; 7 prompts of 8192 in all 131 us (ends, masks,
+// other. 16384 tokens of 32 heads, causal: 1.80 ms, 1.53 PFLOP/s; 7 prompts of 8192 in all 130 us (ends, masks,
 // results and the first products of eight items a CTA). One MMA warp for both tiles, which stood still in its waits and
 // commits, took 2.02 ms.
 //

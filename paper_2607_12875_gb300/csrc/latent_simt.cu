@@ -6,7 +6,7 @@
 // its keys in tiles of 32 through two buffers in shared memory (cp.async) and keeps
 // the weighted sums in registers. Absorbed: a tile's rows are keys and values at once.
 // Bound by the latency of its loads and by shared-memory wavefronts of a few warps: 333 tokens of 8 heads (96 and 64
-// elements) 15.4 us, 11 sequences of up to 500 keys, 8 heads of 256 + 32 elements 15.8 us (tiles of 16 rows, half of
+// elements) 15.4 us, 11 sequences of up to 500 keys, 8 heads of 256 + 32 elements 15.9 us (tiles of 16 rows, half of
 // them empty, and shares of 64 keys: 27.5).
 #include <type_traits>
 

@@ -11,8 +11,8 @@
 // is four exchanges.
 //
 // Bound by HBM (three to four elements moved for one of arithmetic) for many rows: 8192 of 4096 with both outputs
-// 47.4 us, 6.4 TB/s (a warp for a row, which holds it all in registers: 67.6); by one row's loads and the 8 H / 256
-// dependent additions for few: 32 of 7168 5.3 us (11.9).
+// 47.5 us, 6.4 TB/s (a warp for a row, which holds it all in registers: 67.6); by one row's loads and the 8 H / 256
+// dependent additions for few: 32 of 7168 5.5 us (11.9).
 #include "common.cuh"
 #include "e4m3.cuh"
 #include "kernels.h"
